@@ -588,6 +588,129 @@ ptc_status ptc_curves_noalloc(const uint32_t* dist, uint64_t n, const uint64_t* 
                               uint32_t n_cap, uint64_t* hits_host_out, ptc_u128* saved_host_out,
                               ptc_u128* total_cost_host_out, void* stream);
 
+/*
+ * The cached state itself (Sec. 2.1-2.2: the keys and values of a request's
+ * blocks, reused by every request with the same prefix): keys and values in
+ * pages of block_size tokens, the write of new tokens' keys and values, the
+ * attention of new tokens over them, and an eviction inside a request.
+ *
+ * A request's context is a list of pages: request r's key j lies in page
+ * page_ids[page_off[r] + j / block_size] at slot j % block_size.  The dense ids
+ * of ptc_assign_ids with the offsets of ptc_hash_blocks are such a list for a
+ * cache that has a page for every distinct block; requests that share a prefix
+ * then share its pages.  A request's list may be longer than its tokens need.
+ *
+ *   k, v          16-bit floating point (dtype); element (page, head, slot, d) at
+ *                 page * stride[0] + head * stride[1] + slot * stride[2] + d,
+ *                 strides in elements, positive multiples of 8 (the stride of
+ *                 a dimension of size 1 is not used); k and v 16-byte aligned
+ *   n_pages       pages of k and v; an id in page_ids at or above it, where it
+ *                 is needed, is PTC_ERR_INVALID_ARG
+ *   block_size    tokens a page, in [1, PTC_MAX_BLOCK_SIZE]
+ *   head_dim      a multiple of 8 in [16, PTC_MAX_HEAD_DIM]
+ *   page_ids      u32[n_page_ids];  page_off u64[n_req + 1], non-decreasing,
+ *                 page_off[n_req] <= n_page_ids
+ *   kv_len        u32[n_req]: tokens in request r's pages, the new ones of the
+ *                 call included; at most block_size * (page_off[r+1] - page_off[r])
+ *   tok_off       u64[n_req + 1], non-decreasing from 0 to n_tok: request r's new
+ *                 tokens are rows tok_off[r] .. tok_off[r+1] of the call's arrays,
+ *                 and the last of its kv_len[r] tokens
+ *
+ * These calls can be left in flight: with `status` (a device word that the
+ * caller has zeroed) a call returns when its work is enqueued, and the word
+ * takes the ptc_status of the first kind of error a kernel meets (the larger
+ * of several), which later calls leave standing; arguments that the host can
+ * check are still refused by the return value.  Such calls can be captured in
+ * a CUDA graph: lengths and page lists are read on the device.  With status =
+ * NULL they return after reading the outcome, as every other call does.
+ */
+enum { PTC_DTYPE_BF16 = 0, PTC_DTYPE_FP16 = 1 };
+#define PTC_MAX_HEAD_DIM 128u
+typedef struct {
+  void* k;
+  void* v;
+  int64_t k_stride[3], v_stride[3]; /* page, head, slot */
+  const uint32_t* page_ids;
+  const uint64_t* page_off;
+  const uint32_t* kv_len;
+  uint64_t n_page_ids;
+  uint32_t n_pages, n_req, block_size, n_kv_heads, head_dim;
+  int32_t dtype;
+} ptc_paged_kv;
+
+/*
+ * ptc_kv_append — writes new tokens' keys and values into their pages: new
+ * token i of request r (of m = tok_off[r+1] - tok_off[r]) becomes key
+ * kv_len[r] - m + i.  kv_len[r] < m is PTC_ERR_INVALID_ARG; nothing is written
+ * for such a request or one whose pages are malformed.
+ *   k_new, v_new  [n_tok, n_kv_heads, head_dim], the cache's dtype; token and head
+ *                 strides in elements, as for the cache; 16-byte aligned
+ */
+size_t ptc_kv_append_workspace_bytes(uint32_t n_req);
+ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* v_new, const int64_t k_new_stride[2],
+                         const int64_t v_new_stride[2], const uint64_t* tok_off, uint64_t n_tok, void* ws,
+                         size_t ws_bytes, uint32_t* status, void* stream);
+
+/*
+ * ptc_paged_attention — attention of new tokens over their requests' pages,
+ * causal: with n = kv_len[r] and m new tokens, token i sees the keys
+ * j < n - m + 1 + i.  Query head g reads key head g / (n_q_heads / n_kv_heads).
+ *   s_j = scale * <q, k_j>,  lse = log sum_j exp(s_j),  out = sum_j exp(s_j - lse) v_j
+ * A token that sees no key (i < m - n) gets out = 0 and lse = -infinity.
+ * Products are summed in 32 bits; the weights are rounded to the cache's dtype
+ * before they meet the values (their sum is not).  Slots at or after kv_len[r]
+ * may hold anything, NaN included.
+ *   q         [n_tok, n_q_heads, head_dim], the cache's dtype; token and head
+ *             strides in elements, as for the cache; 16-byte aligned
+ *   scale     finite and positive
+ *   max_q_len no request has more new tokens (PTC_ERR_INVALID_ARG otherwise)
+ *   out       [n_tok, n_q_heads, head_dim] contiguous, 16-byte aligned
+ *   lse       f32[n_tok, n_q_heads]
+ * With mass_out the weights that each cached token receives are added up over
+ * the new tokens and over the query heads of its key head, for ptc_kv_evict:
+ *   mass_out[h][S] = mass_in[h][S] + sum exp(s_j - lse),  S = page_off[r] * block_size + j
+ * for j < n, and 0 for the rest of request r's slots.  mass_in and mass_out are
+ * f32[n_kv_heads, mass_stride], mass_stride >= n_page_ids * block_size; mass_in
+ * may be NULL (zeros) or mass_out itself.
+ */
+size_t ptc_paged_attention_workspace_bytes(uint32_t n_req, uint64_t n_tok, uint32_t n_q_heads, uint32_t n_kv_heads,
+                                           uint32_t head_dim);
+ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q, const int64_t q_stride[2],
+                               const uint64_t* tok_off, uint64_t n_tok, uint32_t n_q_heads, uint32_t max_q_len,
+                               float scale, void* out, float* lse, const float* mass_in, float* mass_out,
+                               uint64_t mass_stride, void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
+/*
+ * ptc_kv_evict — cuts every request to at most n_keep tokens a key head by
+ * accumulated attention weight, and moves what is kept to other pages.  With
+ * n = kv_len[r] and b = min(n, n_keep), each key head keeps, where b < n, its
+ * first n_sink tokens, its last n_recent and the heaviest of the rest (of equal
+ * weights the earlier token; NaN counts as lightest, below -infinity), and all
+ * n tokens otherwise.  The kept tokens stay in order: the i-th becomes key i of
+ * the destination pages.  Every head keeps b tokens, so the result is again a
+ * paged cache, which ptc_paged_attention reads with kv_len = new_len; its masks
+ * stay right because all kept tokens are in the past of new ones.
+ *   mass          f32[n_kv_heads, mass_stride] as ptc_paged_attention leaves it
+ *   n_keep        at least 1;  n_sink + n_recent <= n_keep
+ *   max_kv_len    no request has more tokens (PTC_ERR_INVALID_ARG otherwise)
+ *   dst_page_ids, dst_page_off, n_dst_page_ids
+ *                 the pages that take each request's kept tokens, in the same
+ *                 cache, with room for b; they must be no page of the requests
+ *                 and different from each other, which nothing checks
+ *   keep_out      u32[n_req, n_kv_heads, n_keep]: the kept tokens' old positions,
+ *                 PTC_NONE after the b-th
+ *   new_len_out   u32[n_req]: b
+ *   new_mass_out  f32[n_kv_heads, new_mass_stride], new_mass_stride >=
+ *                 n_dst_page_ids * block_size: the kept tokens' weights at their
+ *                 new slots, 0 in the requests' other slots; not mass itself
+ */
+size_t ptc_kv_evict_workspace_bytes(uint32_t n_req, uint32_t n_kv_heads, uint32_t max_kv_len);
+ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, uint64_t mass_stride, uint32_t n_keep,
+                        uint32_t n_sink, uint32_t n_recent, uint32_t max_kv_len, const uint32_t* dst_page_ids,
+                        const uint64_t* dst_page_off, uint64_t n_dst_page_ids, uint32_t* keep_out,
+                        uint32_t* new_len_out, float* new_mass_out, uint64_t new_mass_stride, void* ws,
+                        size_t ws_bytes, uint32_t* status, void* stream);
+
 /* Frees the calling thread's page-locked staging block (see the
  * conventions above); safe to call at any time between calls. */
 void ptc_release_host_staging(void);

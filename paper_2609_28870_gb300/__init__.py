@@ -11,6 +11,9 @@ CUDA kernels.  PyTorch provides device memory and the current CUDA stream.
     dist                 = ptc_stack_distance(prev)
     curves               = ptc_curves(dist, req_blk_off, 16, caps, PTC_COST_MEASURED)
 
+and for the cached state itself (keys and values in pages, see ``kv``):
+ptc_kv_append, ptc_paged_attention, ptc_kv_evict.
+
 Arrays are torch CUDA tensors.  Unsigned 32/64-bit arrays travel as int32 /
 int64 tensors holding the same bits (``u32()`` / ``u64()`` give numpy views).
 There is no CPU fallback: without the built library every call raises.
@@ -25,6 +28,9 @@ import numpy as np
 import torch
 
 from . import build as _build
+from . import kv as _kv
+from .kv import (MAX_HEAD_DIM, PTC_DTYPE_BF16, PTC_DTYPE_FP16, check_status, ptc_kv_append,  # noqa: F401
+                 ptc_kv_evict, ptc_paged_attention)
 
 PTC_NONE = 0xFFFFFFFF
 PTC_COST_UNIFORM, PTC_COST_MEASURED, PTC_COST_LINEAR = 0, 1, 2
@@ -193,6 +199,7 @@ def lib():
                 L.ptc_timer_read.argtypes = [vp, u32]
                 L.ptc_launch_count.restype = u64
                 L.ptc_launch_count.argtypes = []
+                _kv.declare(L)
                 del i64
                 _lib = L
     return _lib
