@@ -626,6 +626,7 @@ ptc_status ptc_curves_noalloc(const uint32_t* dist, uint64_t n, const uint64_t* 
  */
 enum { PTC_DTYPE_BF16 = 0, PTC_DTYPE_FP16 = 1 };
 #define PTC_MAX_HEAD_DIM 128u
+#define PTC_MAX_GROUP 128u
 typedef struct {
   void* k;
   void* v;
@@ -654,7 +655,8 @@ ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* 
 /*
  * ptc_paged_attention — attention of new tokens over their requests' pages,
  * causal: with n = kv_len[r] and m new tokens, token i sees the keys
- * j < n - m + 1 + i.  Query head g reads key head g / (n_q_heads / n_kv_heads).
+ * j < n - m + 1 + i.  Query head g reads key head g / (n_q_heads / n_kv_heads),
+ * of which at most PTC_MAX_GROUP share one.
  *   s_j = scale * <q, k_j>,  lse = log sum_j exp(s_j),  out = sum_j exp(s_j - lse) v_j
  * A token that sees no key (i < m - n) gets out = 0 and lse = -infinity.
  * Products are summed in 32 bits; the weights are rounded to the cache's dtype
@@ -673,8 +675,8 @@ ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* 
  * f32[n_kv_heads, mass_stride], mass_stride >= n_page_ids * block_size; mass_in
  * may be NULL (zeros) or mass_out itself.
  */
-size_t ptc_paged_attention_workspace_bytes(uint32_t n_req, uint64_t n_tok, uint32_t n_q_heads, uint32_t n_kv_heads,
-                                           uint32_t head_dim);
+size_t ptc_paged_attention_workspace_bytes(uint32_t n_req, uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t head_dim,
+                                           uint32_t max_q_len, uint64_t mass_stride /* 0 without mass_out */);
 ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q, const int64_t q_stride[2],
                                const uint64_t* tok_off, uint64_t n_tok, uint32_t n_q_heads, uint32_t max_q_len,
                                float scale, void* out, float* lse, const float* mass_in, float* mass_out,

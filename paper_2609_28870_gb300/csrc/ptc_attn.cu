@@ -1,61 +1,10 @@
 // Attention of new tokens over paged keys and values (ptc_paged_attention).
 #include <cmath>
 
-#include "ptc_kv.cuh"
-#include "ptc_tc.cuh"
+#include "ptc_attn.cuh"
 
 namespace ptc {
 namespace {
-
-// Rows of a query tile, keys of a key tile.  The G query heads of a key head
-// are packed as rows of one matrix, row = token * G + head, so that a key tile
-// is read once for all of them.
-constexpr uint32_t kRows = 256, kKeys = 128;
-constexpr uint32_t kMaxCtas = 512;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// Where a CTA of the tile kernel starts: its first unit, and what that is.
-struct CtaStart {
-  uint64_t u;
-  uint32_t r, h, qt, kv;
-};
-
-// What k_attn_plan leaves for the kernels after it.  The work of a call is a
-// row of units: for every request, key head and query tile, its key tiles.
-// CTA c of C takes the units [U c / C, U (c + 1) / C).
-struct AttnPlan {
-  uint32_t ok, pad;
-  uint64_t units;
-  CtaStart start[kMaxCtas];
-};
-
-struct AttnArgs {
-  KvView kv;
-  const char* q;
-  int64_t q_tok, q_head;
-  const uint64_t* tok_off;
-  uint64_t n_tok;
-  uint32_t n_q_heads, G, max_q_len;
-  float scale;
-  char* out;
-  float* lse;
-  const float* mass_in;
-  float* mass_out;
-  uint64_t mass_stride;
-  AttnPlan* plan;
-  uint64_t* unit_off;  // n_req + 1
-  float* part;         // unnormalised rows of split tiles: [2 * ctas][kRows][D]
-  float2* part_ml;     // their maxima (in powers of two) and sums
-  uint32_t ctas, box;  // box: rows of a tensor copy
-  uint32_t* status;
-};
-
-// Key tiles that query tile qt of a request sees, at least one.
-__device__ __forceinline__ uint32_t key_tiles(uint32_t m, uint32_t n, uint32_t G, uint32_t qt) {
-  const uint32_t rows = m * G, end = (qt + 1) * kRows < rows ? (qt + 1) * kRows : rows;
-  const int64_t sees = (int64_t)n - m + (end - 1) / G + 1;
-  return sees <= (int64_t)kKeys ? 1u : (uint32_t)((sees + kKeys - 1) / kKeys);
-}
 
 // req_search over offsets that this kernel has written itself.
 __device__ __forceinline__ uint32_t unit_search(const uint64_t* off, uint32_t lo, uint32_t hi, uint64_t u) {
@@ -67,14 +16,25 @@ __device__ __forceinline__ uint32_t unit_search(const uint64_t* off, uint32_t lo
   return lo;
 }
 
-// The requests' share of the units, and every CTA's start.  One CTA: the
-// lists are a few KB, and a second pass over them would cost a launch.
+// The requests' share of the units, and every CTA's start; CTA 0 for the tile
+// kernel, CTA 1 (where there is one) for the weights.  The time of a call of
+// few units is a chain of latencies, so what the lists hold is read once and
+// kept in shared memory (the first kPlanThreads requests of it).
 constexpr int kPlanThreads = 1024;
 __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   asm volatile("griddepcontrol.launch_dependents;");
   grid_dep_sync();
-  __shared__ uint64_t s_warp[32];
-  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, G = a.G;
+  __shared__ uint64_t s_warp[32], s_off[kPlanThreads + 1];
+  __shared__ uint32_t s_m[kPlanThreads], s_n[kPlanThreads];
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, tq = a.tq;
+  const bool weights = blockIdx.x == 1;
+  AttnPlan* plan = a.plan + blockIdx.x;
+  uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.x * (R + 1);
+  // a request's first-level tiles, and the units of one of them
+  auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kKeys) : 0u) : query_tiles(m, tq); };
+  auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
+    return weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i);
+  };
   bool bad = tid == 0 && (a.tok_off[0] != 0 || a.tok_off[R] != a.n_tok);
   uint64_t carry = 0;
   for (uint32_t r0 = 0; r0 < R; r0 += kPlanThreads) {
@@ -87,17 +47,17 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
       bad |= wrong;
       m = wrong ? 0 : (uint32_t)(hi - lo);
     }
-    const uint32_t tiles = (m * G + kRows - 1) / kRows;
+    const uint32_t tiles = tiles_of(m, n);
     uint64_t mine = 0;
     if (tiles <= 2)
-      for (uint32_t qt = 0; qt < tiles; ++qt) mine += key_tiles(m, n, G, qt);
+      for (uint32_t i = 0; i < tiles; ++i) mine += units_of(m, n, i);
     // requests of many tiles: a warp adds one up
     for (uint32_t todo = __ballot_sync(kFull, tiles > 2); todo; todo &= todo - 1) {
       const int src = __ffs(todo) - 1;
       const uint32_t mm = __shfl_sync(kFull, m, src), nn = __shfl_sync(kFull, n, src),
                      tt = __shfl_sync(kFull, tiles, src);
       uint64_t sum = 0;
-      for (uint32_t qt = lane; qt < tt; qt += 32) sum += key_tiles(mm, nn, G, qt);
+      for (uint32_t i = lane; i < tt; i += 32) sum += units_of(mm, nn, i);
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kFull, sum, o);
       if (lane == (uint32_t)src) mine = sum;
@@ -116,32 +76,57 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
       if (w < warp) before += s_warp[w];
       all += s_warp[w];
     }
-    if (r < R) a.unit_off[r] = before;
+    if (r < R) unit_off[r] = before;
+    if (r0 == 0) {
+      s_off[tid] = before;
+      s_m[tid] = m;
+      s_n[tid] = n;
+    }
     carry = all;
     __syncthreads();
   }
   bad = __syncthreads_or(bad);
   if (tid == 0) {
-    a.unit_off[R] = carry;
-    a.plan->ok = !bad;
-    a.plan->units = carry;
+    unit_off[R] = carry;
+    plan->ok = !bad;
+    plan->units = carry;
     if (bad) report(a.status, PTC_ERR_INVALID_ARG);
   }
   if (bad) return;
+  const bool shared = R <= kPlanThreads;
+  if (tid == 0 && shared) s_off[R] = carry;
   __syncthreads();
   for (uint32_t c = warp; c < a.ctas; c += 32) {
     const uint64_t u = carry * c / a.ctas;
     CtaStart s{u, 0, 0, 0, 0};
     if (u < carry) {
-      s.r = unit_search(a.unit_off, 0, R - 1, u);
-      const uint32_t m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]), n = a.kv.kv_len[s.r];
-      const uint64_t at = ld_relaxed_u64(a.unit_off + s.r), in = u - at;
-      const uint64_t head = (ld_relaxed_u64(a.unit_off + s.r + 1) - at) / a.kv.H;
+      uint32_t m, n;
+      uint64_t from, to;
+      if (shared) {
+        uint32_t lo = 0, hi = R - 1;
+        while (lo < hi) {
+          const uint32_t mid = lo + (hi - lo + 1) / 2;
+          if (s_off[mid] <= u) lo = mid;
+          else hi = mid - 1;
+        }
+        s.r = lo;
+        m = s_m[lo];
+        n = s_n[lo];
+        from = s_off[lo];
+        to = s_off[lo + 1];
+      } else {
+        s.r = unit_search(unit_off, 0, R - 1, u);
+        m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]);
+        n = a.kv.kv_len[s.r];
+        from = ld_relaxed_u64(unit_off + s.r);
+        to = ld_relaxed_u64(unit_off + s.r + 1);
+      }
+      const uint64_t head = (to - from) / a.kv.H, in = u - from;
       s.h = (uint32_t)(in / head);
-      uint64_t rest = in % head;
-      const uint32_t tiles = (m * G + kRows - 1) / kRows;
-      for (uint32_t q0 = 0; q0 < tiles; q0 += 32) {
-        const uint32_t k = q0 + lane < tiles ? key_tiles(m, n, G, q0 + lane) : 0;
+      uint64_t rest = in - s.h * head;
+      const uint32_t tiles = tiles_of(m, n);
+      for (uint32_t t0 = 0; t0 < tiles; t0 += 32) {
+        const uint32_t k = t0 + lane < tiles ? units_of(m, n, t0 + lane) : 0;
         uint32_t incl = k;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -151,14 +136,14 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
         const uint32_t here = __ballot_sync(kFull, rest < incl);
         if (here) {
           const int src = __ffs(here) - 1;
-          s.qt = q0 + src;
-          s.kv = (uint32_t)rest - __shfl_sync(kFull, incl - k, src);
+          s.major = t0 + src;
+          s.minor = (uint32_t)rest - __shfl_sync(kFull, incl - k, src);
           break;
         }
         rest -= __shfl_sync(kFull, incl, 31);
       }
     }
-    if (lane == 0) a.plan->start[c] = s;
+    if (lane == 0) plan->start[c] = s;
   }
 }
 
@@ -166,17 +151,15 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
 struct Walk {
   uint64_t left, tok0, page0;
   uint32_t r, h, qt, kv0, kv1, nkv;  // key tiles [kv0, kv1) of nkv
-  uint32_t m, n, rows, pages;
+  uint32_t m, n;
   __device__ __forceinline__ void request(const AttnArgs& a) {
     tok0 = a.tok_off[r];
     m = (uint32_t)(a.tok_off[r + 1] - tok0);
     n = a.kv.kv_len[r];
-    rows = m * a.G;
     page0 = a.kv.page_off[r];
-    pages = (uint32_t)(a.kv.page_off[r + 1] - page0);
   }
   __device__ __forceinline__ void part(const AttnArgs& a) {
-    nkv = key_tiles(m, n, a.G, qt);
+    nkv = key_tiles(m, n, a.tq, qt);
     kv1 = nkv - kv0 > left ? kv0 + (uint32_t)left : nkv;
   }
   // False if the CTA has nothing to do.
@@ -187,8 +170,8 @@ struct Walk {
     if (left == 0) return false;
     r = s.r;
     h = s.h;
-    qt = s.qt;
-    kv0 = s.kv;
+    qt = s.major;
+    kv0 = s.minor;
     request(a);
     part(a);
     return true;
@@ -197,7 +180,7 @@ struct Walk {
     left -= kv1 - kv0;
     if (left == 0) return false;
     kv0 = 0;
-    if (++qt * kRows >= rows) {
+    if (++qt * 2 * a.tq >= m) {
       qt = 0;
       if (++h == a.kv.H) {
         h = 0;
@@ -209,6 +192,12 @@ struct Walk {
     }
     part(a);
     return true;
+  }
+  __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const { return qt * 2 * a.tq; }
+  // How the two halves of the softmax share the tile.
+  __device__ __forceinline__ int mode(const AttnArgs& a) const {
+    const uint32_t tokens = m - qt * 2 * a.tq;
+    return tokens > a.tq ? 0 : tokens > a.tq32 ? 1 : 2;
   }
 };
 
@@ -239,187 +228,374 @@ struct Weights<__half> {
 };
 
 // ------------------------------------------------------------------ the tile kernel
-// One CTA an SM walks its units.  Warps 0-3 and 4-7 are the softmax of the
-// query tile's rows 0-127 and 128-255, warp 8 issues the products, warp 9 (with
-// tensor copies; warps 9-11 without) loads keys and values into a ring of
-// tiles.  For key tile j:
+// One CTA an SM walks its units.  Warps 0-3 and 4-7 are the two halves of the
+// softmax, warp 8 issues the products, warp 9 loads keys and values into a
+// ring of tiles (with warp 11 where there are no tensor copies), warp 10 loads
+// the queries of the next tile.  For key tile j:
 //   scores   S = Q K_j^T     128 x 128 sums in tensor memory
 //   softmax  one thread a row: running maximum and sum in 32 bits; weights
 //            exp2(s - max), rounded to 16 bits, over the scores' columns
 //   values   O += P V_j      P from tensor memory, O stays there
-// The two halves alternate: while one is in its softmax, the tensor cores work
-// for the other.  O is rescaled only when a row's maximum has grown by more
-// than a factor of 2^8 since the last time (weights up to 2^8 are as exact as
-// those up to 1), which after the first tiles hardly happens.
+// While one half is in its softmax, the tensor cores work for the other:
+//   kRowsApart    more than 128 rows: each half has its own rows and takes
+//                 every key tile
+//   kTilesApart   up to 128 rows: both halves have the same rows and take key
+//                 tiles in turn; two partial rows are put together at the end
+//   kColumnsApart up to 32 rows (single tokens): the rows stand four times in
+//                 the matrix, and each of the 4 warps takes 32 keys of a tile,
+//                 with zero weights for the others'.  A softmax over 32 keys is
+//                 a quarter of the latency that a tile waits for; the products
+//                 are the same instructions either way.
+// O is rescaled only when a row's maximum has grown by more than a factor of
+// 2^8 since the last time (weights up to 2^8 are as exact as those up to 1),
+// which after the first tiles hardly happens.
+enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
 constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
+constexpr int kScratch = 32768;        // sums of 8 warps, 32 rows and 32 columns
+// Registers a thread: 2 * 128 * 216 + 128 * 72 = 384 * 168, what the block has at launch.
+constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+
+struct TileShared {
+  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], drain;
+  float2 ml[256];
+  uint32_t tmem;
+};
 
 template <int NSLAB>
 struct TileShape {
   static constexpr int kTile = NSLAB * kSlabBytes;
   static constexpr int kRing = NSLAB == 2 ? 5 : 8;
-  static constexpr int kSmem = 2 * kTile + kRing * kTile + 1024;
-};
-
-struct TileShared {
-  uint64_t full[8], empty[8], q_full[2], s_full[2], p_full[2], pv_done[2], drain;
-  uint32_t tmem, abort;
+  // queries of half 0, of half 1 (or scratch), ring, the rest
+  static constexpr int kRest = kTile + kScratch + kRing * kTile;
+  static constexpr int kSmem = kRest + sizeof(TileShared);
+  static_assert(kSmem <= 227 * 1024, "shared memory of a block");
 };
 
 // Tensor memory columns: scores (and weights) of both halves, then their sums.
 __device__ __forceinline__ uint32_t s_col(uint32_t half) { return half * 128; }
 __device__ __forceinline__ uint32_t o_col(uint32_t half) { return 256 + half * 128; }
 
+// Both halves of the softmax.
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// One row of a result: sums over weights, 32 columns.
+template <typename T>
+__device__ __forceinline__ void store_row(char* out, const float (&x)[32], uint32_t col, uint32_t D) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (col + 8 * i < D) {
+      uint4 y;
+      y.x = Weights<T>::pack(x[8 * i], x[8 * i + 1]);
+      y.y = Weights<T>::pack(x[8 * i + 2], x[8 * i + 3]);
+      y.z = Weights<T>::pack(x[8 * i + 4], x[8 * i + 5]);
+      y.w = Weights<T>::pack(x[8 * i + 6], x[8 * i + 7]);
+      *reinterpret_cast<uint4*>(out + 2 * col + 16 * i) = y;
+    }
+}
+__device__ __forceinline__ void store_part(float* part, const float (&x)[32], uint32_t col, uint32_t D) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (col + 4 * i < D)
+      *reinterpret_cast<float4*>(part + col + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+}
+
+// The running maximum and sum of a row.
+struct RowState {
+  float top, l;
+  __device__ __forceinline__ void clear() {
+    top = -INFINITY;
+    l = 0.f;
+  }
+  // The maximum as a power of two, as the weights were scaled by it.
+  template <typename W>
+  __device__ __forceinline__ float top2(float sl2) const {
+    return l != 0.f ? top * sl2 - W::kShift : -INFINITY;  // a NaN sum is not an empty one
+  }
+};
+
+// A wait for the previous product into O, then O times f, where a lane's
+// maximum has grown too far.
+template <int NSLAB>
+__device__ __forceinline__ bool raise_top(RowState& st, float mx, float sl2, float slack, uint32_t o_at, bool first,
+                                          uint32_t bar_o, uint32_t parity) {
+  if (!__any_sync(kFull, mx > st.top + slack)) return true;
+  const float nt = fmaxf(st.top, mx);
+  const float f = st.top == -INFINITY ? 0.f : exp2_approx((st.top - nt) * sl2);
+  st.l *= f;
+  st.top = nt;
+  if (first) return true;
+  if (!mbar_wait(bar_o, parity)) return false;
+  tc_fence_after();
+#pragma unroll 1
+  for (int c = 0; c < NSLAB * 2; ++c) {
+    uint32_t x[32];
+    tmem_ld32(x, o_at + 32 * c);
+    tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+    tmem_st32(o_at + 32 * c, x);
+  }
+  return true;
+}
+
+// 32 scores to weights: their sum, and the weights in 16 columns.
+template <typename T>
+__device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float sub, float2& sum, uint32_t (&y)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float2 e = fma2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), make_float2(sl2, sl2),
+                          make_float2(-sub, -sub));
+    const float2 p = make_float2(exp2_approx(e.x), exp2_approx(e.y));
+    sum = add2(sum, p);
+    y[i] = Weights<T>::pack(p.x, p.y);
+  }
+}
+
 template <typename T, int NSLAB>
-__device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, uint32_t q_smem, uint32_t half) {
+__device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, char* scratch, uint32_t half) {
   using W = Weights<T>;
-  const uint32_t tid = threadIdx.x & 127;
+  const uint32_t tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
   const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
   const uint32_t s_at = tmem + s_col(half), o_at = tmem + o_col(half);
   const uint32_t bar_s = smem_u32(&sh.s_full[half]), bar_p = smem_u32(&sh.p_full[half]),
-                 bar_o = smem_u32(&sh.pv_done[half]), bar_q = smem_u32(&sh.q_full[half]);
+                 bar_o = smem_u32(&sh.pv_done[half]);
   const float sl2 = a.scale * kLog2e, slack = fminf(8.f / sl2, 1e38f);
-  const uint32_t D = a.kv.D;
-  const uint32_t qs = q_smem + half * TileShape<NSLAB>::kTile;
+  const uint32_t D = a.kv.D, G = a.G;
+  const CtaStart start = a.plan->start[blockIdx.x];
   uint32_t done = 0;  // key tiles of this half so far
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const uint32_t row0 = w.qt * kRows + half * 128;
-    if (row0 >= w.rows) continue;
-    // the query rows, zero beyond the request and beyond head_dim
-    const char* q = a.q + 2 * ((int64_t)w.tok0 * a.q_tok + (int64_t)w.h * a.G * a.q_head);
-#pragma unroll 8
-    for (uint32_t i = 0; i < NSLAB * 8; ++i) {
-      const uint32_t id = i * 128 + tid, row = id / (NSLAB * 8), c = id % (NSLAB * 8);
-      uint4 x = make_uint4(0, 0, 0, 0);
-      if (row0 + row < w.rows && c * 8 < D) {
-        const uint32_t t = (row0 + row) / a.G, g = (row0 + row) % a.G;
-        x = *reinterpret_cast<const uint4*>(q + 2 * ((int64_t)t * a.q_tok + (int64_t)g * a.q_head + c * 8));
-      }
-      const uint32_t at = qs + (c / 8) * kSlabBytes + row * 128 + (((c % 8) ^ (row & 7)) * 16);
-      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
-    }
-    fence_async_shared();
-    mbar_arrive(bar_q);
-
-    const uint32_t row = row0 + tid;
-    const bool valid = row < w.rows;
-    const uint32_t t = row / a.G, g = row % a.G;
+    const int mode = w.mode(a);
+    // the thread's row: a token of the request and a head of the group
+    const uint32_t i = mode == kColumnsApart ? lane : tid;
+    const uint32_t t = w.token0(a) + (mode == kRowsApart ? half * a.tq : 0) + i / G, g = i % G;
+    const bool valid = i < a.tq * G && t < w.m;
     const bool active = __any_sync(kFull, valid);
-    int64_t left = valid ? (int64_t)w.n - w.m + t + 1 - (int64_t)w.kv0 * kKeys : 0;  // keys from this tile on that the row sees
-    float top = -INFINITY, l = 0.f;
-    for (uint32_t j = w.kv0; j < w.kv1; ++j, ++done, left -= kKeys) {
-      if (!mbar_wait(bar_s, done & 1)) return false;
-      tc_fence_after();
-      if (active) {
-        const int see = left >= (int64_t)kKeys ? (int)kKeys : left > 0 ? (int)left : 0;
-        const bool masked = __any_sync(kFull, see < (int)kKeys);
-        float mx = -INFINITY;
+    const uint32_t step = mode == kRowsApart ? 1 : 2, j0 = w.kv0 + (mode == kRowsApart ? 0 : half);
+    // keys of the tile at hand and later ones that the row sees
+    int64_t see_all = valid ? (int64_t)w.n - w.m + t + 1 - (int64_t)j0 * kKeys : 0;
+    RowState st;
+    st.clear();
+    if (mode != kColumnsApart) {
+      for (uint32_t j = j0; j < w.kv1; j += step, ++done, see_all -= step * kKeys) {
+        if (!mbar_wait(bar_s, done & 1)) return false;
+        tc_fence_after();
+        if (active) {
+          uint32_t x[4][32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t x[32];
-          tmem_ld32(x, s_at + 32 * c);
+          for (int c = 0; c < 4; ++c) tmem_ld32(x[c], s_at + 32 * c);
           tmem_wait_ld();
-          if (masked) {
+          const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
+          if (__any_sync(kFull, see < (int)kKeys)) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * c + i >= see) x[i] = 0xFF800000u;
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (32 * c + k >= see) x[c][k] = 0xFF800000u;
           }
+          float mx[4];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(x[i]));
+          for (int c = 0; c < 4; ++c) {
+            mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
+#pragma unroll
+            for (int k = 2; k < 32; k += 2)
+              mx[c] = fmaxf(mx[c], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
+          }
+          if (!raise_top<NSLAB>(st, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), sl2, slack, o_at, j == j0, bar_o,
+                                (done - 1) & 1))
+            return false;
+          const float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+          float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t y[16];
+            weigh<T>(x[c], sl2, sub, sum, y);
+            tmem_st16(s_at + 16 * c, y);
+          }
+          st.l += sum.x + sum.y;
+          tmem_wait_st();
         }
-        if (__any_sync(kFull, mx > top + slack)) {
-          const float nt = fmaxf(top, mx);
-          const float f = top == -INFINITY ? 0.f : exp2_approx((top - nt) * sl2);
-          l *= f;
-          top = nt;
-          if (j > w.kv0) {
-            if (!mbar_wait(bar_o, (done - 1) & 1)) return false;
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < NSLAB * 2; ++c) {
-              uint32_t x[32];
-              tmem_ld32(x, o_at + 32 * c);
-              tmem_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
-              tmem_st32(o_at + 32 * c, x);
-            }
-          }
-        }
-        const float sub = (top == -INFINITY ? 0.f : top * sl2) - W::kShift;
-        float l0 = 0.f, l1 = 0.f;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t x[32], y[16];
-          tmem_ld32(x, s_at + 32 * c);
-          tmem_wait_ld();
-          if (masked) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (32 * c + i >= see) x[i] = 0xFF800000u;
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float p0 = exp2_approx(fmaf(__uint_as_float(x[2 * i]), sl2, -sub));
-            const float p1 = exp2_approx(fmaf(__uint_as_float(x[2 * i + 1]), sl2, -sub));
-            l0 += p0;
-            l1 += p1;
-            y[i] = W::pack(p0, p1);
-          }
-          tmem_st16(s_at + 16 * c, y);
-        }
-        l += l0 + l1;
-        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p);
       }
-      tc_fence_before();
-      mbar_arrive(bar_p);
-    }
-    // the sums of the rows
-    if (!mbar_wait(bar_o, (done - 1) & 1)) return false;
-    tc_fence_after();
-    if (active) {
-      const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
-      const bool none = !(l != 0.f);  // no key seen (a NaN sum is not that)
-      const float inv = none ? 0.f : 1.f / l;
-      const uint64_t at = (w.tok0 + t) * a.n_q_heads + w.h * a.G + g;
-      const uint32_t slot = 2 * blockIdx.x + (w.kv0 == a.plan->start[blockIdx.x].kv && w.qt == a.plan->start[blockIdx.x].qt &&
-                                              w.h == a.plan->start[blockIdx.x].h && w.r == a.plan->start[blockIdx.x].r ? 0 : 1);
-      const uint64_t prow = (uint64_t)slot * kRows + half * 128 + tid;
-#pragma unroll
-      for (int c = 0; c < NSLAB * 2; ++c) {
-        uint32_t x[32];
-        tmem_ld32(x, o_at + 32 * c);
+    } else {
+      see_all -= 32 * warp;
+      for (uint32_t j = j0; j < w.kv1; j += step, ++done, see_all -= step * kKeys) {
+        if (!mbar_wait(bar_s, done & 1)) return false;
+        tc_fence_after();
+        uint32_t x[32], y[16], zero[16];
+        tmem_ld32(x, s_at + 32 * warp);
         tmem_wait_ld();
-        if (valid && whole) {
-          char* o = a.out + 2 * (at * D + 32 * c);
+        const int see = see_all >= 32 ? 32 : see_all > 0 ? (int)see_all : 0;
+        if (a.scores && valid) {
+          float* to = a.scores + ((uint64_t)w.h * a.few + lane) * a.mass_stride + w.page0 * a.kv.B + (uint64_t)j * kKeys + 32 * warp;
+          if (see == 32 && (a.mass_stride & 3) == 0 && (w.page0 * a.kv.B & 3) == 0) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t y[4];
+            for (int k = 0; k < 8; ++k)
+              *reinterpret_cast<uint4*>(to + 4 * k) = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+          } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const float lo = none ? 0.f : __uint_as_float(x[8 * i + 2 * k]) * inv;
-              const float hi = none ? 0.f : __uint_as_float(x[8 * i + 2 * k + 1]) * inv;
-              y[k] = W::pack(lo, hi);
-            }
-            if (32 * c + 8 * i < (int)D) *reinterpret_cast<uint4*>(o + 16 * i) = make_uint4(y[0], y[1], y[2], y[3]);
+            for (int k = 0; k < 32; ++k)
+              if (k < see) to[k] = __uint_as_float(x[k]);
           }
-        } else if (valid) {
-          float* o = a.part + prow * D + 32 * c;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (32 * c + 4 * i < (int)D)
-              *reinterpret_cast<uint4*>(o + 4 * i) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
         }
         __syncwarp();
-      }
-      if (valid) {
-        const float top2 = top == -INFINITY ? -INFINITY : top * sl2 - W::kShift;
-        if (whole) a.lse[at] = none ? -INFINITY : (top2 + log2_approx(l)) * kLn2;
-        else a.part_ml[prow] = make_float2(none ? -INFINITY : top2, l);
+        if (__any_sync(kFull, see < 32)) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (k >= see) x[k] = 0xFF800000u;
+        }
+        float mx = __uint_as_float(x[0]);
+#pragma unroll
+        for (int k = 1; k < 32; ++k) mx = fmaxf(mx, __uint_as_float(x[k]));
+        if (!raise_top<NSLAB>(st, mx, sl2, slack, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
+        const float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+        float2 sum = make_float2(0.f, 0.f);
+        weigh<T>(x, sl2, sub, sum, y);
+        st.l += sum.x + sum.y;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) zero[k] = 0;
+#pragma unroll
+        for (uint32_t c = 0; c < 4; ++c) {
+          if (c == warp) tmem_st16(s_at + 16 * c, y);
+          else tmem_st16(s_at + 16 * c, zero);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(bar_p);
       }
     }
-    tc_fence_before();
+    // the sums of the rows
+    const bool some = j0 < w.kv1;  // this half had a key tile
+    if (some && !mbar_wait(bar_o, (done - 1) & 1)) return false;
+    tc_fence_after();
+    const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
+    const bool first = w.kv0 == start.minor && w.qt == start.major && w.h == start.h && w.r == start.r;
+    const uint64_t prow0 = (uint64_t)(2 * blockIdx.x + (first ? 0 : 1)) * kRows;
+    const uint64_t orow0 = w.tok0 * a.n_q_heads + w.h * G;  // row (t, g) is orow0 + t * n_q_heads + g
+    if (mode != kColumnsApart) {
+      float top2 = st.top2<W>(sl2), l = st.l, f0 = 1.f, f1 = 0.f;
+      if (mode == kTilesApart) {
+        if (half == 1) sh.ml[tid] = make_float2(top2, l);
+        softmax_sync();
+        if (half == 0) {
+          const float2 other = sh.ml[tid];
+          const float m2 = fmaxf(top2, other.x);
+          f0 = top2 == -INFINITY ? 0.f : exp2_approx(top2 - m2);
+          f1 = other.x == -INFINITY ? 0.f : exp2_approx(other.x - m2);
+          top2 = m2;
+          l = l * f0 + (other.x == -INFINITY ? 0.f : other.y * f1);
+        }
+      }
+      if (active && (mode == kRowsApart || half == 0)) {
+        const bool none = top2 == -INFINITY;
+        const float inv = whole ? 1.f / l : 1.f;
+        f0 *= inv;
+        f1 *= inv;
+        const uint64_t at = orow0 + (uint64_t)t * a.n_q_heads + g, prow = prow0 + (mode == kRowsApart ? half * 128 : 0) + i;
+        const bool two = mode == kTilesApart && w.kv1 - w.kv0 > 1;
+#pragma unroll 1
+        for (int c = 0; c < NSLAB * 2; ++c) {
+          uint32_t x[32], z[32];
+          tmem_ld32(x, o_at + 32 * c);
+          if (two) tmem_ld32(z, tmem + o_col(1) + 32 * c);
+          tmem_wait_ld();
+          float o[32];
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            o[k] = f0 == 0.f ? 0.f : __uint_as_float(x[k]) * f0;
+            if (two && f1 != 0.f) o[k] = fmaf(__uint_as_float(z[k]), f1, o[k]);
+            if (none) o[k] = 0.f;
+          }
+          if (valid) {
+            if (whole) store_row<T>(a.out + 2 * at * D, o, 32 * c, D);
+            else store_part(a.part + prow * D, o, 32 * c, D);
+          }
+          __syncwarp();
+        }
+        if (valid) {
+          if (whole) a.lse[at] = none ? -INFINITY : (top2 + log2_approx(l)) * kLn2;
+          else a.part_ml[prow] = make_float2(top2, l);
+        }
+      }
+      tc_fence_before();
+      if (mode == kTilesApart) softmax_sync();  // half 1's sums have been read
+    } else {
+      // the eight partial rows of a row
+      const uint32_t rows = (w.m - w.token0(a)) * G, w8 = half * 4 + warp;
+      sh.ml[w8 * 32 + lane] = make_float2(st.top2<W>(sl2), st.l);
+      softmax_sync();
+      float top2 = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) top2 = fmaxf(top2, sh.ml[k * 32 + lane].x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float2 ml = sh.ml[k * 32 + lane];
+        if (ml.x != -INFINITY) l = fmaf(ml.y, exp2_approx(ml.x - top2), l);
+      }
+      const bool none = top2 == -INFINITY;
+      const float mine = st.top2<W>(sl2);
+      float f = mine == -INFINITY ? 0.f : exp2_approx(mine - top2);
+      if (whole && !none) f *= 1.f / l;
+      if (w8 == 0 && valid) {
+        if (whole) a.lse[orow0 + (uint64_t)t * a.n_q_heads + g] = none ? -INFINITY : (top2 + log2_approx(l)) * kLn2;
+        else a.part_ml[prow0 + lane] = make_float2(top2, l);
+      }
+      // columns at a time that fit the scratch: [8 warps][rows][cols], or
+      // [8][rows][32] where there are many rows
+      const uint32_t cols = rows <= 8 ? NSLAB * 64 : 32;
+      float* sums = reinterpret_cast<float*>(scratch);
+      for (uint32_t c0 = 0; c0 < NSLAB * 64; c0 += cols) {
+#pragma unroll 1
+        for (uint32_t c = 0; c < cols; c += 32) {
+          uint32_t x[32];
+          tmem_ld32(x, o_at + c0 + c);
+          tmem_wait_ld();
+          if (lane < rows) {
+            float4* to = reinterpret_cast<float4*>(sums + ((uint64_t)w8 * rows + lane) * cols + c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              // rotated by the row: the lanes' rows are whole multiples of the banks apart
+              const uint32_t at = (k + lane) & 7;
+              float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (f != 0.f)
+                y = make_float4(__uint_as_float(x[4 * k]) * f, __uint_as_float(x[4 * k + 1]) * f,
+                                __uint_as_float(x[4 * k + 2]) * f, __uint_as_float(x[4 * k + 3]) * f);
+              to[at] = y;
+            }
+          }
+          __syncwarp();
+        }
+        tc_fence_before();
+        softmax_sync();
+        for (uint32_t e = threadIdx.x; e < rows * (cols / 4); e += 256) {
+          const uint32_t row = e / (cols / 4), c4 = e % (cols / 4);
+          const uint32_t at = (c4 & ~7u) | ((c4 + row) & 7);
+          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float4 x = *reinterpret_cast<const float4*>(sums + ((uint64_t)k * rows + row) * cols + 4 * at);
+            y.x += x.x;
+            y.y += x.y;
+            y.z += x.z;
+            y.w += x.w;
+          }
+          const uint32_t col = c0 + 4 * c4;
+          if (col < D) {
+            if (whole) {
+              const uint64_t to = orow0 + (uint64_t)(w.token0(a) + row / G) * a.n_q_heads + row % G;
+              *reinterpret_cast<uint2*>(a.out + 2 * (to * D + col)) = make_uint2(W::pack(y.x, y.y), W::pack(y.z, y.w));
+            } else {
+              *reinterpret_cast<float4*>(a.part + (prow0 + row) * D + col) = y;
+            }
+          }
+        }
+        fence_async_shared();
+        softmax_sync();
+      }
+      if (threadIdx.x == 0) mbar_arrive(smem_u32(&sh.q_empty[1]));  // the scratch is the queries' again
+    }
   }
   return true;
 }
@@ -430,65 +606,136 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   constexpr uint32_t kQk = mma_desc(Weights<T>::kBf16, 128, kKeys, false);
   constexpr uint32_t kPv = mma_desc(Weights<T>::kBf16, 128, NSLAB * 64, true);
   const uint32_t lane = threadIdx.x & 31, tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
-  uint32_t item = 0;                 // ring tiles taken so far
-  uint32_t tiles[2] = {0, 0};        // query tiles of each half
-  uint32_t keys[2] = {0, 0};         // key tiles of each half
+  uint32_t item = 0;           // ring tiles before this query tile
+  uint32_t used[2] = {0, 0};   // query tiles of each region
+  uint32_t keys[2] = {0, 0};   // key tiles of each half
   auto full = [&](uint32_t i) { return mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1); };
   auto tile_at = [&](uint32_t i) { return ring + (i % Sh::kRing) * Sh::kTile; };
-  auto scores = [&](uint32_t half, uint32_t k_item) {
+  auto commit = [&](uint64_t& bar) {
+    if (lane == 0) mma_commit(smem_u32(&bar));
+  };
+  auto scores = [&](uint32_t half, uint32_t region, uint32_t k_item) {
     if (lane == 0) {
       for (uint32_t k = 0; k < steps; ++k) {
         const uint32_t off = (k / 4) * kSlabBytes + (k % 4) * 32;
-        mma_ss(tmem + s_col(half), tile_desc(q_smem + half * Sh::kTile + off, 16), tile_desc(tile_at(k_item) + off, 16), kQk, k > 0);
+        mma_ss(tmem + s_col(half), tile_desc(q_smem + region * Sh::kTile + off, 16), tile_desc(tile_at(k_item) + off, 16),
+               kQk, k > 0);
       }
       mma_commit(smem_u32(&sh.s_full[half]));
     }
   };
+  auto values = [&](uint32_t half, uint32_t v_item, bool add) {
+    if (!mbar_wait(smem_u32(&sh.p_full[half]), keys[half]++ & 1)) return false;
+    tc_fence_after();
+    if (lane == 0) {
+#pragma unroll
+      for (uint32_t k = 0; k < kKeys / 16; ++k)
+        mma_ts(tmem + o_col(half), tmem + s_col(half) + k * 8, tile_desc(tile_at(v_item) + k * 2048, kSlabBytes), kPv,
+               add || k > 0);
+      mma_commit(smem_u32(&sh.pv_done[half]));
+    }
+    return true;
+  };
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const uint32_t halves = w.rows - w.qt * kRows > 128 ? 2 : 1, L = w.kv1 - w.kv0;
-    for (uint32_t s = 0; s < halves; ++s) {
-      if (!mbar_wait(smem_u32(&sh.q_full[s]), tiles[s]++ & 1)) return false;
-      if (s == 0 && !full(item)) return false;
-      tc_fence_after();
-      scores(s, item);
-    }
-    if (lane == 0) mma_commit(smem_u32(&sh.empty[item % Sh::kRing]));
-    for (uint32_t j = 0; j < L; ++j, item += 2) {
-      const uint32_t v_item = item + 1, k_next = item + 2;
-      if (!full(v_item)) return false;
+    const int mode = w.mode(a);
+    const uint32_t L = w.kv1 - w.kv0;
+    // slots that hold no token may hold NaN: zero their values (their weights are zero)
+    auto clear_tail = [&](uint32_t j, uint32_t v_item) {
       const uint64_t first = (uint64_t)(w.kv0 + j) * kKeys;
-      if (first + kKeys > w.n) {
-        // slots that hold no token may hold NaN: zero their values (their weights are zero)
-        const uint32_t have = w.n > first ? (uint32_t)(w.n - first) : 0;
-        for (uint32_t i = have * (NSLAB * 8) + lane; i < kKeys * NSLAB * 8; i += 32) {
-          const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8);
-          const uint32_t at = tile_at(v_item) + (c / 8) * kSlabBytes + row * 128 + (c % 8) * 16;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
-        }
-        fence_async_shared();
-        __syncwarp();
+      if (first + kKeys <= w.n) return;
+      const uint32_t have = w.n > first ? (uint32_t)(w.n - first) : 0;
+      for (uint32_t i = have * (NSLAB * 8) + lane; i < kKeys * NSLAB * 8; i += 32) {
+        const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8);
+        const uint32_t at = tile_at(v_item) + (c / 8) * kSlabBytes + row * 128 + (c % 8) * 16;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
       }
-      for (uint32_t s = 0; s < halves; ++s) {
-        if (!mbar_wait(smem_u32(&sh.p_full[s]), keys[s]++ & 1)) return false;
+      fence_async_shared();
+      __syncwarp();
+    };
+    if (!mbar_wait(smem_u32(&sh.q_full[0]), used[0]++ & 1) || !full(item)) return false;
+    tc_fence_after();
+    scores(0, 0, item);
+    if (mode == kRowsApart) {
+      if (!mbar_wait(smem_u32(&sh.q_full[1]), used[1]++ & 1)) return false;
+      tc_fence_after();
+      scores(1, 1, item);
+      commit(sh.empty[item % Sh::kRing]);
+      if (L == 1) {
+        commit(sh.q_empty[0]);
+        commit(sh.q_empty[1]);
+      }
+      for (uint32_t j = 0; j < L; ++j) {
+        const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
+        if (!full(v_item)) return false;
+        clear_tail(j, v_item);
+        for (uint32_t s = 0; s < 2; ++s) {
+          if (!values(s, v_item, j > 0)) return false;
+          if (s == 1) commit(sh.empty[v_item % Sh::kRing]);
+          if (j + 1 < L) {
+            if (s == 0 && !full(k_next)) return false;
+            // in order after the product above, which reads the weights that these scores overwrite
+            scores(s, s, k_next);
+            if (j + 2 == L) commit(sh.q_empty[s]);
+          }
+        }
+        if (j + 1 < L) commit(sh.empty[k_next % Sh::kRing]);
+      }
+    } else {
+      commit(sh.empty[item % Sh::kRing]);
+      if (L > 1) {
+        if (!full(item + 2)) return false;
         tc_fence_after();
-        if (lane == 0) {
+        scores(1, 0, item + 2);
+        commit(sh.empty[(item + 2) % Sh::kRing]);
+      }
+      if (L <= 2) commit(sh.q_empty[0]);
+      for (uint32_t j = 0; j < L; ++j) {
+        const uint32_t v_item = item + 2 * j + 1, k_next = item + 2 * j + 4;
+        if (!full(v_item)) return false;
+        clear_tail(j, v_item);
+        if (!values(j & 1, v_item, j > 1)) return false;
+        commit(sh.empty[v_item % Sh::kRing]);
+        if (j + 2 < L) {
+          if (!full(k_next)) return false;
+          scores(j & 1, 0, k_next);
+          commit(sh.empty[k_next % Sh::kRing]);
+          if (j + 3 == L) commit(sh.q_empty[0]);
+        }
+      }
+    }
+    item += 2 * L;
+  }
+  return true;
+}
+
+// Queries by tensor copies, a tile ahead of the products.
+template <int NSLAB>
+__device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* mq,
+                                           const CUtensorMap* mq32, uint32_t q_smem, uint32_t (&loads)[2]) {
+  using Sh = TileShape<NSLAB>;
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t used[2] = {0, 0};
+  Walk w;
+  for (bool more = w.begin(a); more; more = w.next(a)) {
+    const int mode = w.mode(a);
+    const int tok = (int)(w.tok0 + w.token0(a));
+    // a region is the query rows' or, in half 1's place, the scratch of kColumnsApart
+    for (uint32_t s = 0; s < (mode == kTilesApart ? 1u : 2u); ++s) {
+      if (used[s] && !mbar_wait(smem_u32(&sh.q_empty[s]), (used[s] - 1) & 1)) return false;
+      ++used[s];
+      const uint32_t bar = smem_u32(&sh.q_full[s]), dst = q_smem + s * Sh::kTile;
+      if (lane == 0 && mode != kColumnsApart) {
+        mbar_expect(bar, NSLAB * a.tq * a.G * 128);
 #pragma unroll
-          for (uint32_t k = 0; k < kKeys / 16; ++k)
-            mma_ts(tmem + o_col(s), tmem + s_col(s) + k * 8, tile_desc(tile_at(v_item) + k * 2048, kSlabBytes), kPv,
-                   j > 0 || k > 0);
-          mma_commit(smem_u32(&sh.pv_done[s]));
-        }
-        if (j + 1 < L) {
-          if (s == 0 && !full(k_next)) return false;
-          // in order after the product above, which reads the weights these scores overwrite
-          scores(s, k_next);
-        }
+        for (int c = 0; c < NSLAB; ++c) tma_load_4d(dst + c * kSlabBytes, mq, bar, 64 * c, 0, (int)w.h, tok + (int)(s * a.tq));
+      } else if (lane == 0 && s == 0) {
+        mbar_expect(bar, 4 * NSLAB * a.tq32 * a.G * 128);
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int c = 0; c < NSLAB; ++c) tma_load_4d(dst + c * kSlabBytes + x * 4096, mq32, bar, 64 * c, 0, (int)w.h, tok);
       }
-      if (lane == 0) {
-        mma_commit(smem_u32(&sh.empty[v_item % Sh::kRing]));
-        if (j + 1 < L) mma_commit(smem_u32(&sh.empty[k_next % Sh::kRing]));
-      }
+      if (mode != kColumnsApart || s == 0) ++loads[s];
     }
   }
   return true;
@@ -533,11 +780,11 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
 }
 
 // The same for page sizes that are no multiple of 8 (a swizzled tile takes
-// copies of whole groups of 8 rows): 96 threads copy 16 bytes each.
+// copies of whole groups of 8 rows): 64 threads copy 16 bytes each.
 template <int NSLAB>
 __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, uint32_t ring) {
   using Sh = TileShape<NSLAB>;
-  const uint32_t tid = threadIdx.x - 288;
+  const uint32_t tid = (threadIdx.x & 31) + (threadIdx.x >= 352 ? 32 : 0);
   uint32_t issued = 0, landed = 0;
   auto land = [&](uint32_t upto) {
     fence_async_shared();
@@ -553,7 +800,7 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
         const char* src = kv == 0 ? a.kv.k : a.kv.v;
         const int64_t sp = kv == 0 ? a.kv.ks_page : a.kv.vs_page, ss = kv == 0 ? a.kv.ks_slot : a.kv.vs_slot;
         const int64_t head = w.h * (kv == 0 ? a.kv.ks_head : a.kv.vs_head);
-        for (uint32_t i = tid; i < kKeys * NSLAB * 8; i += 96) {
+        for (uint32_t i = tid; i < kKeys * NSLAB * 8; i += 64) {
           const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8);
           const uint64_t key = (uint64_t)j * kKeys + row;
           bool in = key < w.n && c * 8 < a.kv.D;
@@ -578,26 +825,31 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
 }
 
 template <typename T, int NSLAB, bool TMA>
-__global__ void __launch_bounds__(kTileThreads, 1) k_attn_tiles(const __grid_constant__ CUtensorMap mk,
-                                                                const __grid_constant__ CUtensorMap mv, AttnArgs a) {
+__global__ void __launch_bounds__(kTileThreads, 1)
+    k_attn_tiles(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                 const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mq32, const AttnArgs a) {
   using Sh = TileShape<NSLAB>;
-  extern __shared__ char smem_raw[];
-  __shared__ TileShared sh;
-  const uint32_t q_smem = (smem_u32(smem_raw) + 1023) & ~1023u, ring = q_smem + 2 * Sh::kTile;
+  extern __shared__ __align__(1024) char smem_raw[];
+  TileShared& sh = *reinterpret_cast<TileShared*>(smem_raw + Sh::kRest);
+  const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + Sh::kTile + kScratch;
   const uint32_t warp = threadIdx.x >> 5;
+  if (q_smem & 1023) {  // swizzled tiles start at whole groups of 8 rows
+    if (threadIdx.x == 0) report(a.status, PTC_ERR_CUDA);
+    return;
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < Sh::kRing; ++i) {
-      mbar_init(smem_u32(&sh.full[i]), TMA ? 1 : 96);
+      mbar_init(smem_u32(&sh.full[i]), TMA ? 1 : 64);
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&sh.q_full[i]), 128);
+      mbar_init(smem_u32(&sh.q_full[i]), 1);
+      mbar_init(smem_u32(&sh.q_empty[i]), 1);
       mbar_init(smem_u32(&sh.s_full[i]), 1);
       mbar_init(smem_u32(&sh.p_full[i]), 128);
       mbar_init(smem_u32(&sh.pv_done[i]), 1);
     }
     mbar_init(smem_u32(&sh.drain), 1);
-    sh.abort = 0;
     fence_mbar_init();
   }
   if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
@@ -606,37 +858,40 @@ __global__ void __launch_bounds__(kTileThreads, 1) k_attn_tiles(const __grid_con
   tc_fence_after();
   grid_dep_sync();
   const bool go = a.plan->ok != 0;
-  uint32_t issued = 0;
-  if (go) {
-    bool fine = true;
-    if (warp < 8) {
-      fine = softmax_role<T, NSLAB>(a, sh, q_smem, warp / 4);
+  bool fine = true;
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    if (go) fine = softmax_role<T, NSLAB>(a, sh, smem_raw + Sh::kTile, warp / 4);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    uint32_t issued = 0, loads[2] = {0, 0};
+    if (!go) {
     } else if (warp == 8) {
       fine = product_role<T, NSLAB>(a, sh, q_smem, ring);
       // every product and every arrival it owes is done before the CTA ends
       if ((threadIdx.x & 31) == 0) mma_commit(smem_u32(&sh.drain));
       __syncwarp();
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
-    } else if (TMA) {
-      if (warp == 9) fine = copy_role<NSLAB>(a, sh, &mk, &mv, ring, issued);
-    } else {
+    } else if (warp == 10) {
+      fine = query_role<NSLAB>(a, sh, &mq, &mq32, q_smem, loads);
+    } else if (!TMA) {
       fine = gather_role<NSLAB>(a, sh, ring);
+    } else if (warp == 9) {
+      fine = copy_role<NSLAB>(a, sh, &mk, &mv, ring, issued);
     }
     if (!fine) {
-      sh.abort = 1;
-      report(a.status, PTC_ERR_TIMEOUT);
+      // given up: let the copies in flight land
+      for (uint32_t i = issued > Sh::kRing ? issued - Sh::kRing : 0; i < issued; ++i)
+        (void)mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1);
+      for (int s = 0; s < 2; ++s)
+        if (loads[s]) (void)mbar_wait(smem_u32(&sh.q_full[s]), (loads[s] - 1) & 1);
+      if (!TMA) cp_async_wait<0>();
     }
   }
+  if (!fine) report(a.status, PTC_ERR_TIMEOUT);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (sh.abort && TMA && warp == 9) {
-    // given up: let the copies in flight land
-    for (uint32_t i = issued > Sh::kRing ? issued - Sh::kRing : 0; i < issued; ++i)
-      (void)mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1);
-  }
-  if (sh.abort && !TMA) cp_async_wait<0>();
-  __syncthreads();
   if (warp == 8) tmem_free(sh.tmem, 512);
 }
 
@@ -649,17 +904,17 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
   const uint32_t c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.kv.D;
   const uint64_t U = a.plan->units, C = a.ctas;
   const CtaStart s = a.plan->start[c];
-  if (s.u == U * (c + 1) / C || s.kv == 0) return;
+  if (s.u == U * (c + 1) / C || s.minor == 0) return;
   auto cta_of = [&](uint64_t u) { return (uint32_t)(((u + 1) * C - 1) / U); };
-  const uint64_t first = s.u - s.kv;
+  const uint64_t first = s.u - s.minor;
   const uint32_t c0 = cta_of(first);
   if (cta_of(s.u - 1) != c0) return;
   const uint64_t tok0 = a.tok_off[s.r];
-  const uint32_t m = (uint32_t)(a.tok_off[s.r + 1] - tok0), n = a.kv.kv_len[s.r], rows = m * a.G;
-  const uint32_t nkv = key_tiles(m, n, a.G, s.qt), c1 = cta_of(first + nkv - 1);
+  const uint32_t m = (uint32_t)(a.tok_off[s.r + 1] - tok0), n = a.kv.kv_len[s.r];
+  const uint32_t nkv = key_tiles(m, n, a.tq, s.major), c1 = cta_of(first + nkv - 1);
   for (uint32_t i = blockIdx.y * 32 + warp; i < blockIdx.y * 32 + 32; i += 8) {
-    const uint32_t row = s.qt * kRows + i;
-    if (row >= rows) break;
+    const uint32_t in = i & 127, t = s.major * 2 * a.tq + (i >> 7) * a.tq + in / a.G;
+    if (in >= a.tq * a.G || t >= m) continue;
     auto slot_row = [&](uint32_t x) {
       return (uint64_t)(2 * x + (x == c0 && a.plan->start[x].u != first ? 1 : 0)) * kRows + i;
     };
@@ -681,7 +936,7 @@ __global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
     }
     const bool none = top == -INFINITY;
     const float inv = none ? 0.f : 1.f / l;
-    const uint64_t at = (tok0 + row / a.G) * a.n_q_heads + s.h * a.G + row % a.G;
+    const uint64_t at = (tok0 + t) * a.n_q_heads + s.h * a.G + in % a.G;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (lane + 32 * k < D) reinterpret_cast<T*>(a.out)[at * D + lane + 32 * k] = static_cast<T>(o[k] * inv);
@@ -699,39 +954,6 @@ __device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float acc)
 #pragma unroll
   for (int i = 0; i < 8; ++i) acc = fmaf(to_f(x[i]), to_f(y[i]), acc);
   return acc;
-}
-
-// One thread a slot and key head: its weights over every row that sees it.
-template <typename T>
-__global__ void __launch_bounds__(128) k_attn_mass(AttnArgs a) {
-  grid_dep_sync();
-  if (!a.plan->ok) return;
-  const uint32_t h = blockIdx.y;
-  const uint64_t total = a.kv.page_off[a.kv.n_req] - a.kv.page_off[0];
-  const uint64_t slot = (uint64_t)blockIdx.x * 128 + threadIdx.x;
-  if (slot >= total * a.kv.B) return;
-  const uint64_t page_at = a.kv.page_off[0] + slot / a.kv.B;
-  const uint32_t r = req_search(a.kv.page_off, 0, a.kv.n_req - 1, page_at);
-  const int64_t j = (int64_t)((page_at - a.kv.page_off[r]) * a.kv.B + slot % a.kv.B);
-  const uint64_t at = h * a.mass_stride + page_at * a.kv.B + slot % a.kv.B;
-  const int64_t n = a.kv.kv_len[r], t0 = a.tok_off[r], m = (int64_t)a.tok_off[r + 1] - t0;
-  float sum = 0.f;
-  if (j < n) {
-    const uint32_t page = a.kv.page_ids[page_at];
-    if (page < a.kv.n_pages) {
-      const char* k = a.kv.k + 2 * (page * a.kv.ks_page + h * a.kv.ks_head + (j % a.kv.B) * a.kv.ks_slot);
-      for (int64_t i = j > n - m ? j - (n - m) : 0; i < m; ++i)
-        for (uint32_t g = 0; g < a.G; ++g) {
-          const char* q = a.q + 2 * ((t0 + i) * a.q_tok + (h * a.G + g) * a.q_head);
-          float s = 0.f;
-          for (uint32_t d = 0; d < a.kv.D; d += 8)
-            s = dot8<T>(*reinterpret_cast<const uint4*>(q + 2 * d), *reinterpret_cast<const uint4*>(k + 2 * d), s);
-          sum += expf(s * a.scale - a.lse[(t0 + i) * a.n_q_heads + h * a.G + g]);
-        }
-    }
-    if (a.mass_in) sum += a.mass_in[at];
-  }
-  a.mass_out[at] = sum;
 }
 
 // cuTensorMapEncodeTiled, from the driver that the runtime has loaded.
@@ -752,12 +974,9 @@ EncodeFn encoder() {
   return fn;
 }
 
-// The cache as [page][head][slot][d], read 64 columns by `box` slots at a time.
-bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_t page, int64_t head, int64_t slot,
-               uint32_t box) {
-  const cuuint64_t dims[4] = {kv.D, kv.B, kv.H, kv.n_pages};
-  const cuuint64_t strides[3] = {2 * (cuuint64_t)slot, 2 * (cuuint64_t)head, 2 * (cuuint64_t)page};
-  const cuuint32_t boxes[4] = {64, box, 1, 1}, steps[4] = {1, 1, 1, 1};
+bool encode(CUtensorMap* map, bool bf16, void* base, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3],
+            const cuuint32_t (&boxes)[4]) {
+  const cuuint32_t steps[4] = {1, 1, 1, 1};
   const EncodeFn fn = encoder();
   return fn && fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides,
                   boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -765,63 +984,94 @@ bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_
 }
 
 template <typename T, int NSLAB, bool TMA>
-ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
-  if (cudaFuncSetAttribute(k_attn_tiles<T, NSLAB, TMA>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           TileShape<NSLAB>::kSmem) != cudaSuccess)
-    return PTC_ERR_CUDA;
-  PTC_KERNEL("k_attn_tiles", s, (k_attn_tiles<T, NSLAB, TMA>), a.ctas, kTileThreads, TileShape<NSLAB>::kSmem, mk, mv, a);
+ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  if (!large_smem(k_attn_tiles<T, NSLAB, TMA>, TileShape<NSLAB>::kSmem, ready)) return PTC_ERR_CUDA;
+  PTC_KERNEL("k_attn_tiles", s, (k_attn_tiles<T, NSLAB, TMA>), a.ctas, kTileThreads, TileShape<NSLAB>::kSmem, m[0], m[1],
+             m[2], m[3], a);
   return PTC_OK;
 }
 
 template <typename T>
 ptc_status launch(AttnArgs& a, cudaStream_t s) {
-  PTC_KERNEL("k_attn_plan", s, k_attn_plan, 1, kPlanThreads, 0, a);
+  constexpr bool bf16 = Weights<T>::kBf16;
+  const bool by_tiles = a.mass_out && !a.scores && a.n_tok;  // the weights' own tiles
+  PTC_KERNEL("k_attn_plan", s, k_attn_plan, by_tiles ? 2 : 1, kPlanThreads, 0, a);
+  CUtensorMap m[4] = {};
+  bool tma = false;
   if (a.n_tok) {
-    CUtensorMap mk{}, mv{};
     // copies of whole groups of 8 rows that neither leave a page nor a tile
     a.box = 128;
     while (a.kv.B % a.box) a.box /= 2;
-    const bool tma = a.box >= 8 && a.kv.n_pages > 0;
-    if (tma && (!cache_map(&mk, a.kv, Weights<T>::kBf16, a.kv.k, a.kv.ks_page, a.kv.ks_head, a.kv.ks_slot, a.box) ||
-                !cache_map(&mv, a.kv, Weights<T>::kBf16, a.kv.v, a.kv.vs_page, a.kv.vs_head, a.kv.vs_slot, a.box)))
+    tma = a.box >= 8 && a.kv.n_pages > 0;
+    if (tma && (!cache_map(&m[0], a.kv, bf16, a.kv.k, a.kv.ks_page, a.kv.ks_head, a.kv.ks_slot, a.box) ||
+                !cache_map(&m[1], a.kv, bf16, a.kv.v, a.kv.vs_page, a.kv.vs_head, a.kv.vs_slot, a.box)))
       return PTC_ERR_CUDA;
-    const ptc_status st = a.kv.D > 64 ? (tma ? launch_tiles<T, 2, true>(a, mk, mv, s) : launch_tiles<T, 2, false>(a, mk, mv, s))
-                                      : (tma ? launch_tiles<T, 1, true>(a, mk, mv, s) : launch_tiles<T, 1, false>(a, mk, mv, s));
+    if (!tokens_map(&m[2], a, bf16, a.tq) || (a.tq32 && !tokens_map(&m[3], a, bf16, a.tq32))) return PTC_ERR_CUDA;
+    const ptc_status st = a.kv.D > 64 ? (tma ? launch_tiles<T, 2, true>(a, m, s) : launch_tiles<T, 2, false>(a, m, s))
+                                      : (tma ? launch_tiles<T, 1, true>(a, m, s) : launch_tiles<T, 1, false>(a, m, s));
     if (st != PTC_OK) return st;
     PTC_KERNEL("k_attn_join", s, k_attn_join<T>, dim3(a.ctas, kRows / 32), 256, 0, a);
   }
-  if (a.mass_out && a.kv.n_page_ids)
-    PTC_KERNEL("k_attn_mass", s, k_attn_mass<T>, dim3((uint32_t)((a.kv.n_page_ids * a.kv.B + 127) / 128), a.kv.H), 128,
-               0, a);
-  return PTC_OK;
+  return a.mass_out && a.kv.n_page_ids ? launch_mass(a, bf16, m[0], m[2], tma, s) : PTC_OK;
 }
 
-// Workspace: the status word, the plan, the unit offsets and the parts.
+// Workspace: the status word, the plans, the unit offsets, the parts, the scores.
 struct AttnWs {
-  size_t plan, units, ml, part, total;
+  size_t plan, units, ml, part, mass, scores, total;
 };
-AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D) {
+AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D, uint64_t scores) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   AttnWs w;
   w.plan = kKvStatusBytes;
-  w.units = w.plan + up(sizeof(AttnPlan));
-  w.ml = w.units + up((size_t)(n_req + 1) * 8);
+  w.units = w.plan + up(2 * sizeof(AttnPlan));
+  w.ml = w.units + up(2 * (size_t)(n_req + 1) * 8);
   w.part = w.ml + up((size_t)2 * ctas * kRows * 8);
-  w.total = w.part + up((size_t)2 * ctas * kRows * D * 4);
+  w.mass = w.part + up((size_t)2 * ctas * kRows * D * 4);
+  w.scores = w.mass + up((size_t)2 * ctas * kKeys * 4);
+  w.total = w.scores + up(scores * 4);
   return w;
 }
 uint32_t tile_ctas() {
-  const int n = num_sms();
-  return n < (int)kMaxCtas ? (uint32_t)n : kMaxCtas;
+  static const uint32_t n = [] {
+    const int x = num_sms();
+    return x < (int)kMaxCtas ? (uint32_t)x : kMaxCtas;
+  }();
+  return n;
+}
+// Scores kept for the weights: none without them or where requests have more rows.
+uint64_t kept_scores(uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t max_q_len, uint64_t mass_stride) {
+  const uint64_t rows = (uint64_t)max_q_len * (n_kv_heads ? n_q_heads / n_kv_heads : 0);
+  return rows <= kFewRows ? rows * n_kv_heads * mass_stride : 0;
 }
 
 }  // namespace
+
+// The cache as [page][head][slot][d], read 64 columns by `box` slots at a time.
+bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_t page, int64_t head, int64_t slot,
+               uint32_t box) {
+  const cuuint64_t dims[4] = {kv.D, kv.B, kv.H, kv.n_pages};
+  const cuuint64_t strides[3] = {2 * (cuuint64_t)slot, 2 * (cuuint64_t)head, 2 * (cuuint64_t)page};
+  const cuuint32_t boxes[4] = {64, box, 1, 1};
+  return encode(map, bf16, base, dims, strides, boxes);
+}
+
+// The queries as [token][key head][head of the group][d], read 64 columns by
+// `tokens` whole tokens of one key head at a time.
+bool tokens_map(CUtensorMap* map, const AttnArgs& a, bool bf16, uint32_t tokens) {
+  const cuuint64_t dims[4] = {a.kv.D, a.G, a.kv.H, a.n_tok};
+  const cuuint64_t strides[3] = {2 * (cuuint64_t)a.q_head, 2 * (cuuint64_t)a.q_head * a.G, 2 * (cuuint64_t)a.q_tok};
+  const cuuint32_t boxes[4] = {64, a.G, 1, tokens};
+  return encode(map, bf16, const_cast<char*>(a.q), dims, strides, boxes);
+}
+
 }  // namespace ptc
 
 using namespace ptc;
 
-extern "C" size_t ptc_paged_attention_workspace_bytes(uint32_t n_req, uint64_t, uint32_t, uint32_t, uint32_t head_dim) {
-  return attn_ws(n_req, tile_ctas(), head_dim).total;
+extern "C" size_t ptc_paged_attention_workspace_bytes(uint32_t n_req, uint32_t n_q_heads, uint32_t n_kv_heads,
+                                                      uint32_t head_dim, uint32_t max_q_len, uint64_t mass_stride) {
+  return attn_ws(n_req, tile_ctas(), head_dim, kept_scores(n_q_heads, n_kv_heads, max_q_len, mass_stride)).total;
 }
 
 extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q, const int64_t q_stride[2],
@@ -833,12 +1083,15 @@ extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q,
   const ptc_status st = kv_view(kv, &a.kv);
   if (st != PTC_OK) return st;
   if (!tok_off || !q_stride || n_q_heads < 1 || n_q_heads % kv->n_kv_heads) return PTC_ERR_INVALID_ARG;
+  if (n_q_heads / kv->n_kv_heads > kMaxGroup) return PTC_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale) || (n_tok && !kv->n_req)) return PTC_ERR_INVALID_ARG;
-  if (n_tok > (uint64_t(1) << 31) || n_tok * n_q_heads > (uint64_t(1) << 31) || kv->n_page_ids * kv->block_size > (uint64_t(1) << 38))
+  if (!std::isfinite(scale * kLog2e)) return PTC_ERR_INVALID_ARG;
+  if (n_tok > 0x7FFFFFFFu || n_tok * n_q_heads > (uint64_t(1) << 31) || kv->n_page_ids * kv->block_size > (uint64_t(1) << 38))
     return PTC_ERR_OVERFLOW;
   if (mass_out ? mass_stride / kv->block_size < kv->n_page_ids : mass_in != nullptr) return PTC_ERR_INVALID_ARG;
   if (kv->n_pages > 0x7FFFFFFFu) return PTC_ERR_OVERFLOW;  // tensor copies have signed coordinates
-  const AttnWs at = attn_ws(kv->n_req, tile_ctas(), kv->head_dim);
+  const uint64_t scores = mass_out ? kept_scores(n_q_heads, kv->n_kv_heads, max_q_len, mass_stride) : 0;
+  const AttnWs at = attn_ws(kv->n_req, tile_ctas(), kv->head_dim, scores);
   if (!ws_ok(ws, ws_bytes, at.total)) return PTC_ERR_WORKSPACE;
   if (kv->n_req == 0) return PTC_OK;
   if (n_tok && (!aligned16(q) || !aligned16(out) || !lse)) return PTC_ERR_INVALID_ARG;
@@ -854,6 +1107,8 @@ extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q,
   a.n_q_heads = n_q_heads;
   a.G = n_q_heads / kv->n_kv_heads;
   a.max_q_len = max_q_len;
+  a.tq = 128 / a.G;
+  a.tq32 = 32 / a.G;
   a.scale = scale;
   a.out = static_cast<char*>(out);
   a.lse = lse;
@@ -866,6 +1121,9 @@ extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q,
   a.unit_off = reinterpret_cast<uint64_t*>(w + at.units);
   a.part_ml = reinterpret_cast<float2*>(w + at.ml);
   a.part = reinterpret_cast<float*>(w + at.part);
+  a.part_mass = reinterpret_cast<float*>(w + at.mass);
+  a.scores = scores && n_tok ? reinterpret_cast<float*>(w + at.scores) : nullptr;
+  a.few = max_q_len * a.G;
   if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
   const ptc_status run = kv->dtype == PTC_DTYPE_BF16 ? launch<__nv_bfloat16>(a, s) : launch<__half>(a, s);
   if (run != PTC_OK) return run;

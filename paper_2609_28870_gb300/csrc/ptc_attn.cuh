@@ -1,0 +1,97 @@
+// Attention over pages: what its kernels share (ptc_attn.cu: plan, tiles,
+// join, the C entry point; ptc_mass.cu: the accumulated weights).
+#pragma once
+
+#include <atomic>
+
+#include "ptc_kv.cuh"
+#include "ptc_tc.cuh"
+
+namespace ptc {
+
+// The G query heads of a key head are packed as rows of one matrix, token by
+// token, so that a key tile is read once for all of them.  128 rows hold
+// tq = 128 / G whole tokens; a query tile is two such halves.
+constexpr uint32_t kRows = 256, kKeys = 128;
+constexpr uint32_t kMaxGroup = PTC_MAX_GROUP;
+constexpr uint32_t kMaxCtas = 512;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Where a CTA starts: its first unit, and what that is: for the tile kernel
+// the key tile `minor` of query tile `major`, for the weights the query tile
+// `minor` (after the first one that sees it) of key tile `major`.
+struct CtaStart {
+  uint64_t u;
+  uint32_t r, h, major, minor;
+};
+
+// What k_attn_plan leaves for the kernels after it.  Their work is a row of
+// units, for every request and key head its pairs of a query tile and a key
+// tile; CTA c of C takes the units [U c / C, U (c + 1) / C).
+struct AttnPlan {
+  uint32_t ok, pad;
+  uint64_t units;
+  CtaStart start[kMaxCtas];
+};
+
+struct AttnArgs {
+  KvView kv;
+  const char* q;
+  int64_t q_tok, q_head;
+  const uint64_t* tok_off;
+  uint64_t n_tok;
+  uint32_t n_q_heads, G, max_q_len;
+  uint32_t tq, tq32;   // whole tokens in 128 and in 32 rows
+  float scale;
+  char* out;
+  float* lse;
+  const float* mass_in;
+  float* mass_out;
+  uint64_t mass_stride;
+  AttnPlan* plan;      // [0] tiles, [1] weights
+  uint64_t* unit_off;  // [0] and [1]: n_req + 1
+  float* part;         // unnormalised rows of split tiles: [2 * ctas][kRows][D]
+  float2* part_ml;     // their maxima (in powers of two) and sums
+  float* part_mass;    // weights of split key tiles: [2 * ctas][kKeys]
+  float* scores;       // scores of few rows, [n_kv_heads][few][slots], or null
+  uint32_t few;
+  uint32_t ctas, box;  // box: rows of a tensor copy of keys or values
+  uint32_t* status;
+};
+
+__host__ __device__ __forceinline__ uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
+
+// Query tiles of a request, and the key tiles that one of them sees, at least one.
+__device__ __forceinline__ uint32_t query_tiles(uint32_t m, uint32_t tq) { return div_up(m, 2 * tq); }
+__device__ __forceinline__ uint32_t key_tiles(uint32_t m, uint32_t n, uint32_t tq, uint32_t qt) {
+  const uint32_t end = (qt + 1) * 2 * tq < m ? (qt + 1) * 2 * tq : m;
+  const int64_t sees = (int64_t)n - m + end;
+  return sees <= (int64_t)kKeys ? 1u : (uint32_t)((sees + kKeys - 1) / kKeys);
+}
+// The first half tile of queries that sees anything of key tile kt.
+__device__ __forceinline__ uint32_t first_seeing(uint32_t m, uint32_t n, uint32_t tq, uint32_t kt) {
+  const int64_t t = (int64_t)kt * kKeys - ((int64_t)n - m);
+  return t <= 0 ? 0u : (uint32_t)t / tq;
+}
+
+// Host side (ptc_attn.cu, ptc_mass.cu).
+// Lets a kernel have `bytes` of dynamic shared memory, once on every device.
+template <typename F>
+bool large_smem(F* kernel, int bytes, std::atomic<uint64_t>& ready) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (ready.load(std::memory_order_relaxed) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  ready.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
+bool tokens_map(CUtensorMap* map, const AttnArgs& a, bool bf16, uint32_t tokens);
+bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_t page, int64_t head, int64_t slot,
+               uint32_t box);
+// Most rows of a request whose scores are kept for the weights; see ptc_mass.cu.
+constexpr uint32_t kFewRows = 16;
+ptc_status launch_mass(const AttnArgs& a, bool bf16, const CUtensorMap& mk, const CUtensorMap& mq, bool tma,
+                       cudaStream_t s);
+
+}  // namespace ptc

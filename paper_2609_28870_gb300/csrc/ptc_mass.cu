@@ -1,0 +1,458 @@
+// Accumulated attention weights (ptc_paged_attention with mass_out): for every
+// cached token and key head the sum of its weights over the call's queries,
+//   sum over rows i of exp2(scale log2(e) s_ij - log2(e) lse_i),
+// once the rows' lse are known.  Two ways:
+//   few rows    requests of up to kFewRows rows (single tokens): the tile
+//               kernel leaves the scores, 4 bytes a row, token and key head,
+//               and one pass adds them up.  Reading the keys again would be 2 D
+//               bytes a token and key head: 256 at D = 128, against 8 a row
+//               written and read.
+//   many rows   the scores are computed again, transposed: one thread a token
+//               adds up its column of rows without a word to its neighbours.
+#include <type_traits>
+
+#include "ptc_attn.cuh"
+
+namespace ptc {
+namespace {
+
+// ------------------------------------------------------------------ few rows
+constexpr int kRowThreads = 256;
+constexpr uint32_t kRowSlots = 4 * kRowThreads;
+
+__global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
+  grid_dep_sync();
+  if (!a.plan->ok) return;
+  __shared__ uint32_t s_r;
+  const uint32_t R = a.kv.n_req, B = a.kv.B, h = blockIdx.y;
+  const uint64_t first = a.kv.page_off[0] * B, end = a.kv.page_off[R] * B;
+  const uint64_t s0 = first + (uint64_t)blockIdx.x * kRowSlots;
+  if (s0 >= end) return;
+  if (threadIdx.x == 0) s_r = req_search(a.kv.page_off, 0, R - 1, s0 / B);
+  __syncthreads();
+  uint32_t r = s_r;
+  const bool four = B % 4 == 0 && a.mass_stride % 4 == 0 && (((uintptr_t)a.mass_in | (uintptr_t)a.mass_out) & 15) == 0;
+  const uint32_t width = four ? 4 : 1;
+  for (uint32_t pass = 0; pass < 4 / width; ++pass) {
+    const uint64_t slot = s0 + ((uint64_t)pass * kRowThreads + threadIdx.x) * width;
+    if (slot >= end) return;
+    while (r + 1 < R && a.kv.page_off[r + 1] * B <= slot) ++r;
+    const int64_t j = (int64_t)(slot - a.kv.page_off[r] * B), n = a.kv.kv_len[r];
+    const uint64_t tok0 = a.tok_off[r];
+    const int64_t m = (int64_t)(a.tok_off[r + 1] - tok0);
+    const uint64_t at = h * a.mass_stride + slot;
+    const float* score = a.scores + (uint64_t)h * a.few * a.mass_stride + slot;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (j < n) {
+      const float sl2 = a.scale * kLog2e;
+      const int64_t sees0 = n - m + 1;  // keys that the first token sees
+      for (uint32_t i = 0; i < (uint32_t)m * a.G; ++i) {
+        const int64_t sees = sees0 + i / a.G;
+        if (j >= sees) continue;
+        const float off = a.lse[(tok0 + i / a.G) * a.n_q_heads + h * a.G + i % a.G] * kLog2e;
+        float x[4];
+        if (four) {
+          // what lies past the row's last key is not used
+          const float4 y = *reinterpret_cast<const float4*>(score + i * a.mass_stride);
+          x[0] = y.x;
+          x[1] = y.y;
+          x[2] = y.z;
+          x[3] = y.w;
+        } else {
+          x[0] = score[i * a.mass_stride];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if ((uint32_t)k < width && j + k < sees) sum[k] += exp2_approx(fmaf(x[k], sl2, -off));
+      }
+    }
+    if (four) {
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (j < n && a.mass_in) o = *reinterpret_cast<const float4*>(a.mass_in + at);
+      o.x = j < n ? o.x + sum[0] : 0.f;
+      o.y = j + 1 < n ? o.y + sum[1] : 0.f;
+      o.z = j + 2 < n ? o.z + sum[2] : 0.f;
+      o.w = j + 3 < n ? o.w + sum[3] : 0.f;
+      *reinterpret_cast<float4*>(a.mass_out + at) = o;
+    } else {
+      a.mass_out[at] = j < n ? (a.mass_in ? a.mass_in[at] : 0.f) + sum[0] : 0.f;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ many rows
+// One CTA an SM walks its units, (key tile, half a query tile) pairs.  Scores
+// transposed, S = K Q^T: 128 keys in the lanes of tensor memory, up to 128
+// query rows in its columns, four such products in turn.  Warps 0-3 and 4-7 take
+// products in turn and add up exp2(s - lse) along a row of S, which is a
+// column of the scores; warp 8 issues the products, warp 9 loads key tiles
+// (with warp 11 where there are no tensor copies), warp 10 queries.
+constexpr int kMassThreads = 384;
+constexpr int kSlab = 128 * 128;
+
+template <int NSLAB>
+struct MassShape {
+  static constexpr int kTile = NSLAB * kSlab;
+  static constexpr int kSmem = 6 * kTile + 1024;  // 2 key tiles, 4 query tiles
+};
+
+struct MassShared {
+  uint64_t k_full[2], k_empty[2], q_full[4], q_empty[4], s_full[4], s_empty[4], drain;
+  float lse[2][2][128];  // negated, in powers of two: of either half, two units
+  float sum[2][128];
+  uint32_t tmem;
+};
+
+struct MassWalk {
+  uint64_t left, tok0, page0;
+  uint32_t r, h, kt, q0, q1;  // half query tiles [q0, q1)
+  uint32_t first, count;      // the first one that sees the key tile, and how many do
+  uint32_t m, n;
+  __device__ __forceinline__ void request(const AttnArgs& a) {
+    tok0 = a.tok_off[r];
+    m = (uint32_t)(a.tok_off[r + 1] - tok0);
+    n = a.kv.kv_len[r];
+    page0 = a.kv.page_off[r];
+  }
+  __device__ __forceinline__ void part(const AttnArgs& a, uint32_t minor) {
+    first = first_seeing(m, n, a.tq, kt);
+    count = div_up(m, a.tq) - first;
+    q0 = first + minor;
+    q1 = count - minor > left ? q0 + (uint32_t)left : first + count;
+  }
+  __device__ __forceinline__ bool begin(const AttnArgs& a) {
+    const AttnPlan* p = a.plan + 1;
+    const uint64_t U = p->units, c = blockIdx.x;
+    const CtaStart s = p->start[c];
+    left = U * (c + 1) / a.ctas - s.u;
+    if (left == 0) return false;
+    r = s.r;
+    h = s.h;
+    kt = s.major;
+    request(a);
+    part(a, s.minor);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const AttnArgs& a) {
+    left -= q1 - q0;
+    if (left == 0) return false;
+    if ((uint64_t)++kt * kKeys >= n) {
+      kt = 0;
+      if (++h == a.kv.H) {
+        h = 0;
+        do {
+          if (++r == a.kv.n_req) return false;
+          request(a);
+        } while (m == 0 || n == 0);
+      }
+    }
+    part(a, 0);
+    return true;
+  }
+  __device__ __forceinline__ uint32_t rows(const AttnArgs& a, uint32_t q) const {
+    const uint32_t t = m - q * a.tq;
+    return (t < a.tq ? t : a.tq) * a.G;
+  }
+};
+
+__device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uint32_t half) {
+  const uint32_t tid = threadIdx.x & 127;
+  const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
+  const float sl2 = a.scale * kLog2e;
+  uint32_t unit = 0, mine = 0, seg = 0;
+  MassWalk w;
+  for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
+    const uint64_t key = (uint64_t)w.kt * kKeys + tid;
+    const int64_t t_first = (int64_t)key - ((int64_t)w.n - w.m);  // the first token that sees the key
+    // lse of a query tile's row `tid`; rows that are none count nothing below
+    auto lse_of = [&](uint32_t q) {
+      const uint32_t rows = w.rows(a, q);
+      if (tid >= rows) return 0.f;
+      const uint64_t t = w.tok0 + (uint64_t)q * a.tq + tid / a.G;
+      return -kLog2e * a.lse[t * a.n_q_heads + w.h * a.G + tid % a.G];
+    };
+    uint32_t q = w.q0 + ((unit & 1) == half ? 0 : 1);
+    float ahead = q < w.q1 ? lse_of(q) : 0.f, total = 0.f;
+    for (; q < w.q1; q += 2, ++mine) {
+      const uint32_t u = unit + (q - w.q0), buf = u & 3;
+      float* lse = sh.lse[half][mine & 1];
+      lse[tid] = ahead;
+      asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
+      if (q + 2 < w.q1) ahead = lse_of(q + 2);
+      if (!mbar_wait(smem_u32(&sh.s_full[buf]), (u >> 2) & 1)) return false;
+      tc_fence_after();
+      const uint32_t rows = w.rows(a, q);
+      const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G;
+      const int lo = lo64 <= 0 ? 0 : lo64 >= 128 ? 128 : (int)lo64, hi = (int)rows;
+      const bool masked = __any_sync(kFull, lo > 0 || (hi & 31));
+      float2 sum = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int c = 0; c < hi; c += 32) {
+        uint32_t x[32];
+        tmem_ld32(x, tmem + buf * 128 + c);
+        tmem_wait_ld();
+        const float2* off = reinterpret_cast<const float2*>(lse + c);
+        if (!masked) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float2 e = fma2(make_float2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])),
+                                  make_float2(sl2, sl2), off[k]);
+            sum = add2(sum, make_float2(exp2_approx(e.x), exp2_approx(e.y)));
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const float e = exp2_approx(fmaf(__uint_as_float(x[k]), sl2, lse[c + k]));
+            if (c + k >= lo && c + k < hi) sum.x += e;
+          }
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(smem_u32(&sh.s_empty[buf]));
+      total += sum.x + sum.y;
+    }
+    unit += w.q1 - w.q0;
+    if (half == 1) sh.sum[seg & 1][tid] = total;
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (half == 0) {
+      total += sh.sum[seg & 1][tid];
+      if (w.q0 == w.first && w.q1 == w.first + w.count) {
+        if (key < w.n) {
+          const uint64_t at = w.h * a.mass_stride + w.page0 * a.kv.B + key;
+          a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + total;
+        }
+      } else {
+        a.part_mass[(2 * (uint64_t)blockIdx.x + (seg == 0 ? 0 : 1)) * kKeys + tid] = total;
+      }
+    }
+  }
+  return true;
+}
+
+template <typename T, int NSLAB>
+__device__ __forceinline__ bool mass_products(const AttnArgs& a, MassShared& sh, uint32_t smem) {
+  using Sh = MassShape<NSLAB>;
+  constexpr bool bf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+  const uint32_t lane = threadIdx.x & 31, tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
+  uint32_t unit = 0, seg = 0;
+  MassWalk w;
+  for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
+    const uint32_t k_at = smem + (seg & 1) * Sh::kTile;
+    if (!mbar_wait(smem_u32(&sh.k_full[seg & 1]), (seg >> 1) & 1)) return false;
+    for (uint32_t q = w.q0; q < w.q1; ++q, ++unit) {
+      const uint32_t buf = unit & 3, q_at = smem + (2 + buf) * Sh::kTile;
+      if (!mbar_wait(smem_u32(&sh.q_full[buf]), (unit >> 2) & 1)) return false;
+      if (unit >= 4 && !mbar_wait(smem_u32(&sh.s_empty[buf]), ((unit >> 2) - 1) & 1)) return false;
+      tc_fence_after();
+      if (lane == 0) {
+        const uint32_t desc = mma_desc(bf16, 128, (w.rows(a, q) + 15) & ~15u, false);
+        for (uint32_t k = 0; k < steps; ++k) {
+          const uint32_t off = (k / 4) * kSlab + (k % 4) * 32;
+          mma_ss(tmem + buf * 128, tile_desc(k_at + off, 16), tile_desc(q_at + off, 16), desc, k > 0);
+        }
+        mma_commit(smem_u32(&sh.s_full[buf]));
+        mma_commit(smem_u32(&sh.q_empty[buf]));
+        if (q + 1 == w.q1) mma_commit(smem_u32(&sh.k_empty[seg & 1]));
+      }
+      __syncwarp();
+    }
+  }
+  return true;
+}
+
+template <int NSLAB>
+__device__ __forceinline__ bool mass_queries(const AttnArgs& a, MassShared& sh, const CUtensorMap* mq, uint32_t smem,
+                                             uint32_t& unit) {
+  using Sh = MassShape<NSLAB>;
+  const uint32_t lane = threadIdx.x & 31;
+  MassWalk w;
+  for (bool more = w.begin(a); more; more = w.next(a))
+    for (uint32_t q = w.q0; q < w.q1; ++q, ++unit) {
+      const uint32_t buf = unit & 3, bar = smem_u32(&sh.q_full[buf]), dst = smem + (2 + buf) * Sh::kTile;
+      if (unit >= 4 && !mbar_wait(smem_u32(&sh.q_empty[buf]), ((unit >> 2) - 1) & 1)) return false;
+      if (lane == 0) {
+        mbar_expect(bar, NSLAB * a.tq * a.G * 128);
+#pragma unroll
+        for (int c = 0; c < NSLAB; ++c)
+          tma_load_4d(dst + c * kSlab, mq, bar, 64 * c, 0, (int)w.h, (int)(w.tok0 + (uint64_t)q * a.tq));
+      }
+      __syncwarp();
+    }
+  return true;
+}
+
+// Key tiles, by tensor copies (one warp) or 16 bytes at a time (two).  Pages
+// that the cache does not have were reported by the tile kernel.
+template <int NSLAB, bool TMA>
+__device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, const CUtensorMap* mk, uint32_t smem,
+                                          uint32_t& seg) {
+  using Sh = MassShape<NSLAB>;
+  const uint32_t lane = threadIdx.x & 31;
+  const uint32_t tid = lane + (threadIdx.x >= 352 ? 32 : 0);
+  MassWalk w;
+  for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
+    const uint32_t at = seg & 1, bar = smem_u32(&sh.k_full[at]), dst = smem + at * Sh::kTile;
+    const uint32_t* ids = a.kv.page_ids + w.page0;
+    if (seg >= 2 && !mbar_wait(smem_u32(&sh.k_empty[at]), ((seg >> 1) - 1) & 1)) return false;
+    if constexpr (TMA) {
+      const uint32_t boxes = kKeys / a.box;
+      const uint64_t key = (uint64_t)w.kt * kKeys + lane * a.box;
+      int page = (int)a.kv.n_pages, slot = 0;
+      if (lane < boxes && key < w.n) {
+        const uint32_t id = __ldg(ids + key / a.kv.B);
+        if (id < a.kv.n_pages) page = (int)id;
+        slot = (int)(key % a.kv.B);
+      }
+      if (lane == 0) mbar_expect(bar, Sh::kTile);
+      __syncwarp();
+      if (lane < boxes)
+#pragma unroll
+        for (int s = 0; s < NSLAB; ++s) tma_load_4d(dst + s * kSlab + lane * a.box * 128, mk, bar, 64 * s, slot, (int)w.h, page);
+    } else {
+      for (uint32_t i = tid; i < kKeys * NSLAB * 8; i += 64) {
+        const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8);
+        const uint64_t key = (uint64_t)w.kt * kKeys + row;
+        bool in = key < w.n && c * 8 < a.kv.D;
+        const char* p = a.kv.k;
+        if (in) {
+          const uint32_t id = __ldg(ids + key / a.kv.B);
+          in = id < a.kv.n_pages;
+          if (in)
+            p += 2 * (id * a.kv.ks_page + w.h * a.kv.ks_head + (int64_t)(key % a.kv.B) * a.kv.ks_slot + c * 8);
+        }
+        cp_async16(dst + (c / 8) * kSlab + row * 128 + (((c % 8) ^ (row & 7)) * 16), p, in);
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_async_shared();
+      mbar_arrive(bar);
+    }
+  }
+  return true;
+}
+
+template <typename T, int NSLAB, bool TMA>
+__global__ void __launch_bounds__(kMassThreads, 1)
+    k_mass_tiles(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mq, const AttnArgs a) {
+  extern __shared__ char smem_raw[];
+  __shared__ MassShared sh;
+  const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
+  const uint32_t warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.k_full[i]), TMA ? 1 : 64);
+      mbar_init(smem_u32(&sh.k_empty[i]), 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&sh.q_full[i]), 1);
+      mbar_init(smem_u32(&sh.q_empty[i]), 1);
+      mbar_init(smem_u32(&sh.s_full[i]), 1);
+      mbar_init(smem_u32(&sh.s_empty[i]), 128);
+    }
+    mbar_init(smem_u32(&sh.drain), 1);
+    fence_mbar_init();
+  }
+  if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  grid_dep_sync();
+  bool fine = true;
+  if (a.plan[1].ok) {
+    uint32_t segs = 0, units = 0;
+    if (warp < 8) {
+      fine = mass_sums(a, sh, warp / 4);
+    } else if (warp == 8) {
+      fine = mass_products<T, NSLAB>(a, sh, smem);
+      // every product and every arrival it owes is done before the CTA ends
+      if ((threadIdx.x & 31) == 0) mma_commit(smem_u32(&sh.drain));
+      __syncwarp();
+      fine &= mbar_wait(smem_u32(&sh.drain), 0);
+    } else if (warp == 10) {
+      fine = mass_queries<NSLAB>(a, sh, &mq, smem, units);
+      if (!fine)  // given up: let the copies in flight land
+        for (uint32_t u = units > 4 ? units - 4 : 0; u < units; ++u)
+          (void)mbar_wait(smem_u32(&sh.q_full[u & 3]), (u >> 2) & 1);
+    } else if (warp == 9 || !TMA) {
+      fine = mass_keys<NSLAB, TMA>(a, sh, &mk, smem, segs);
+      if (!fine && TMA)
+        for (uint32_t k = segs > 2 ? segs - 2 : 0; k < segs; ++k)
+          (void)mbar_wait(smem_u32(&sh.k_full[k & 1]), (k >> 1) & 1);
+    }
+  }
+  if (!fine) report(a.status, PTC_ERR_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) tmem_free(sh.tmem, 512);
+}
+
+// blockIdx.y = 0: the key tiles that CTAs of the kernel above share, as
+// k_attn_join does it for query tiles.  1: what no unit covers, the slots
+// past every request's tokens and the requests without queries.
+__global__ void __launch_bounds__(128) k_mass_join(const AttnArgs a) {
+  grid_dep_sync();
+  const AttnPlan* plan = a.plan + 1;
+  if (!plan->ok) return;
+  const uint32_t c = blockIdx.x, tid = threadIdx.x;
+  if (blockIdx.y == 1) {
+    for (uint64_t p = c; p < (uint64_t)a.kv.n_req * a.kv.H; p += gridDim.x) {
+      const uint32_t r = (uint32_t)(p / a.kv.H), h = (uint32_t)(p % a.kv.H);
+      const uint64_t at = h * a.mass_stride + a.kv.page_off[r] * a.kv.B, n = a.kv.kv_len[r];
+      const uint64_t room = (a.kv.page_off[r + 1] - a.kv.page_off[r]) * a.kv.B;
+      for (uint64_t j = (a.tok_off[r] == a.tok_off[r + 1] ? 0 : n) + tid; j < room; j += 128)
+        a.mass_out[at + j] = j < n && a.mass_in ? a.mass_in[at + j] : 0.f;
+    }
+    return;
+  }
+  const uint64_t U = plan->units, C = a.ctas;
+  const CtaStart s = plan->start[c];
+  if (s.u == U * (c + 1) / C || s.minor == 0) return;
+  auto cta_of = [&](uint64_t u) { return (uint32_t)(((u + 1) * C - 1) / U); };
+  const uint64_t first = s.u - s.minor;
+  const uint32_t c0 = cta_of(first);
+  if (cta_of(s.u - 1) != c0) return;
+  const uint32_t m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]), n = a.kv.kv_len[s.r];
+  const uint32_t c1 = cta_of(first + div_up(m, a.tq) - first_seeing(m, n, a.tq, s.major) - 1);
+  const uint64_t key = (uint64_t)s.major * kKeys + tid;
+  if (key >= n) return;
+  float sum = 0.f;
+  for (uint32_t x = c0; x <= c1; ++x) {
+    if (U * x / C == U * (x + 1) / C) continue;
+    sum += a.part_mass[(2 * (uint64_t)x + (x == c0 && plan->start[x].u != first ? 1 : 0)) * kKeys + tid];
+  }
+  const uint64_t at = s.h * a.mass_stride + a.kv.page_off[s.r] * a.kv.B + key;
+  a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum;
+}
+
+template <typename T, int NSLAB, bool TMA>
+ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap& mk, const CUtensorMap& mq, cudaStream_t s) {
+  static std::atomic<uint64_t> ready{0};
+  if (!large_smem(k_mass_tiles<T, NSLAB, TMA>, MassShape<NSLAB>::kSmem, ready)) return PTC_ERR_CUDA;
+  PTC_KERNEL("k_mass_tiles", s, (k_mass_tiles<T, NSLAB, TMA>), a.ctas, kMassThreads, MassShape<NSLAB>::kSmem, mk, mq, a);
+  return PTC_OK;
+}
+
+template <typename T>
+ptc_status launch_by_tiles(const AttnArgs& a, const CUtensorMap& mk, const CUtensorMap& mq, bool tma, cudaStream_t s) {
+  if (a.kv.D > 64) return tma ? launch_tiles<T, 2, true>(a, mk, mq, s) : launch_tiles<T, 2, false>(a, mk, mq, s);
+  return tma ? launch_tiles<T, 1, true>(a, mk, mq, s) : launch_tiles<T, 1, false>(a, mk, mq, s);
+}
+
+}  // namespace
+
+ptc_status launch_mass(const AttnArgs& a, bool bf16, const CUtensorMap& mk, const CUtensorMap& mq, bool tma,
+                       cudaStream_t s) {
+  if (a.scores || a.n_tok == 0) {
+    const uint64_t slots = a.kv.n_page_ids * a.kv.B;
+    PTC_KERNEL("k_mass_rows", s, k_mass_rows, dim3((uint32_t)((slots + kRowSlots - 1) / kRowSlots), a.kv.H), kRowThreads, 0,
+               a);
+    return PTC_OK;
+  }
+  const ptc_status st = bf16 ? launch_by_tiles<__nv_bfloat16>(a, mk, mq, tma, s) : launch_by_tiles<__half>(a, mk, mq, tma, s);
+  if (st != PTC_OK) return st;
+  PTC_KERNEL("k_mass_join", s, k_mass_join, dim3(a.ctas, 2), 128, 0, a);
+  return PTC_OK;
+}
+
+}  // namespace ptc

@@ -49,7 +49,7 @@ def declare(L) -> None:
     L.ptc_kv_append.restype = st
     L.ptc_kv_append.argtypes = [kv, vp, vp, _Strides, _Strides, vp, u64, vp, sz, vp, vp]
     L.ptc_paged_attention_workspace_bytes.restype = sz
-    L.ptc_paged_attention_workspace_bytes.argtypes = [u32, u64, u32, u32, u32]
+    L.ptc_paged_attention_workspace_bytes.argtypes = [u32, u32, u32, u32, u32, u64]
     L.ptc_paged_attention.restype = st
     L.ptc_paged_attention.argtypes = [kv, vp, _Strides, vp, u64, u32, u32, ctypes.c_float, vp, vp, vp, vp, u64, vp, sz,
                                       vp, vp]
@@ -174,7 +174,7 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
             raise ValueError("mass: expected one row a key head")
         stride = mass_out.shape[1]
     L = p.lib()
-    need = L.ptc_paged_attention_workspace_bytes(kv.n_req, T, Hq, kv.n_kv_heads, kv.head_dim)
+    need = L.ptc_paged_attention_workspace_bytes(kv.n_req, Hq, kv.n_kv_heads, kv.head_dim, int(max_q_len), stride)
     w = p._workspace(need, dev, ws)
     rc = L.ptc_paged_attention(ctypes.byref(kv), q.data_ptr(), qs, tok_off.data_ptr(), T, Hq, int(max_q_len),
                                1 / math.sqrt(kv.head_dim) if scale is None else float(scale), out.data_ptr(),

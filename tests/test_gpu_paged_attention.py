@@ -178,7 +178,7 @@ def test_graph_replay_reads_new_lengths():
     from tests.kv_util import close, reference
     c = cache([(1, 500), (1, 900)], Hq=8, Hkv=2, D=128)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
-    ws = torch.empty(ptc.lib().ptc_paged_attention_workspace_bytes(2, 2, 8, 2, 128), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(ptc.lib().ptc_paged_attention_workspace_bytes(2, 8, 2, 128, 1, 0), dtype=torch.uint8, device="cuda")
     out = torch.empty_like(c.q)
     lse = torch.empty(c.q.shape[:2], dtype=torch.float32, device="cuda")
     run = lambda: ptc.ptc_paged_attention(c.q, *c.table(), c.tok_off, c.kv_len, 1, out=out, lse=lse, ws=ws, status=status)
