@@ -248,7 +248,9 @@ struct Weights<__half> {
 //                 are the same instructions either way.
 // O is rescaled only when a row's maximum has grown by more than a factor of
 // 2^8 since the last time (weights up to 2^8 are as exact as those up to 1),
-// which after the first tiles hardly happens.
+// which after the first tiles hardly happens.  So the weights of a tile are
+// first taken with the maximum as it stands, while the tile's own is still being
+// found, and again only if that shows it has to move.
 enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
 constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
@@ -331,12 +333,25 @@ __device__ __forceinline__ bool raise_top(RowState& st, float mx, float sl2, flo
   for (int c = 0; c < NSLAB * 2; ++c) {
     uint32_t x[32];
     tmem_ld32(x, o_at + 32 * c);
-    tmem_wait_ld();
+    tmem_wait_ld(x);
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
     tmem_st32(o_at + 32 * c, x);
   }
   return true;
+}
+
+__device__ __forceinline__ float max32(const uint32_t (&x)[32]) {
+  float m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = __uint_as_float(x[i]);
+#pragma unroll
+    for (int k = i + 4; k + 4 < 32; k += 8)
+      m[i] = fmaxf(m[i], fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 4])));
+    m[i] = fmaxf(m[i], __uint_as_float(x[i + 28]));
+  }
+  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
 // 32 scores to weights: their sum, and the weights in 16 columns.
@@ -383,41 +398,48 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         tc_fence_after();
         if (active) {
           uint32_t x[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(x[c], s_at + 32 * c);
-          tmem_wait_ld();
           const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
-          if (__any_sync(kFull, see < (int)kKeys)) {
+          const bool masked = __any_sync(kFull, see < (int)kKeys);
+          const bool guess = j != j0 && !masked;
+          float mx = -INFINITY;
+          float2 sum = make_float2(0.f, 0.f);
+          float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+          tmem_ld32(x[0], s_at);
+          tmem_wait_ld(x[0]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c) {
+            if (c < 3) tmem_ld32(x[c + 1], s_at + 32 * (c + 1));
+            if (masked) {
 #pragma unroll
               for (int k = 0; k < 32; ++k)
                 if (32 * c + k >= see) x[c][k] = 0xFF800000u;
+            }
+            mx = fmaxf(mx, max32(x[c]));
+            if (guess) {
+              uint32_t y[16];
+              weigh<T>(x[c], sl2, sub, sum, y);
+              if (c < 3) tmem_wait_ld(x[c + 1]);
+              tmem_st16(s_at + 16 * c, y);
+            } else if (c < 3) {
+              tmem_wait_ld(x[c + 1]);
+            }
           }
-          float mx[4];
+          if (!guess || __any_sync(kFull, mx > st.top + slack)) {
+            if (!raise_top<NSLAB>(st, mx, sl2, slack, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
+            sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+            sum = make_float2(0.f, 0.f);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            mx[c] = fmaxf(__uint_as_float(x[c][0]), __uint_as_float(x[c][1]));
-#pragma unroll
-            for (int k = 2; k < 32; k += 2)
-              mx[c] = fmaxf(mx[c], fmaxf(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])));
-          }
-          if (!raise_top<NSLAB>(st, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), sl2, slack, o_at, j == j0, bar_o,
-                                (done - 1) & 1))
-            return false;
-          const float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
-          float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t y[16];
-            weigh<T>(x[c], sl2, sub, sum, y);
-            tmem_st16(s_at + 16 * c, y);
+            for (int c = 0; c < 4; ++c) {
+              uint32_t y[16];
+              weigh<T>(x[c], sl2, sub, sum, y);
+              tmem_st16(s_at + 16 * c, y);
+            }
           }
           st.l += sum.x + sum.y;
           tmem_wait_st();
         }
         tc_fence_before();
-        mbar_arrive(bar_p);
+        mbar_arrive_warp(bar_p);
       }
     } else {
       see_all -= 32 * warp;
@@ -426,7 +448,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         tc_fence_after();
         uint32_t x[32], y[16], zero[16];
         tmem_ld32(x, s_at + 32 * warp);
-        tmem_wait_ld();
+        tmem_wait_ld(x);
         const int see = see_all >= 32 ? 32 : see_all > 0 ? (int)see_all : 0;
         if (a.scores && valid) {
           float* to = a.scores + ((uint64_t)w.h * a.few + lane) * a.mass_stride + w.page0 * a.kv.B + (uint64_t)j * kKeys + 32 * warp;
@@ -446,10 +468,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
           for (int k = 0; k < 32; ++k)
             if (k >= see) x[k] = 0xFF800000u;
         }
-        float mx = __uint_as_float(x[0]);
-#pragma unroll
-        for (int k = 1; k < 32; ++k) mx = fmaxf(mx, __uint_as_float(x[k]));
-        if (!raise_top<NSLAB>(st, mx, sl2, slack, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
+        if (!raise_top<NSLAB>(st, max32(x), sl2, slack, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
         const float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
         float2 sum = make_float2(0.f, 0.f);
         weigh<T>(x, sl2, sub, sum, y);
@@ -463,7 +482,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(bar_p);
+        mbar_arrive_warp(bar_p);
       }
     }
     // the sums of the rows
@@ -499,8 +518,11 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         for (int c = 0; c < NSLAB * 2; ++c) {
           uint32_t x[32], z[32];
           tmem_ld32(x, o_at + 32 * c);
-          if (two) tmem_ld32(z, tmem + o_col(1) + 32 * c);
-          tmem_wait_ld();
+          tmem_wait_ld(x);
+          if (two) {
+            tmem_ld32(z, tmem + o_col(1) + 32 * c);
+            tmem_wait_ld(z);
+          }
           float o[32];
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
@@ -551,7 +573,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         for (uint32_t c = 0; c < cols; c += 32) {
           uint32_t x[32];
           tmem_ld32(x, o_at + c0 + c);
-          tmem_wait_ld();
+          tmem_wait_ld(x);
           if (lane < rows) {
             float4* to = reinterpret_cast<float4*>(sums + ((uint64_t)w8 * rows + lane) * cols + c);
 #pragma unroll
@@ -612,28 +634,32 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   auto full = [&](uint32_t i) { return mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1); };
   auto tile_at = [&](uint32_t i) { return ring + (i % Sh::kRing) * Sh::kTile; };
   auto commit = [&](uint64_t& bar) {
-    if (lane == 0) mma_commit(smem_u32(&bar));
+    if (elect_lane()) mma_commit(smem_u32(&bar));
   };
   auto scores = [&](uint32_t half, uint32_t region, uint32_t k_item) {
-    if (lane == 0) {
-      for (uint32_t k = 0; k < steps; ++k) {
+    const uint64_t da = tile_desc(q_smem + region * Sh::kTile, 16), db = tile_desc(tile_at(k_item), 16);
+    if (elect_lane()) {
+      mma_ss<false>(tmem + s_col(half), da, db, kQk);
+#pragma unroll
+      for (uint32_t k = 1; k < NSLAB * 4; ++k) {
         const uint32_t off = (k / 4) * kSlabBytes + (k % 4) * 32;
-        mma_ss(tmem + s_col(half), tile_desc(q_smem + region * Sh::kTile + off, 16), tile_desc(tile_at(k_item) + off, 16),
-               kQk, k > 0);
+        if (k < steps) mma_ss<true>(tmem + s_col(half), desc_at(da, off), desc_at(db, off), kQk);
       }
       mma_commit(smem_u32(&sh.s_full[half]));
     }
+    __syncwarp();
   };
   auto values = [&](uint32_t half, uint32_t v_item, bool add) {
     if (!mbar_wait(smem_u32(&sh.p_full[half]), keys[half]++ & 1)) return false;
     tc_fence_after();
-    if (lane == 0) {
+    const uint64_t db = tile_desc(tile_at(v_item), kSlabBytes);
+    if (elect_lane()) {
 #pragma unroll
       for (uint32_t k = 0; k < kKeys / 16; ++k)
-        mma_ts(tmem + o_col(half), tmem + s_col(half) + k * 8, tile_desc(tile_at(v_item) + k * 2048, kSlabBytes), kPv,
-               add || k > 0);
+        mma_ts(tmem + o_col(half), tmem + s_col(half) + k * 8, desc_at(db, k * 2048), kPv, add || k > 0);
       mma_commit(smem_u32(&sh.pv_done[half]));
     }
+    __syncwarp();
     return true;
   };
   Walk w;
@@ -846,7 +872,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
       mbar_init(smem_u32(&sh.q_full[i]), 1);
       mbar_init(smem_u32(&sh.q_empty[i]), 1);
       mbar_init(smem_u32(&sh.s_full[i]), 1);
-      mbar_init(smem_u32(&sh.p_full[i]), 128);
+      mbar_init(smem_u32(&sh.p_full[i]), 4);
       mbar_init(smem_u32(&sh.pv_done[i]), 1);
     }
     mbar_init(smem_u32(&sh.drain), 1);
@@ -869,7 +895,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     } else if (warp == 8) {
       fine = product_role<T, NSLAB>(a, sh, q_smem, ring);
       // every product and every arrival it owes is done before the CTA ends
-      if ((threadIdx.x & 31) == 0) mma_commit(smem_u32(&sh.drain));
+      if (elect_lane()) mma_commit(smem_u32(&sh.drain));
       __syncwarp();
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
     } else if (warp == 10) {

@@ -190,7 +190,7 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
       for (int c = 0; c < hi; c += 32) {
         uint32_t x[32];
         tmem_ld32(x, tmem + buf * 128 + c);
-        tmem_wait_ld();
+        tmem_wait_ld(x);
         const float2* off = reinterpret_cast<const float2*>(lse + c);
         if (!masked) {
 #pragma unroll
@@ -208,7 +208,7 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
         }
       }
       tc_fence_before();
-      mbar_arrive(smem_u32(&sh.s_empty[buf]));
+      mbar_arrive_warp(smem_u32(&sh.s_empty[buf]));
       total += sum.x + sum.y;
     }
     unit += w.q1 - w.q0;
@@ -233,7 +233,7 @@ template <typename T, int NSLAB>
 __device__ __forceinline__ bool mass_products(const AttnArgs& a, MassShared& sh, uint32_t smem) {
   using Sh = MassShape<NSLAB>;
   constexpr bool bf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
-  const uint32_t lane = threadIdx.x & 31, tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
+  const uint32_t tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
   uint32_t unit = 0, seg = 0;
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
@@ -244,11 +244,14 @@ __device__ __forceinline__ bool mass_products(const AttnArgs& a, MassShared& sh,
       if (!mbar_wait(smem_u32(&sh.q_full[buf]), (unit >> 2) & 1)) return false;
       if (unit >= 4 && !mbar_wait(smem_u32(&sh.s_empty[buf]), ((unit >> 2) - 1) & 1)) return false;
       tc_fence_after();
-      if (lane == 0) {
-        const uint32_t desc = mma_desc(bf16, 128, (w.rows(a, q) + 15) & ~15u, false);
-        for (uint32_t k = 0; k < steps; ++k) {
+      const uint32_t desc = mma_desc(bf16, 128, (w.rows(a, q) + 15) & ~15u, false);
+      const uint64_t da = tile_desc(k_at, 16), db = tile_desc(q_at, 16);
+      if (elect_lane()) {
+        mma_ss<false>(tmem + buf * 128, da, db, desc);
+#pragma unroll
+        for (uint32_t k = 1; k < NSLAB * 4; ++k) {
           const uint32_t off = (k / 4) * kSlab + (k % 4) * 32;
-          mma_ss(tmem + buf * 128, tile_desc(k_at + off, 16), tile_desc(q_at + off, 16), desc, k > 0);
+          if (k < steps) mma_ss<true>(tmem + buf * 128, desc_at(da, off), desc_at(db, off), desc);
         }
         mma_commit(smem_u32(&sh.s_full[buf]));
         mma_commit(smem_u32(&sh.q_empty[buf]));
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
       mbar_init(smem_u32(&sh.q_full[i]), 1);
       mbar_init(smem_u32(&sh.q_empty[i]), 1);
       mbar_init(smem_u32(&sh.s_full[i]), 1);
-      mbar_init(smem_u32(&sh.s_empty[i]), 128);
+      mbar_init(smem_u32(&sh.s_empty[i]), 4);
     }
     mbar_init(smem_u32(&sh.drain), 1);
     fence_mbar_init();
@@ -365,7 +368,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
     } else if (warp == 8) {
       fine = mass_products<T, NSLAB>(a, sh, smem);
       // every product and every arrival it owes is done before the CTA ends
-      if ((threadIdx.x & 31) == 0) mma_commit(smem_u32(&sh.drain));
+      if (elect_lane()) mma_commit(smem_u32(&sh.drain));
       __syncwarp();
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
     } else if (warp == 10) {
