@@ -211,7 +211,7 @@ struct Weights;
 template <>
 struct Weights<__nv_bfloat16> {
   static constexpr bool kBf16 = true;
-  static constexpr float kShift = 0.f;
+  static constexpr float kShift = 0.f, kScale = 1.f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
@@ -220,7 +220,7 @@ struct Weights<__nv_bfloat16> {
 template <>
 struct Weights<__half> {
   static constexpr bool kBf16 = false;
-  static constexpr float kShift = 7.f;
+  static constexpr float kShift = 7.f, kScale = 128.f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __half2 x = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
@@ -254,7 +254,8 @@ struct Weights<__half> {
 enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
 constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
-constexpr int kScratch = 32768;        // sums of 8 warps, 32 rows and 32 columns
+// 4 KB a softmax warp: rows on their way out; the sums of 8 warps, 32 rows and 32 columns.
+constexpr int kStage = 8 * 4096;
 // Registers a thread: 2 * 128 * 216 + 128 * 72 = 384 * 168, what the block has at launch.
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 
@@ -264,12 +265,16 @@ struct TileShared {
   uint32_t tmem;
 };
 
-template <int NSLAB>
+// FEW: every request of the call has so few rows that its tiles are all
+// kColumnsApart.  There is no second half of queries then, and the ring has
+// its place: 5 tiles of 32 KB keep more of the cache in flight than 4.
+template <int NSLAB, bool FEW>
 struct TileShape {
   static constexpr int kTile = NSLAB * kSlabBytes;
-  static constexpr int kRing = NSLAB == 2 ? 5 : 8;
-  // queries of half 0, of half 1 (or scratch), ring, the rest
-  static constexpr int kRest = kTile + kScratch + kRing * kTile;
+  static constexpr uint32_t kRing = NSLAB == 1 ? 8 : FEW ? 5 : 4;
+  static constexpr int kQueries = FEW ? 1 : 2;
+  // queries, ring, stage, the rest
+  static constexpr int kRest = kQueries * kTile + kRing * kTile + kStage;
   static constexpr int kSmem = kRest + sizeof(TileShared);
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
 };
@@ -281,25 +286,22 @@ __device__ __forceinline__ uint32_t o_col(uint32_t half) { return 256 + half * 1
 // Both halves of the softmax.
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
-// One row of a result: sums over weights, 32 columns.
-template <typename T>
-__device__ __forceinline__ void store_row(char* out, const float (&x)[32], uint32_t col, uint32_t D) {
+// 128 bytes a lane to the lanes' places in global memory, `pieces` of 16 bytes
+// of each, by way of the warp's stage: a store then covers 128 bytes of 4 rows
+// and not 16 of 32 (which made this a third of the time of a short tile).
+__device__ __forceinline__ void emit(char* stage, const uint4 (&x)[8], char* to, uint32_t rows, uint32_t pieces) {
+  const uint32_t lane = threadIdx.x & 31;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (col + 8 * i < D) {
-      uint4 y;
-      y.x = Weights<T>::pack(x[8 * i], x[8 * i + 1]);
-      y.y = Weights<T>::pack(x[8 * i + 2], x[8 * i + 3]);
-      y.z = Weights<T>::pack(x[8 * i + 4], x[8 * i + 5]);
-      y.w = Weights<T>::pack(x[8 * i + 6], x[8 * i + 7]);
-      *reinterpret_cast<uint4*>(out + 2 * col + 16 * i) = y;
-    }
-}
-__device__ __forceinline__ void store_part(float* part, const float (&x)[32], uint32_t col, uint32_t D) {
+  for (uint32_t k = 0; k < 8; ++k) *reinterpret_cast<uint4*>(stage + lane * 128 + (k ^ (lane & 7)) * 16) = x[k];
+  __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (col + 4 * i < D)
-      *reinterpret_cast<float4*>(part + col + 4 * i) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+  for (uint32_t i = 0; i < 8; ++i) {
+    const uint32_t row = i * 4 + lane / 8, k = lane & 7;
+    const uint4 y = *reinterpret_cast<const uint4*>(stage + row * 128 + (k ^ (row & 7)) * 16);
+    char* p = reinterpret_cast<char*>(__shfl_sync(kFull, reinterpret_cast<uint64_t>(to), row));
+    if ((rows >> row & 1) && k < pieces) *reinterpret_cast<uint4*>(p + 16 * k) = y;
+  }
+  __syncwarp();
 }
 
 // The running maximum and sum of a row.
@@ -316,12 +318,12 @@ struct RowState {
   }
 };
 
-// A wait for the previous product into O, then O times f, where a lane's
-// maximum has grown too far.
+// Moves the maximum of a row up to mx; O, once the product before is done,
+// and what was summed so far shrink with it.
 template <int NSLAB>
-__device__ __forceinline__ bool raise_top(RowState& st, float mx, float sl2, float slack, uint32_t o_at, bool first,
+__device__ __forceinline__ bool raise_top(RowState& st, float mx, float sl2, uint32_t o_at, bool first,
                                           uint32_t bar_o, uint32_t parity) {
-  if (!__any_sync(kFull, mx > st.top + slack)) return true;
+  if (!__any_sync(kFull, mx > st.top)) return true;
   const float nt = fmaxf(st.top, mx);
   const float f = st.top == -INFINITY ? 0.f : exp2_approx((st.top - nt) * sl2);
   st.l *= f;
@@ -356,86 +358,101 @@ __device__ __forceinline__ float max32(const uint32_t (&x)[32]) {
 
 // 32 scores to weights: their sum, and the weights in 16 columns.
 template <typename T>
-__device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float sub, float2& sum, uint32_t (&y)[16]) {
+__device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float sub, float2 (&sum)[2], uint32_t (&y)[16]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float2 e = fma2(make_float2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), make_float2(sl2, sl2),
                           make_float2(-sub, -sub));
     const float2 p = make_float2(exp2_approx(e.x), exp2_approx(e.y));
-    sum = add2(sum, p);
+    sum[i & 1] = add2(sum[i & 1], p);
     y[i] = Weights<T>::pack(p.x, p.y);
   }
 }
 
-template <typename T, int NSLAB>
-__device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, char* scratch, uint32_t half) {
+// The maximum moves when a tile's sum of a row passes this (128 weights of at
+// most 1 stay below it; no weight is larger than their sum).
+constexpr float kMove = 256.f;
+
+template <typename T, int NSLAB, bool FEW>
+__device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, char* stages, uint32_t half) {
   using W = Weights<T>;
   const uint32_t tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
   const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
   const uint32_t s_at = tmem + s_col(half), o_at = tmem + o_col(half);
   const uint32_t bar_s = smem_u32(&sh.s_full[half]), bar_p = smem_u32(&sh.p_full[half]),
                  bar_o = smem_u32(&sh.pv_done[half]);
-  const float sl2 = a.scale * kLog2e, slack = fminf(8.f / sl2, 1e38f);
+  const float sl2 = a.scale * kLog2e;
   const uint32_t D = a.kv.D, G = a.G;
   const CtaStart start = a.plan->start[blockIdx.x];
+  char* stage = stages + (half * 4 + warp) * 4096;
   uint32_t done = 0;  // key tiles of this half so far
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const int mode = w.mode(a);
+    const int mode = FEW ? kColumnsApart : w.mode(a);
     // the thread's row: a token of the request and a head of the group
     const uint32_t i = mode == kColumnsApart ? lane : tid;
     const uint32_t t = w.token0(a) + (mode == kRowsApart ? half * a.tq : 0) + i / G, g = i % G;
     const bool valid = i < a.tq * G && t < w.m;
-    const bool active = __any_sync(kFull, valid);
+    const uint32_t rows = __ballot_sync(kFull, valid);
     const uint32_t step = mode == kRowsApart ? 1 : 2, j0 = w.kv0 + (mode == kRowsApart ? 0 : half);
-    // keys of the tile at hand and later ones that the row sees
-    int64_t see_all = valid ? (int64_t)w.n - w.m + t + 1 - (int64_t)j0 * kKeys : 0;
+    // keys of the tile at hand and later ones that the row sees; what a row
+    // computes that is none is not used and moves nothing
+    int64_t see_all = valid ? (int64_t)w.n - w.m + t + 1 - (int64_t)j0 * kKeys : INT64_MAX / 2;
     RowState st;
     st.clear();
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, see_all -= step * kKeys) {
         if (!mbar_wait(bar_s, done & 1)) return false;
         tc_fence_after();
-        if (active) {
-          uint32_t x[4][32];
+        if (rows) {
+          uint32_t x[4][32], y[16];
           const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
           const bool masked = __any_sync(kFull, see < (int)kKeys);
-          const bool guess = j != j0 && !masked;
-          float mx = -INFINITY;
-          float2 sum = make_float2(0.f, 0.f);
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+          bool move = true;
           tmem_ld32(x[0], s_at);
           tmem_wait_ld(x[0]);
+          if (j != j0 && !masked) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c < 3) tmem_ld32(x[c + 1], s_at + 32 * (c + 1));
-            if (masked) {
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (32 * c + k >= see) x[c][k] = 0xFF800000u;
-            }
-            mx = fmaxf(mx, max32(x[c]));
-            if (guess) {
-              uint32_t y[16];
+            for (int c = 0; c < 4; ++c) {
+              if (c < 3) tmem_ld32(x[c + 1], s_at + 32 * (c + 1));
               weigh<T>(x[c], sl2, sub, sum, y);
               if (c < 3) tmem_wait_ld(x[c + 1]);
               tmem_st16(s_at + 16 * c, y);
-            } else if (c < 3) {
-              tmem_wait_ld(x[c + 1]);
+            }
+            const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            move = __any_sync(kFull, valid && !(total <= kMove * W::kScale));
+            if (!move) st.l += total;
+          } else {
+#pragma unroll
+            for (int c = 1; c < 4; ++c) {
+              tmem_ld32(x[c], s_at + 32 * c);
+              tmem_wait_ld(x[c]);
             }
           }
-          if (!guess || __any_sync(kFull, mx > st.top + slack)) {
-            if (!raise_top<NSLAB>(st, mx, sl2, slack, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
-            sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
-            sum = make_float2(0.f, 0.f);
+          if (move) {
+            float mx = -INFINITY;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-              uint32_t y[16];
+              if (masked) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                  if (32 * c + k >= see) x[c][k] = 0xFF800000u;
+              }
+              mx = fmaxf(mx, max32(x[c]));
+            }
+            if (!valid) mx = -INFINITY;
+            if (!raise_top<NSLAB>(st, mx, sl2, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
+            sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
               weigh<T>(x[c], sl2, sub, sum, y);
               tmem_st16(s_at + 16 * c, y);
             }
+            st.l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           }
-          st.l += sum.x + sum.y;
           tmem_wait_st();
         }
         tc_fence_before();
@@ -468,11 +485,18 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
           for (int k = 0; k < 32; ++k)
             if (k >= see) x[k] = 0xFF800000u;
         }
-        if (!raise_top<NSLAB>(st, max32(x), sl2, slack, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
-        const float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
-        float2 sum = make_float2(0.f, 0.f);
+        float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         weigh<T>(x, sl2, sub, sum, y);
-        st.l += sum.x + sum.y;
+        float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        if (__any_sync(kFull, j == j0 || (valid && !(total <= kMove * W::kScale)))) {
+          if (!raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
+          sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+          sum[0] = sum[1] = make_float2(0.f, 0.f);
+          weigh<T>(x, sl2, sub, sum, y);
+          total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        }
+        st.l += total;
 #pragma unroll
         for (int k = 0; k < 16; ++k) zero[k] = 0;
 #pragma unroll
@@ -507,34 +531,53 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
           l = l * f0 + (other.x == -INFINITY ? 0.f : other.y * f1);
         }
       }
-      if (active && (mode == kRowsApart || half == 0)) {
+      if (rows && (mode == kRowsApart || half == 0)) {
         const bool none = top2 == -INFINITY;
         const float inv = whole ? 1.f / l : 1.f;
         f0 *= inv;
         f1 *= inv;
         const uint64_t at = orow0 + (uint64_t)t * a.n_q_heads + g, prow = prow0 + (mode == kRowsApart ? half * 128 : 0) + i;
         const bool two = mode == kTilesApart && w.kv1 - w.kv0 > 1;
-#pragma unroll 1
-        for (int c = 0; c < NSLAB * 2; ++c) {
-          uint32_t x[32], z[32];
-          tmem_ld32(x, o_at + 32 * c);
+        auto sums_of = [&](uint32_t col, uint32_t(&x)[32]) {
+          tmem_ld32(x, o_at + col);
           tmem_wait_ld(x);
-          if (two) {
-            tmem_ld32(z, tmem + o_col(1) + 32 * c);
-            tmem_wait_ld(z);
-          }
-          float o[32];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            o[k] = f0 == 0.f ? 0.f : __uint_as_float(x[k]) * f0;
-            if (two && f1 != 0.f) o[k] = fmaf(__uint_as_float(z[k]), f1, o[k]);
-            if (none) o[k] = 0.f;
+          for (int k = 0; k < 32; ++k) x[k] = none || f0 == 0.f ? 0u : __float_as_uint(__uint_as_float(x[k]) * f0);
+          if (two) {
+            uint32_t z[32];
+            tmem_ld32(z, tmem + o_col(1) + col);
+            tmem_wait_ld(z);
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if (!none && f1 != 0.f) x[k] = __float_as_uint(fmaf(__uint_as_float(z[k]), f1, __uint_as_float(x[k])));
           }
-          if (valid) {
-            if (whole) store_row<T>(a.out + 2 * at * D, o, 32 * c, D);
-            else store_part(a.part + prow * D, o, 32 * c, D);
+        };
+        if (whole) {
+#pragma unroll 1
+          for (uint32_t col = 0; col < NSLAB * 64; col += 64) {
+            uint4 y[8];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t x[32];
+              sums_of(col + 32 * c, x);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                auto two16 = [&](int e) { return W::pack(__uint_as_float(x[8 * k + e]), __uint_as_float(x[8 * k + e + 1])); };
+                y[4 * c + k] = make_uint4(two16(0), two16(2), two16(4), two16(6));
+              }
+            }
+            emit(stage, y, a.out + 2 * (at * D + col), rows, (D - col) / 8);
           }
-          __syncwarp();
+        } else {
+#pragma unroll 1
+          for (uint32_t col = 0; col < D; col += 32) {
+            uint32_t x[32];
+            sums_of(col, x);
+            uint4 y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+            emit(stage, y, reinterpret_cast<char*>(a.part + prow * D + col), rows, (D - col) / 4);
+          }
         }
         if (valid) {
           if (whole) a.lse[at] = none ? -INFINITY : (top2 + log2_approx(l)) * kLn2;
@@ -545,7 +588,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
       if (mode == kTilesApart) softmax_sync();  // half 1's sums have been read
     } else {
       // the eight partial rows of a row
-      const uint32_t rows = (w.m - w.token0(a)) * G, w8 = half * 4 + warp;
+      const uint32_t count = (w.m - w.token0(a)) * G, w8 = half * 4 + warp;
       sh.ml[w8 * 32 + lane] = make_float2(st.top2<W>(sl2), st.l);
       softmax_sync();
       float top2 = -INFINITY, l = 0.f;
@@ -564,18 +607,18 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         if (whole) a.lse[orow0 + (uint64_t)t * a.n_q_heads + g] = none ? -INFINITY : (top2 + log2_approx(l)) * kLn2;
         else a.part_ml[prow0 + lane] = make_float2(top2, l);
       }
-      // columns at a time that fit the scratch: [8 warps][rows][cols], or
+      // columns at a time that fit the stage: [8 warps][rows][cols], or
       // [8][rows][32] where there are many rows
-      const uint32_t cols = rows <= 8 ? NSLAB * 64 : 32;
-      float* sums = reinterpret_cast<float*>(scratch);
+      const uint32_t cols = count <= 8 ? NSLAB * 64 : 32;
+      float* sums = reinterpret_cast<float*>(stages);
       for (uint32_t c0 = 0; c0 < NSLAB * 64; c0 += cols) {
 #pragma unroll 1
         for (uint32_t c = 0; c < cols; c += 32) {
           uint32_t x[32];
           tmem_ld32(x, o_at + c0 + c);
           tmem_wait_ld(x);
-          if (lane < rows) {
-            float4* to = reinterpret_cast<float4*>(sums + ((uint64_t)w8 * rows + lane) * cols + c);
+          if (lane < count) {
+            float4* to = reinterpret_cast<float4*>(sums + ((uint64_t)w8 * count + lane) * cols + c);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               // rotated by the row: the lanes' rows are whole multiples of the banks apart
@@ -591,13 +634,13 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         }
         tc_fence_before();
         softmax_sync();
-        for (uint32_t e = threadIdx.x; e < rows * (cols / 4); e += 256) {
+        for (uint32_t e = threadIdx.x; e < count * (cols / 4); e += 256) {
           const uint32_t row = e / (cols / 4), c4 = e % (cols / 4);
           const uint32_t at = (c4 & ~7u) | ((c4 + row) & 7);
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float4 x = *reinterpret_cast<const float4*>(sums + ((uint64_t)k * rows + row) * cols + 4 * at);
+            const float4 x = *reinterpret_cast<const float4*>(sums + ((uint64_t)k * count + row) * cols + 4 * at);
             y.x += x.x;
             y.y += x.y;
             y.z += x.z;
@@ -613,18 +656,16 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
             }
           }
         }
-        fence_async_shared();
         softmax_sync();
       }
-      if (threadIdx.x == 0) mbar_arrive(smem_u32(&sh.q_empty[1]));  // the scratch is the queries' again
     }
   }
   return true;
 }
 
-template <typename T, int NSLAB>
+template <typename T, int NSLAB, bool FEW>
 __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, uint32_t q_smem, uint32_t ring) {
-  using Sh = TileShape<NSLAB>;
+  using Sh = TileShape<NSLAB, FEW>;
   constexpr uint32_t kQk = mma_desc(Weights<T>::kBf16, 128, kKeys, false);
   constexpr uint32_t kPv = mma_desc(Weights<T>::kBf16, 128, NSLAB * 64, true);
   const uint32_t lane = threadIdx.x & 31, tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
@@ -664,7 +705,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   };
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const int mode = w.mode(a);
+    const int mode = FEW ? kColumnsApart : w.mode(a);
     const uint32_t L = w.kv1 - w.kv0;
     // slots that hold no token may hold NaN: zero their values (their weights are zero)
     auto clear_tail = [&](uint32_t j, uint32_t v_item) {
@@ -736,32 +777,30 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
 }
 
 // Queries by tensor copies, a tile ahead of the products.
-template <int NSLAB>
+template <int NSLAB, bool FEW>
 __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* mq,
                                            const CUtensorMap* mq32, uint32_t q_smem, uint32_t (&loads)[2]) {
-  using Sh = TileShape<NSLAB>;
+  using Sh = TileShape<NSLAB, FEW>;
   const uint32_t lane = threadIdx.x & 31;
-  uint32_t used[2] = {0, 0};
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const int mode = w.mode(a);
+    const int mode = FEW ? kColumnsApart : w.mode(a);
     const int tok = (int)(w.tok0 + w.token0(a));
-    // a region is the query rows' or, in half 1's place, the scratch of kColumnsApart
-    for (uint32_t s = 0; s < (mode == kTilesApart ? 1u : 2u); ++s) {
-      if (used[s] && !mbar_wait(smem_u32(&sh.q_empty[s]), (used[s] - 1) & 1)) return false;
-      ++used[s];
+    for (uint32_t s = 0; s < (mode == kRowsApart ? 2u : 1u); ++s) {
+      if (loads[s] && !mbar_wait(smem_u32(&sh.q_empty[s]), (loads[s] - 1) & 1)) return false;
+      ++loads[s];
       const uint32_t bar = smem_u32(&sh.q_full[s]), dst = q_smem + s * Sh::kTile;
       if (lane == 0 && mode != kColumnsApart) {
         mbar_expect(bar, NSLAB * a.tq * a.G * 128);
 #pragma unroll
         for (int c = 0; c < NSLAB; ++c) tma_load_4d(dst + c * kSlabBytes, mq, bar, 64 * c, 0, (int)w.h, tok + (int)(s * a.tq));
-      } else if (lane == 0 && s == 0) {
+      } else if (lane == 0) {
         mbar_expect(bar, 4 * NSLAB * a.tq32 * a.G * 128);
         for (int x = 0; x < 4; ++x)
 #pragma unroll
           for (int c = 0; c < NSLAB; ++c) tma_load_4d(dst + c * kSlabBytes + x * 4096, mq32, bar, 64 * c, 0, (int)w.h, tok);
       }
-      if (mode != kColumnsApart || s == 0) ++loads[s];
+      __syncwarp();
     }
   }
   return true;
@@ -771,35 +810,45 @@ __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, co
 // of the page size and of the tile) and slab.  Stretches at or past the
 // request's end and pages that the cache does not have read as zeros: their
 // page coordinate is n_pages, which is out of range.
-template <int NSLAB>
+template <int NSLAB, bool FEW>
 __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* mk, const CUtensorMap* mv,
                                           uint32_t ring, uint32_t& issued) {
-  using Sh = TileShape<NSLAB>;
+  using Sh = TileShape<NSLAB, FEW>;
   const uint32_t lane = threadIdx.x & 31, boxes = kKeys / a.box;
   Walk w;
-  for (bool more = w.begin(a); more; more = w.next(a)) {
-    const uint32_t* ids = a.kv.page_ids + w.page0;
-    for (uint32_t j = w.kv0; j < w.kv1; ++j) {
-      const uint64_t key = (uint64_t)j * kKeys + lane * a.box;
-      int page = (int)a.kv.n_pages, slot = 0;
-      if (lane < boxes && key < w.n) {
-        const uint32_t id = __ldg(ids + key / a.kv.B);
-        if (id < a.kv.n_pages) page = (int)id;
-        else report(a.status, PTC_ERR_INVALID_ARG);
-        slot = (int)(key % a.kv.B);
-      }
+  if (!w.begin(a)) return true;
+  // the page of the lane's stretch of key tile j, asked for a tile ahead
+  uint32_t j = w.kv0, id = 0, slot = 0, head = 0;
+  bool in = false;
+  auto ask = [&] {
+    const uint32_t key = j * kKeys + lane * a.box, at = key / a.kv.B;
+    in = lane < boxes && key < w.n;
+    slot = key - at * a.kv.B;
+    head = w.h;
+    id = in ? __ldg(a.kv.page_ids + w.page0 + at) : 0;
+  };
+  ask();
+  for (bool more = true; more;) {
+    int page = (int)a.kv.n_pages;
+    if (in && id < a.kv.n_pages) page = (int)id;
+    else if (in) report(a.status, PTC_ERR_INVALID_ARG);
+    const int s0 = in ? (int)slot : 0, h0 = (int)head;
+    if (++j == w.kv1) {
+      more = w.next(a);
+      j = w.kv0;
+    }
+    if (more) ask();
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv, ++issued) {
-        const uint32_t at = issued % Sh::kRing;
-        if (issued >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / Sh::kRing - 1) & 1)) return false;
-        const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + lane * a.box * 128;
-        if (lane == 0) mbar_expect(bar, Sh::kTile);
-        __syncwarp();
-        if (lane < boxes)
+    for (int kv = 0; kv < 2; ++kv, ++issued) {
+      const uint32_t at = issued % Sh::kRing;
+      if (issued >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / Sh::kRing - 1) & 1)) return false;
+      const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + lane * a.box * 128;
+      if (lane == 0) mbar_expect(bar, Sh::kTile);
+      __syncwarp();
+      if (lane < boxes)
 #pragma unroll
-          for (int s = 0; s < NSLAB; ++s)
-            tma_load_4d(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, slot, (int)w.h, page);
-      }
+        for (int s = 0; s < NSLAB; ++s)
+          tma_load_4d(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, s0, h0, page);
     }
   }
   return true;
@@ -807,9 +856,9 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
 
 // The same for page sizes that are no multiple of 8 (a swizzled tile takes
 // copies of whole groups of 8 rows): 64 threads copy 16 bytes each.
-template <int NSLAB>
+template <int NSLAB, bool FEW>
 __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, uint32_t ring) {
-  using Sh = TileShape<NSLAB>;
+  using Sh = TileShape<NSLAB, FEW>;
   const uint32_t tid = (threadIdx.x & 31) + (threadIdx.x >= 352 ? 32 : 0);
   uint32_t issued = 0, landed = 0;
   auto land = [&](uint32_t upto) {
@@ -828,7 +877,7 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
         const int64_t head = w.h * (kv == 0 ? a.kv.ks_head : a.kv.vs_head);
         for (uint32_t i = tid; i < kKeys * NSLAB * 8; i += 64) {
           const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8);
-          const uint64_t key = (uint64_t)j * kKeys + row;
+          const uint32_t key = j * kKeys + row;
           bool in = key < w.n && c * 8 < a.kv.D;
           const char* p = src;
           if (in) {
@@ -850,21 +899,21 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
   return true;
 }
 
-template <typename T, int NSLAB, bool TMA>
+template <typename T, int NSLAB, bool TMA, bool FEW>
 __global__ void __launch_bounds__(kTileThreads, 1)
     k_attn_tiles(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                  const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mq32, const AttnArgs a) {
-  using Sh = TileShape<NSLAB>;
+  using Sh = TileShape<NSLAB, FEW>;
   extern __shared__ __align__(1024) char smem_raw[];
   TileShared& sh = *reinterpret_cast<TileShared*>(smem_raw + Sh::kRest);
-  const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + Sh::kTile + kScratch;
+  const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + Sh::kQueries * Sh::kTile;
   const uint32_t warp = threadIdx.x >> 5;
   if (q_smem & 1023) {  // swizzled tiles start at whole groups of 8 rows
     if (threadIdx.x == 0) report(a.status, PTC_ERR_CUDA);
     return;
   }
   if (threadIdx.x == 0) {
-    for (int i = 0; i < Sh::kRing; ++i) {
+    for (uint32_t i = 0; i < Sh::kRing; ++i) {
       mbar_init(smem_u32(&sh.full[i]), TMA ? 1 : 64);
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
@@ -887,23 +936,23 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   bool fine = true;
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    if (go) fine = softmax_role<T, NSLAB>(a, sh, smem_raw + Sh::kTile, warp / 4);
+    if (go) fine = softmax_role<T, NSLAB, FEW>(a, sh, smem_raw + Sh::kRest - kStage, warp / 4);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     uint32_t issued = 0, loads[2] = {0, 0};
     if (!go) {
     } else if (warp == 8) {
-      fine = product_role<T, NSLAB>(a, sh, q_smem, ring);
+      fine = product_role<T, NSLAB, FEW>(a, sh, q_smem, ring);
       // every product and every arrival it owes is done before the CTA ends
       if (elect_lane()) mma_commit(smem_u32(&sh.drain));
       __syncwarp();
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
     } else if (warp == 10) {
-      fine = query_role<NSLAB>(a, sh, &mq, &mq32, q_smem, loads);
+      fine = query_role<NSLAB, FEW>(a, sh, &mq, &mq32, q_smem, loads);
     } else if (!TMA) {
-      fine = gather_role<NSLAB>(a, sh, ring);
+      fine = gather_role<NSLAB, FEW>(a, sh, ring);
     } else if (warp == 9) {
-      fine = copy_role<NSLAB>(a, sh, &mk, &mv, ring, issued);
+      fine = copy_role<NSLAB, FEW>(a, sh, &mk, &mv, ring, issued);
     }
     if (!fine) {
       // given up: let the copies in flight land
@@ -1009,13 +1058,18 @@ bool encode(CUtensorMap* map, bool bf16, void* base, const cuuint64_t (&dims)[4]
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int NSLAB, bool TMA>
-ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], cudaStream_t s) {
+template <typename T, int NSLAB, bool TMA, bool FEW>
+ptc_status launch_one(const AttnArgs& a, const CUtensorMap (&m)[4], cudaStream_t s) {
+  constexpr int smem = TileShape<NSLAB, FEW>::kSmem;
   static std::atomic<uint64_t> ready{0};
-  if (!large_smem(k_attn_tiles<T, NSLAB, TMA>, TileShape<NSLAB>::kSmem, ready)) return PTC_ERR_CUDA;
-  PTC_KERNEL("k_attn_tiles", s, (k_attn_tiles<T, NSLAB, TMA>), a.ctas, kTileThreads, TileShape<NSLAB>::kSmem, m[0], m[1],
-             m[2], m[3], a);
+  if (!large_smem(k_attn_tiles<T, NSLAB, TMA, FEW>, smem, ready)) return PTC_ERR_CUDA;
+  PTC_KERNEL("k_attn_tiles", s, (k_attn_tiles<T, NSLAB, TMA, FEW>), a.ctas, kTileThreads, smem, m[0], m[1], m[2], m[3], a);
   return PTC_OK;
+}
+template <typename T, int NSLAB>
+ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], bool tma, cudaStream_t s) {
+  if (a.max_q_len <= a.tq32) return tma ? launch_one<T, NSLAB, true, true>(a, m, s) : launch_one<T, NSLAB, false, true>(a, m, s);
+  return tma ? launch_one<T, NSLAB, true, false>(a, m, s) : launch_one<T, NSLAB, false, false>(a, m, s);
 }
 
 template <typename T>
@@ -1034,8 +1088,7 @@ ptc_status launch(AttnArgs& a, cudaStream_t s) {
                 !cache_map(&m[1], a.kv, bf16, a.kv.v, a.kv.vs_page, a.kv.vs_head, a.kv.vs_slot, a.box)))
       return PTC_ERR_CUDA;
     if (!tokens_map(&m[2], a, bf16, a.tq) || (a.tq32 && !tokens_map(&m[3], a, bf16, a.tq32))) return PTC_ERR_CUDA;
-    const ptc_status st = a.kv.D > 64 ? (tma ? launch_tiles<T, 2, true>(a, m, s) : launch_tiles<T, 2, false>(a, m, s))
-                                      : (tma ? launch_tiles<T, 1, true>(a, m, s) : launch_tiles<T, 1, false>(a, m, s));
+    const ptc_status st = a.kv.D > 64 ? launch_tiles<T, 2>(a, m, tma, s) : launch_tiles<T, 1>(a, m, tma, s);
     if (st != PTC_OK) return st;
     PTC_KERNEL("k_attn_join", s, k_attn_join<T>, dim3(a.ctas, kRows / 32), 256, 0, a);
   }
