@@ -260,7 +260,7 @@ constexpr int kStage = 8 * 4096;
 constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 
 struct TileShared {
-  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2], pv_done[2], drain;
+  uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2][2], drain;
   float2 ml[256];
   uint32_t tmem;
 };
@@ -279,9 +279,11 @@ struct TileShape {
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
 };
 
-// Tensor memory columns: scores (and weights) of both halves, then their sums.
+// Tensor memory columns: scores of both halves, then their sums.  The weights
+// of keys 0-63 and of keys 64-127 lie in the first 32 columns of their own scores.
 __device__ __forceinline__ uint32_t s_col(uint32_t half) { return half * 128; }
 __device__ __forceinline__ uint32_t o_col(uint32_t half) { return 256 + half * 128; }
+__device__ __forceinline__ uint32_t p_col(uint32_t half, uint32_t key) { return half * 128 + (key & 64) + (key & 63) / 2; }
 
 // Both halves of the softmax.
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -369,8 +371,8 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
   }
 }
 
-// The maximum moves when a tile's sum of a row passes this (128 weights of at
-// most 1 stay below it; no weight is larger than their sum).
+// The maximum moves when a row's sum of 64 (or 32) weights passes this: as many
+// of at most 1 stay below it, and no weight is larger than their sum.
 constexpr float kMove = 256.f;
 
 template <typename T, int NSLAB, bool FEW>
@@ -379,13 +381,14 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
   const uint32_t tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
   const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
   const uint32_t s_at = tmem + s_col(half), o_at = tmem + o_col(half);
-  const uint32_t bar_s = smem_u32(&sh.s_full[half]), bar_p = smem_u32(&sh.p_full[half]),
-                 bar_o = smem_u32(&sh.pv_done[half]);
+  const uint32_t bar_s = smem_u32(&sh.s_full[half]);
+  const uint32_t bar_p[2] = {smem_u32(&sh.p_full[half][0]), smem_u32(&sh.p_full[half][1])};
+  const uint32_t bar_o[2] = {smem_u32(&sh.pv_done[half][0]), smem_u32(&sh.pv_done[half][1])};
   const float sl2 = a.scale * kLog2e;
   const uint32_t D = a.kv.D, G = a.G;
   const CtaStart start = a.plan->start[blockIdx.x];
   char* stage = stages + (half * 4 + warp) * 4096;
-  uint32_t done = 0;  // key tiles of this half so far
+  uint32_t done = 0, parted = 0;  // key tiles of this half so far, and those in two parts
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const int mode = FEW ? kColumnsApart : w.mode(a);
@@ -401,62 +404,62 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     RowState st;
     st.clear();
     if (mode != kColumnsApart) {
-      for (uint32_t j = j0; j < w.kv1; j += step, ++done, see_all -= step * kKeys) {
+      for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
         if (!mbar_wait(bar_s, done & 1)) return false;
         tc_fence_after();
-        if (rows) {
-          uint32_t x[4][32], y[16];
-          const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
-          const bool masked = __any_sync(kFull, see < (int)kKeys);
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
-          bool move = true;
-          tmem_ld32(x[0], s_at);
-          tmem_wait_ld(x[0]);
-          if (j != j0 && !masked) {
+        const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
+        const bool masked = __any_sync(kFull, see < (int)kKeys);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              if (c < 3) tmem_ld32(x[c + 1], s_at + 32 * (c + 1));
-              weigh<T>(x[c], sl2, sub, sum, y);
-              if (c < 3) tmem_wait_ld(x[c + 1]);
-              tmem_st16(s_at + 16 * c, y);
-            }
-            const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-            move = __any_sync(kFull, valid && !(total <= kMove * W::kScale));
-            if (!move) st.l += total;
-          } else {
-#pragma unroll
-            for (int c = 1; c < 4; ++c) {
-              tmem_ld32(x[c], s_at + 32 * c);
-              tmem_wait_ld(x[c]);
-            }
-          }
-          if (move) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
+        for (int part = 0; part < 2; ++part) {
+          if (rows) {
+            const uint32_t x_at = s_at + 64 * part;
+            uint32_t x[2][32], y[16];
+            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+            const bool first = j == j0 && part == 0;
+            auto hide = [&](int c) {
               if (masked) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
-                  if (32 * c + k >= see) x[c][k] = 0xFF800000u;
+                  if (64 * part + 32 * c + k >= see) x[c][k] = 0xFF800000u;
               }
-              mx = fmaxf(mx, max32(x[c]));
+            };
+            tmem_ld32(x[0], x_at);
+            tmem_wait_ld(x[0]);
+            tmem_ld32(x[1], x_at + 32);
+            hide(0);
+            bool move = first;
+            if (!first) {
+              weigh<T>(x[0], sl2, sub, sum, y);
+              tmem_wait_ld(x[1]);
+              tmem_st16(x_at, y);
+              hide(1);
+              weigh<T>(x[1], sl2, sub, sum, y);
+              tmem_st16(x_at + 16, y);
+              const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+              move = __any_sync(kFull, valid && !(total <= kMove * W::kScale));
+              if (!move) st.l += total;
+            } else {
+              tmem_wait_ld(x[1]);
+              hide(1);
             }
-            if (!valid) mx = -INFINITY;
-            if (!raise_top<NSLAB>(st, mx, sl2, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
-            sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
-            sum[0] = sum[1] = make_float2(0.f, 0.f);
+            if (move) {
+              const float mx = valid ? fmaxf(max32(x[0]), max32(x[1])) : -INFINITY;
+              if (!raise_top<NSLAB>(st, mx, sl2, o_at, first, bar_o[1 - part], (part ? parted : done - 1) & 1)) return false;
+              sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
+              sum[0] = sum[1] = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              weigh<T>(x[c], sl2, sub, sum, y);
-              tmem_st16(s_at + 16 * c, y);
+              for (int c = 0; c < 2; ++c) {
+                weigh<T>(x[c], sl2, sub, sum, y);
+                tmem_st16(x_at + 16 * c, y);
+              }
+              st.l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
             }
-            st.l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+            tmem_wait_st();
           }
-          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive_warp(bar_p[part]);
         }
-        tc_fence_before();
-        mbar_arrive_warp(bar_p);
       }
     } else {
       see_all -= 32 * warp;
@@ -490,7 +493,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         weigh<T>(x, sl2, sub, sum, y);
         float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         if (__any_sync(kFull, j == j0 || (valid && !(total <= kMove * W::kScale)))) {
-          if (!raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o, (done - 1) & 1)) return false;
+          if (!raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o[1], (done - 1) & 1)) return false;
           sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
           sum[0] = sum[1] = make_float2(0.f, 0.f);
           weigh<T>(x, sl2, sub, sum, y);
@@ -501,17 +504,17 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         for (int k = 0; k < 16; ++k) zero[k] = 0;
 #pragma unroll
         for (uint32_t c = 0; c < 4; ++c) {
-          if (c == warp) tmem_st16(s_at + 16 * c, y);
-          else tmem_st16(s_at + 16 * c, zero);
+          if (c == warp) tmem_st16(tmem + p_col(half, 32 * c), y);
+          else tmem_st16(tmem + p_col(half, 32 * c), zero);
         }
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive_warp(bar_p);
+        mbar_arrive_warp(bar_p[1]);
       }
     }
     // the sums of the rows
     const bool some = j0 < w.kv1;  // this half had a key tile
-    if (some && !mbar_wait(bar_o, (done - 1) & 1)) return false;
+    if (some && !mbar_wait(bar_o[1], (done - 1) & 1)) return false;
     tc_fence_after();
     const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
     const bool first = w.kv0 == start.minor && w.qt == start.major && w.h == start.h && w.r == start.r;
@@ -610,7 +613,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
       // columns at a time that fit the stage: [8 warps][rows][cols], or
       // [8][rows][32] where there are many rows
       const uint32_t cols = count <= 8 ? NSLAB * 64 : 32;
-      float* sums = reinterpret_cast<float*>(stages);
+      float* buf = reinterpret_cast<float*>(stages);
       for (uint32_t c0 = 0; c0 < NSLAB * 64; c0 += cols) {
 #pragma unroll 1
         for (uint32_t c = 0; c < cols; c += 32) {
@@ -618,7 +621,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
           tmem_ld32(x, o_at + c0 + c);
           tmem_wait_ld(x);
           if (lane < count) {
-            float4* to = reinterpret_cast<float4*>(sums + ((uint64_t)w8 * count + lane) * cols + c);
+            float4* to = reinterpret_cast<float4*>(buf + ((uint64_t)w8 * count + lane) * cols + c);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               // rotated by the row: the lanes' rows are whole multiples of the banks apart
@@ -640,7 +643,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
           float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float4 x = *reinterpret_cast<const float4*>(sums + ((uint64_t)k * count + row) * cols + 4 * at);
+            const float4 x = *reinterpret_cast<const float4*>(buf + ((uint64_t)k * count + row) * cols + 4 * at);
             y.x += x.x;
             y.y += x.y;
             y.z += x.z;
@@ -671,7 +674,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   const uint32_t lane = threadIdx.x & 31, tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
   uint32_t item = 0;           // ring tiles before this query tile
   uint32_t used[2] = {0, 0};   // query tiles of each region
-  uint32_t keys[2] = {0, 0};   // key tiles of each half
+  uint32_t weights[2][2] = {};  // of each half: weights by part
   auto full = [&](uint32_t i) { return mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1); };
   auto tile_at = [&](uint32_t i) { return ring + (i % Sh::kRing) * Sh::kTile; };
   auto commit = [&](uint64_t& bar) {
@@ -690,17 +693,28 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
     }
     __syncwarp();
   };
-  auto values = [&](uint32_t half, uint32_t v_item, bool add) {
-    if (!mbar_wait(smem_u32(&sh.p_full[half]), keys[half]++ & 1)) return false;
-    tc_fence_after();
+  // The weights of keys 0-63 and of 64-127 come one after the other (`apart`),
+  // each as soon as it is there, or together.  Either way the second barrier
+  // tells that the tile's product is done.
+  auto values = [&](uint32_t half, uint32_t v_item, bool add, bool apart) {
     const uint64_t db = tile_desc(tile_at(v_item), kSlabBytes);
-    if (elect_lane()) {
 #pragma unroll
-      for (uint32_t k = 0; k < kKeys / 16; ++k)
-        mma_ts(tmem + o_col(half), tmem + s_col(half) + k * 8, desc_at(db, k * 2048), kPv, add || k > 0);
-      mma_commit(smem_u32(&sh.pv_done[half]));
+    for (uint32_t part = 0; part < 2; ++part) {
+      if ((part || apart) && !mbar_wait(smem_u32(&sh.p_full[half][part]), weights[half][part]++ & 1)) return false;
+      if (!part && !apart) continue;
+      tc_fence_after();
+      if (elect_lane()) {
+        if (part && !apart)
+#pragma unroll
+          for (uint32_t k = 0; k < 4; ++k)
+            mma_ts(tmem + o_col(half), tmem + p_col(half, 16 * k), desc_at(db, k * 2048), kPv, add || k > 0);
+#pragma unroll
+        for (uint32_t k = 4 * part; k < 4 * part + 4; ++k)
+          mma_ts(tmem + o_col(half), tmem + p_col(half, 16 * k), desc_at(db, k * 2048), kPv, add || k > 0);
+        mma_commit(smem_u32(&sh.pv_done[half][part]));
+      }
+      __syncwarp();
     }
-    __syncwarp();
     return true;
   };
   Walk w;
@@ -737,7 +751,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
         if (!full(v_item)) return false;
         clear_tail(j, v_item);
         for (uint32_t s = 0; s < 2; ++s) {
-          if (!values(s, v_item, j > 0)) return false;
+          if (!values(s, v_item, j > 0, true)) return false;
           if (s == 1) commit(sh.empty[v_item % Sh::kRing]);
           if (j + 1 < L) {
             if (s == 0 && !full(k_next)) return false;
@@ -761,7 +775,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
         const uint32_t v_item = item + 2 * j + 1, k_next = item + 2 * j + 4;
         if (!full(v_item)) return false;
         clear_tail(j, v_item);
-        if (!values(j & 1, v_item, j > 1)) return false;
+        if (!values(j & 1, v_item, j > 1, mode != kColumnsApart)) return false;
         commit(sh.empty[v_item % Sh::kRing]);
         if (j + 2 < L) {
           if (!full(k_next)) return false;
@@ -921,8 +935,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
       mbar_init(smem_u32(&sh.q_full[i]), 1);
       mbar_init(smem_u32(&sh.q_empty[i]), 1);
       mbar_init(smem_u32(&sh.s_full[i]), 1);
-      mbar_init(smem_u32(&sh.p_full[i]), 4);
-      mbar_init(smem_u32(&sh.pv_done[i]), 1);
+      for (int part = 0; part < 2; ++part) {
+        mbar_init(smem_u32(&sh.p_full[i][part]), 4);
+        mbar_init(smem_u32(&sh.pv_done[i][part]), 1);
+      }
     }
     mbar_init(smem_u32(&sh.drain), 1);
     fence_mbar_init();

@@ -1,7 +1,7 @@
 // Fifth-generation tensor cores, tensor memory, tensor copies and the shared
 // memory barriers between them (sm_103a), as the attention kernels use them.
 //
-//  * Waits on barriers are bounded: mbar_wait gives up after kMbarPolls tries.
+//  * Waits on barriers are bounded: mbar_wait gives up after kMbarCycles.
 //  * Tiles in shared memory are slabs of 64 16-bit columns: a row is 128
 //    bytes, and the 16-byte pieces of row i are permuted by i % 8 (the
 //    128-byte swizzle of tensor copies and of matrix operands).
@@ -13,7 +13,7 @@
 
 namespace ptc {
 
-constexpr uint32_t kMbarPolls = 1u << 21;  // about a second: half a microsecond each after the first few
+constexpr long long kMbarCycles = 4000000000ll;  // about two seconds
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -46,10 +46,11 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 // converged.  False if the phase did not complete in time: the caller gives up.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   bool ok = mbar_try(bar, parity);
+  if (!ok) {
+    const long long began = clock64();
 #pragma unroll 1
-  for (uint32_t i = 0; !ok && i < kMbarPolls; ++i) {
-    ok = mbar_try(bar, parity);
-    if (i > 4096) __nanosleep(500);
+    do ok = mbar_try(bar, parity);
+    while (!ok && clock64() - began < kMbarCycles);
   }
   return __all_sync(0xFFFFFFFFu, ok);
 }
