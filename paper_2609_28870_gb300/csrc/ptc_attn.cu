@@ -28,15 +28,17 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   __shared__ uint32_t s_m[kPlanThreads], s_n[kPlanThreads];
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, tq = a.tq;
   const bool weights = blockIdx.x == 1;
+  const uint32_t extra = weights ? kMassExtra : kTileExtra;
   AttnPlan* plan = a.plan + blockIdx.x;
   uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.x * (R + 1);
   // a request's first-level tiles, and the units of one of them
   auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kKeys) : 0u) : query_tiles(m, tq); };
   auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
-    return weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i);
+    return extra + (weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i));
   };
   bool bad = tid == 0 && (a.tok_off[0] != 0 || a.tok_off[R] != a.n_tok);
   uint64_t carry = 0;
+  for (uint32_t c = tid; c < kMaxCtas; c += kPlanThreads) plan->arrived[c] = 0;
   for (uint32_t r0 = 0; r0 < R; r0 += kPlanThreads) {
     const uint32_t r = r0 + tid;
     uint32_t m = 0, n = 0;
@@ -96,17 +98,20 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   const bool shared = R <= kPlanThreads;
   if (tid == 0 && shared) s_off[R] = carry;
   __syncthreads();
-  for (uint32_t c = warp; c < a.ctas; c += 32) {
-    const uint64_t u = carry * c / a.ctas;
-    CtaStart s{u, 0, 0, 0, 0};
-    if (u < carry) {
+  // 64-bit divisions are long; hardly a call needs one
+  auto ratio = [](uint64_t x, uint64_t y) { return x >> 32 || y >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y); };
+  const uint64_t each = ratio(carry, a.ctas);
+  const uint32_t over = (uint32_t)(carry - each * a.ctas);
+  for (uint32_t c = warp; c <= a.ctas; c += 32) {
+    CtaStart s{each * c + over * c / a.ctas, 0, 0, 0, 0};
+    if (s.u < carry) {
       uint32_t m, n;
       uint64_t from, to;
       if (shared) {
         uint32_t lo = 0, hi = R - 1;
         while (lo < hi) {
           const uint32_t mid = lo + (hi - lo + 1) / 2;
-          if (s_off[mid] <= u) lo = mid;
+          if (s_off[mid] <= s.u) lo = mid;
           else hi = mid - 1;
         }
         s.r = lo;
@@ -115,14 +120,14 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
         from = s_off[lo];
         to = s_off[lo + 1];
       } else {
-        s.r = unit_search(unit_off, 0, R - 1, u);
+        s.r = unit_search(unit_off, 0, R - 1, s.u);
         m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]);
         n = a.kv.kv_len[s.r];
         from = ld_relaxed_u64(unit_off + s.r);
         to = ld_relaxed_u64(unit_off + s.r + 1);
       }
-      const uint64_t head = (to - from) / a.kv.H, in = u - from;
-      s.h = (uint32_t)(in / head);
+      const uint64_t head = ratio(to - from, a.kv.H), in = s.u - from;
+      s.h = (uint32_t)ratio(in, head);
       uint64_t rest = in - s.h * head;
       const uint32_t tiles = tiles_of(m, n);
       for (uint32_t t0 = 0; t0 < tiles; t0 += 32) {
@@ -137,7 +142,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
         if (here) {
           const int src = __ffs(here) - 1;
           s.major = t0 + src;
-          s.minor = (uint32_t)rest - __shfl_sync(kFull, incl - k, src);
+          const uint32_t at = (uint32_t)rest - __shfl_sync(kFull, incl - k, src);
+          s.minor = at > extra ? at - extra : 0;
+          if (at <= extra) s.u -= at;
           break;
         }
         rest -= __shfl_sync(kFull, incl, 31);
@@ -149,8 +156,9 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
 
 // The query tiles that a CTA has a part in, in order, with the part.
 struct Walk {
-  uint64_t left, tok0, page0;
+  uint64_t left, u, tok0, page0;     // units left, the part's first unit
   uint32_t r, h, qt, kv0, kv1, nkv;  // key tiles [kv0, kv1) of nkv
+  uint32_t extra;                    // units before the first key tile
   uint32_t m, n;
   __device__ __forceinline__ void request(const AttnArgs& a) {
     tok0 = a.tok_off[r];
@@ -160,14 +168,15 @@ struct Walk {
   }
   __device__ __forceinline__ void part(const AttnArgs& a) {
     nkv = key_tiles(m, n, a.tq, qt);
-    kv1 = nkv - kv0 > left ? kv0 + (uint32_t)left : nkv;
+    extra = kv0 ? 0 : kTileExtra;
+    kv1 = nkv - kv0 + extra > left ? kv0 + (uint32_t)left - extra : nkv;
   }
   // False if the CTA has nothing to do.
   __device__ __forceinline__ bool begin(const AttnArgs& a) {
-    const uint64_t U = a.plan->units, c = blockIdx.x;
-    const CtaStart s = a.plan->start[c];
-    left = U * (c + 1) / a.ctas - s.u;
+    const CtaStart s = a.plan->start[blockIdx.x];
+    left = a.plan->start[blockIdx.x + 1].u - s.u;
     if (left == 0) return false;
+    u = s.u;
     r = s.r;
     h = s.h;
     qt = s.major;
@@ -177,7 +186,9 @@ struct Walk {
     return true;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a) {
-    left -= kv1 - kv0;
+    const uint32_t had = kv1 - kv0 + extra;
+    left -= had;
+    u += had;
     if (left == 0) return false;
     kv0 = 0;
     if (++qt * 2 * a.tq >= m) {
@@ -194,6 +205,9 @@ struct Walk {
     return true;
   }
   __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const { return qt * 2 * a.tq; }
+  // The units of the whole tile.
+  __device__ __forceinline__ uint64_t from() const { return kv0 ? u - kv0 - kTileExtra : u; }
+  __device__ __forceinline__ uint64_t to() const { return from() + kTileExtra + nkv; }
   // How the two halves of the softmax share the tile.
   __device__ __forceinline__ int mode(const AttnArgs& a) const {
     const uint32_t tokens = m - qt * 2 * a.tq;
@@ -262,7 +276,7 @@ constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 struct TileShared {
   uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2][2], drain;
   float2 ml[256];
-  uint32_t tmem;
+  uint32_t tmem, last, count;
 };
 
 // FEW: every request of the call has so few rows that its tiles are all
@@ -374,6 +388,78 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
 // The maximum moves when a row's sum of 64 (or 32) weights passes this: as many
 // of at most 1 stay below it, and no weight is larger than their sum.
 constexpr float kMove = 256.f;
+
+// The parts of a split tile put together, by all of the softmax: one thread a
+// row for its maximum and sum, then one warp a row, four rows at a time.
+// `slots` are the parts' places, in the order of the keys.
+template <typename T>
+__device__ __noinline__ void join_parts(const AttnArgs& a, TileShared& sh, const Walk& w, const uint32_t* slots,
+                                        uint32_t count) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.kv.D;
+  const uint32_t t0 = w.token0(a);
+  auto place = [&](uint32_t i, uint32_t& t) {  // of row i of the tile: its token; false if it is none
+    const uint32_t in = i & 127;
+    t = t0 + (i >> 7) * a.tq + in / a.G;
+    return in < a.tq * a.G && t < w.m;
+  };
+  uint32_t t;
+  if (place(threadIdx.x, t)) {
+    const float2* ml = a.part_ml + threadIdx.x;
+    float top = -INFINITY, l = 0.f;
+#pragma unroll 4
+    for (uint32_t p = 0; p < count; ++p) top = fmaxf(top, __ldcg(ml + slots[p] * kRows).x);
+#pragma unroll 4
+    for (uint32_t p = 0; p < count; ++p) {
+      const float2 x = __ldcg(ml + slots[p] * kRows);
+      l = fmaf(x.y, x.x == -INFINITY ? 0.f : exp2_approx(x.x - top), l);
+    }
+    const bool none = top == -INFINITY;
+    sh.ml[threadIdx.x] = make_float2(none ? 0.f : top, none ? 0.f : 1.f / l);
+    a.lse[(w.tok0 + t) * a.n_q_heads + w.h * a.G + (threadIdx.x & 127) % a.G] = none ? -INFINITY : (top + log2_approx(l)) * kLn2;
+  }
+  softmax_sync();
+  for (uint32_t i0 = warp * 4; i0 < kRows; i0 += 32) {
+    bool ok[4];
+    uint64_t at[4];
+    float4 o[4];
+    float2 mt[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      ok[k] = place(i0 + k, t);
+      at[k] = (w.tok0 + t) * a.n_q_heads + w.h * a.G + ((i0 + k) & 127) % a.G;
+      o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      mt[k] = sh.ml[i0 + k];
+    }
+    if (!ok[0]) continue;  // rows of a half are none from some row on
+    const bool in = 4 * lane < D;
+#pragma unroll 2
+    for (uint32_t p = 0; p < count; ++p) {
+      const uint64_t row = (uint64_t)slots[p] * kRows + i0;
+      float2 ml[4];
+      float4 x[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // (a part's place has all kRows rows; those that are none are not used)
+        ml[k] = __ldcg(a.part_ml + row + k);
+        x[k] = in ? __ldcg(reinterpret_cast<const float4*>(a.part + (row + k) * D + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (ml[k].x == -INFINITY) continue;  // the row saw no key of the part
+        const float f = exp2_approx(ml[k].x - mt[k].x) * mt[k].y;
+        o[k].x = fmaf(x[k].x, f, o[k].x);
+        o[k].y = fmaf(x[k].y, f, o[k].y);
+        o[k].z = fmaf(x[k].z, f, o[k].z);
+        o[k].w = fmaf(x[k].w, f, o[k].w);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (ok[k] && in)
+        *reinterpret_cast<uint2*>(a.out + 2 * (at[k] * D + 4 * lane)) =
+            make_uint2(Weights<T>::pack(o[k].x, o[k].y), Weights<T>::pack(o[k].z, o[k].w));
+  }
+}
 
 template <typename T, int NSLAB, bool FEW>
 __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, char* stages, uint32_t half) {
@@ -661,6 +747,37 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         }
         softmax_sync();
       }
+    }
+    if (!whole) {
+      // the last of the tile's CTAs to come here finds all parts in place
+      __threadfence();
+      softmax_sync();
+      uint32_t* slots = reinterpret_cast<uint32_t*>(stages);
+      if (threadIdx.x < 32) {
+        const Sharers s = sharers(a.plan, a.ctas, w.from(), w.to());
+        uint32_t last = 0;
+        if (lane == 0) last = atomicAdd(&a.plan->arrived[s.c0], 1u) + 1 == s.count;
+        __threadfence();
+        last = __shfl_sync(kFull, last, 0);
+        if (last) {
+          uint32_t n = 0;
+          for (uint32_t x0 = s.c0; x0 <= s.c1; x0 += 32) {
+            const uint32_t x = x0 + lane;
+            const uint64_t u = x <= s.c1 ? a.plan->start[x].u : 0, v = x <= s.c1 ? a.plan->start[x + 1].u : 0;
+            const uint32_t has = __ballot_sync(kFull, v > u);
+            // a CTA's first part, or (of the tile's first CTA, where it began with another tile) its last
+            if (v > u) slots[n + __popc(has & ((1u << lane) - 1))] = 2 * x + (u < w.from() ? 1 : 0);
+            n += __popc(has);
+          }
+        }
+        if (lane == 0) {
+          sh.last = last;
+          sh.count = s.count;
+        }
+      }
+      softmax_sync();
+      if (sh.last) join_parts<T>(a, sh, w, slots, sh.count);
+      softmax_sync();
     }
   }
   return true;
@@ -986,67 +1103,6 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   if (warp == 8) tmem_free(sh.tmem, 512);
 }
 
-// The rows of split tiles: CTA c looks whether its start is the first cut of
-// a tile, and then puts that tile's parts together.  blockIdx.y: 32 rows.
-template <typename T>
-__global__ void __launch_bounds__(256) k_attn_join(AttnArgs a) {
-  grid_dep_sync();
-  if (!a.plan->ok) return;
-  const uint32_t c = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, D = a.kv.D;
-  const uint64_t U = a.plan->units, C = a.ctas;
-  const CtaStart s = a.plan->start[c];
-  if (s.u == U * (c + 1) / C || s.minor == 0) return;
-  auto cta_of = [&](uint64_t u) { return (uint32_t)(((u + 1) * C - 1) / U); };
-  const uint64_t first = s.u - s.minor;
-  const uint32_t c0 = cta_of(first);
-  if (cta_of(s.u - 1) != c0) return;
-  const uint64_t tok0 = a.tok_off[s.r];
-  const uint32_t m = (uint32_t)(a.tok_off[s.r + 1] - tok0), n = a.kv.kv_len[s.r];
-  const uint32_t nkv = key_tiles(m, n, a.tq, s.major), c1 = cta_of(first + nkv - 1);
-  for (uint32_t i = blockIdx.y * 32 + warp; i < blockIdx.y * 32 + 32; i += 8) {
-    const uint32_t in = i & 127, t = s.major * 2 * a.tq + (i >> 7) * a.tq + in / a.G;
-    if (in >= a.tq * a.G || t >= m) continue;
-    auto slot_row = [&](uint32_t x) {
-      return (uint64_t)(2 * x + (x == c0 && a.plan->start[x].u != first ? 1 : 0)) * kRows + i;
-    };
-    auto empty = [&](uint32_t x) { return U * x / C == U * (x + 1) / C; };
-    float top = -INFINITY;
-    for (uint32_t x = c0; x <= c1; ++x)
-      if (!empty(x)) top = fmaxf(top, a.part_ml[slot_row(x)].x);
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t x = c0; x <= c1; ++x) {
-      if (empty(x)) continue;
-      const uint64_t at = slot_row(x);
-      const float2 ml = a.part_ml[at];
-      if (ml.x == -INFINITY) continue;  // its part of the row saw no key
-      const float f = exp2_approx(ml.x - top);
-      l = fmaf(ml.y, f, l);
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (lane + 32 * k < D) o[k] = fmaf(a.part[at * D + lane + 32 * k], f, o[k]);
-    }
-    const bool none = top == -INFINITY;
-    const float inv = none ? 0.f : 1.f / l;
-    const uint64_t at = (tok0 + t) * a.n_q_heads + s.h * a.G + in % a.G;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (lane + 32 * k < D) reinterpret_cast<T*>(a.out)[at * D + lane + 32 * k] = static_cast<T>(o[k] * inv);
-    if (lane == 0) a.lse[at] = none ? -INFINITY : (top + log2_approx(l)) * kLn2;
-  }
-}
-
-template <typename T>
-__device__ __forceinline__ float to_f(T x) { return static_cast<float>(x); }
-
-template <typename T>
-__device__ __forceinline__ float dot8(const uint4& a, const uint4& b, float acc) {
-  const T* x = reinterpret_cast<const T*>(&a);
-  const T* y = reinterpret_cast<const T*>(&b);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) acc = fmaf(to_f(x[i]), to_f(y[i]), acc);
-  return acc;
-}
-
 // cuTensorMapEncodeTiled, from the driver that the runtime has loaded.
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -1106,7 +1162,6 @@ ptc_status launch(AttnArgs& a, cudaStream_t s) {
     if (!tokens_map(&m[2], a, bf16, a.tq) || (a.tq32 && !tokens_map(&m[3], a, bf16, a.tq32))) return PTC_ERR_CUDA;
     const ptc_status st = a.kv.D > 64 ? launch_tiles<T, 2>(a, m, tma, s) : launch_tiles<T, 1>(a, m, tma, s);
     if (st != PTC_OK) return st;
-    PTC_KERNEL("k_attn_join", s, k_attn_join<T>, dim3(a.ctas, kRows / 32), 256, 0, a);
   }
   return a.mass_out && a.kv.n_page_ids ? launch_mass(a, bf16, m[0], m[2], tma, s) : PTC_OK;
 }

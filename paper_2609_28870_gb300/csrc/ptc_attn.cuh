@@ -26,12 +26,16 @@ struct CtaStart {
 };
 
 // What k_attn_plan leaves for the kernels after it.  Their work is a row of
-// units, for every request and key head its pairs of a query tile and a key
-// tile; CTA c of C takes the units [U c / C, U (c + 1) / C).
+// units: for every request, key head and first-level tile (a query tile, or a
+// key tile for the weights) `extra` units for what a tile costs by itself, then
+// one for every pair with a second-level tile.  CTA c of C takes the units from
+// start[c].u to start[c + 1].u, about U / C of them: a cut that falls among the
+// extra units is moved to before the tile.
 struct AttnPlan {
   uint32_t ok, pad;
   uint64_t units;
-  CtaStart start[kMaxCtas];
+  CtaStart start[kMaxCtas + 1];
+  uint32_t arrived[kMaxCtas];  // parts of the split tile that begins in CTA c
 };
 
 struct AttnArgs {
@@ -58,6 +62,31 @@ struct AttnArgs {
   uint32_t ctas, box;  // box: rows of a tensor copy of keys or values
   uint32_t* status;
 };
+
+// Units that a tile costs by itself: the softmax's first steps and the sums'
+// way out take about as long as three key tiles (measured on a step of mixed
+// chunks: TODO), a key tile's sum of weights about one query tile.
+constexpr uint32_t kTileExtra = 3, kMassExtra = 1;
+
+// The CTAs that share the units [from, to) of a split tile, c0 the first.
+struct Sharers {
+  uint32_t c0, c1, count;
+};
+// By a whole warp, over the plan's starts.
+__device__ __forceinline__ Sharers sharers(const AttnPlan* plan, uint32_t ctas, uint64_t from, uint64_t to) {
+  const uint32_t lane = threadIdx.x & 31;
+  uint32_t before = 0, until = 0, inside = 0;
+  for (uint32_t x = lane; x < ctas; x += 32) {
+    const uint64_t u = plan->start[x].u, v = plan->start[x + 1].u;
+    before += u <= from;
+    until += u < to;
+    inside += u > from && u < to && v > u;
+  }
+  before = __reduce_add_sync(kFull, before);
+  until = __reduce_add_sync(kFull, until);
+  inside = __reduce_add_sync(kFull, inside);
+  return {before - 1, until - 1, inside + 1};
+}
 
 __host__ __device__ __forceinline__ uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 

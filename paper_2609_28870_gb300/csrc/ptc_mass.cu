@@ -107,6 +107,7 @@ struct MassWalk {
   uint64_t left, tok0, page0;
   uint32_t r, h, kt, q0, q1;  // half query tiles [q0, q1)
   uint32_t first, count;      // the first one that sees the key tile, and how many do
+  uint32_t extra;             // units before the first of them
   uint32_t m, n;
   __device__ __forceinline__ void request(const AttnArgs& a) {
     tok0 = a.tok_off[r];
@@ -118,13 +119,13 @@ struct MassWalk {
     first = first_seeing(m, n, a.tq, kt);
     count = div_up(m, a.tq) - first;
     q0 = first + minor;
-    q1 = count - minor > left ? q0 + (uint32_t)left : first + count;
+    extra = minor ? 0 : kMassExtra;
+    q1 = count - minor + extra > left ? q0 + (uint32_t)left - extra : first + count;
   }
   __device__ __forceinline__ bool begin(const AttnArgs& a) {
     const AttnPlan* p = a.plan + 1;
-    const uint64_t U = p->units, c = blockIdx.x;
-    const CtaStart s = p->start[c];
-    left = U * (c + 1) / a.ctas - s.u;
+    const CtaStart s = p->start[blockIdx.x];
+    left = p->start[blockIdx.x + 1].u - s.u;
     if (left == 0) return false;
     r = s.r;
     h = s.h;
@@ -134,7 +135,7 @@ struct MassWalk {
     return true;
   }
   __device__ __forceinline__ bool next(const AttnArgs& a) {
-    left -= q1 - q0;
+    left -= q1 - q0 + extra;
     if (left == 0) return false;
     if ((uint64_t)++kt * kKeys >= n) {
       kt = 0;
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
 }
 
 // blockIdx.y = 0: the key tiles that CTAs of the kernel above share, as
-// k_attn_join does it for query tiles.  1: what no unit covers, the slots
+// the tile kernel does it for query tiles.  1: what no unit covers, the slots
 // past every request's tokens and the requests without queries.
 __global__ void __launch_bounds__(128) k_mass_join(const AttnArgs a) {
   grid_dep_sync();
@@ -408,21 +409,19 @@ __global__ void __launch_bounds__(128) k_mass_join(const AttnArgs a) {
     }
     return;
   }
-  const uint64_t U = plan->units, C = a.ctas;
   const CtaStart s = plan->start[c];
-  if (s.u == U * (c + 1) / C || s.minor == 0) return;
-  auto cta_of = [&](uint64_t u) { return (uint32_t)(((u + 1) * C - 1) / U); };
-  const uint64_t first = s.u - s.minor;
-  const uint32_t c0 = cta_of(first);
-  if (cta_of(s.u - 1) != c0) return;
+  if (s.u == plan->start[c + 1].u || s.minor == 0) return;
   const uint32_t m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]), n = a.kv.kv_len[s.r];
-  const uint32_t c1 = cta_of(first + div_up(m, a.tq) - first_seeing(m, n, a.tq, s.major) - 1);
+  const uint64_t first = s.u - s.minor - kMassExtra;
+  const Sharers sh = sharers(plan, a.ctas, first, first + kMassExtra + div_up(m, a.tq) - first_seeing(m, n, a.tq, s.major));
+  for (uint32_t x = sh.c0 + 1; x < c; ++x)
+    if (plan->start[x].u < plan->start[x + 1].u) return;  // not the first cut
   const uint64_t key = (uint64_t)s.major * kKeys + tid;
   if (key >= n) return;
   float sum = 0.f;
-  for (uint32_t x = c0; x <= c1; ++x) {
-    if (U * x / C == U * (x + 1) / C) continue;
-    sum += a.part_mass[(2 * (uint64_t)x + (x == c0 && plan->start[x].u != first ? 1 : 0)) * kKeys + tid];
+  for (uint32_t x = sh.c0; x <= sh.c1; ++x) {
+    if (x != sh.c0 && plan->start[x].u == plan->start[x + 1].u) continue;
+    sum += a.part_mass[(2 * (uint64_t)x + (x == sh.c0 && plan->start[x].u != first ? 1 : 0)) * kKeys + tid];
   }
   const uint64_t at = s.h * a.mass_stride + a.kv.page_off[s.r] * a.kv.B + key;
   a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum;
