@@ -29,7 +29,7 @@ import torch
 
 from . import build as _build
 from . import kv as _kv
-from .kv import (MAX_HEAD_DIM, PTC_DTYPE_BF16, PTC_DTYPE_FP16, check_status, ptc_kv_append,  # noqa: F401
+from .kv import (MAX_GROUP, MAX_HEAD_DIM, PTC_DTYPE_BF16, PTC_DTYPE_FP16, check_status, ptc_kv_append,  # noqa: F401
                  ptc_kv_evict, ptc_paged_attention)
 
 PTC_NONE = 0xFFFFFFFF

@@ -20,95 +20,106 @@ waits and raises what went wrong.  Without it a call waits and raises itself.
 from __future__ import annotations
 
 import ctypes
-import math
+import struct
+import sys
 
 import torch
 
 PTC_DTYPE_BF16, PTC_DTYPE_FP16 = 0, 1
-MAX_HEAD_DIM = 128
+MAX_HEAD_DIM, MAX_GROUP = 128, 128
 _DTYPES = {torch.bfloat16: PTC_DTYPE_BF16, torch.float16: PTC_DTYPE_FP16}
 
-
-class PagedKv(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride", ctypes.c_int64 * 3),
-                ("v_stride", ctypes.c_int64 * 3), ("page_ids", ctypes.c_void_p), ("page_off", ctypes.c_void_p),
-                ("kv_len", ctypes.c_void_p), ("n_page_ids", ctypes.c_uint64), ("n_pages", ctypes.c_uint32),
-                ("n_req", ctypes.c_uint32), ("block_size", ctypes.c_uint32), ("n_kv_heads", ctypes.c_uint32),
-                ("head_dim", ctypes.c_uint32), ("dtype", ctypes.c_int32)]
-
-
-_Strides = ctypes.c_int64 * 2
+# ptc_paged_kv and two strides, as the C compiler lays them out.  A decode step
+# makes one of these calls a layer, so the calls are marshalled in as few steps
+# as Python allows.
+PAGED_KV = struct.Struct("@PP6qPPPQ5Ii")
+_STRIDES = struct.Struct("@2q")
 
 
 def declare(L) -> None:
     """The argument types of the library's calls on paged keys and values."""
     vp, u32, u64, sz, st = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_size_t, ctypes.c_int
-    kv = ctypes.POINTER(PagedKv)
+    packed = ctypes.c_char_p
     L.ptc_kv_append_workspace_bytes.restype = sz
     L.ptc_kv_append_workspace_bytes.argtypes = [u32]
     L.ptc_kv_append.restype = st
-    L.ptc_kv_append.argtypes = [kv, vp, vp, _Strides, _Strides, vp, u64, vp, sz, vp, vp]
+    L.ptc_kv_append.argtypes = [packed, vp, vp, packed, packed, vp, u64, vp, sz, vp, vp]
     L.ptc_paged_attention_workspace_bytes.restype = sz
     L.ptc_paged_attention_workspace_bytes.argtypes = [u32, u32, u32, u32, u32, u64]
     L.ptc_paged_attention.restype = st
-    L.ptc_paged_attention.argtypes = [kv, vp, _Strides, vp, u64, u32, u32, ctypes.c_float, vp, vp, vp, vp, u64, vp, sz,
+    L.ptc_paged_attention.argtypes = [packed, vp, packed, vp, u64, u32, u32, ctypes.c_float, vp, vp, vp, vp, u64, vp, sz,
                                       vp, vp]
     L.ptc_kv_evict_workspace_bytes.restype = sz
     L.ptc_kv_evict_workspace_bytes.argtypes = [u32, u32, u32]
     L.ptc_kv_evict.restype = st
-    L.ptc_kv_evict.argtypes = [kv, vp, u64, u32, u32, u32, u32, vp, vp, u64, vp, vp, vp, u64, vp, sz, vp, vp]
+    L.ptc_kv_evict.argtypes = [packed, vp, u64, u32, u32, u32, u32, vp, vp, u64, vp, vp, vp, u64, vp, sz, vp, vp]
 
 
 def _pkg():
-    import paper_2609_28870_gb300 as ptc
-    return ptc
+    return sys.modules[__package__]
 
 
-def _want(t: torch.Tensor, dtype, name: str, dev, dims: int = 1) -> None:
-    if t.dtype != dtype or t.dim() != dims or t.device != dev:
-        raise ValueError(f"{name}: expected a {dims}-dimensional {dtype} tensor on {dev}")
+def _want(t: torch.Tensor, dtype, name: str, dev: int, dims: int = 1) -> None:
+    if t.dtype is not dtype or t.dim() != dims or t.get_device() != dev:
+        raise ValueError(f"{name}: expected a {dims}-dimensional {dtype} tensor on cuda:{dev}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous tensor")
 
 
-def _paged(k, v, page_ids, page_off, kv_len) -> PagedKv:
-    dev = _pkg()._dev(k)
-    if k.dtype not in _DTYPES or v.dtype != k.dtype or k.dim() != 4 or v.shape != k.shape or v.device != dev:
+def _paged(k, v, page_ids, page_off, kv_len, shape, dev: int) -> bytes:
+    """The packed ptc_paged_kv; shape is k's, dev its device's index."""
+    if dev < 0:
+        raise ValueError("expected a CUDA tensor")
+    if k.dtype not in _DTYPES or v.dtype is not k.dtype or len(shape) != 4 or v.shape != shape or v.get_device() != dev:
         raise ValueError("k and v: expected bfloat16 or float16 tensors [pages, key heads, block_size, head_dim] of one shape")
-    if k.shape[3] != 1 and (k.stride(3) != 1 or v.stride(3) != 1):
+    k0, k1, k2, k3 = k.stride()
+    v0, v1, v2, v3 = v.stride()
+    if shape[3] != 1 and (k3 != 1 or v3 != 1):
         raise ValueError("k and v: expected a contiguous last dimension")
     _want(page_ids, torch.int32, "page_ids", dev)
     _want(page_off, torch.int64, "page_off", dev)
     _want(kv_len, torch.int32, "kv_len", dev)
-    if page_off.numel() != kv_len.numel() + 1:
+    n_req = kv_len.shape[0]
+    if page_off.shape[0] != n_req + 1:
         raise ValueError("page_off: expected one entry more than kv_len")
-    ks, vs, shape = k.stride(), v.stride(), k.shape
-    return PagedKv(k.data_ptr(), v.data_ptr(), (ks[0], ks[1], ks[2]), (vs[0], vs[1], vs[2]), page_ids.data_ptr(),
-                   page_off.data_ptr(), kv_len.data_ptr(), page_ids.numel(), shape[0], kv_len.numel(), shape[2],
-                   shape[1], shape[3], _DTYPES[k.dtype])
+    return PAGED_KV.pack(k.data_ptr(), v.data_ptr(), k0, k1, k2, v0, v1, v2, page_ids.data_ptr(), page_off.data_ptr(),
+                         kv_len.data_ptr(), page_ids.shape[0], shape[0], n_req, shape[2], shape[1], shape[3],
+                         _DTYPES[k.dtype])
 
 
-def _tokens(x, name: str, k, tok_off, heads: int | None = None):
-    if x.dtype != k.dtype or x.dim() != 3 or x.shape[2] != k.shape[3] or x.device != k.device or (
-            heads is not None and x.shape[1] != heads):
-        raise ValueError(f"{name}: expected a {k.dtype} tensor [tokens, heads, {k.shape[3]}] on {k.device}")
-    if x.stride(2) != 1:
+def _tokens(x, name: str, k, dev: int, head_dim: int, heads: int | None = None) -> bytes:
+    shape = x.shape
+    if x.dtype is not k.dtype or len(shape) != 3 or shape[2] != head_dim or x.get_device() != dev or (
+            heads is not None and shape[1] != heads):
+        raise ValueError(f"{name}: expected a {k.dtype} tensor [tokens, heads, {head_dim}] on cuda:{dev}")
+    a, b, c = x.stride()
+    if c != 1:
         raise ValueError(f"{name}: expected a contiguous last dimension")
-    return _Strides(x.stride(0), x.stride(1))
+    return _STRIDES.pack(a, b)
 
 
-def _off(tok_off, kv_len) -> None:
-    _want(tok_off, torch.int64, "tok_off", kv_len.device)
-    if tok_off.numel() != kv_len.numel() + 1:
+def _off(tok_off, kv_len, dev: int) -> None:
+    _want(tok_off, torch.int64, "tok_off", dev)
+    if tok_off.shape[0] != kv_len.shape[0] + 1:
         raise ValueError("tok_off: expected one entry more than kv_len")
 
 
-def _status(status, dev):
+def _status(status, dev: int):
     if status is None:
         return None
-    if status.dtype != torch.int32 or status.numel() != 1 or status.device != dev:
+    if status.dtype is not torch.int32 or status.numel() != 1 or status.get_device() != dev:
         raise ValueError("status: expected one int32 on the cache's device")
     return status.data_ptr()
+
+
+def _room(k, need: int, dev: int, ws):
+    if ws is not None and ws.numel() >= need and ws.get_device() == dev:
+        return ws
+    return k.new_empty(max(need, 256), dtype=torch.uint8)
+
+
+def _stream(dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def check_status(status: torch.Tensor, call: str = "ptc") -> None:
@@ -124,16 +135,16 @@ def ptc_kv_append(k_new, v_new, k, v, page_ids, page_off, tok_off, kv_len, ws: t
                   status: torch.Tensor | None = None) -> None:
     """Writes the new tokens' keys and values ([tokens, key heads, head_dim])
     into their requests' pages, as the last tokens of kv_len."""
-    p = _pkg()
-    kv = _paged(k, v, page_ids, page_off, kv_len)
-    _off(tok_off, kv_len)
-    ks, vs = _tokens(k_new, "k_new", k, tok_off, k.shape[1]), _tokens(v_new, "v_new", k, tok_off, k.shape[1])
+    p, dev, shape = _pkg(), k.get_device(), k.shape
+    kv = _paged(k, v, page_ids, page_off, kv_len, shape, dev)
+    _off(tok_off, kv_len, dev)
+    ks, vs = _tokens(k_new, "k_new", k, dev, shape[3], shape[1]), _tokens(v_new, "v_new", k, dev, shape[3], shape[1])
     if v_new.shape != k_new.shape:
         raise ValueError("v_new: expected k_new's shape")
     L = p.lib()
-    w = p._workspace(L.ptc_kv_append_workspace_bytes(kv.n_req), k.device, ws)
-    rc = L.ptc_kv_append(ctypes.byref(kv), k_new.data_ptr(), v_new.data_ptr(), ks, vs, tok_off.data_ptr(),
-                         k_new.shape[0], w.data_ptr(), w.numel(), _status(status, k.device), p._stream(k.device))
+    w = _room(k, L.ptc_kv_append_workspace_bytes(kv_len.shape[0]), dev, ws)
+    rc = L.ptc_kv_append(kv, k_new.data_ptr(), v_new.data_ptr(), ks, vs, tok_off.data_ptr(), k_new.shape[0],
+                         w.data_ptr(), w.numel(), _status(status, dev), _stream(dev))
     p._check("ptc_kv_append", rc)
 
 
@@ -146,22 +157,25 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
     accumulated so far, float32 [key heads, slots]) or ``mass_out`` (where the
     new sums go; may be ``mass`` itself) also the accumulated weights.  ``scale``
     defaults to head_dim ** -0.5."""
-    p = _pkg()
-    kv = _paged(k, v, page_ids, page_off, kv_len)
-    _off(tok_off, kv_len)
-    qs = _tokens(q, "q", k, tok_off)
-    dev, T, Hq = k.device, q.shape[0], q.shape[1]
+    p, dev, shape = _pkg(), k.get_device(), k.shape
+    kv = _paged(k, v, page_ids, page_off, kv_len, shape, dev)
+    _off(tok_off, kv_len, dev)
+    D = shape[3]
+    qs = _tokens(q, "q", k, dev, D)
+    T, Hq, _ = q.shape
     if out is None:
-        out = torch.empty((T, Hq, kv.head_dim), dtype=q.dtype, device=dev)
+        out = q.new_empty((T, Hq, D))
     elif out.shape != q.shape:
         raise ValueError("out: expected q's shape")
+    else:
+        _want(out, q.dtype, "out", dev, 3)
     if lse is None:
-        lse = torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        lse = q.new_empty((T, Hq), dtype=torch.float32)
     elif lse.shape != q.shape[:2]:
         raise ValueError("lse: expected q's first two dimensions")
-    _want(out, q.dtype, "out", dev, 3)
-    _want(lse, torch.float32, "lse", dev, 2)
-    stride = 0
+    else:
+        _want(lse, torch.float32, "lse", dev, 2)
+    slots, m_in, m_out = 0, None, None
     if mass is not None or mass_out is not None:
         if mass_out is None:
             mass_out = torch.empty_like(mass)
@@ -170,16 +184,15 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
             _want(mass, torch.float32, "mass", dev, 2)
             if mass.shape != mass_out.shape:
                 raise ValueError("mass: expected mass_out's shape")
-        if mass_out.shape[0] != kv.n_kv_heads:
+            m_in = mass.data_ptr()
+        if mass_out.shape[0] != shape[1]:
             raise ValueError("mass: expected one row a key head")
-        stride = mass_out.shape[1]
+        slots, m_out = mass_out.shape[1], mass_out.data_ptr()
     L = p.lib()
-    need = L.ptc_paged_attention_workspace_bytes(kv.n_req, Hq, kv.n_kv_heads, kv.head_dim, int(max_q_len), stride)
-    w = p._workspace(need, dev, ws)
-    rc = L.ptc_paged_attention(ctypes.byref(kv), q.data_ptr(), qs, tok_off.data_ptr(), T, Hq, int(max_q_len),
-                               1 / math.sqrt(kv.head_dim) if scale is None else float(scale), out.data_ptr(),
-                               lse.data_ptr(), p._ptr(mass), p._ptr(mass_out), stride, w.data_ptr(), w.numel(),
-                               _status(status, dev), p._stream(dev))
+    w = _room(k, L.ptc_paged_attention_workspace_bytes(kv_len.shape[0], Hq, shape[1], D, max_q_len, slots), dev, ws)
+    rc = L.ptc_paged_attention(kv, q.data_ptr(), qs, tok_off.data_ptr(), T, Hq, max_q_len,
+                               D ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(), m_in, m_out, slots,
+                               w.data_ptr(), w.numel(), _status(status, dev), _stream(dev))
     p._check("ptc_paged_attention", rc)
     return (out, lse) if mass_out is None else (out, lse, mass_out)
 
@@ -190,27 +203,27 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
     last n_recent and the heaviest others) and moves them to the destination
     pages.  Returns (keep int32 [requests, key heads, n_keep], new_len int32,
     new_mass float32 [key heads, destination slots])."""
-    p = _pkg()
-    kv = _paged(k, v, page_ids, page_off, kv_len)
-    dev = k.device
+    p, dev, shape = _pkg(), k.get_device(), k.shape
+    kv = _paged(k, v, page_ids, page_off, kv_len, shape, dev)
     _want(mass, torch.float32, "mass", dev, 2)
     _want(dst_page_ids, torch.int32, "dst_page_ids", dev)
     _want(dst_page_off, torch.int64, "dst_page_off", dev)
-    if dst_page_off.numel() != kv_len.numel() + 1:
+    n_req, heads = kv_len.shape[0], shape[1]
+    if dst_page_off.shape[0] != n_req + 1:
         raise ValueError("dst_page_off: expected one entry more than kv_len")
-    if mass.shape[0] != kv.n_kv_heads:
+    if mass.shape[0] != heads:
         raise ValueError("mass: expected one row a key head")
     if min(n_keep, n_sink, n_recent, max_kv_len) < 0:
         raise ValueError("n_keep, n_sink, n_recent and max_kv_len: expected no negative numbers")
-    keep = torch.empty((kv.n_req, kv.n_kv_heads, n_keep), dtype=torch.int32, device=dev)
-    new_len = torch.empty(kv.n_req, dtype=torch.int32, device=dev)
-    slots = dst_page_ids.numel() * kv.block_size
-    new_mass = torch.empty((kv.n_kv_heads, slots), dtype=torch.float32, device=dev)
+    keep = kv_len.new_empty((n_req, heads, n_keep))
+    new_len = kv_len.new_empty(n_req)
+    slots = dst_page_ids.shape[0] * shape[2]
+    new_mass = mass.new_empty((heads, slots))
     L = p.lib()
-    w = p._workspace(L.ptc_kv_evict_workspace_bytes(kv.n_req, kv.n_kv_heads, max_kv_len), dev, ws)
-    rc = L.ptc_kv_evict(ctypes.byref(kv), mass.data_ptr(), mass.shape[1], n_keep, n_sink, n_recent, max_kv_len,
-                        dst_page_ids.data_ptr(), dst_page_off.data_ptr(), dst_page_ids.numel(), keep.data_ptr(),
-                        new_len.data_ptr(), new_mass.data_ptr(), slots, w.data_ptr(), w.numel(),
-                        _status(status, dev), p._stream(dev))
+    w = _room(k, L.ptc_kv_evict_workspace_bytes(n_req, heads, max_kv_len), dev, ws)
+    rc = L.ptc_kv_evict(kv, mass.data_ptr(), mass.shape[1], n_keep, n_sink, n_recent, max_kv_len,
+                        dst_page_ids.data_ptr(), dst_page_off.data_ptr(), dst_page_ids.shape[0], keep.data_ptr(),
+                        new_len.data_ptr(), new_mass.data_ptr(), slots, w.data_ptr(), w.numel(), _status(status, dev),
+                        _stream(dev))
     p._check("ptc_kv_evict", rc)
     return keep, new_len, new_mass
