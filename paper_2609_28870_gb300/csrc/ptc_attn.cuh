@@ -2,8 +2,6 @@
 // join, the C entry point; ptc_mass.cu: the accumulated weights).
 #pragma once
 
-#include <atomic>
-
 #include "ptc_kv.cuh"
 #include "ptc_tc.cuh"
 
@@ -104,17 +102,6 @@ __device__ __forceinline__ uint32_t first_seeing(uint32_t m, uint32_t n, uint32_
 }
 
 // Host side (ptc_attn.cu, ptc_mass.cu).
-// Lets a kernel have `bytes` of dynamic shared memory, once on every device.
-template <typename F>
-bool large_smem(F* kernel, int bytes, std::atomic<uint64_t>& ready) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  const uint64_t bit = uint64_t(1) << (dev & 63);
-  if (ready.load(std::memory_order_relaxed) & bit) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-  ready.fetch_or(bit, std::memory_order_relaxed);
-  return true;
-}
 bool tokens_map(CUtensorMap* map, const AttnArgs& a, bool bf16, uint32_t tokens);
 bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_t page, int64_t head, int64_t slot,
                uint32_t box);

@@ -67,6 +67,8 @@ __global__ void __launch_bounds__(kApThreads) k_kv_append(AppendArgs a) {
 }
 
 // ------------------------------------------------------------------ evict
+__host__ __device__ __forceinline__ uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
+
 struct EvictArgs {
   KvView kv;
   const float* mass;
@@ -90,113 +92,210 @@ __device__ __forceinline__ uint32_t order_of(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelBins = 2048;
+// The kept tokens of a request and key head: the weight that the need-th
+// heaviest of [n_sink, n - n_recent) has, by a radix search over 11, 11 and 10
+// bits of the ordered weights, then the positions above it, and the first of
+// those equal to it, in order.  Reading the weights is a few microseconds, so the
+// time is the chain of passes over one request's tokens: a cluster of CTAs
+// takes them, each a slice that it reads once and keeps in shared memory (or
+// reads again in every pass, where a slice is longer than that), and adds its
+// histogram and its counts up with the others' through their shared memory.
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
+constexpr uint32_t kSelBins = 2048;
+constexpr uint32_t kSelSlice = 40960;     // tokens of a slice that shared memory holds
+constexpr uint32_t kSelMaxCluster = 8;
 
-// One CTA a request and key head: the threshold weight by a radix search
-// (11, 11 and 10 bits, histograms in shared memory), then the kept positions
-// in order by a scan.
-__global__ void __launch_bounds__(kSelThreads) k_evict_select(EvictArgs a) {
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t rank) {
+  uint32_t at, v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ uint4 ld_cluster4(const uint32_t* p, uint32_t rank) {
+  uint32_t at;
+  uint4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+struct SelShared {
+  alignas(16) uint32_t hist[2][kSelBins];  // of even and odd passes
+  uint32_t warp[kSelWarps], ties[kSelWarps];
+  uint32_t bin, above, in_bin;
+  uint32_t count[2];           // of the slice: kept above the threshold, equal to it
+};
+
+__global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs a, uint32_t clusters, uint32_t slice_cap) {
   grid_dep_sync();
-  __shared__ uint32_t s_hist[kSelBins];
-  __shared__ uint32_t s_warp[32], s_warp2[32];
-  __shared__ uint32_t s_bin, s_above;
-  const uint32_t h = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  extern __shared__ uint32_t s_keys[];  // slice_cap of them, or none
+  __shared__ SelShared sh;
+  const uint32_t rank = blockIdx.x % clusters, h = blockIdx.x / clusters, r = blockIdx.y;
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t n = a.kv.kv_len[r], b = n < a.n_keep ? n : a.n_keep;
   const uint64_t d0 = a.dst_off[r], d1 = a.dst_off[r + 1];
   const bool ok = n <= a.max_kv_len && pages_hold(a.kv, r, n) && d0 <= d1 && d1 <= a.n_dst_ids &&
                   b <= (d1 - d0) * a.kv.B;
-  if (h == 0 && tid == 0) {
+  if (h == 0 && rank == 0 && tid == 0) {
     a.ok[r] = ok;
     a.new_len[r] = b;
     if (!ok) report(a.status, PTC_ERR_INVALID_ARG);
   }
-  if (!ok) return;
+  if (!ok) return;  // the whole cluster
   uint32_t* keep = a.keep + ((uint64_t)r * a.kv.H + h) * a.n_keep;
-  for (uint32_t i = b + tid; i < a.n_keep; i += kSelThreads) keep[i] = kNone;
+  const float* w = a.mass + h * a.mass_stride + a.kv.page_off[r] * a.kv.B;
+  float* new_w = a.new_mass + h * a.new_mass_stride + d0 * a.kv.B;
+  const uint32_t all = clusters * kSelThreads, me = rank * kSelThreads + tid;
+  for (uint32_t i = b + me; i < a.n_keep; i += all) keep[i] = kNone;
+  for (uint64_t i = b + me; i < (d1 - d0) * a.kv.B; i += all) new_w[i] = 0.f;
   if (b == n) {
-    for (uint32_t i = tid; i < n; i += kSelThreads) keep[i] = i;
+    for (uint32_t i = me; i < n; i += all) {
+      keep[i] = i;
+      new_w[i] = w[i];
+    }
     return;
   }
-  const float* w = a.mass + h * a.mass_stride + a.kv.page_off[r] * a.kv.B;
+  // the slice: a whole number of 32 tokens a warp
+  const uint32_t per_warp = (div_up(n, clusters * kSelWarps) + 31) & ~31u, slice = per_warp * kSelWarps;
+  const uint32_t s0 = rank * slice < n ? rank * slice : n, s1 = s0 + slice < n ? s0 + slice : n;
+  const bool held = slice <= slice_cap;
+  if (held) {
+#pragma unroll 8
+    for (uint32_t j = s0 + tid; j < s1; j += kSelThreads) s_keys[j - s0] = order_of(w[j]);
+    __syncthreads();
+  }
+  auto key_of = [&](uint32_t j) { return held ? s_keys[j - s0] : order_of(w[j]); };
   const uint32_t lo = a.n_sink, hi = n - a.n_recent;
   uint32_t need = b - a.n_sink - a.n_recent;
-  // the need-th largest of [lo, hi): prefix holds the bits settled so far
+  // prefix holds the bits of the threshold settled so far
   uint32_t prefix = 0, mask = 0;
+  bool whole_bin = false;
   if (need) {
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-      for (uint32_t i = tid; i < kSelBins; i += kSelThreads) s_hist[i] = 0;
+    const uint32_t f0 = s0 > lo ? s0 : lo, f1 = s1 < hi ? s1 : hi;
+#pragma unroll 1
+    for (int pass = 0; pass < 3 && !whole_bin; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t bins = pass == 2 ? 1024 : 2048;
+      uint32_t* hist = sh.hist[pass & 1];
+      for (uint32_t i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
       __syncthreads();
-      for (uint32_t j = lo + tid; j < hi; j += kSelThreads) {
-        const uint32_t o = order_of(w[j]);
-        if ((o & mask) == prefix) atomicAdd(&s_hist[(o >> shift) & ((1u << bits) - 1)], 1u);
+#pragma unroll 4
+      for (uint32_t j0 = f0 - (f0 & 31) + warp * 32; j0 < f1; j0 += kSelThreads) {
+        const uint32_t j = j0 + lane;
+        const uint32_t k = j >= f0 && j < f1 ? key_of(j) : 0;
+        const bool in = j >= f0 && j < f1 && (k & mask) == prefix;
+        const uint32_t some = __ballot_sync(kFull, in);
+        if (!some) continue;
+        const uint32_t bin = (k >> shift) & (bins - 1);
+        // equal weights (a warp's all in one bin) count at once
+        const uint32_t one = __shfl_sync(kFull, bin, __ffs(some) - 1);
+        if (__all_sync(kFull, !in || bin == one)) {
+          if (lane == 0) atomicAdd(&hist[one], __popc(some));
+        } else if (in) {
+          atomicAdd(&hist[bin], 1u);
+        }
       }
-      __syncthreads();
-      // bins from the top: thread t has bins 2047 - 2t and 2046 - 2t
-      const uint32_t c0 = s_hist[kSelBins - 1 - 2 * tid], c1 = s_hist[kSelBins - 2 - 2 * tid];
-      uint32_t x = c0 + c1;
+      cluster_sync_all();
+      // bins from the top: thread t has four from 2047 - 4t down
+      uint32_t c[4] = {0, 0, 0, 0};
+      for (uint32_t x = 0; x < clusters; ++x) {
+        const uint4 v = ld_cluster4(hist + kSelBins - 4 - 4 * tid, x);
+        c[0] += v.w;
+        c[1] += v.z;
+        c[2] += v.y;
+        c[3] += v.x;
+      }
+      uint32_t incl = c[0] + c[1] + c[2] + c[3];
+      const uint32_t mine = incl;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(kFull, x, o);
-        if (lane >= (uint32_t)o) x += y;
+        const uint32_t y = __shfl_up_sync(kFull, incl, o);
+        if (lane >= (uint32_t)o) incl += y;
       }
-      if (lane == 31) s_warp[warp] = x;
+      if (lane == 31) sh.warp[warp] = incl;
       __syncthreads();
-      uint32_t before = x - c0 - c1;
-      for (uint32_t i = 0; i < warp; ++i) before += s_warp[i];
-      if (before < need && need <= before + c0) {
-        s_bin = kSelBins - 1 - 2 * tid;
-        s_above = before;
-      } else if (before + c0 < need && need <= before + c0 + c1) {
-        s_bin = kSelBins - 2 - 2 * tid;
-        s_above = before + c0;
+      uint32_t before = incl - mine;
+      for (uint32_t x = 0; x < warp; ++x) before += sh.warp[x];
+#pragma unroll
+      for (uint32_t x = 0; x < 4; ++x) {
+        if (before < need && need <= before + c[x]) {
+          sh.bin = kSelBins - 1 - 4 * tid - x;
+          sh.above = before;
+          sh.in_bin = c[x];
+        }
+        before += c[x];
       }
       __syncthreads();
-      prefix |= s_bin << shift;
-      mask |= ((1u << bits) - 1) << shift;
-      need -= s_above;
+      prefix |= sh.bin << shift;
+      mask |= (bins - 1) << shift;
+      need -= sh.above;
+      whole_bin = need == sh.in_bin;  // all of the bin is kept: what is left of the bits does not matter
       __syncthreads();
     }
   } else {
-    prefix = 0xFFFFFFFFu;  // above every weight
+    prefix = mask = 0xFFFFFFFFu;  // above every weight
   }
-  // kept: sinks, recent tokens, weights above the threshold, and the first `need` equal to it
-  uint32_t kept = 0, ties = 0;
-  for (uint32_t base = 0; base < n; base += kSelThreads) {
-    const uint32_t j = base + tid;
-    bool more = false, tie = false;
-    if (j < n) {
-      if (j < lo || j >= hi) {
-        more = true;
-      } else {
-        const uint32_t o = order_of(w[j]);
-        more = o > prefix;
-        tie = o == prefix;
-      }
+  // a warp's stretch of the slice: how many are above the threshold (or kept
+  // in any case), how many equal to it; then where they go
+  const uint32_t t0 = s0 + warp * per_warp < s1 ? s0 + warp * per_warp : s1;
+  const uint32_t t1 = t0 + per_warp < s1 ? t0 + per_warp : s1;
+  auto look = [&](uint32_t j0, uint32_t& above, uint32_t& equal) {
+    const uint32_t j = j0 + lane;
+    bool up = false, eq = false;
+    if (j < t1) {
+      const uint32_t k = key_of(j) & mask;
+      const bool mid = j >= lo && j < hi;
+      up = !mid || k > prefix;
+      eq = mid && k == prefix;
     }
-    const uint32_t bt = __ballot_sync(kFull, tie);
-    if (lane == 0) s_warp2[warp] = __popc(bt);
-    __syncthreads();
-    uint32_t t_before = ties, t_all = ties;
-    for (uint32_t i = 0; i < 32; ++i) {
-      if (i < warp) t_before += s_warp2[i];
-      t_all += s_warp2[i];
-    }
-    if (tie && t_before + __popc(bt & ((1u << lane) - 1)) < need) more = true;
-    const uint32_t bk = __ballot_sync(kFull, more);
-    if (lane == 0) s_warp[warp] = __popc(bk);
-    __syncthreads();
-    uint32_t k_before = kept, k_all = kept;
-    for (uint32_t i = 0; i < 32; ++i) {
-      if (i < warp) k_before += s_warp[i];
-      k_all += s_warp[i];
-    }
-    if (more) keep[k_before + __popc(bk & ((1u << lane) - 1))] = j;
-    kept = k_all;
-    ties = t_all;
-    __syncthreads();
+    above = __ballot_sync(kFull, up);
+    equal = __ballot_sync(kFull, eq);
+  };
+  uint32_t n_up = 0, n_eq = 0;
+  for (uint32_t j0 = t0; j0 < t1; j0 += 32) {
+    uint32_t above, equal;
+    look(j0, above, equal);
+    n_up += __popc(above);
+    n_eq += __popc(equal);
   }
+  if (lane == 0) {
+    sh.warp[warp] = n_up;
+    sh.ties[warp] = n_eq;
+  }
+  __syncthreads();
+  uint32_t up_at = 0, eq_at = 0;
+  for (uint32_t x = 0; x < warp; ++x) {
+    up_at += sh.warp[x];
+    eq_at += sh.ties[x];
+  }
+  if (tid == kSelThreads - 1) {
+    sh.count[0] = up_at + n_up;
+    sh.count[1] = eq_at + n_eq;
+  }
+  cluster_sync_all();
+  for (uint32_t x = 0; x < rank; ++x) {
+    up_at += ld_cluster(&sh.count[0], x);
+    eq_at += ld_cluster(&sh.count[1], x);
+  }
+  for (uint32_t j0 = t0; j0 < t1; j0 += 32) {
+    uint32_t above, equal;
+    look(j0, above, equal);
+    const uint32_t below = (1u << lane) - 1, j = j0 + lane;
+    const uint32_t rank_eq = eq_at + __popc(equal & below), rank_up = up_at + __popc(above & below);
+    const bool tie = (equal >> lane & 1) && rank_eq < need;
+    if ((above >> lane & 1) || tie) {
+      const uint32_t at = rank_up + (rank_eq < need ? rank_eq : need);
+      keep[at] = j;
+      new_w[at] = w[j];
+    }
+    up_at += __popc(above);
+    eq_at += __popc(equal);
+  }
+  cluster_sync_all();  // no CTA ends while another reads its counts
 }
 
 constexpr int kMvThreads = 256;
@@ -208,10 +307,8 @@ __global__ void __launch_bounds__(kMvThreads) k_evict_move(EvictArgs a) {
   const uint32_t h = blockIdx.y, r = blockIdx.z, i0 = blockIdx.x * kMvRows;
   if (!a.ok[r]) return;
   const uint32_t b = a.new_len[r], n = a.kv.kv_len[r];
-  const uint64_t p0 = a.kv.page_off[r], d0 = a.dst_off[r], room = (a.dst_off[r + 1] - d0) * a.kv.B;
+  const uint64_t p0 = a.kv.page_off[r], d0 = a.dst_off[r];
   const uint32_t* keep = a.keep + ((uint64_t)r * a.kv.H + h) * a.n_keep;
-  if (blockIdx.x == 0)
-    for (uint64_t i = b + threadIdx.x; i < room; i += kMvThreads) a.new_mass[h * a.new_mass_stride + d0 * a.kv.B + i] = 0.f;
   const uint32_t rows = i0 >= b ? 0 : (b - i0 < kMvRows ? b - i0 : kMvRows), chunks = a.kv.D / 8;
   for (uint32_t x = threadIdx.x; x < rows * chunks; x += kMvThreads) {
     const uint32_t i = i0 + x / chunks, d = (x % chunks) * 8;
@@ -228,9 +325,37 @@ __global__ void __launch_bounds__(kMvThreads) k_evict_move(EvictArgs a) {
     const uint4 vx = *reinterpret_cast<const uint4*>(a.kv.v + 2 * (ps * a.kv.vs_page + ss * a.kv.vs_slot + vh));
     *reinterpret_cast<uint4*>(a.kv.k + 2 * (pd * a.kv.ks_page + sd * a.kv.ks_slot + kh)) = kx;
     *reinterpret_cast<uint4*>(a.kv.v + 2 * (pd * a.kv.vs_page + sd * a.kv.vs_slot + vh)) = vx;
-    if (d == 0)
-      a.new_mass[h * a.new_mass_stride + d0 * a.kv.B + i] = a.mass[h * a.mass_stride + p0 * a.kv.B + j];
   }
+}
+
+// CTAs a request and head: enough that a slice is at most 4,096 tokens (the
+// passes over a slice are then as short as the exchanges between them), as long
+// as all of them are on the GPU at once (two an SM), but no slices longer than
+// shared memory holds if there is a way.
+void launch_select(const EvictArgs& a, cudaStream_t s) {
+  const uint64_t pairs = (uint64_t)a.kv.H * a.kv.n_req, room = 2 * (uint64_t)num_sms();
+  uint32_t c = 1;
+  auto slice = [&](uint32_t x) { return div_up(a.max_kv_len, x); };
+  while (c < kSelMaxCluster && ((slice(c) > 4096 && 2 * c * pairs <= room) || slice(c) > kSelSlice / 4)) c *= 2;
+  // slices are rounded up to whole warps of 32 tokens
+  const uint32_t cap = slice(c) + 1024 <= kSelSlice ? slice(c) + 1024 : 0, smem = cap * 4;
+  static std::atomic<uint64_t> ready{0};
+  (void)large_smem(k_evict_select, kSelSlice * 4, ready);  // a failure shows at the launch
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = c;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(a.kv.H * c, a.kv.n_req);
+  cfg.blockDim = kSelThreads;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  (void)cudaLaunchKernelEx(&cfg, k_evict_select, a, c, cap);
 }
 
 size_t evict_bytes(uint32_t n_req) { return kKvStatusBytes + ((size_t)n_req * 4 + 255) / 256 * 256; }
@@ -310,7 +435,7 @@ extern "C" ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, ui
   a.new_mass_stride = new_mass_stride;
   a.ok = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + kKvStatusBytes);
   if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
-  PTC_KERNEL("k_evict_select", s, k_evict_select, dim3(kv->n_kv_heads, kv->n_req), kSelThreads, 0, a);
+  PTC_LAUNCH("k_evict_select", s, launch_select(a, s));
   const uint32_t most = n_keep < max_kv_len ? n_keep : max_kv_len;
   const uint32_t gx = most ? (most + kMvRows - 1) / kMvRows : 1;
   PTC_KERNEL("k_evict_move", s, k_evict_move, dim3(gx, kv->n_kv_heads, kv->n_req), kMvThreads, 0, a);

@@ -2,6 +2,8 @@
 // cache, the stream-ordered status word and the host-side argument checks.
 #pragma once
 
+#include <atomic>
+
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -86,6 +88,18 @@ inline ptc_status kv_end(uint32_t* status, const uint32_t* word, cudaStream_t s)
   if (cudaStreamSynchronize(s) != cudaSuccess) return PTC_ERR_CUDA;
   timer_resolve();
   return static_cast<ptc_status>(*reinterpret_cast<const uint32_t*>(pin));
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory, once on every device.
+template <typename F>
+bool large_smem(F* kernel, int bytes, std::atomic<uint64_t>& ready) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (ready.load(std::memory_order_relaxed) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  ready.fetch_or(bit, std::memory_order_relaxed);
+  return true;
 }
 
 constexpr size_t kKvStatusBytes = 256;

@@ -83,11 +83,14 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
 // ------------------------------------------------------------------ many rows
 // One CTA an SM walks its units, (key tile, half a query tile) pairs.  Scores
 // transposed, S = K Q^T: 128 keys in the lanes of tensor memory, up to 128
-// query rows in its columns, four such products in turn.  Warps 0-3 and 4-7 take
-// products in turn and add up exp2(s - lse) along a row of S, which is a
-// column of the scores; warp 8 issues the products, warp 9 loads key tiles
-// (with warp 11 where there are no tensor copies), warp 10 queries.
-constexpr int kMassThreads = 384;
+// query rows in its columns, four such products in turn.  Four groups of 4
+// warps take products in turn and add up exp2(s - lse) along a row of S, which
+// is a column of the scores (two groups, with half as many loads of scores in
+// flight, took 1,500 cycles a product of 512); warp 16 issues the products, warp
+// 17 loads key tiles (with warp 19 where there are no tensor copies), warp 18
+// queries.
+constexpr uint32_t kGroups = 4;
+constexpr int kMassThreads = kGroups * 128 + 128;
 constexpr int kSlab = 128 * 128;
 
 template <int NSLAB>
@@ -98,8 +101,8 @@ struct MassShape {
 
 struct MassShared {
   uint64_t k_full[2], k_empty[2], q_full[4], q_empty[4], s_full[4], s_empty[4], drain;
-  float lse[2][2][128];  // negated, in powers of two: of either half, two units
-  float sum[2][128];
+  float lse[kGroups][2][128];  // negated, in powers of two: of a group, two units
+  float sum[2][kGroups][128];  // of a key tile, two key tiles
   uint32_t tmem;
 };
 
@@ -156,7 +159,7 @@ struct MassWalk {
   }
 };
 
-__device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uint32_t half) {
+__device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uint32_t group) {
   const uint32_t tid = threadIdx.x & 127;
   const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
   const float sl2 = a.scale * kLog2e;
@@ -172,14 +175,14 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
       const uint64_t t = w.tok0 + (uint64_t)q * a.tq + tid / a.G;
       return -kLog2e * a.lse[t * a.n_q_heads + w.h * a.G + tid % a.G];
     };
-    uint32_t q = w.q0 + ((unit & 1) == half ? 0 : 1);
+    uint32_t q = w.q0 + ((group - unit) & (kGroups - 1));
     float ahead = q < w.q1 ? lse_of(q) : 0.f, total = 0.f;
-    for (; q < w.q1; q += 2, ++mine) {
+    for (; q < w.q1; q += kGroups, ++mine) {
       const uint32_t u = unit + (q - w.q0), buf = u & 3;
-      float* lse = sh.lse[half][mine & 1];
+      float* lse = sh.lse[group][mine & 1];
       lse[tid] = ahead;
-      asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory");
-      if (q + 2 < w.q1) ahead = lse_of(q + 2);
+      asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");
+      if (q + kGroups < w.q1) ahead = lse_of(q + kGroups);
       if (!mbar_wait(smem_u32(&sh.s_full[buf]), (u >> 2) & 1)) return false;
       tc_fence_after();
       const uint32_t rows = w.rows(a, q);
@@ -213,10 +216,11 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
       total += sum.x + sum.y;
     }
     unit += w.q1 - w.q0;
-    if (half == 1) sh.sum[seg & 1][tid] = total;
-    asm volatile("bar.sync 1, 256;" ::: "memory");
-    if (half == 0) {
-      total += sh.sum[seg & 1][tid];
+    if (group) sh.sum[seg & 1][group][tid] = total;
+    asm volatile("bar.sync 1, 512;" ::: "memory");
+    if (group == 0) {
+#pragma unroll
+      for (uint32_t k = 1; k < kGroups; ++k) total += sh.sum[seg & 1][k][tid];
       if (w.q0 == w.first && w.q1 == w.first + w.count) {
         if (key < w.n) {
           const uint64_t at = w.h * a.mass_stride + w.page0 * a.kv.B + key;
@@ -292,7 +296,7 @@ __device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, con
                                           uint32_t& seg) {
   using Sh = MassShape<NSLAB>;
   const uint32_t lane = threadIdx.x & 31;
-  const uint32_t tid = lane + (threadIdx.x >= 352 ? 32 : 0);
+  const uint32_t tid = lane + (threadIdx.x >= 608 ? 32 : 0);
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
     const uint32_t at = seg & 1, bar = smem_u32(&sh.k_full[at]), dst = smem + at * Sh::kTile;
@@ -356,7 +360,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
     mbar_init(smem_u32(&sh.drain), 1);
     fence_mbar_init();
   }
-  if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
+  if (warp == 16) tmem_alloc(smem_u32(&sh.tmem), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -364,20 +368,20 @@ __global__ void __launch_bounds__(kMassThreads, 1)
   bool fine = true;
   if (a.plan[1].ok) {
     uint32_t segs = 0, units = 0;
-    if (warp < 8) {
+    if (warp < 16) {
       fine = mass_sums(a, sh, warp / 4);
-    } else if (warp == 8) {
+    } else if (warp == 16) {
       fine = mass_products<T, NSLAB>(a, sh, smem);
       // every product and every arrival it owes is done before the CTA ends
       if (elect_lane()) mma_commit(smem_u32(&sh.drain));
       __syncwarp();
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
-    } else if (warp == 10) {
+    } else if (warp == 18) {
       fine = mass_queries<NSLAB>(a, sh, &mq, smem, units);
       if (!fine)  // given up: let the copies in flight land
         for (uint32_t u = units > 4 ? units - 4 : 0; u < units; ++u)
           (void)mbar_wait(smem_u32(&sh.q_full[u & 3]), (u >> 2) & 1);
-    } else if (warp == 9 || !TMA) {
+    } else if (warp == 17 || !TMA) {
       fine = mass_keys<NSLAB, TMA>(a, sh, &mk, smem, segs);
       if (!fine && TMA)
         for (uint32_t k = segs > 2 ? segs - 2 : 0; k < segs; ++k)
@@ -388,7 +392,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 8) tmem_free(sh.tmem, 512);
+  if (warp == 16) tmem_free(sh.tmem, 512);
 }
 
 // blockIdx.y = 0: the key tiles that CTAs of the kernel above share, as
