@@ -85,9 +85,12 @@ struct EvictArgs {
   uint32_t* status;
 };
 
-// Weights as integers in the same order: NaN lowest, -0 equal to 0.
+// Weights as integers in the same order: NaN lowest (1), -0 equal to 0, and
+// +infinity below kForced, which stands for tokens that are kept in any case;
+// 0 stands for no token.
+constexpr uint32_t kForced = 0xFFFFFFFFu;
 __device__ __forceinline__ uint32_t order_of(float w) {
-  if (w != w) return 0u;
+  if (w != w) return 1u;
   const uint32_t u = __float_as_uint(w + 0.0f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -115,16 +118,19 @@ __device__ __forceinline__ uint32_t ld_cluster(const uint32_t* p, uint32_t rank)
   return v;
 }
 
-__device__ __forceinline__ uint4 ld_cluster4(const uint32_t* p, uint32_t rank) {
-  uint32_t at;
-  uint4 v;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-  return v;
+// Inclusive sums along the warp.
+__device__ __forceinline__ uint32_t scan_warp(uint32_t x) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(kFull, x, o);
+    if ((threadIdx.x & 31) >= (uint32_t)o) x += y;
+  }
+  return x;
 }
 
 struct SelShared {
-  alignas(16) uint32_t hist[2][kSelBins];  // of even and odd passes
+  uint32_t hist[2][kSelBins];  // of even and odd passes
+  uint32_t coarse[2][64];      // sums of 32 bins
   uint32_t warp[kSelWarps], ties[kSelWarps];
   uint32_t bin, above, in_bin;
   uint32_t count[2];           // of the slice: kept above the threshold, equal to it
@@ -132,7 +138,7 @@ struct SelShared {
 
 __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs a, uint32_t clusters, uint32_t slice_cap) {
   grid_dep_sync();
-  extern __shared__ uint32_t s_keys[];  // slice_cap of them, or none
+  extern __shared__ __align__(16) float s_w[];  // slice_cap of them, or none
   __shared__ SelShared sh;
   const uint32_t rank = blockIdx.x % clusters, h = blockIdx.x / clusters, r = blockIdx.y;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -159,23 +165,46 @@ __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs
     }
     return;
   }
-  // the slice: a whole number of 32 tokens a warp
-  const uint32_t per_warp = (div_up(n, clusters * kSelWarps) + 31) & ~31u, slice = per_warp * kSelWarps;
-  const uint32_t s0 = rank * slice < n ? rank * slice : n, s1 = s0 + slice < n ? s0 + slice : n;
+  // the slice: a whole number of 128 tokens a warp
+  const uint32_t per_warp = (div_up(n, clusters * kSelWarps) + 127) & ~127u, slice = per_warp * kSelWarps;
+  const uint32_t s0 = rank * slice;
+  const uint32_t lo = a.n_sink, hi = n - a.n_recent;
   const bool held = slice <= slice_cap;
   if (held) {
-#pragma unroll 8
-    for (uint32_t j = s0 + tid; j < s1; j += kSelThreads) s_keys[j - s0] = order_of(w[j]);
+    // eight loads in flight a thread (past the end: the last token's weight, not used)
+    for (uint32_t j0 = tid; j0 < slice; j0 += 8 * kSelThreads) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const uint32_t j = s0 + j0 + u * kSelThreads;
+        x[u] = __ldg(w + (j < n ? j : n - 1));
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (j0 + u * kSelThreads < slice) s_w[j0 + u * kSelThreads] = x[u];
+    }
     __syncthreads();
   }
-  auto key_of = [&](uint32_t j) { return held ? s_keys[j - s0] : order_of(w[j]); };
-  const uint32_t lo = a.n_sink, hi = n - a.n_recent;
+  // four tokens of the slice
+  auto weights_of = [&](uint32_t j) {
+    if (held) return *reinterpret_cast<const float4*>(s_w + j);
+    auto one = [&](uint32_t x) { return __ldg(w + (s0 + x < n ? s0 + x : n - 1)); };
+    return make_float4(one(j), one(j + 1), one(j + 2), one(j + 3));
+  };
+  auto keys_of = [&](uint32_t j, const float4& x) {
+    uint4 k = make_uint4(order_of(x.x), order_of(x.y), order_of(x.z), order_of(x.w));
+    const uint32_t at = s0 + j;
+    if (at < lo || at + 4 > hi) {
+      auto one = [&](uint32_t y, uint32_t key) { return y >= n ? 0u : y < lo || y >= hi ? kForced : key; };
+      k = make_uint4(one(at, k.x), one(at + 1, k.y), one(at + 2, k.z), one(at + 3, k.w));
+    }
+    return k;
+  };
   uint32_t need = b - a.n_sink - a.n_recent;
   // prefix holds the bits of the threshold settled so far
   uint32_t prefix = 0, mask = 0;
   bool whole_bin = false;
   if (need) {
-    const uint32_t f0 = s0 > lo ? s0 : lo, f1 = s1 < hi ? s1 : hi;
 #pragma unroll 1
     for (int pass = 0; pass < 3 && !whole_bin; ++pass) {
       const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
@@ -183,51 +212,60 @@ __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs
       uint32_t* hist = sh.hist[pass & 1];
       for (uint32_t i = tid; i < kSelBins; i += kSelThreads) hist[i] = 0;
       __syncthreads();
-#pragma unroll 4
-      for (uint32_t j0 = f0 - (f0 & 31) + warp * 32; j0 < f1; j0 += kSelThreads) {
-        const uint32_t j = j0 + lane;
-        const uint32_t k = j >= f0 && j < f1 ? key_of(j) : 0;
-        const bool in = j >= f0 && j < f1 && (k & mask) == prefix;
-        const uint32_t some = __ballot_sync(kFull, in);
-        if (!some) continue;
-        const uint32_t bin = (k >> shift) & (bins - 1);
-        // equal weights (a warp's all in one bin) count at once
-        const uint32_t one = __shfl_sync(kFull, bin, __ffs(some) - 1);
-        if (__all_sync(kFull, !in || bin == one)) {
-          if (lane == 0) atomicAdd(&hist[one], __popc(some));
-        } else if (in) {
-          atomicAdd(&hist[bin], 1u);
+#pragma unroll 2
+      for (uint32_t j = 4 * tid; j < slice; j += 4 * kSelThreads) {
+        const uint4 v = keys_of(j, weights_of(j));
+        const uint32_t k[4] = {v.x, v.y, v.z, v.w};
+        // a run of equal weights counts at once
+        const uint32_t b0 = (v.x >> shift) & (bins - 1);
+        const bool in0 = (v.x & mask) == prefix;
+        if (v.x == v.y && v.x == v.z && v.x == v.w) {
+          if (in0) atomicAdd(&hist[b0], 4u);
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if ((k[x] & mask) == prefix) atomicAdd(&hist[(k[x] >> shift) & (bins - 1)], 1u);
         }
+      }
+      __syncthreads();
+      // sums of 32 bins; then one warp looks for the bin, first among the
+      // cluster's sums, then among the 32 bins
+#pragma unroll
+      for (uint32_t x = warp * (64 / kSelWarps); x < (warp + 1) * (64 / kSelWarps); ++x) {
+        // bins of kForced in the first pass: weights end below
+        const uint32_t at = 32 * x + lane, all_of = __reduce_add_sync(kFull, pass == 0 && at > 2044 ? 0u : hist[at]);
+        if (lane == 0) sh.coarse[pass & 1][x] = all_of;
       }
       cluster_sync_all();
-      // bins from the top: thread t has four from 2047 - 4t down
-      uint32_t c[4] = {0, 0, 0, 0};
-      for (uint32_t x = 0; x < clusters; ++x) {
-        const uint4 v = ld_cluster4(hist + kSelBins - 4 - 4 * tid, x);
-        c[0] += v.w;
-        c[1] += v.z;
-        c[2] += v.y;
-        c[3] += v.x;
-      }
-      uint32_t incl = c[0] + c[1] + c[2] + c[3];
-      const uint32_t mine = incl;
+      if (warp == 0) {
+        uint32_t c[2] = {0, 0};  // sums 63 - 2 lane and 62 - 2 lane
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(kFull, incl, o);
-        if (lane >= (uint32_t)o) incl += y;
-      }
-      if (lane == 31) sh.warp[warp] = incl;
-      __syncthreads();
-      uint32_t before = incl - mine;
-      for (uint32_t x = 0; x < warp; ++x) before += sh.warp[x];
-#pragma unroll
-      for (uint32_t x = 0; x < 4; ++x) {
-        if (before < need && need <= before + c[x]) {
-          sh.bin = kSelBins - 1 - 4 * tid - x;
-          sh.above = before;
-          sh.in_bin = c[x];
+        for (uint32_t x = 0; x < kSelMaxCluster; ++x) {
+          if (x >= clusters) break;
+          c[0] += ld_cluster(&sh.coarse[pass & 1][63 - 2 * lane], x);
+          c[1] += ld_cluster(&sh.coarse[pass & 1][62 - 2 * lane], x);
         }
-        before += c[x];
+        uint32_t before = scan_warp(c[0] + c[1]) - c[0] - c[1];
+        // the first sum, from the top, that reaches `need`
+        const bool one = before < need && need <= before + c[0];
+        const bool two = before + c[0] < need && need <= before + c[0] + c[1];
+        const int src = __ffs(__ballot_sync(kFull, one || two)) - 1;
+        const uint32_t at = __shfl_sync(kFull, one ? 63 - 2 * lane : 62 - 2 * lane, src);
+        const uint32_t up = __shfl_sync(kFull, one ? before : before + c[0], src);
+        const uint32_t mine = 32 * at + 31 - lane;  // of the 32 bins, from the top
+        uint32_t k = 0;
+#pragma unroll
+        for (uint32_t x = 0; x < kSelMaxCluster; ++x) {
+          if (x >= clusters) break;
+          k += ld_cluster(hist + mine, x);
+        }
+        if (pass == 0 && mine > 2044) k = 0;
+        before = up + scan_warp(k) - k;
+        if (before < need && need <= before + k) {
+          sh.bin = mine;
+          sh.above = before;
+          sh.in_bin = k;
+        }
       }
       __syncthreads();
       prefix |= sh.bin << shift;
@@ -237,31 +275,29 @@ __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs
       __syncthreads();
     }
   } else {
-    prefix = mask = 0xFFFFFFFFu;  // above every weight
+    prefix = kForced - 1;  // above every weight
+    mask = 0xFFFFFFFFu;
   }
   // a warp's stretch of the slice: how many are above the threshold (or kept
-  // in any case), how many equal to it; then where they go
-  const uint32_t t0 = s0 + warp * per_warp < s1 ? s0 + warp * per_warp : s1;
-  const uint32_t t1 = t0 + per_warp < s1 ? t0 + per_warp : s1;
-  auto look = [&](uint32_t j0, uint32_t& above, uint32_t& equal) {
-    const uint32_t j = j0 + lane;
-    bool up = false, eq = false;
-    if (j < t1) {
-      const uint32_t k = key_of(j) & mask;
-      const bool mid = j >= lo && j < hi;
-      up = !mid || k > prefix;
-      eq = mid && k == prefix;
-    }
-    above = __ballot_sync(kFull, up);
-    equal = __ballot_sync(kFull, eq);
+  // in any case), how many equal to it; then where they go.  Both counts in one
+  // word, 16 bits each (a lane's four tokens, a warp's 128).
+  const uint32_t t0 = warp * per_warp, t1 = t0 + per_warp;
+  auto look = [&](uint32_t j, const float4& x) {
+    const uint4 v = keys_of(j + 4 * lane, x);
+    const uint32_t k[4] = {v.x & mask, v.y & mask, v.z & mask, v.w & mask};
+    uint32_t bits = 0;  // above: bits 0-3, equal: bits 16-19
+#pragma unroll
+    for (int x = 0; x < 4; ++x) bits |= (k[x] > prefix ? 1u << x : 0u) | (k[x] == prefix ? 0x10000u << x : 0u);
+    return bits;
   };
   uint32_t n_up = 0, n_eq = 0;
-  for (uint32_t j0 = t0; j0 < t1; j0 += 32) {
-    uint32_t above, equal;
-    look(j0, above, equal);
-    n_up += __popc(above);
-    n_eq += __popc(equal);
+  for (uint32_t j = t0; j < t1; j += 128) {
+    const uint32_t bits = look(j, weights_of(j + 4 * lane));
+    n_up += __popc(bits & 0xFFFFu);
+    n_eq += __popc(bits >> 16);
   }
+  n_up = __reduce_add_sync(kFull, n_up);
+  n_eq = __reduce_add_sync(kFull, n_eq);
   if (lane == 0) {
     sh.warp[warp] = n_up;
     sh.ties[warp] = n_eq;
@@ -281,20 +317,35 @@ __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs
     up_at += ld_cluster(&sh.count[0], x);
     eq_at += ld_cluster(&sh.count[1], x);
   }
-  for (uint32_t j0 = t0; j0 < t1; j0 += 32) {
-    uint32_t above, equal;
-    look(j0, above, equal);
-    const uint32_t below = (1u << lane) - 1, j = j0 + lane;
-    const uint32_t rank_eq = eq_at + __popc(equal & below), rank_up = up_at + __popc(above & below);
-    const bool tie = (equal >> lane & 1) && rank_eq < need;
-    if ((above >> lane & 1) || tie) {
-      const uint32_t at = rank_up + (rank_eq < need ? rank_eq : need);
-      keep[at] = j;
-      new_w[at] = w[j];
+  if (n_up || n_eq)
+    for (uint32_t j = t0; j < t1; j += 128) {
+      const float4 x4 = weights_of(j + 4 * lane);
+      const float raw[4] = {x4.x, x4.y, x4.z, x4.w};
+      const uint32_t bits = look(j, x4);
+      const uint32_t mine = __popc(bits & 0xFFFFu) | __popc(bits >> 16) << 16;
+      uint32_t incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(kFull, incl, o);
+        if (lane >= (uint32_t)o) incl += y;
+      }
+      const uint32_t before = incl - mine;
+      uint32_t up = up_at + (before & 0xFFFFu), eq = eq_at + (before >> 16);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const bool above = bits >> x & 1, equal = bits >> (16 + x) & 1;
+        if (above || (equal && eq < need)) {
+          const uint32_t at = up + (eq < need ? eq : need), from = s0 + j + 4 * lane + x;
+          keep[at] = from;
+          new_w[at] = raw[x];
+        }
+        up += above;
+        eq += equal;
+      }
+      const uint32_t total = __shfl_sync(kFull, incl, 31);
+      up_at += total & 0xFFFFu;
+      eq_at += total >> 16;
     }
-    up_at += __popc(above);
-    eq_at += __popc(equal);
-  }
   cluster_sync_all();  // no CTA ends while another reads its counts
 }
 
@@ -337,8 +388,8 @@ void launch_select(const EvictArgs& a, cudaStream_t s) {
   uint32_t c = 1;
   auto slice = [&](uint32_t x) { return div_up(a.max_kv_len, x); };
   while (c < kSelMaxCluster && ((slice(c) > 4096 && 2 * c * pairs <= room) || slice(c) > kSelSlice / 4)) c *= 2;
-  // slices are rounded up to whole warps of 32 tokens
-  const uint32_t cap = slice(c) + 1024 <= kSelSlice ? slice(c) + 1024 : 0, smem = cap * 4;
+  // slices are rounded up to 128 tokens a warp
+  const uint32_t cap = slice(c) + 2048 <= kSelSlice ? slice(c) + 2048 : 0, smem = cap * 4;
   static std::atomic<uint64_t> ready{0};
   (void)large_smem(k_evict_select, kSelSlice * 4, ready);  // a failure shows at the launch
   cudaLaunchAttribute attr[2];
