@@ -16,10 +16,12 @@ __device__ __forceinline__ uint32_t unit_search(const uint64_t* off, uint32_t lo
   return lo;
 }
 
-// The requests' share of the units, and every CTA's start; CTA 0 for the tile
-// kernel, CTA 1 (where there is one) for the weights.  The time of a call of
-// few units is a chain of latencies, so what the lists hold is read once and
-// kept in shared memory (the first kPlanThreads requests of it).
+// The requests' share of the units, and every CTA's start; blockIdx.y = 0 for
+// the tile kernel, 1 (where there is one) for the weights.  The time of a call
+// of few units is a chain of latencies: what the lists hold is read once and
+// kept in shared memory (the first kPlanThreads requests of it), and the CTAs
+// here add it up each for itself and find 32 starts each, one a warp (one CTA
+// for all starts took 10 us, of which 8 were spent on them).
 constexpr int kPlanThreads = 1024;
 __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   asm volatile("griddepcontrol.launch_dependents;");
@@ -27,10 +29,10 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   __shared__ uint64_t s_warp[32], s_off[kPlanThreads + 1];
   __shared__ uint32_t s_m[kPlanThreads], s_n[kPlanThreads];
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, tq = a.tq;
-  const bool weights = blockIdx.x == 1;
+  const bool weights = blockIdx.y == 1;
   const uint32_t extra = weights ? kMassExtra : kTileExtra;
-  AttnPlan* plan = a.plan + blockIdx.x;
-  uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.x * (R + 1);
+  AttnPlan* plan = a.plan + blockIdx.y;
+  uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.y * (R + 1);
   // a request's first-level tiles, and the units of one of them
   auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kKeys) : 0u) : query_tiles(m, tq); };
   auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
@@ -38,14 +40,15 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   };
   bool bad = tid == 0 && (a.tok_off[0] != 0 || a.tok_off[R] != a.n_tok);
   uint64_t carry = 0;
-  for (uint32_t c = tid; c < kMaxCtas; c += kPlanThreads) plan->arrived[c] = 0;
+  if (blockIdx.x == 0 && tid < kMaxCtas) plan->arrived[tid] = 0;
   for (uint32_t r0 = 0; r0 < R; r0 += kPlanThreads) {
     const uint32_t r = r0 + tid;
     uint32_t m = 0, n = 0;
     if (r < R) {
       const uint64_t lo = a.tok_off[r], hi = a.tok_off[r + 1];
       n = a.kv.kv_len[r];
-      const bool wrong = lo > hi || hi > a.n_tok || hi - lo > a.max_q_len || !pages_hold(a.kv, r, n);
+      const bool hold = pages_hold(a.kv, r, n);
+      const bool wrong = (lo > hi) | (hi > a.n_tok) | (hi - lo > a.max_q_len) | !hold;
       bad |= wrong;
       m = wrong ? 0 : (uint32_t)(hi - lo);
     }
@@ -73,11 +76,14 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
     }
     if (lane == 31) s_warp[warp] = incl;
     __syncthreads();
-    uint64_t before = carry + incl - mine, all = carry;
-    for (uint32_t w = 0; w < 32; ++w) {
-      if (w < warp) before += s_warp[w];
-      all += s_warp[w];
+    uint64_t sums = s_warp[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t y = __shfl_up_sync(kFull, sums, o);
+      if (lane >= (uint32_t)o) sums += y;
     }
+    const uint64_t earlier = __shfl_sync(kFull, sums, warp ? warp - 1 : 0);
+    const uint64_t before = carry + incl - mine + (warp ? earlier : 0), all = carry + __shfl_sync(kFull, sums, 31);
     if (r < R) unit_off[r] = before;
     if (r0 == 0) {
       s_off[tid] = before;
@@ -90,8 +96,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   bad = __syncthreads_or(bad);
   if (tid == 0) {
     unit_off[R] = carry;
-    plan->ok = !bad;
-    plan->units = carry;
+    if (blockIdx.x == 0) plan->ok = !bad;
     if (bad) report(a.status, PTC_ERR_INVALID_ARG);
   }
   if (bad) return;
@@ -102,10 +107,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   auto ratio = [](uint64_t x, uint64_t y) { return x >> 32 || y >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y); };
   const uint64_t each = ratio(carry, a.ctas);
   const uint32_t over = (uint32_t)(carry - each * a.ctas);
-  for (uint32_t c = warp; c <= a.ctas; c += 32) {
-    CtaStart s{each * c + over * c / a.ctas, 0, 0, 0, 0};
+  const uint32_t c = blockIdx.x * 32 + warp;
+  if (c <= a.ctas) {
+    CtaStart s{};
+    s.u = each * c + over * c / a.ctas;
+    uint32_t m = 0, n = 0;
     if (s.u < carry) {
-      uint32_t m, n;
       uint64_t from, to;
       if (shared) {
         uint32_t lo = 0, hi = R - 1;
@@ -144,11 +151,25 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
           s.major = t0 + src;
           const uint32_t at = (uint32_t)rest - __shfl_sync(kFull, incl - k, src);
           s.minor = at > extra ? at - extra : 0;
-          if (at <= extra) s.u -= at;
+          const uint32_t all = __shfl_sync(kFull, k, src) - extra;
+          const uint32_t least = weights || m - s.major * 2 * tq <= a.tq32 ? 1 : kPartMin;
+          if (s.minor < least) {
+            s.u -= at;
+            s.minor = 0;
+          } else if (all - s.minor < least) {
+            s.u += extra + all - at;
+            s.minor = all;
+          }
           break;
         }
         rest -= __shfl_sync(kFull, incl, 31);
       }
+    }
+    if (s.u < carry) {
+      s.m = m;
+      s.n = n;
+      s.tok0 = a.tok_off[s.r];
+      s.page0 = a.kv.page_off[s.r];
     }
     if (lane == 0) plan->start[c] = s;
   }
@@ -160,6 +181,7 @@ struct Walk {
   uint32_t r, h, qt, kv0, kv1, nkv;  // key tiles [kv0, kv1) of nkv
   uint32_t extra;                    // units before the first key tile
   uint32_t m, n;
+  bool first;                        // the CTA's first part
   __device__ __forceinline__ void request(const AttnArgs& a) {
     tok0 = a.tok_off[r];
     m = (uint32_t)(a.tok_off[r + 1] - tok0);
@@ -171,25 +193,8 @@ struct Walk {
     extra = kv0 ? 0 : kTileExtra;
     kv1 = nkv - kv0 + extra > left ? kv0 + (uint32_t)left - extra : nkv;
   }
-  // False if the CTA has nothing to do.
-  __device__ __forceinline__ bool begin(const AttnArgs& a) {
-    const CtaStart s = a.plan->start[blockIdx.x];
-    left = a.plan->start[blockIdx.x + 1].u - s.u;
-    if (left == 0) return false;
-    u = s.u;
-    r = s.r;
-    h = s.h;
-    qt = s.major;
-    kv0 = s.minor;
-    request(a);
-    part(a);
-    return true;
-  }
-  __device__ __forceinline__ bool next(const AttnArgs& a) {
-    const uint32_t had = kv1 - kv0 + extra;
-    left -= had;
-    u += had;
-    if (left == 0) return false;
+  // The next query tile.
+  __device__ __forceinline__ bool step(const AttnArgs& a) {
     kv0 = 0;
     if (++qt * 2 * a.tq >= m) {
       qt = 0;
@@ -201,6 +206,33 @@ struct Walk {
         } while (m == 0);
       }
     }
+    return true;
+  }
+  // False if the CTA has nothing to do.
+  __device__ __forceinline__ bool begin(const AttnArgs& a) {
+    const CtaStart s = a.plan->start[blockIdx.x];
+    left = a.plan->start[blockIdx.x + 1].u - s.u;
+    if (left == 0) return false;
+    u = s.u;
+    first = true;
+    r = s.r;
+    h = s.h;
+    qt = s.major;
+    kv0 = s.minor;
+    tok0 = s.tok0;
+    m = s.m;
+    n = s.n;
+    page0 = s.page0;
+    if (kv0 && kv0 == key_tiles(m, n, a.tq, qt) && !step(a)) return false;
+    part(a);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const AttnArgs& a) {
+    const uint32_t had = kv1 - kv0 + extra;
+    left -= had;
+    u += had;
+    first = false;
+    if (left == 0 || !step(a)) return false;
     part(a);
     return true;
   }
@@ -276,7 +308,8 @@ constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
 struct TileShared {
   uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2][2], drain;
   float2 ml[256];
-  uint32_t tmem, last, count;
+  uint32_t tmem, last, count, c0;
+  uint16_t slots[kMaxCtas];  // a split tile's parts, in the order of the keys
 };
 
 // FEW: every request of the call has so few rows that its tiles are all
@@ -389,75 +422,104 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
 // of at most 1 stay below it, and no weight is larger than their sum.
 constexpr float kMove = 256.f;
 
-// The parts of a split tile put together, by all of the softmax: one thread a
-// row for its maximum and sum, then one warp a row, four rows at a time.
-// `slots` are the parts' places, in the order of the keys.
-template <typename T>
-__device__ __noinline__ void join_parts(const AttnArgs& a, TileShared& sh, const Walk& w, const uint32_t* slots,
-                                        uint32_t count) {
-  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.kv.D;
-  const uint32_t t0 = w.token0(a);
-  auto place = [&](uint32_t i, uint32_t& t) {  // of row i of the tile: its token; false if it is none
-    const uint32_t in = i & 127;
-    t = t0 + (i >> 7) * a.tq + in / a.G;
-    return in < a.tq * a.G && t < w.m;
-  };
-  uint32_t t;
-  if (place(threadIdx.x, t)) {
-    const float2* ml = a.part_ml + threadIdx.x;
-    float top = -INFINITY, l = 0.f;
-#pragma unroll 4
-    for (uint32_t p = 0; p < count; ++p) top = fmaxf(top, __ldcg(ml + slots[p] * kRows).x);
-#pragma unroll 4
-    for (uint32_t p = 0; p < count; ++p) {
-      const float2 x = __ldcg(ml + slots[p] * kRows);
-      l = fmaf(x.y, x.x == -INFINITY ? 0.f : exp2_approx(x.x - top), l);
-    }
-    const bool none = top == -INFINITY;
-    sh.ml[threadIdx.x] = make_float2(none ? 0.f : top, none ? 0.f : 1.f / l);
-    a.lse[(w.tok0 + t) * a.n_q_heads + w.h * a.G + (threadIdx.x & 127) % a.G] = none ? -INFINITY : (top + log2_approx(l)) * kLn2;
+// Who has a part of the tile, and where; by one warp.
+__device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, const Walk& w) {
+  const uint32_t lane = threadIdx.x & 31;
+  const uint64_t from = w.from();
+  const Sharers s = sharers(a.plan, a.ctas, from, w.to());
+  uint32_t n = 0;
+  for (uint32_t x0 = s.c0; x0 <= s.c1; x0 += 32) {
+    const uint32_t x = x0 + lane;
+    const uint64_t u = x <= s.c1 ? a.plan->start[x].u : 0, v = x <= s.c1 ? a.plan->start[x + 1].u : 0;
+    const uint32_t has = __ballot_sync(kFull, v > u);
+    // a CTA's first part, or (of the tile's first CTA, where it began with another tile) its last
+    if (v > u) sh.slots[n + __popc(has & ((1u << lane) - 1))] = (uint16_t)(2 * x + (u < from ? 1 : 0));
+    n += __popc(has);
   }
-  softmax_sync();
-  for (uint32_t i0 = warp * 4; i0 < kRows; i0 += 32) {
-    bool ok[4];
-    uint64_t at[4];
-    float4 o[4];
-    float2 mt[4];
+  if (lane == 0) {
+    sh.c0 = s.c0;
+    sh.count = s.count;
+  }
+  __syncwarp();
+}
+
+// The parts of a split tile put together, by all of the softmax: a warp takes
+// ROWS rows at a time.  Lane p looks at part p's maximum and sum of a row; then
+// the lanes have 4 columns each, and the parts are added up in the order of the
+// keys.
+template <typename T, int ROWS>
+__device__ __noinline__ void join_parts(const AttnArgs& a, const TileShared& sh, const Walk& w) {
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.kv.D, count = sh.count;
+  const uint32_t t0 = w.token0(a);
+  const bool in = 4 * lane < D;
+  for (uint32_t i0 = warp * ROWS; i0 < (ROWS == 1 ? 32 : kRows); i0 += 8 * ROWS) {
+    bool ok[ROWS];
+    uint64_t at[ROWS];
+    float top[ROWS], l[ROWS];
+    float2 ml[ROWS];
+    float4 o[ROWS];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      ok[k] = place(i0 + k, t);
-      at[k] = (w.tok0 + t) * a.n_q_heads + w.h * a.G + ((i0 + k) & 127) % a.G;
+    for (int k = 0; k < ROWS; ++k) {
+      // row i of the tile: its half, token and head
+      const uint32_t i = (i0 + k) & 127, t = t0 + ((i0 + k) >> 7) * a.tq + i / a.G;
+      ok[k] = i < a.tq * a.G && t < w.m;
+      at[k] = (w.tok0 + t) * a.n_q_heads + w.h * a.G + i % a.G;
+      top[k] = -INFINITY;
+      l[k] = 0.f;
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      mt[k] = sh.ml[i0 + k];
     }
     if (!ok[0]) continue;  // rows of a half are none from some row on
-    const bool in = 4 * lane < D;
-#pragma unroll 2
-    for (uint32_t p = 0; p < count; ++p) {
-      const uint64_t row = (uint64_t)slots[p] * kRows + i0;
-      float2 ml[4];
-      float4 x[4];
+    auto look = [&](uint32_t p0) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // (a part's place has all kRows rows; those that are none are not used)
-        ml[k] = __ldcg(a.part_ml + row + k);
-        x[k] = in ? __ldcg(reinterpret_cast<const float4*>(a.part + (row + k) * D + 4 * lane)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < ROWS; ++k)
+        ml[k] = p0 + lane < count ? __ldcg(a.part_ml + sh.slots[p0 + lane] * kRows + i0 + k) : make_float2(-INFINITY, 0.f);
+    };
+    for (uint32_t p0 = 0; p0 < count; p0 += 32) {
+      look(p0);
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) {
+        float mx = ml[k].x;
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, x));
+        const float nt = fmaxf(top[k], mx), base = nt == -INFINITY ? 0.f : nt;
+        float sum = ml[k].x == -INFINITY ? 0.f : ml[k].y * exp2_approx(ml[k].x - base);
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(kFull, sum, x);
+        l[k] = l[k] * exp2_approx(top[k] - base) + sum;
+        top[k] = nt;
       }
+    }
+    for (uint32_t p0 = 0; p0 < count; p0 += 32) {
+      if (count > 32) look(p0);
+      float f[ROWS];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        if (ml[k].x == -INFINITY) continue;  // the row saw no key of the part
-        const float f = exp2_approx(ml[k].x - mt[k].x) * mt[k].y;
-        o[k].x = fmaf(x[k].x, f, o[k].x);
-        o[k].y = fmaf(x[k].y, f, o[k].y);
-        o[k].z = fmaf(x[k].z, f, o[k].z);
-        o[k].w = fmaf(x[k].w, f, o[k].w);
+      for (int k = 0; k < ROWS; ++k) f[k] = ml[k].x == -INFINITY ? 0.f : exp2_approx(ml[k].x - top[k]) / l[k];
+      const uint32_t n = count - p0 < 32 ? count - p0 : 32;
+#pragma unroll (8 / ROWS)
+      for (uint32_t p = 0; p < n; ++p) {
+        const float* row = a.part + ((uint64_t)sh.slots[p0 + p] * kRows + i0) * D + 4 * lane;
+        float4 x[ROWS];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k)  // (a part's place has all kRows rows; those that are none are not used)
+          x[k] = in ? __ldcg(reinterpret_cast<const float4*>(row + k * D)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+          const float fp = __shfl_sync(kFull, f[k], p);
+          if (fp == 0.f) continue;  // the row saw no key of the part
+          o[k].x = fmaf(x[k].x, fp, o[k].x);
+          o[k].y = fmaf(x[k].y, fp, o[k].y);
+          o[k].z = fmaf(x[k].z, fp, o[k].z);
+          o[k].w = fmaf(x[k].w, fp, o[k].w);
+        }
       }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < ROWS; ++k) {
       if (ok[k] && in)
         *reinterpret_cast<uint2*>(a.out + 2 * (at[k] * D + 4 * lane)) =
             make_uint2(Weights<T>::pack(o[k].x, o[k].y), Weights<T>::pack(o[k].z, o[k].w));
+      if (ok[k] && lane == 0) a.lse[at[k]] = top[k] == -INFINITY ? -INFINITY : (top[k] + log2_approx(l[k])) * kLn2;
+    }
   }
 }
 
@@ -472,7 +534,6 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
   const uint32_t bar_o[2] = {smem_u32(&sh.pv_done[half][0]), smem_u32(&sh.pv_done[half][1])};
   const float sl2 = a.scale * kLog2e;
   const uint32_t D = a.kv.D, G = a.G;
-  const CtaStart start = a.plan->start[blockIdx.x];
   char* stage = stages + (half * 4 + warp) * 4096;
   uint32_t done = 0, parted = 0;  // key tiles of this half so far, and those in two parts
   Walk w;
@@ -489,6 +550,8 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     int64_t see_all = valid ? (int64_t)w.n - w.m + t + 1 - (int64_t)j0 * kKeys : INT64_MAX / 2;
     RowState st;
     st.clear();
+    const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
+    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w);
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
         if (!mbar_wait(bar_s, done & 1)) return false;
@@ -602,9 +665,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     const bool some = j0 < w.kv1;  // this half had a key tile
     if (some && !mbar_wait(bar_o[1], (done - 1) & 1)) return false;
     tc_fence_after();
-    const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
-    const bool first = w.kv0 == start.minor && w.qt == start.major && w.h == start.h && w.r == start.r;
-    const uint64_t prow0 = (uint64_t)(2 * blockIdx.x + (first ? 0 : 1)) * kRows;
+    const uint64_t prow0 = (uint64_t)(2 * blockIdx.x + (w.first ? 0 : 1)) * kRows;
     const uint64_t orow0 = w.tok0 * a.n_q_heads + w.h * G;  // row (t, g) is orow0 + t * n_q_heads + g
     if (mode != kColumnsApart) {
       float top2 = st.top2<W>(sl2), l = st.l, f0 = 1.f, f1 = 0.f;
@@ -752,31 +813,15 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
       // the last of the tile's CTAs to come here finds all parts in place
       __threadfence();
       softmax_sync();
-      uint32_t* slots = reinterpret_cast<uint32_t*>(stages);
-      if (threadIdx.x < 32) {
-        const Sharers s = sharers(a.plan, a.ctas, w.from(), w.to());
-        uint32_t last = 0;
-        if (lane == 0) last = atomicAdd(&a.plan->arrived[s.c0], 1u) + 1 == s.count;
+      if (threadIdx.x == 0) {
+        sh.last = atomicAdd(&a.plan->arrived[sh.c0], 1u) + 1 == sh.count;
         __threadfence();
-        last = __shfl_sync(kFull, last, 0);
-        if (last) {
-          uint32_t n = 0;
-          for (uint32_t x0 = s.c0; x0 <= s.c1; x0 += 32) {
-            const uint32_t x = x0 + lane;
-            const uint64_t u = x <= s.c1 ? a.plan->start[x].u : 0, v = x <= s.c1 ? a.plan->start[x + 1].u : 0;
-            const uint32_t has = __ballot_sync(kFull, v > u);
-            // a CTA's first part, or (of the tile's first CTA, where it began with another tile) its last
-            if (v > u) slots[n + __popc(has & ((1u << lane) - 1))] = 2 * x + (u < w.from() ? 1 : 0);
-            n += __popc(has);
-          }
-        }
-        if (lane == 0) {
-          sh.last = last;
-          sh.count = s.count;
-        }
       }
       softmax_sync();
-      if (sh.last) join_parts<T>(a, sh, w, slots, sh.count);
+      if (sh.last) {
+        if (mode == kColumnsApart) join_parts<T, 1>(a, sh, w);
+        else join_parts<T, 4>(a, sh, w);
+      }
       softmax_sync();
     }
   }
@@ -1148,7 +1193,7 @@ template <typename T>
 ptc_status launch(AttnArgs& a, cudaStream_t s) {
   constexpr bool bf16 = Weights<T>::kBf16;
   const bool by_tiles = a.mass_out && !a.scores && a.n_tok;  // the weights' own tiles
-  PTC_KERNEL("k_attn_plan", s, k_attn_plan, by_tiles ? 2 : 1, kPlanThreads, 0, a);
+  PTC_KERNEL("k_attn_plan", s, k_attn_plan, dim3(a.ctas / 32 + 1, by_tiles ? 2 : 1), kPlanThreads, 0, a);
   CUtensorMap m[4] = {};
   bool tma = false;
   if (a.n_tok) {

@@ -12,15 +12,15 @@ namespace ptc {
 // tq = 128 / G whole tokens; a query tile is two such halves.
 constexpr uint32_t kRows = 256, kKeys = 128;
 constexpr uint32_t kMaxGroup = PTC_MAX_GROUP;
-constexpr uint32_t kMaxCtas = 512;
+constexpr uint32_t kMaxCtas = 256;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Where a CTA starts: its first unit, and what that is: for the tile kernel
 // the key tile `minor` of query tile `major`, for the weights the query tile
 // `minor` (after the first one that sees it) of key tile `major`.
 struct CtaStart {
-  uint64_t u;
-  uint32_t r, h, major, minor;
+  uint64_t u, tok0, page0;  // tok0, page0, m, n: of request r
+  uint32_t r, h, major, minor, m, n;
 };
 
 // What k_attn_plan leaves for the kernels after it.  Their work is a row of
@@ -28,10 +28,10 @@ struct CtaStart {
 // key tile for the weights) `extra` units for what a tile costs by itself, then
 // one for every pair with a second-level tile.  CTA c of C takes the units from
 // start[c].u to start[c + 1].u, about U / C of them: a cut that falls among the
-// extra units is moved to before the tile.
+// extra units or would leave a short part is moved to before or after the tile
+// (there, `minor` is past its last second-level tile).
 struct AttnPlan {
   uint32_t ok, pad;
-  uint64_t units;
   CtaStart start[kMaxCtas + 1];
   uint32_t arrived[kMaxCtas];  // parts of the split tile that begins in CTA c
 };
@@ -65,6 +65,9 @@ struct AttnArgs {
 // way out take about as long as three key tiles (measured on a step of mixed
 // chunks: TODO), a key tile's sum of weights about one query tile.
 constexpr uint32_t kTileExtra = 3, kMassExtra = 1;
+// Fewest key tiles of a part.  A part of up to 256 rows costs their sums' way
+// through memory (6 us for two parts of 256 rows); one of few rows hardly any.
+constexpr uint32_t kPartMin = 4;
 
 // The CTAs that share the units [from, to) of a split tile, c0 the first.
 struct Sharers {

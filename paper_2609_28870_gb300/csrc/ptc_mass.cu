@@ -133,7 +133,10 @@ struct MassWalk {
     r = s.r;
     h = s.h;
     kt = s.major;
-    request(a);
+    tok0 = s.tok0;
+    m = s.m;
+    n = s.n;
+    page0 = s.page0;
     part(a, s.minor);
     return true;
   }
