@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   AttnPlan* plan = a.plan + blockIdx.y;
   uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.y * (R + 1);
   // a request's first-level tiles, and the units of one of them
-  auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kKeys) : 0u) : query_tiles(m, tq); };
+  auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kMassKeys) : 0u) : query_tiles(m, tq); };
   auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
     return extra + (weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i));
   };
@@ -302,8 +302,8 @@ constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
 // 4 KB a softmax warp: rows on their way out; the sums of 8 warps, 32 rows and 32 columns.
 constexpr int kStage = 8 * 4096;
-// Registers a thread: 2 * 128 * 216 + 128 * 72 = 384 * 168, what the block has at launch.
-constexpr int kSoftmaxRegs = 216, kOtherRegs = 72;
+// Registers a thread: 2 * 128 * 200 + 128 * 104 = 384 * 168, what the block has at launch.
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 104;
 
 struct TileShared {
   uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2][2], drain;
@@ -370,15 +370,15 @@ struct RowState {
 // Moves the maximum of a row up to mx; O, once the product before is done,
 // and what was summed so far shrink with it.
 template <int NSLAB>
-__device__ __forceinline__ bool raise_top(RowState& st, float mx, float sl2, uint32_t o_at, bool first,
-                                          uint32_t bar_o, uint32_t parity) {
-  if (!__any_sync(kFull, mx > st.top)) return true;
+__device__ __forceinline__ void raise_top(RowState& st, float mx, float sl2, uint32_t o_at, bool first,
+                                          uint32_t bar_o, uint32_t parity, bool& alive) {
+  if (!__any_sync(kFull, mx > st.top)) return;
   const float nt = fmaxf(st.top, mx);
   const float f = st.top == -INFINITY ? 0.f : exp2_approx((st.top - nt) * sl2);
   st.l *= f;
   st.top = nt;
-  if (first) return true;
-  if (!mbar_wait(bar_o, parity)) return false;
+  if (first) return;
+  if (alive) alive = mbar_wait(bar_o, parity);
   tc_fence_after();
 #pragma unroll 1
   for (int c = 0; c < NSLAB * 2; ++c) {
@@ -389,7 +389,6 @@ __device__ __forceinline__ bool raise_top(RowState& st, float mx, float sl2, uin
     for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
     tmem_st32(o_at + 32 * c, x);
   }
-  return true;
 }
 
 __device__ __forceinline__ float max32(const uint32_t (&x)[32]) {
@@ -423,10 +422,9 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
 constexpr float kMove = 256.f;
 
 // Who has a part of the tile, and where; by one warp.
-__device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, const Walk& w) {
+__device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, uint64_t from, uint64_t to) {
   const uint32_t lane = threadIdx.x & 31;
-  const uint64_t from = w.from();
-  const Sharers s = sharers(a.plan, a.ctas, from, w.to());
+  const Sharers s = sharers(a.plan, a.ctas, from, to);
   uint32_t n = 0;
   for (uint32_t x0 = s.c0; x0 <= s.c1; x0 += 32) {
     const uint32_t x = x0 + lane;
@@ -448,9 +446,9 @@ __device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, con
 // the lanes have 4 columns each, and the parts are added up in the order of the
 // keys.
 template <typename T, int ROWS>
-__device__ __noinline__ void join_parts(const AttnArgs& a, const TileShared& sh, const Walk& w) {
+__device__ __noinline__ void join_parts(const AttnArgs& a, const TileShared& sh, uint64_t tok0, uint32_t m, uint32_t t0,
+                                        uint32_t h) {
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = a.kv.D, count = sh.count;
-  const uint32_t t0 = w.token0(a);
   const bool in = 4 * lane < D;
   for (uint32_t i0 = warp * ROWS; i0 < (ROWS == 1 ? 32 : kRows); i0 += 8 * ROWS) {
     bool ok[ROWS];
@@ -462,8 +460,8 @@ __device__ __noinline__ void join_parts(const AttnArgs& a, const TileShared& sh,
     for (int k = 0; k < ROWS; ++k) {
       // row i of the tile: its half, token and head
       const uint32_t i = (i0 + k) & 127, t = t0 + ((i0 + k) >> 7) * a.tq + i / a.G;
-      ok[k] = i < a.tq * a.G && t < w.m;
-      at[k] = (w.tok0 + t) * a.n_q_heads + w.h * a.G + i % a.G;
+      ok[k] = i < a.tq * a.G && t < m;
+      at[k] = (tok0 + t) * a.n_q_heads + h * a.G + i % a.G;
       top[k] = -INFINITY;
       l[k] = 0.f;
       o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -535,6 +533,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
   const float sl2 = a.scale * kLog2e;
   const uint32_t D = a.kv.D, G = a.G;
   char* stage = stages + (half * 4 + warp) * 4096;
+  bool alive = true;  // a warp that has given up waiting runs on without, for the others at the barriers
   uint32_t done = 0, parted = 0;  // key tiles of this half so far, and those in two parts
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
@@ -551,55 +550,58 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     RowState st;
     st.clear();
     const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
-    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w);
+    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w.from(), w.to());
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
-        if (!mbar_wait(bar_s, done & 1)) return false;
+        if (alive) alive = mbar_wait(bar_s, done & 1);
         tc_fence_after();
         const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
         const bool masked = __any_sync(kFull, see < (int)kKeys);
+        uint32_t x[4][32];
+        if (rows) {
+          tmem_ld32(x[0], s_at);
+          tmem_ld32(x[1], s_at + 32);
+        }
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
           if (rows) {
             const uint32_t x_at = s_at + 64 * part;
-            uint32_t x[2][32], y[16];
+            uint32_t y[16];
             float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
             float sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
             const bool first = j == j0 && part == 0;
-            auto hide = [&](int c) {
-              if (masked) {
+            tmem_wait_ld(x[2 * part]);
+            tmem_wait_ld(x[2 * part + 1]);
+            if (part == 0) {  // the second part's scores come in behind the first's weights
+              tmem_ld32(x[2], s_at + 64);
+              tmem_ld32(x[3], s_at + 96);
+            }
+            if (masked) {
+#pragma unroll
+              for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
-                  if (64 * part + 32 * c + k >= see) x[c][k] = 0xFF800000u;
-              }
-            };
-            tmem_ld32(x[0], x_at);
-            tmem_wait_ld(x[0]);
-            tmem_ld32(x[1], x_at + 32);
-            hide(0);
+                  if (64 * part + 32 * c + k >= see) x[2 * part + c][k] = 0xFF800000u;
+            }
             bool move = first;
             if (!first) {
-              weigh<T>(x[0], sl2, sub, sum, y);
-              tmem_wait_ld(x[1]);
-              tmem_st16(x_at, y);
-              hide(1);
-              weigh<T>(x[1], sl2, sub, sum, y);
-              tmem_st16(x_at + 16, y);
+#pragma unroll
+              for (int c = 0; c < 2; ++c) {
+                weigh<T>(x[2 * part + c], sl2, sub, sum, y);
+                tmem_st16(x_at + 16 * c, y);
+              }
               const float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
               move = __any_sync(kFull, valid && !(total <= kMove * W::kScale));
               if (!move) st.l += total;
-            } else {
-              tmem_wait_ld(x[1]);
-              hide(1);
             }
             if (move) {
-              const float mx = valid ? fmaxf(max32(x[0]), max32(x[1])) : -INFINITY;
-              if (!raise_top<NSLAB>(st, mx, sl2, o_at, first, bar_o[1 - part], (part ? parted : done - 1) & 1)) return false;
+              const float mx = valid ? fmaxf(max32(x[2 * part]), max32(x[2 * part + 1])) : -INFINITY;
+              raise_top<NSLAB>(st, mx, sl2, o_at, first, bar_o[1 - part], (part ? parted : done - 1) & 1, alive);
               sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
               sum[0] = sum[1] = make_float2(0.f, 0.f);
 #pragma unroll
               for (int c = 0; c < 2; ++c) {
-                weigh<T>(x[c], sl2, sub, sum, y);
+                weigh<T>(x[2 * part + c], sl2, sub, sum, y);
                 tmem_st16(x_at + 16 * c, y);
               }
               st.l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
@@ -613,7 +615,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     } else {
       see_all -= 32 * warp;
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, see_all -= step * kKeys) {
-        if (!mbar_wait(bar_s, done & 1)) return false;
+        if (alive) alive = mbar_wait(bar_s, done & 1);
         tc_fence_after();
         uint32_t x[32], y[16], zero[16];
         tmem_ld32(x, s_at + 32 * warp);
@@ -642,7 +644,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         weigh<T>(x, sl2, sub, sum, y);
         float total = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         if (__any_sync(kFull, j == j0 || (valid && !(total <= kMove * W::kScale)))) {
-          if (!raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o[1], (done - 1) & 1)) return false;
+          raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o[1], (done - 1) & 1, alive);
           sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
           sum[0] = sum[1] = make_float2(0.f, 0.f);
           weigh<T>(x, sl2, sub, sum, y);
@@ -663,7 +665,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     }
     // the sums of the rows
     const bool some = j0 < w.kv1;  // this half had a key tile
-    if (some && !mbar_wait(bar_o[1], (done - 1) & 1)) return false;
+    if (some && alive) alive = mbar_wait(bar_o[1], (done - 1) & 1);
     tc_fence_after();
     const uint64_t prow0 = (uint64_t)(2 * blockIdx.x + (w.first ? 0 : 1)) * kRows;
     const uint64_t orow0 = w.tok0 * a.n_q_heads + w.h * G;  // row (t, g) is orow0 + t * n_q_heads + g
@@ -819,13 +821,13 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
       }
       softmax_sync();
       if (sh.last) {
-        if (mode == kColumnsApart) join_parts<T, 1>(a, sh, w);
-        else join_parts<T, 4>(a, sh, w);
+        if (mode == kColumnsApart) join_parts<T, 1>(a, sh, w.tok0, w.m, w.token0(a), w.h);
+        else join_parts<T, 4>(a, sh, w.tok0, w.m, w.token0(a), w.h);
       }
       softmax_sync();
     }
   }
-  return true;
+  return alive;
 }
 
 template <typename T, int NSLAB, bool FEW>
@@ -1223,7 +1225,7 @@ AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D, uint64_t scores) {
   w.ml = w.units + up(2 * (size_t)(n_req + 1) * 8);
   w.part = w.ml + up((size_t)2 * ctas * kRows * 8);
   w.mass = w.part + up((size_t)2 * ctas * kRows * D * 4);
-  w.scores = w.mass + up((size_t)2 * ctas * kKeys * 4);
+  w.scores = w.mass + up((size_t)2 * ctas * kMassKeys * 4);
   w.total = w.scores + up(scores * 4);
   return w;
 }

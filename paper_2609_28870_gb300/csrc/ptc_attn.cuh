@@ -11,6 +11,7 @@ namespace ptc {
 // token, so that a key tile is read once for all of them.  128 rows hold
 // tq = 128 / G whole tokens; a query tile is two such halves.
 constexpr uint32_t kRows = 256, kKeys = 128;
+constexpr uint32_t kMassKeys = 256;  // keys of a tile of the weights' kernel
 constexpr uint32_t kMaxGroup = PTC_MAX_GROUP;
 constexpr uint32_t kMaxCtas = 256;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -54,7 +55,7 @@ struct AttnArgs {
   uint64_t* unit_off;  // [0] and [1]: n_req + 1
   float* part;         // unnormalised rows of split tiles: [2 * ctas][kRows][D]
   float2* part_ml;     // their maxima (in powers of two) and sums
-  float* part_mass;    // weights of split key tiles: [2 * ctas][kKeys]
+  float* part_mass;    // weights of split key tiles: [2 * ctas][kMassKeys]
   float* scores;       // scores of few rows, [n_kv_heads][few][slots], or null
   uint32_t few;
   uint32_t ctas, box;  // box: rows of a tensor copy of keys or values
@@ -98,9 +99,9 @@ __device__ __forceinline__ uint32_t key_tiles(uint32_t m, uint32_t n, uint32_t t
   const int64_t sees = (int64_t)n - m + end;
   return sees <= (int64_t)kKeys ? 1u : (uint32_t)((sees + kKeys - 1) / kKeys);
 }
-// The first half tile of queries that sees anything of key tile kt.
+// The first half tile of queries that sees anything of the weights' key tile kt.
 __device__ __forceinline__ uint32_t first_seeing(uint32_t m, uint32_t n, uint32_t tq, uint32_t kt) {
-  const int64_t t = (int64_t)kt * kKeys - ((int64_t)n - m);
+  const int64_t t = (int64_t)kt * kMassKeys - ((int64_t)n - m);
   return t <= 0 ? 0u : (uint32_t)t / tq;
 }
 

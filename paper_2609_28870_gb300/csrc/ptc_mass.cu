@@ -9,6 +9,7 @@
 //               written and read.
 //   many rows   the scores are computed again, transposed: one thread a token
 //               adds up its column of rows without a word to its neighbours.
+#include <cstddef>
 #include <type_traits>
 
 #include "ptc_attn.cuh"
@@ -81,29 +82,35 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
 }
 
 // ------------------------------------------------------------------ many rows
-// One CTA an SM walks its units, (key tile, half a query tile) pairs.  Scores
-// transposed, S = K Q^T: 128 keys in the lanes of tensor memory, up to 128
-// query rows in its columns, four such products in turn.  Four groups of 4
-// warps take products in turn and add up exp2(s - lse) along a row of S, which
-// is a column of the scores (two groups, with half as many loads of scores in
-// flight, took 1,500 cycles a product of 512); warp 16 issues the products, warp
-// 17 loads key tiles (with warp 19 where there are no tensor copies), warp 18
-// queries.
-constexpr uint32_t kGroups = 4;
-constexpr int kMassThreads = kGroups * 128 + 128;
+// One CTA an SM walks its units, pairs of 256 keys and half a query tile.
+// Scores transposed, S = K Q^T: 128 keys in the lanes of tensor memory, up to
+// 128 query rows in its columns, for both halves of the keys and two units at a
+// time.  Four groups of 4 warps, one a half of the keys and every other unit,
+// add up exp2(s - lse) along a row of S, which is a column of the scores; warp
+// 16 issues the products, warp 17 loads keys (with warp 19 where there are no
+// tensor copies), warp 18 queries.
+// Queries stream past resident keys: 32 KB (at D = 128) a unit.  With 128 keys
+// a unit that stream, at 7.4 TB/s out of L2, was the bound; with 256 keys the
+// exponentials are, 512 cycles of a quarter of an SM for 128 by 128 scores.
+constexpr int kMassThreads = 640;
 constexpr int kSlab = 128 * 128;
+constexpr uint32_t kQueryRing = 3;
+
+struct MassShared {
+  uint64_t k_full[2], k_empty[2], q_full[kQueryRing], q_empty[kQueryRing], s_full[4], s_empty[4], drain;
+  alignas(16) float lse[2][128];  // negated, in powers of two: of even and odd units (read four at a time)
+  float sum[2][128];  // of odd units: both halves of the keys
+  uint32_t tmem;
+};
 
 template <int NSLAB>
 struct MassShape {
   static constexpr int kTile = NSLAB * kSlab;
-  static constexpr int kSmem = 6 * kTile + 1024;  // 2 key tiles, 4 query tiles
-};
-
-struct MassShared {
-  uint64_t k_full[2], k_empty[2], q_full[4], q_empty[4], s_full[4], s_empty[4], drain;
-  float lse[kGroups][2][128];  // negated, in powers of two: of a group, two units
-  float sum[2][kGroups][128];  // of a key tile, two key tiles
-  uint32_t tmem;
+  static constexpr int kQueries = 4 * kTile;  // behind two key tiles of two halves
+  static constexpr int kRest = kQueries + kQueryRing * kTile;
+  static constexpr int kSmem = kRest + sizeof(MassShared);
+  static_assert(kSmem <= 227 * 1024, "shared memory of a block");
+  static_assert(kRest % 16 == 0 && offsetof(MassShared, lse) % 16 == 0, "16-byte reads");
 };
 
 struct MassWalk {
@@ -143,7 +150,7 @@ struct MassWalk {
   __device__ __forceinline__ bool next(const AttnArgs& a) {
     left -= q1 - q0 + extra;
     if (left == 0) return false;
-    if ((uint64_t)++kt * kKeys >= n) {
+    if ((uint64_t)++kt * kMassKeys >= n) {
       kt = 0;
       if (++h == a.kv.H) {
         h = 0;
@@ -156,6 +163,8 @@ struct MassWalk {
     part(a, 0);
     return true;
   }
+  // Whether there are keys in the tile's second half.
+  __device__ __forceinline__ bool two() const { return n > kt * kMassKeys + kKeys; }
   __device__ __forceinline__ uint32_t rows(const AttnArgs& a, uint32_t q) const {
     const uint32_t t = m - q * a.tq;
     return (t < a.tq ? t : a.tq) * a.G;
@@ -163,109 +172,128 @@ struct MassWalk {
 };
 
 __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uint32_t group) {
-  const uint32_t tid = threadIdx.x & 127;
+  const uint32_t tid = threadIdx.x & 127, half = group & 1, odd = group >> 1, buf = group;
   const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
   const float sl2 = a.scale * kLog2e;
+  auto odd_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + odd) : "memory"); };
   uint32_t unit = 0, mine = 0, seg = 0;
+  bool alive = true;  // a warp that has given up waiting runs on without, for the others at the barriers
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
-    const uint64_t key = (uint64_t)w.kt * kKeys + tid;
+    const uint64_t key = (uint64_t)w.kt * kMassKeys + half * kKeys + tid;
     const int64_t t_first = (int64_t)key - ((int64_t)w.n - w.m);  // the first token that sees the key
+    const bool on = half == 0 || w.two();
     // lse of a query tile's row `tid`; rows that are none count nothing below
     auto lse_of = [&](uint32_t q) {
-      const uint32_t rows = w.rows(a, q);
-      if (tid >= rows) return 0.f;
+      if (tid >= w.rows(a, q)) return 0.f;
       const uint64_t t = w.tok0 + (uint64_t)q * a.tq + tid / a.G;
       return -kLog2e * a.lse[t * a.n_q_heads + w.h * a.G + tid % a.G];
     };
-    uint32_t q = w.q0 + ((group - unit) & (kGroups - 1));
-    float ahead = q < w.q1 ? lse_of(q) : 0.f, total = 0.f;
-    for (; q < w.q1; q += kGroups, ++mine) {
-      const uint32_t u = unit + (q - w.q0), buf = u & 3;
-      float* lse = sh.lse[group][mine & 1];
-      lse[tid] = ahead;
-      asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory");
-      if (q + kGroups < w.q1) ahead = lse_of(q + kGroups);
-      if (!mbar_wait(smem_u32(&sh.s_full[buf]), (u >> 2) & 1)) return false;
-      tc_fence_after();
-      const uint32_t rows = w.rows(a, q);
-      const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G;
-      const int lo = lo64 <= 0 ? 0 : lo64 >= 128 ? 128 : (int)lo64, hi = (int)rows;
-      const bool masked = __any_sync(kFull, lo > 0 || (hi & 31));
-      float2 sum = make_float2(0.f, 0.f);
-#pragma unroll 1
-      for (int c = 0; c < hi; c += 32) {
-        uint32_t x[32];
-        tmem_ld32(x, tmem + buf * 128 + c);
-        tmem_wait_ld(x);
-        const float2* off = reinterpret_cast<const float2*>(lse + c);
-        if (!masked) {
+    uint32_t q = w.q0 + ((odd ^ unit) & 1);
+    float ahead = half == 0 && q < w.q1 ? lse_of(q) : 0.f, total = 0.f;
+    for (; q < w.q1; q += 2) {
+      if (half == 0) sh.lse[odd][tid] = ahead;
+      odd_sync();
+      if (half == 0 && q + 2 < w.q1) ahead = lse_of(q + 2);
+      if (on) {
+        if (alive) alive = mbar_wait(smem_u32(&sh.s_full[buf]), mine++ & 1);
+        tc_fence_after();
+        const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G;
+        const int lo = lo64 <= 0 ? 0 : lo64 >= 128 ? 128 : (int)lo64, hi = (int)w.rows(a, q);
+        const bool masked = __any_sync(kFull, lo > 0 || (hi & 31));
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        uint32_t x[2][32];
+        tmem_ld32(x[0], tmem + buf * 128);
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float2 e = fma2(make_float2(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])),
-                                  make_float2(sl2, sl2), off[k]);
-            sum = add2(sum, make_float2(exp2_approx(e.x), exp2_approx(e.y)));
-          }
-        } else {
+        for (int c = 0; c < 4; ++c) {
+          if (32 * c < hi) {
+            tmem_wait_ld(x[c & 1]);
+            if (32 * (c + 1) < hi) tmem_ld32(x[(c + 1) & 1], tmem + buf * 128 + 32 * (c + 1));
+            const float4* off = reinterpret_cast<const float4*>(sh.lse[odd] + 32 * c);
 #pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            const float e = exp2_approx(fmaf(__uint_as_float(x[k]), sl2, lse[c + k]));
-            if (c + k >= lo && c + k < hi) sum.x += e;
+            for (int k = 0; k < 8; ++k) {
+              const float4 o = off[k];
+              const float2 e0 = fma2(make_float2(__uint_as_float(x[c & 1][4 * k]), __uint_as_float(x[c & 1][4 * k + 1])),
+                                     make_float2(sl2, sl2), make_float2(o.x, o.y));
+              const float2 e1 = fma2(make_float2(__uint_as_float(x[c & 1][4 * k + 2]), __uint_as_float(x[c & 1][4 * k + 3])),
+                                     make_float2(sl2, sl2), make_float2(o.z, o.w));
+              float2 p0 = make_float2(exp2_approx(e0.x), exp2_approx(e0.y)), p1 = make_float2(exp2_approx(e1.x), exp2_approx(e1.y));
+              if (masked) {
+                const int at = 32 * c + 4 * k;
+                p0.x = at >= lo && at < hi ? p0.x : 0.f;
+                p0.y = at + 1 >= lo && at + 1 < hi ? p0.y : 0.f;
+                p1.x = at + 2 >= lo && at + 2 < hi ? p1.x : 0.f;
+                p1.y = at + 3 >= lo && at + 3 < hi ? p1.y : 0.f;
+              }
+              sum[0] = add2(sum[0], p0);
+              sum[1] = add2(sum[1], p1);
+            }
           }
         }
+        tc_fence_before();
+        mbar_arrive_warp(smem_u32(&sh.s_empty[buf]));
+        total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
-      tc_fence_before();
-      mbar_arrive_warp(smem_u32(&sh.s_empty[buf]));
-      total += sum.x + sum.y;
+      odd_sync();  // the lse have been read
     }
     unit += w.q1 - w.q0;
-    if (group) sh.sum[seg & 1][group][tid] = total;
+    if (odd) sh.sum[half][tid] = total;
     asm volatile("bar.sync 1, 512;" ::: "memory");
-    if (group == 0) {
-#pragma unroll
-      for (uint32_t k = 1; k < kGroups; ++k) total += sh.sum[seg & 1][k][tid];
+    if (!odd) {
+      total += sh.sum[half][tid];
       if (w.q0 == w.first && w.q1 == w.first + w.count) {
         if (key < w.n) {
           const uint64_t at = w.h * a.mass_stride + w.page0 * a.kv.B + key;
           a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + total;
         }
       } else {
-        a.part_mass[(2 * (uint64_t)blockIdx.x + (seg == 0 ? 0 : 1)) * kKeys + tid] = total;
+        a.part_mass[(2 * (uint64_t)blockIdx.x + (seg == 0 ? 0 : 1)) * kMassKeys + half * kKeys + tid] = total;
       }
     }
+    asm volatile("bar.sync 1, 512;" ::: "memory");
   }
-  return true;
+  return alive;
 }
 
 template <typename T, int NSLAB>
 __device__ __forceinline__ bool mass_products(const AttnArgs& a, MassShared& sh, uint32_t smem) {
   using Sh = MassShape<NSLAB>;
-  constexpr bool bf16 = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+  constexpr bool bf16 = !std::is_same<T, __half>::value;
   const uint32_t tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
-  uint32_t unit = 0, seg = 0;
+  uint32_t unit = 0, seg = 0, used[4] = {0, 0, 0, 0};
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
-    const uint32_t k_at = smem + (seg & 1) * Sh::kTile;
+    const uint32_t k_at = smem + (seg & 1) * 2 * Sh::kTile, halves = w.two() ? 2 : 1;
     if (!mbar_wait(smem_u32(&sh.k_full[seg & 1]), (seg >> 1) & 1)) return false;
     for (uint32_t q = w.q0; q < w.q1; ++q, ++unit) {
-      const uint32_t buf = unit & 3, q_at = smem + (2 + buf) * Sh::kTile;
-      if (!mbar_wait(smem_u32(&sh.q_full[buf]), (unit >> 2) & 1)) return false;
-      if (unit >= 4 && !mbar_wait(smem_u32(&sh.s_empty[buf]), ((unit >> 2) - 1) & 1)) return false;
-      tc_fence_after();
+      const uint32_t ring = unit % kQueryRing, q_at = smem + Sh::kQueries + ring * Sh::kTile;
+      if (!mbar_wait(smem_u32(&sh.q_full[ring]), (unit / kQueryRing) & 1)) return false;
       const uint32_t desc = mma_desc(bf16, 128, (w.rows(a, q) + 15) & ~15u, false);
-      const uint64_t da = tile_desc(k_at, 16), db = tile_desc(q_at, 16);
-      if (elect_lane()) {
-        mma_ss<false>(tmem + buf * 128, da, db, desc);
+      const uint64_t db = tile_desc(q_at, 16);
 #pragma unroll
-        for (uint32_t k = 1; k < NSLAB * 4; ++k) {
-          const uint32_t off = (k / 4) * kSlab + (k % 4) * 32;
-          if (k < steps) mma_ss<true>(tmem + buf * 128, desc_at(da, off), desc_at(db, off), desc);
+      for (uint32_t half = 0; half < 2; ++half) {
+        if (half >= halves) break;
+        const uint32_t buf = (unit & 1) * 2 + half;
+        uint32_t& n = (unit & 1) ? used[2 + half] : used[half];
+        if (n && !mbar_wait(smem_u32(&sh.s_empty[buf]), (n - 1) & 1)) return false;
+        ++n;
+        tc_fence_after();
+        const uint64_t da = tile_desc(k_at + half * Sh::kTile, 16);
+        if (elect_lane()) {
+          mma_ss<false>(tmem + buf * 128, da, db, desc);
+#pragma unroll
+          for (uint32_t k = 1; k < NSLAB * 4; ++k) {
+            const uint32_t off = (k / 4) * kSlab + (k % 4) * 32;
+            if (k < steps) mma_ss<true>(tmem + buf * 128, desc_at(da, off), desc_at(db, off), desc);
+          }
+          mma_commit(smem_u32(&sh.s_full[buf]));
+          if (half + 1 == halves) {
+            mma_commit(smem_u32(&sh.q_empty[ring]));
+            if (q + 1 == w.q1) mma_commit(smem_u32(&sh.k_empty[seg & 1]));
+          }
         }
-        mma_commit(smem_u32(&sh.s_full[buf]));
-        mma_commit(smem_u32(&sh.q_empty[buf]));
-        if (q + 1 == w.q1) mma_commit(smem_u32(&sh.k_empty[seg & 1]));
+        __syncwarp();
       }
-      __syncwarp();
     }
   }
   return true;
@@ -279,8 +307,8 @@ __device__ __forceinline__ bool mass_queries(const AttnArgs& a, MassShared& sh, 
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a))
     for (uint32_t q = w.q0; q < w.q1; ++q, ++unit) {
-      const uint32_t buf = unit & 3, bar = smem_u32(&sh.q_full[buf]), dst = smem + (2 + buf) * Sh::kTile;
-      if (unit >= 4 && !mbar_wait(smem_u32(&sh.q_empty[buf]), ((unit >> 2) - 1) & 1)) return false;
+      const uint32_t at = unit % kQueryRing, bar = smem_u32(&sh.q_full[at]), dst = smem + Sh::kQueries + at * Sh::kTile;
+      if (unit >= kQueryRing && !mbar_wait(smem_u32(&sh.q_empty[at]), (unit / kQueryRing - 1) & 1)) return false;
       if (lane == 0) {
         mbar_expect(bar, NSLAB * a.tq * a.G * 128);
 #pragma unroll
@@ -302,27 +330,31 @@ __device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, con
   const uint32_t tid = lane + (threadIdx.x >= 608 ? 32 : 0);
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
-    const uint32_t at = seg & 1, bar = smem_u32(&sh.k_full[at]), dst = smem + at * Sh::kTile;
+    const uint32_t at = seg & 1, bar = smem_u32(&sh.k_full[at]), halves = w.two() ? 2 : 1;
     const uint32_t* ids = a.kv.page_ids + w.page0;
     if (seg >= 2 && !mbar_wait(smem_u32(&sh.k_empty[at]), ((seg >> 1) - 1) & 1)) return false;
     if constexpr (TMA) {
       const uint32_t boxes = kKeys / a.box;
-      const uint64_t key = (uint64_t)w.kt * kKeys + lane * a.box;
-      int page = (int)a.kv.n_pages, slot = 0;
-      if (lane < boxes && key < w.n) {
-        const uint32_t id = __ldg(ids + key / a.kv.B);
-        if (id < a.kv.n_pages) page = (int)id;
-        slot = (int)(key % a.kv.B);
-      }
-      if (lane == 0) mbar_expect(bar, Sh::kTile);
+      if (lane == 0) mbar_expect(bar, halves * Sh::kTile);
       __syncwarp();
-      if (lane < boxes)
+      for (uint32_t half = 0; half < halves; ++half) {
+        const uint32_t dst = smem + (at * 2 + half) * Sh::kTile;
+        const uint32_t key = w.kt * kMassKeys + half * kKeys + lane * a.box;
+        int page = (int)a.kv.n_pages, slot = 0;
+        if (lane < boxes && key < w.n) {
+          const uint32_t id = __ldg(ids + key / a.kv.B);
+          if (id < a.kv.n_pages) page = (int)id;
+          slot = (int)(key % a.kv.B);
+        }
+        if (lane < boxes)
 #pragma unroll
-        for (int s = 0; s < NSLAB; ++s) tma_load_4d(dst + s * kSlab + lane * a.box * 128, mk, bar, 64 * s, slot, (int)w.h, page);
+          for (int s = 0; s < NSLAB; ++s)
+            tma_load_4d(dst + s * kSlab + lane * a.box * 128, mk, bar, 64 * s, slot, (int)w.h, page);
+      }
     } else {
-      for (uint32_t i = tid; i < kKeys * NSLAB * 8; i += 64) {
-        const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8);
-        const uint64_t key = (uint64_t)w.kt * kKeys + row;
+      for (uint32_t i = tid; i < halves * kKeys * NSLAB * 8; i += 64) {
+        const uint32_t row = i / (NSLAB * 8), c = i % (NSLAB * 8), half = row / kKeys, in_half = row % kKeys;
+        const uint32_t key = w.kt * kMassKeys + row;
         bool in = key < w.n && c * 8 < a.kv.D;
         const char* p = a.kv.k;
         if (in) {
@@ -331,7 +363,7 @@ __device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, con
           if (in)
             p += 2 * (id * a.kv.ks_page + w.h * a.kv.ks_head + (int64_t)(key % a.kv.B) * a.kv.ks_slot + c * 8);
         }
-        cp_async16(dst + (c / 8) * kSlab + row * 128 + (((c % 8) ^ (row & 7)) * 16), p, in);
+        cp_async16(smem + (at * 2 + half) * Sh::kTile + (c / 8) * kSlab + in_half * 128 + (((c % 8) ^ (in_half & 7)) * 16), p, in);
       }
       cp_async_commit();
       cp_async_wait<0>();
@@ -345,18 +377,25 @@ __device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, con
 template <typename T, int NSLAB, bool TMA>
 __global__ void __launch_bounds__(kMassThreads, 1)
     k_mass_tiles(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mq, const AttnArgs a) {
-  extern __shared__ char smem_raw[];
-  __shared__ MassShared sh;
-  const uint32_t smem = (smem_u32(smem_raw) + 1023) & ~1023u;
+  using Sh = MassShape<NSLAB>;
+  extern __shared__ __align__(1024) char smem_raw[];
+  MassShared& sh = *reinterpret_cast<MassShared*>(smem_raw + Sh::kRest);
+  const uint32_t smem = smem_u32(smem_raw);
   const uint32_t warp = threadIdx.x >> 5;
+  if (smem & 1023) {  // swizzled tiles start at whole groups of 8 rows
+    if (threadIdx.x == 0) report(a.status, PTC_ERR_CUDA);
+    return;
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sh.k_full[i]), TMA ? 1 : 64);
       mbar_init(smem_u32(&sh.k_empty[i]), 1);
     }
-    for (int i = 0; i < 4; ++i) {
+    for (uint32_t i = 0; i < kQueryRing; ++i) {
       mbar_init(smem_u32(&sh.q_full[i]), 1);
       mbar_init(smem_u32(&sh.q_empty[i]), 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(smem_u32(&sh.s_full[i]), 1);
       mbar_init(smem_u32(&sh.s_empty[i]), 4);
     }
@@ -382,8 +421,8 @@ __global__ void __launch_bounds__(kMassThreads, 1)
     } else if (warp == 18) {
       fine = mass_queries<NSLAB>(a, sh, &mq, smem, units);
       if (!fine)  // given up: let the copies in flight land
-        for (uint32_t u = units > 4 ? units - 4 : 0; u < units; ++u)
-          (void)mbar_wait(smem_u32(&sh.q_full[u & 3]), (u >> 2) & 1);
+        for (uint32_t u = units > kQueryRing ? units - kQueryRing : 0; u < units; ++u)
+          (void)mbar_wait(smem_u32(&sh.q_full[u % kQueryRing]), (u / kQueryRing) & 1);
     } else if (warp == 17 || !TMA) {
       fine = mass_keys<NSLAB, TMA>(a, sh, &mk, smem, segs);
       if (!fine && TMA)
@@ -401,7 +440,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
 // blockIdx.y = 0: the key tiles that CTAs of the kernel above share, as
 // the tile kernel does it for query tiles.  1: what no unit covers, the slots
 // past every request's tokens and the requests without queries.
-__global__ void __launch_bounds__(128) k_mass_join(const AttnArgs a) {
+__global__ void __launch_bounds__(kMassKeys) k_mass_join(const AttnArgs a) {
   grid_dep_sync();
   const AttnPlan* plan = a.plan + 1;
   if (!plan->ok) return;
@@ -411,7 +450,7 @@ __global__ void __launch_bounds__(128) k_mass_join(const AttnArgs a) {
       const uint32_t r = (uint32_t)(p / a.kv.H), h = (uint32_t)(p % a.kv.H);
       const uint64_t at = h * a.mass_stride + a.kv.page_off[r] * a.kv.B, n = a.kv.kv_len[r];
       const uint64_t room = (a.kv.page_off[r + 1] - a.kv.page_off[r]) * a.kv.B;
-      for (uint64_t j = (a.tok_off[r] == a.tok_off[r + 1] ? 0 : n) + tid; j < room; j += 128)
+      for (uint64_t j = (a.tok_off[r] == a.tok_off[r + 1] ? 0 : n) + tid; j < room; j += kMassKeys)
         a.mass_out[at + j] = j < n && a.mass_in ? a.mass_in[at + j] : 0.f;
     }
     return;
@@ -423,12 +462,12 @@ __global__ void __launch_bounds__(128) k_mass_join(const AttnArgs a) {
   const Sharers sh = sharers(plan, a.ctas, first, first + kMassExtra + div_up(m, a.tq) - first_seeing(m, n, a.tq, s.major));
   for (uint32_t x = sh.c0 + 1; x < c; ++x)
     if (plan->start[x].u < plan->start[x + 1].u) return;  // not the first cut
-  const uint64_t key = (uint64_t)s.major * kKeys + tid;
+  const uint64_t key = (uint64_t)s.major * kMassKeys + tid;
   if (key >= n) return;
   float sum = 0.f;
   for (uint32_t x = sh.c0; x <= sh.c1; ++x) {
     if (x != sh.c0 && plan->start[x].u == plan->start[x + 1].u) continue;
-    sum += a.part_mass[(2 * (uint64_t)x + (x == sh.c0 && plan->start[x].u != first ? 1 : 0)) * kKeys + tid];
+    sum += a.part_mass[(2 * (uint64_t)x + (x == sh.c0 && plan->start[x].u != first ? 1 : 0)) * kMassKeys + tid];
   }
   const uint64_t at = s.h * a.mass_stride + a.kv.page_off[s.r] * a.kv.B + key;
   a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + sum;
@@ -460,7 +499,7 @@ ptc_status launch_mass(const AttnArgs& a, bool bf16, const CUtensorMap& mk, cons
   }
   const ptc_status st = bf16 ? launch_by_tiles<__nv_bfloat16>(a, mk, mq, tma, s) : launch_by_tiles<__half>(a, mk, mq, tma, s);
   if (st != PTC_OK) return st;
-  PTC_KERNEL("k_mass_join", s, k_mass_join, dim3(a.ctas, 2), 128, 0, a);
+  PTC_KERNEL("k_mass_join", s, k_mass_join, dim3(a.ctas, 2), kMassKeys, 0, a);
   return PTC_OK;
 }
 

@@ -115,7 +115,7 @@ def _status(status, dev: int):
 def _room(k, need: int, dev: int, ws):
     if ws is not None and ws.numel() >= need and ws.get_device() == dev:
         return ws
-    return k.new_empty(max(need, 256), dtype=torch.uint8)
+    return torch.empty(max(need, 256), dtype=torch.uint8, device=k.device)
 
 
 def _stream(dev: int) -> int:
@@ -164,13 +164,13 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
     qs = _tokens(q, "q", k, dev, D)
     T, Hq, _ = q.shape
     if out is None:
-        out = q.new_empty((T, Hq, D))
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
     elif out.shape != q.shape:
         raise ValueError("out: expected q's shape")
     else:
         _want(out, q.dtype, "out", dev, 3)
     if lse is None:
-        lse = q.new_empty((T, Hq), dtype=torch.float32)
+        lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device)
     elif lse.shape != q.shape[:2]:
         raise ValueError("lse: expected q's first two dimensions")
     else:
@@ -215,10 +215,10 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
         raise ValueError("mass: expected one row a key head")
     if min(n_keep, n_sink, n_recent, max_kv_len) < 0:
         raise ValueError("n_keep, n_sink, n_recent and max_kv_len: expected no negative numbers")
-    keep = kv_len.new_empty((n_req, heads, n_keep))
-    new_len = kv_len.new_empty(n_req)
+    keep = torch.empty((n_req, heads, n_keep), dtype=torch.int32, device=k.device)
+    new_len = torch.empty(n_req, dtype=torch.int32, device=k.device)
     slots = dst_page_ids.shape[0] * shape[2]
-    new_mass = mass.new_empty((heads, slots))
+    new_mass = torch.empty((heads, slots), dtype=torch.float32, device=k.device)
     L = p.lib()
     w = _room(k, L.ptc_kv_evict_workspace_bytes(n_req, heads, max_kv_len), dev, ws)
     rc = L.ptc_kv_evict(kv, mass.data_ptr(), mass.shape[1], n_keep, n_sink, n_recent, max_kv_len,
