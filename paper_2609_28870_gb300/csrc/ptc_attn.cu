@@ -881,6 +881,47 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
     }
     return true;
   };
+  // Key tiles [0, plain) of L of a kRowsApart tile, by one lane.  before[s][part]:
+  // uses of the weights' barriers so far, by their parity.
+  auto steady = [&](uint32_t L, uint32_t plain, uint32_t item0, const uint32_t (&before)[2][2]) {
+    const uint64_t k_base = tile_desc(ring, 16), v_base = tile_desc(ring, kSlabBytes);
+    const uint64_t q_desc[2] = {tile_desc(q_smem, 16), tile_desc(q_smem + Sh::kTile, 16)};
+#pragma unroll 1
+    for (uint32_t j = 0; j < plain; ++j) {
+      const uint32_t v_item = item0 + 2 * j + 1, k_next = v_item + 1;
+      const uint32_t v_at = v_item % Sh::kRing, k_at = k_next % Sh::kRing;
+      const uint64_t v_desc = desc_at(v_base, v_at * Sh::kTile), k_desc = desc_at(k_base, k_at * Sh::kTile);
+      const bool more = j + 1 < L;
+      if (!mbar_wait_lane(smem_u32(&sh.full[v_at]), (v_item / Sh::kRing) & 1)) return false;
+#pragma unroll
+      for (uint32_t s = 0; s < 2; ++s) {
+#pragma unroll
+        for (uint32_t part = 0; part < 2; ++part) {
+          if (!mbar_wait_lane(smem_u32(&sh.p_full[s][part]), (before[s][part] + j) & 1)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (uint32_t k = 4 * part; k < 4 * part + 4; ++k)
+            mma_ts(tmem + o_col(s), tmem + p_col(s, 16 * k), desc_at(v_desc, k * 2048), kPv, j > 0 || k > 0);
+          mma_commit(smem_u32(&sh.pv_done[s][part]));
+        }
+        if (s == 1) mma_commit(smem_u32(&sh.empty[v_at]));
+        if (more) {
+          if (s == 0 && !mbar_wait_lane(smem_u32(&sh.full[k_at]), (k_next / Sh::kRing) & 1)) return false;
+          // in order after the product above, which reads the weights that these scores overwrite
+          mma_ss<false>(tmem + s_col(s), q_desc[s], k_desc, kQk);
+#pragma unroll
+          for (uint32_t k = 1; k < NSLAB * 4; ++k) {
+            const uint32_t off = (k / 4) * kSlabBytes + (k % 4) * 32;
+            if (k < steps) mma_ss<true>(tmem + s_col(s), desc_at(q_desc[s], off), desc_at(k_desc, off), kQk);
+          }
+          mma_commit(smem_u32(&sh.s_full[s]));
+          if (j + 2 == L) mma_commit(smem_u32(&sh.q_empty[s]));
+        }
+      }
+      if (more) mma_commit(smem_u32(&sh.empty[k_at]));
+    }
+    return true;
+  };
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const int mode = FEW ? kColumnsApart : w.mode(a);
@@ -910,7 +951,17 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
         commit(sh.q_empty[0]);
         commit(sh.q_empty[1]);
       }
-      for (uint32_t j = 0; j < L; ++j) {
+      // All tiles but one that has slots to clear: one lane by itself, as the
+      // tensor cores wait whenever their queue runs dry between two products
+      // (with the warp's votes in between, a unit took 3,030 cycles for 2,048 of
+      // products).
+      const uint32_t plain = (uint64_t)w.kv1 * kKeys > w.n ? L - 1 : L;
+      bool ok = true;
+      if (elect_lane()) ok = steady(L, plain, item, weights);
+      if (!__all_sync(kFull, ok)) return false;
+      for (uint32_t s = 0; s < 2; ++s)
+        for (uint32_t part = 0; part < 2; ++part) weights[s][part] += plain;
+      for (uint32_t j = plain; j < L; ++j) {
         const uint32_t v_item = item + 2 * j + 1, k_next = v_item + 1;
         if (!full(v_item)) return false;
         clear_tail(j, v_item);

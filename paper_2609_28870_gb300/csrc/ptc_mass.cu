@@ -171,6 +171,21 @@ struct MassWalk {
   }
 };
 
+// The weights of 32 rows added to a key's sum.
+__device__ __forceinline__ void add_weights(const uint32_t (&x)[32], const float* lse, float sl2, float2 (&sum)[2]) {
+  const float4* off = reinterpret_cast<const float4*>(lse);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float4 o = off[k];
+    const float2 e0 = fma2(make_float2(__uint_as_float(x[4 * k]), __uint_as_float(x[4 * k + 1])), make_float2(sl2, sl2),
+                           make_float2(o.x, o.y));
+    const float2 e1 = fma2(make_float2(__uint_as_float(x[4 * k + 2]), __uint_as_float(x[4 * k + 3])), make_float2(sl2, sl2),
+                           make_float2(o.z, o.w));
+    sum[0] = add2(sum[0], make_float2(exp2_approx(e0.x), exp2_approx(e0.y)));
+    sum[1] = add2(sum[1], make_float2(exp2_approx(e1.x), exp2_approx(e1.y)));
+  }
+}
+
 __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uint32_t group) {
   const uint32_t tid = threadIdx.x & 127, half = group & 1, odd = group >> 1, buf = group;
   const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
@@ -201,38 +216,41 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
         const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G;
         const int lo = lo64 <= 0 ? 0 : lo64 >= 128 ? 128 : (int)lo64, hi = (int)w.rows(a, q);
         const bool masked = __any_sync(kFull, lo > 0 || (hi & 31));
-        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        uint32_t x[2][32];
-        tmem_ld32(x[0], tmem + buf * 128);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          if (32 * c < hi) {
-            tmem_wait_ld(x[c & 1]);
-            if (32 * (c + 1) < hi) tmem_ld32(x[(c + 1) & 1], tmem + buf * 128 + 32 * (c + 1));
-            const float4* off = reinterpret_cast<const float4*>(sh.lse[odd] + 32 * c);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float4 o = off[k];
-              const float2 e0 = fma2(make_float2(__uint_as_float(x[c & 1][4 * k]), __uint_as_float(x[c & 1][4 * k + 1])),
-                                     make_float2(sl2, sl2), make_float2(o.x, o.y));
-              const float2 e1 = fma2(make_float2(__uint_as_float(x[c & 1][4 * k + 2]), __uint_as_float(x[c & 1][4 * k + 3])),
-                                     make_float2(sl2, sl2), make_float2(o.z, o.w));
-              float2 p0 = make_float2(exp2_approx(e0.x), exp2_approx(e0.y)), p1 = make_float2(exp2_approx(e1.x), exp2_approx(e1.y));
-              if (masked) {
-                const int at = 32 * c + 4 * k;
-                p0.x = at >= lo && at < hi ? p0.x : 0.f;
-                p0.y = at + 1 >= lo && at + 1 < hi ? p0.y : 0.f;
-                p1.x = at + 2 >= lo && at + 2 < hi ? p1.x : 0.f;
-                p1.y = at + 3 >= lo && at + 3 < hi ? p1.y : 0.f;
-              }
-              sum[0] = add2(sum[0], p0);
-              sum[1] = add2(sum[1], p1);
+        const uint32_t s_at = tmem + buf * 128;
+        if (!masked) {
+          // a multiple of 32 rows that all see the keys; the next 32 scores come in behind
+          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+          uint32_t x[2][32];
+          tmem_ld32(x[0], s_at);
+#pragma unroll 1
+          for (int c = 0; c < hi; c += 64) {
+            tmem_wait_ld(x[0]);
+            if (c + 32 < hi) tmem_ld32(x[1], s_at + c + 32);
+            add_weights(x[0], sh.lse[odd] + c, sl2, sum);
+            if (c + 32 < hi) {
+              tmem_wait_ld(x[1]);
+              if (c + 64 < hi) tmem_ld32(x[0], s_at + c + 64);
+              add_weights(x[1], sh.lse[odd] + c + 32, sl2, sum);
             }
           }
+          total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        } else {
+          float sum = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < hi; c += 32) {
+            uint32_t x[32];
+            tmem_ld32(x, s_at + c);
+            tmem_wait_ld(x);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float p = exp2_approx(fmaf(__uint_as_float(x[k]), sl2, sh.lse[odd][c + k]));
+              if (c + k >= lo && c + k < hi) sum += p;
+            }
+          }
+          total += sum;
         }
         tc_fence_before();
         mbar_arrive_warp(smem_u32(&sh.s_empty[buf]));
-        total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
       }
       odd_sync();  // the lse have been read
     }

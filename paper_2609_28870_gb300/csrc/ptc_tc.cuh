@@ -55,6 +55,17 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
   return __all_sync(0xFFFFFFFFu, ok);
 }
 
+// The same by one lane.
+__device__ __forceinline__ bool mbar_wait_lane(uint32_t bar, uint32_t parity) {
+  if (mbar_try(bar, parity)) return true;
+  const long long began = clock64();
+#pragma unroll 1
+  do {
+    if (mbar_try(bar, parity)) return true;
+  } while (clock64() - began < kMbarCycles);
+  return false;
+}
+
 // Generic-proxy writes to shared memory become visible to copies and matrix operands.
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_mbar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
