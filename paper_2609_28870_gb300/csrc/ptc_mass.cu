@@ -85,13 +85,15 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
 // One CTA an SM walks its units, pairs of 256 keys and half a query tile.
 // Scores transposed, S = K Q^T: 128 keys in the lanes of tensor memory, up to
 // 128 query rows in its columns, for both halves of the keys and two units at a
-// time.  Four groups of 4 warps, one a half of the keys and every other unit,
-// add up exp2(s - lse) along a row of S, which is a column of the scores; warp
-// 16 issues the products, warp 17 loads keys (with warp 19 where there are no
+// time.  Four groups of 4 warps, one a half of the rows and every other unit,
+// add up exp2(s - lse) along rows of S, which are columns of the scores; a thread
+// has a key of either half, so that an lse is read once for two scores.  Warp 16
+// issues the products, warp 17 loads keys (with warp 19 where there are no
 // tensor copies), warp 18 queries.
-// Queries stream past resident keys: 32 KB (at D = 128) a unit.  With 128 keys
-// a unit that stream, at 7.4 TB/s out of L2, was the bound; with 256 keys the
-// exponentials are, 512 cycles of a quarter of an SM for 128 by 128 scores.
+// What bounds it is shared memory, 128 bytes a cycle: a unit's products read 128
+// KB, its queries are 32 KB, the lse 32 KB (at D = 128), 1,540 cycles for 1,024
+// of products and as many of exponentials.  (With 128 keys a unit the queries'
+// stream out of L2, 7.4 TB/s, was the bound.)
 constexpr int kMassThreads = 640;
 constexpr int kSlab = 128 * 128;
 constexpr uint32_t kQueryRing = 3;
@@ -99,7 +101,7 @@ constexpr uint32_t kQueryRing = 3;
 struct MassShared {
   uint64_t k_full[2], k_empty[2], q_full[kQueryRing], q_empty[kQueryRing], s_full[4], s_empty[4], drain;
   alignas(16) float lse[2][128];  // negated, in powers of two: of even and odd units (read four at a time)
-  float sum[2][128];  // of odd units: both halves of the keys
+  float sum[2][128];  // of one group: both halves of the keys
   uint32_t tmem;
 };
 
@@ -171,33 +173,37 @@ struct MassWalk {
   }
 };
 
-// The weights of 32 rows added to a key's sum.
-__device__ __forceinline__ void add_weights(const uint32_t (&x)[32], const float* lse, float sl2, float2 (&sum)[2]) {
+// The weights of 32 rows added to the sums of a key of either half.
+__device__ __forceinline__ void add_weights(const uint32_t (&x)[2][32], const float* lse, float sl2, float2 (&sum)[2]) {
   const float4* off = reinterpret_cast<const float4*>(lse);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const float4 o = off[k];
-    const float2 e0 = fma2(make_float2(__uint_as_float(x[4 * k]), __uint_as_float(x[4 * k + 1])), make_float2(sl2, sl2),
-                           make_float2(o.x, o.y));
-    const float2 e1 = fma2(make_float2(__uint_as_float(x[4 * k + 2]), __uint_as_float(x[4 * k + 3])), make_float2(sl2, sl2),
-                           make_float2(o.z, o.w));
-    sum[0] = add2(sum[0], make_float2(exp2_approx(e0.x), exp2_approx(e0.y)));
-    sum[1] = add2(sum[1], make_float2(exp2_approx(e1.x), exp2_approx(e1.y)));
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const float2 e0 = fma2(make_float2(__uint_as_float(x[half][4 * k]), __uint_as_float(x[half][4 * k + 1])),
+                             make_float2(sl2, sl2), make_float2(o.x, o.y));
+      const float2 e1 = fma2(make_float2(__uint_as_float(x[half][4 * k + 2]), __uint_as_float(x[half][4 * k + 3])),
+                             make_float2(sl2, sl2), make_float2(o.z, o.w));
+      sum[half] = add2(sum[half], make_float2(exp2_approx(e0.x), exp2_approx(e0.y)));
+      sum[half] = add2(sum[half], make_float2(exp2_approx(e1.x), exp2_approx(e1.y)));
+    }
   }
 }
 
 __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uint32_t group) {
-  const uint32_t tid = threadIdx.x & 127, half = group & 1, odd = group >> 1, buf = group;
-  const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16);
+  const uint32_t tid = threadIdx.x & 127, side = group & 1, odd = group >> 1;
+  const uint32_t tmem = sh.tmem + ((tid & ~31u) << 16) + odd * 256;
   const float sl2 = a.scale * kLog2e;
   auto odd_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(2 + odd) : "memory"); };
-  uint32_t unit = 0, mine = 0, seg = 0;
+  auto all_sync = [] { asm volatile("bar.sync 1, 512;" ::: "memory"); };
+  uint32_t unit = 0, seg = 0, uses[2] = {0, 0};
   bool alive = true;  // a warp that has given up waiting runs on without, for the others at the barriers
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
-    const uint64_t key = (uint64_t)w.kt * kMassKeys + half * kKeys + tid;
+    const uint32_t key = w.kt * kMassKeys + tid;  // and key + kKeys
     const int64_t t_first = (int64_t)key - ((int64_t)w.n - w.m);  // the first token that sees the key
-    const bool on = half == 0 || w.two();
+    const bool two = w.two();
     // lse of a query tile's row `tid`; rows that are none count nothing below
     auto lse_of = [&](uint32_t q) {
       if (tid >= w.rows(a, q)) return 0.f;
@@ -205,70 +211,71 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
       return -kLog2e * a.lse[t * a.n_q_heads + w.h * a.G + tid % a.G];
     };
     uint32_t q = w.q0 + ((odd ^ unit) & 1);
-    float ahead = half == 0 && q < w.q1 ? lse_of(q) : 0.f, total = 0.f;
+    float ahead = side == 0 && q < w.q1 ? lse_of(q) : 0.f;
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
     for (; q < w.q1; q += 2) {
-      if (half == 0) sh.lse[odd][tid] = ahead;
+      if (side == 0) sh.lse[odd][tid] = ahead;
       odd_sync();
-      if (half == 0 && q + 2 < w.q1) ahead = lse_of(q + 2);
-      if (on) {
-        if (alive) alive = mbar_wait(smem_u32(&sh.s_full[buf]), mine++ & 1);
-        tc_fence_after();
-        const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G;
-        const int lo = lo64 <= 0 ? 0 : lo64 >= 128 ? 128 : (int)lo64, hi = (int)w.rows(a, q);
-        const bool masked = __any_sync(kFull, lo > 0 || (hi & 31));
-        const uint32_t s_at = tmem + buf * 128;
+      if (side == 0 && q + 2 < w.q1) ahead = lse_of(q + 2);
+      if (alive) alive = mbar_wait(smem_u32(&sh.s_full[2 * odd]), uses[0]++ & 1);
+      if (two && alive) alive = mbar_wait(smem_u32(&sh.s_full[2 * odd + 1]), uses[1]++ & 1);
+      tc_fence_after();
+      // the rows that see either key, from `lo` on
+      const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G, lo64b = lo64 + (int64_t)kKeys * a.G;
+      const int lo = lo64 <= 0 ? 0 : lo64 >= 128 ? 128 : (int)lo64, lo_b = lo64b <= 0 ? 0 : lo64b >= 128 ? 128 : (int)lo64b;
+      const int rows = (int)w.rows(a, q), from = 64 * (int)side, to = rows < from + 64 ? rows : from + 64;
+      const bool masked = __any_sync(kFull, lo > from || (two && lo_b > from) || ((rows & 31) && to == rows));
+#pragma unroll 1
+      for (int c = from; c < to; c += 32) {
+        uint32_t x[2][32];
+        tmem_ld32(x[0], tmem + c);
+        tmem_ld32(x[1], tmem + 128 + c);  // (where there is no second half, anything, and not used)
+        tmem_wait_ld(x[0]);
+        tmem_wait_ld(x[1]);
         if (!masked) {
-          // a multiple of 32 rows that all see the keys; the next 32 scores come in behind
-          float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-          uint32_t x[2][32];
-          tmem_ld32(x[0], s_at);
-#pragma unroll 1
-          for (int c = 0; c < hi; c += 64) {
-            tmem_wait_ld(x[0]);
-            if (c + 32 < hi) tmem_ld32(x[1], s_at + c + 32);
-            add_weights(x[0], sh.lse[odd] + c, sl2, sum);
-            if (c + 32 < hi) {
-              tmem_wait_ld(x[1]);
-              if (c + 64 < hi) tmem_ld32(x[0], s_at + c + 64);
-              add_weights(x[1], sh.lse[odd] + c + 32, sl2, sum);
-            }
-          }
-          total += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+          add_weights(x, sh.lse[odd] + c, sl2, sum);
         } else {
-          float sum = 0.f;
-#pragma unroll 1
-          for (int c = 0; c < hi; c += 32) {
-            uint32_t x[32];
-            tmem_ld32(x, s_at + c);
-            tmem_wait_ld(x);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const float p = exp2_approx(fmaf(__uint_as_float(x[k]), sl2, sh.lse[odd][c + k]));
-              if (c + k >= lo && c + k < hi) sum += p;
-            }
+          for (int k = 0; k < 32; ++k) {
+            const float off = sh.lse[odd][c + k];
+            const float p0 = exp2_approx(fmaf(__uint_as_float(x[0][k]), sl2, off));
+            const float p1 = exp2_approx(fmaf(__uint_as_float(x[1][k]), sl2, off));
+            if (c + k >= lo && c + k < rows) sum[0].x += p0;
+            if (c + k >= lo_b && c + k < rows) sum[1].x += p1;
           }
-          total += sum;
         }
-        tc_fence_before();
-        mbar_arrive_warp(smem_u32(&sh.s_empty[buf]));
       }
+      tc_fence_before();
+      mbar_arrive_warp(smem_u32(&sh.s_empty[2 * odd]));
+      if (two) mbar_arrive_warp(smem_u32(&sh.s_empty[2 * odd + 1]));
       odd_sync();  // the lse have been read
     }
     unit += w.q1 - w.q0;
-    if (odd) sh.sum[half][tid] = total;
-    asm volatile("bar.sync 1, 512;" ::: "memory");
-    if (!odd) {
-      total += sh.sum[half][tid];
-      if (w.q0 == w.first && w.q1 == w.first + w.count) {
-        if (key < w.n) {
-          const uint64_t at = w.h * a.mass_stride + w.page0 * a.kv.B + key;
-          a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + total;
+    // the four groups' sums (where there is no second half, its are not used)
+    float total[2] = {sum[0].x + sum[0].y, sum[1].x + sum[1].y};
+    all_sync();
+    float (*place)[128] = side == 0 ? sh.lse : sh.sum;
+    if (odd) place[0][tid] = total[0], place[1][tid] = total[1];
+    all_sync();
+    if (!odd) total[0] += place[0][tid], total[1] += place[1][tid];
+    all_sync();
+    if (group == 1) place[0][tid] = total[0], place[1][tid] = total[1];
+    all_sync();
+    if (group == 0) {
+      const bool whole = w.q0 == w.first && w.q1 == w.first + w.count;
+#pragma unroll
+      for (uint32_t half = 0; half < 2; ++half) {
+        const uint32_t k = key + half * kKeys;
+        total[half] += sh.sum[half][tid];
+        if (!whole) {
+          a.part_mass[(2 * (uint64_t)blockIdx.x + (seg == 0 ? 0 : 1)) * kMassKeys + half * kKeys + tid] = total[half];
+        } else if (k < w.n) {
+          const uint64_t at = w.h * a.mass_stride + w.page0 * a.kv.B + k;
+          a.mass_out[at] = (a.mass_in ? a.mass_in[at] : 0.f) + total[half];
         }
-      } else {
-        a.part_mass[(2 * (uint64_t)blockIdx.x + (seg == 0 ? 0 : 1)) * kMassKeys + half * kKeys + tid] = total;
       }
     }
-    asm volatile("bar.sync 1, 512;" ::: "memory");
+    all_sync();
   }
   return alive;
 }
@@ -415,7 +422,7 @@ __global__ void __launch_bounds__(kMassThreads, 1)
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(smem_u32(&sh.s_full[i]), 1);
-      mbar_init(smem_u32(&sh.s_empty[i]), 4);
+      mbar_init(smem_u32(&sh.s_empty[i]), 8);
     }
     mbar_init(smem_u32(&sh.drain), 1);
     fence_mbar_init();
