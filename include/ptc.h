@@ -643,7 +643,8 @@ typedef struct {
  * ptc_kv_append — writes new tokens' keys and values into their pages: new
  * token i of request r (of m = tok_off[r+1] - tok_off[r]) becomes key
  * kv_len[r] - m + i.  kv_len[r] < m is PTC_ERR_INVALID_ARG; nothing is written
- * for such a request or one whose pages are malformed.
+ * for such a request or one whose pages are malformed.  With status, ws may be
+ * NULL.
  *   k_new, v_new  [n_tok, n_kv_heads, head_dim], the cache's dtype; token and head
  *                 strides in elements, as for the cache; 16-byte aligned
  */
@@ -661,7 +662,8 @@ ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* 
  * A token that sees no key (i < m - n) gets out = 0 and lse = -infinity.
  * Products are summed in 32 bits; the weights are rounded to the cache's dtype
  * before they meet the values (their sum is not).  Slots at or after kv_len[r]
- * may hold anything, NaN included.
+ * may hold anything, NaN included; a NaN or infinite value before that may
+ * reach any new token of its request, also one that does not see it.
  *   q         [n_tok, n_q_heads, head_dim], the cache's dtype; token and head
  *             strides in elements, as for the cache; 16-byte aligned
  *   scale     finite and positive
@@ -692,6 +694,8 @@ ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q, const int6
  * the destination pages.  Every head keeps b tokens, so the result is again a
  * paged cache, which ptc_paged_attention reads with kv_len = new_len; its masks
  * stay right because all kept tokens are in the past of new ones.
+ * With status, ws may be NULL.
+ *   n_req         at most 65,535
  *   mass          f32[n_kv_heads, mass_stride] as ptc_paged_attention leaves it
  *   n_keep        at least 1;  n_sink + n_recent <= n_keep
  *   max_kv_len    no request has more tokens (PTC_ERR_INVALID_ARG otherwise)

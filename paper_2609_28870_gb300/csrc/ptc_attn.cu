@@ -30,13 +30,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   __shared__ uint32_t s_m[kPlanThreads], s_n[kPlanThreads];
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, tq = a.tq;
   const bool weights = blockIdx.y == 1;
-  const uint32_t extra = weights ? kMassExtra : kTileExtra;
+  auto extra_of = [&](uint32_t m, uint32_t i) { return weights ? kMassExtra : tile_extra(m, tq, a.tq32, i); };
   AttnPlan* plan = a.plan + blockIdx.y;
   uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.y * (R + 1);
   // a request's first-level tiles, and the units of one of them
   auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kMassKeys) : 0u) : query_tiles(m, tq); };
   auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
-    return extra + (weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i));
+    return extra_of(m, i) + (weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i));
   };
   bool bad = tid == 0 && (a.tok_off[0] != 0 || a.tok_off[R] != a.n_tok);
   uint64_t carry = 0;
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
         if (here) {
           const int src = __ffs(here) - 1;
           s.major = t0 + src;
-          const uint32_t at = (uint32_t)rest - __shfl_sync(kFull, incl - k, src);
+          const uint32_t at = (uint32_t)rest - __shfl_sync(kFull, incl - k, src), extra = extra_of(m, s.major);
           s.minor = at > extra ? at - extra : 0;
           const uint32_t all = __shfl_sync(kFull, k, src) - extra;
           const uint32_t least = weights || m - s.major * 2 * tq <= a.tq32 ? 1 : kPartMin;
@@ -190,7 +190,7 @@ struct Walk {
   }
   __device__ __forceinline__ void part(const AttnArgs& a) {
     nkv = key_tiles(m, n, a.tq, qt);
-    extra = kv0 ? 0 : kTileExtra;
+    extra = kv0 ? 0 : tile_extra(m, a.tq, a.tq32, qt);
     kv1 = nkv - kv0 + extra > left ? kv0 + (uint32_t)left - extra : nkv;
   }
   // The next query tile.
@@ -238,8 +238,12 @@ struct Walk {
   }
   __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const { return qt * 2 * a.tq; }
   // The units of the whole tile.
-  __device__ __forceinline__ uint64_t from() const { return kv0 ? u - kv0 - kTileExtra : u; }
-  __device__ __forceinline__ uint64_t to() const { return from() + kTileExtra + nkv; }
+  __device__ __forceinline__ uint64_t from(const AttnArgs& a) const {
+    return kv0 ? u - kv0 - tile_extra(m, a.tq, a.tq32, qt) : u;
+  }
+  __device__ __forceinline__ uint64_t to(const AttnArgs& a) const {
+    return from(a) + tile_extra(m, a.tq, a.tq32, qt) + nkv;
+  }
   // How the two halves of the softmax share the tile.
   __device__ __forceinline__ int mode(const AttnArgs& a) const {
     const uint32_t tokens = m - qt * 2 * a.tq;
@@ -550,7 +554,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     RowState st;
     st.clear();
     const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
-    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w.from(), w.to());
+    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w.from(a), w.to(a));
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
         if (alive) alive = mbar_wait(bar_s, done & 1);

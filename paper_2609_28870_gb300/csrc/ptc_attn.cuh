@@ -62,10 +62,12 @@ struct AttnArgs {
   uint32_t* status;
 };
 
-// Units that a tile costs by itself: the softmax's first steps and the sums'
-// way out take about as long as three key tiles (measured on a step of mixed
-// chunks: TODO), a key tile's sum of weights about one query tile.
-constexpr uint32_t kTileExtra = 3, kMassExtra = 1;
+// Units that a tile costs by itself (the softmax's first steps, the sums' way
+// out).  A step of mixed chunks took 549, 494, 489 and 500 us with 1, 2, 3 and 5
+// for every tile, 64 single tokens 179, 182, 185 and 191 us: a tile of few rows
+// costs one key tile, any other three.  A key tile's sum of weights costs about
+// one query tile.
+constexpr uint32_t kTileExtra = 3, kFewExtra = 1, kMassExtra = 1;
 // Fewest key tiles of a part.  A part of up to 256 rows costs their sums' way
 // through memory (6 us for two parts of 256 rows); one of few rows hardly any.
 constexpr uint32_t kPartMin = 4;
@@ -98,6 +100,10 @@ __device__ __forceinline__ uint32_t key_tiles(uint32_t m, uint32_t n, uint32_t t
   const uint32_t end = (qt + 1) * 2 * tq < m ? (qt + 1) * 2 * tq : m;
   const int64_t sees = (int64_t)n - m + end;
   return sees <= (int64_t)kKeys ? 1u : (uint32_t)((sees + kKeys - 1) / kKeys);
+}
+// What query tile qt costs by itself.
+__device__ __forceinline__ uint32_t tile_extra(uint32_t m, uint32_t tq, uint32_t tq32, uint32_t qt) {
+  return m - qt * 2 * tq <= tq32 ? kFewExtra : kTileExtra;
 }
 // The first half tile of queries that sees anything of the weights' key tile kt.
 __device__ __forceinline__ uint32_t first_seeing(uint32_t m, uint32_t n, uint32_t tq, uint32_t kt) {

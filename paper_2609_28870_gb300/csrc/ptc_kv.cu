@@ -81,9 +81,14 @@ struct EvictArgs {
   uint32_t* new_len;
   float* new_mass;
   uint64_t new_mass_stride;
-  uint32_t* ok;  // per request: 1 if its lists are sound
   uint32_t* status;
 };
+
+// Whether request r's lists are sound and the destination has room for its b tokens.
+__device__ __forceinline__ bool evict_ok(const EvictArgs& a, uint32_t r, uint32_t n, uint32_t b) {
+  const uint64_t d0 = a.dst_off[r], d1 = a.dst_off[r + 1];
+  return pages_hold(a.kv, r, n) && n <= a.max_kv_len && d0 <= d1 && d1 <= a.n_dst_ids && b <= (d1 - d0) * a.kv.B;
+}
 
 // Weights as integers in the same order: NaN lowest (1), -0 equal to 0, and
 // +infinity below kForced, which stands for tokens that are kept in any case;
@@ -144,10 +149,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t n = a.kv.kv_len[r], b = n < a.n_keep ? n : a.n_keep;
   const uint64_t d0 = a.dst_off[r], d1 = a.dst_off[r + 1];
-  const bool ok = n <= a.max_kv_len && pages_hold(a.kv, r, n) && d0 <= d1 && d1 <= a.n_dst_ids &&
-                  b <= (d1 - d0) * a.kv.B;
+  const bool ok = evict_ok(a, r, n, b);
   if (h == 0 && rank == 0 && tid == 0) {
-    a.ok[r] = ok;
     a.new_len[r] = b;
     if (!ok) report(a.status, PTC_ERR_INVALID_ARG);
   }
@@ -356,11 +359,11 @@ constexpr uint32_t kMvRows = 32;
 __global__ void __launch_bounds__(kMvThreads) k_evict_move(EvictArgs a) {
   grid_dep_sync();
   const uint32_t h = blockIdx.y, r = blockIdx.z, i0 = blockIdx.x * kMvRows;
-  if (!a.ok[r]) return;
-  const uint32_t b = a.new_len[r], n = a.kv.kv_len[r];
+  const uint32_t n = a.kv.kv_len[r], b = n < a.n_keep ? n : a.n_keep;
+  if (i0 >= b || !evict_ok(a, r, n, b)) return;
   const uint64_t p0 = a.kv.page_off[r], d0 = a.dst_off[r];
   const uint32_t* keep = a.keep + ((uint64_t)r * a.kv.H + h) * a.n_keep;
-  const uint32_t rows = i0 >= b ? 0 : (b - i0 < kMvRows ? b - i0 : kMvRows), chunks = a.kv.D / 8;
+  const uint32_t rows = b - i0 < kMvRows ? b - i0 : kMvRows, chunks = a.kv.D / 8;
   for (uint32_t x = threadIdx.x; x < rows * chunks; x += kMvThreads) {
     const uint32_t i = i0 + x / chunks, d = (x % chunks) * 8;
     const uint32_t j = keep[i];
@@ -409,7 +412,6 @@ void launch_select(const EvictArgs& a, cudaStream_t s) {
   (void)cudaLaunchKernelEx(&cfg, k_evict_select, a, c, cap);
 }
 
-size_t evict_bytes(uint32_t n_req) { return kKvStatusBytes + ((size_t)n_req * 4 + 255) / 256 * 256; }
 
 }  // namespace
 }  // namespace ptc
@@ -427,7 +429,7 @@ extern "C" ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, c
   if (st != PTC_OK) return st;
   if (!tok_off || !k_new_stride || !v_new_stride || (n_tok && !kv->n_req)) return PTC_ERR_INVALID_ARG;
   if (n_tok > (uint64_t(1) << 31)) return PTC_ERR_OVERFLOW;
-  if (!ws_ok(ws, ws_bytes, kKvStatusBytes)) return PTC_ERR_WORKSPACE;
+  if (!status && !ws_ok(ws, ws_bytes, kKvStatusBytes)) return PTC_ERR_WORKSPACE;
   if (n_tok == 0) return PTC_OK;
   if (!aligned16(k_new) || !aligned16(v_new)) return PTC_ERR_INVALID_ARG;
   const uint32_t ext[2] = {(uint32_t)n_tok, kv->n_kv_heads};
@@ -449,7 +451,7 @@ extern "C" ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, c
   return kv_end(status, a.status, s);
 }
 
-extern "C" size_t ptc_kv_evict_workspace_bytes(uint32_t n_req, uint32_t, uint32_t) { return evict_bytes(n_req); }
+extern "C" size_t ptc_kv_evict_workspace_bytes(uint32_t, uint32_t, uint32_t) { return kKvStatusBytes; }
 
 extern "C" ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, uint64_t mass_stride, uint32_t n_keep,
                                    uint32_t n_sink, uint32_t n_recent, uint32_t max_kv_len,
@@ -463,7 +465,7 @@ extern "C" ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, ui
   if (n_keep < 1 || (uint64_t)n_sink + n_recent > n_keep) return PTC_ERR_INVALID_ARG;
   if (!dst_page_off || (n_dst_page_ids && !dst_page_ids)) return PTC_ERR_INVALID_ARG;
   if (n_keep > (1u << 30) || max_kv_len > (1u << 31)) return PTC_ERR_OVERFLOW;
-  if (!ws_ok(ws, ws_bytes, evict_bytes(kv->n_req))) return PTC_ERR_WORKSPACE;
+  if (!status && !ws_ok(ws, ws_bytes, kKvStatusBytes)) return PTC_ERR_WORKSPACE;
   if (kv->n_req == 0) return PTC_OK;
   if ((kv->n_page_ids && !mass) || (n_dst_page_ids && (!new_mass_out || new_mass_out == mass))) return PTC_ERR_INVALID_ARG;
   if (!keep_out || !new_len_out) return PTC_ERR_INVALID_ARG;
@@ -484,7 +486,6 @@ extern "C" ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, ui
   a.new_len = new_len_out;
   a.new_mass = new_mass_out;
   a.new_mass_stride = new_mass_stride;
-  a.ok = reinterpret_cast<uint32_t*>(static_cast<char*>(ws) + kKvStatusBytes);
   if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
   PTC_LAUNCH("k_evict_select", s, launch_select(a, s));
   const uint32_t most = n_keep < max_kv_len ? n_keep : max_kv_len;

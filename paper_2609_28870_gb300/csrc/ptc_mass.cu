@@ -47,24 +47,28 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
     if (j < n) {
       const float sl2 = a.scale * kLog2e;
       const int64_t sees0 = n - m + 1;  // keys that the first token sees
-      for (uint32_t i = 0; i < (uint32_t)m * a.G; ++i) {
-        const int64_t sees = sees0 + i / a.G;
-        if (j >= sees) continue;
-        const float off = a.lse[(tok0 + i / a.G) * a.n_q_heads + h * a.G + i % a.G] * kLog2e;
-        float x[4];
-        if (four) {
+      const uint32_t rows = (uint32_t)m * a.G;
+      const float* lse = a.lse + tok0 * a.n_q_heads + h * a.G;
+      for (uint32_t i0 = 0; i0 < rows; i0 += 4) {
+        float4 x[4];
+        float off[4];
+        int64_t sees[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {  // four rows' loads in flight
+          const uint32_t i = i0 + u < rows ? i0 + u : i0, t = i / a.G;
+          sees[u] = i0 + u < rows ? sees0 + t : 0;
+          off[u] = lse[(uint64_t)t * a.n_q_heads + (i - t * a.G)] * kLog2e;
+          const float* p = score + i * a.mass_stride;
           // what lies past the row's last key is not used
-          const float4 y = *reinterpret_cast<const float4*>(score + i * a.mass_stride);
-          x[0] = y.x;
-          x[1] = y.y;
-          x[2] = y.z;
-          x[3] = y.w;
-        } else {
-          x[0] = score[i * a.mass_stride];
+          x[u] = four ? *reinterpret_cast<const float4*>(p) : make_float4(*p, 0.f, 0.f, 0.f);
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if ((uint32_t)k < width && j + k < sees) sum[k] += exp2_approx(fmaf(x[k], sl2, -off));
+        for (uint32_t u = 0; u < 4; ++u) {
+          const float y[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if ((uint32_t)k < width && j + k < sees[u]) sum[k] += exp2_approx(fmaf(y[k], sl2, -off[u]));
+        }
       }
     }
     if (four) {

@@ -118,6 +118,10 @@ def _room(k, need: int, dev: int, ws):
     return torch.empty(max(need, 256), dtype=torch.uint8, device=k.device)
 
 
+def _place(w):
+    return (None, 0) if w is None else (w.data_ptr(), w.numel())
+
+
 def _stream(dev: int) -> int:
     return torch._C._cuda_getCurrentRawStream(dev)
 
@@ -142,9 +146,9 @@ def ptc_kv_append(k_new, v_new, k, v, page_ids, page_off, tok_off, kv_len, ws: t
     if v_new.shape != k_new.shape:
         raise ValueError("v_new: expected k_new's shape")
     L = p.lib()
-    w = _room(k, L.ptc_kv_append_workspace_bytes(kv_len.shape[0]), dev, ws)
+    w = _room(k, L.ptc_kv_append_workspace_bytes(kv_len.shape[0]), dev, ws) if status is None else None
     rc = L.ptc_kv_append(kv, k_new.data_ptr(), v_new.data_ptr(), ks, vs, tok_off.data_ptr(), k_new.shape[0],
-                         w.data_ptr(), w.numel(), _status(status, dev), _stream(dev))
+                         *_place(w), _status(status, dev), _stream(dev))
     p._check("ptc_kv_append", rc)
 
 
@@ -220,10 +224,9 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
     slots = dst_page_ids.shape[0] * shape[2]
     new_mass = torch.empty((heads, slots), dtype=torch.float32, device=k.device)
     L = p.lib()
-    w = _room(k, L.ptc_kv_evict_workspace_bytes(n_req, heads, max_kv_len), dev, ws)
+    w = _room(k, L.ptc_kv_evict_workspace_bytes(n_req, heads, max_kv_len), dev, ws) if status is None else None
     rc = L.ptc_kv_evict(kv, mass.data_ptr(), mass.shape[1], n_keep, n_sink, n_recent, max_kv_len,
                         dst_page_ids.data_ptr(), dst_page_off.data_ptr(), dst_page_ids.shape[0], keep.data_ptr(),
-                        new_len.data_ptr(), new_mass.data_ptr(), slots, w.data_ptr(), w.numel(), _status(status, dev),
-                        _stream(dev))
+                        new_len.data_ptr(), new_mass.data_ptr(), slots, *_place(w), _status(status, dev), _stream(dev))
     p._check("ptc_kv_evict", rc)
     return keep, new_len, new_mass
