@@ -255,7 +255,7 @@ struct Walk {
 // Attention weights of bf16 caches are rounded as they are.  Those of fp16
 // caches are scaled by 2^7 first: a weight far below the running maximum would
 // otherwise fall among fp16's subnormals (below 2^-14) and a long row of small
-// weights would be lost; with the lazy maximum's 2^8 the largest is 2^15.
+// weights would be lost; with kMove's 2^8 the largest is 2^15.
 template <typename T>
 struct Weights;
 template <>
@@ -294,13 +294,21 @@ struct Weights<__half> {
 //   kColumnsApart up to 32 rows (single tokens): the rows stand four times in
 //                 the matrix, and each of the 4 warps takes 32 keys of a tile,
 //                 with zero weights for the others'.  A softmax over 32 keys is
-//                 a quarter of the latency that a tile waits for; the products
-//                 are the same instructions either way.
-// O is rescaled only when a row's maximum has grown by more than a factor of
-// 2^8 since the last time (weights up to 2^8 are as exact as those up to 1),
-// which after the first tiles hardly happens.  So the weights of a tile are
-// first taken with the maximum as it stands, while the tile's own is still being
-// found, and again only if that shows it has to move.
+//                 a quarter of the latency that a tile waits for (64 single
+//                 tokens: 307 us with whole rows, 204 so); the products are the
+//                 same instructions either way.
+// The maximum that weights are taken with need not be the row's: weights up to
+// 2^8 are as exact as those up to 1.  So it is only looked for, and O only
+// rescaled, when 64 weights add up to more than 2^8, which after the first tile
+// hardly happens (2.02 -> 1.38 ms for 4,096 tokens at 32K, with the products'
+// descriptors made outside the issuing lane).
+//
+// Bounds.  Single tokens: HBM; 12 contexts of 32K to 131K, 1.81 GB, take 277 us,
+// 6.5 TB/s.  Chunks: a unit of 256 rows and 128 keys is 2,048 cycles of products
+// at D = 128.  It takes 3,030 (4,096 tokens at 32K: 1.32 ms, 1.56 PFLOP/s, the
+// tensor pipe 68% active): the products read 192 KB of shared memory and the
+// copies write 64, 2,048 cycles at 128 bytes a cycle too, and a half's own
+// chain (softmax 1,260, its two products 1,024, four hand-overs) is 2,600.
 enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
 constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
@@ -422,7 +430,8 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
 }
 
 // The maximum moves when a row's sum of 64 (or 32) weights passes this: as many
-// of at most 1 stay below it, and no weight is larger than their sum.
+// of at most 1 stay below it, and no weight is larger than their sum.  (For fp16
+// the weights, and with them this, are 2^7 times as large.)
 constexpr float kMove = 256.f;
 
 // Who has a part of the tile, and where; by one warp.
