@@ -181,7 +181,7 @@ struct MassWalk {
 };
 
 // The weights of 32 rows added to the sums of a key of either half.
-__device__ __forceinline__ void add_weights(const uint32_t (&x)[2][32], const float* lse, float sl2, float2 (&sum)[2]) {
+__device__ __forceinline__ void add_weights(const uint32_t (&x)[2][32], const float* lse, float sl2, float2 (&sum)[2][2]) {
   const float4* off = reinterpret_cast<const float4*>(lse);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
@@ -192,8 +192,8 @@ __device__ __forceinline__ void add_weights(const uint32_t (&x)[2][32], const fl
                              make_float2(sl2, sl2), make_float2(o.x, o.y));
       const float2 e1 = fma2(make_float2(__uint_as_float(x[half][4 * k + 2]), __uint_as_float(x[half][4 * k + 3])),
                              make_float2(sl2, sl2), make_float2(o.z, o.w));
-      sum[half] = add2(sum[half], make_float2(exp2_approx(e0.x), exp2_approx(e0.y)));
-      sum[half] = add2(sum[half], make_float2(exp2_approx(e1.x), exp2_approx(e1.y)));
+      sum[half][0] = add2(sum[half][0], make_float2(exp2_approx(e0.x), exp2_approx(e0.y)));
+      sum[half][1] = add2(sum[half][1], make_float2(exp2_approx(e1.x), exp2_approx(e1.y)));
     }
   }
 }
@@ -219,7 +219,7 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
     };
     uint32_t q = w.q0 + ((odd ^ unit) & 1);
     float ahead = side == 0 && q < w.q1 ? lse_of(q) : 0.f;
-    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    float2 sum[2][2] = {};
     for (; q < w.q1; q += 2) {
       if (side == 0) sh.lse[odd][tid] = ahead;
       odd_sync();
@@ -247,8 +247,8 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
             const float off = sh.lse[odd][c + k];
             const float p0 = exp2_approx(fmaf(__uint_as_float(x[0][k]), sl2, off));
             const float p1 = exp2_approx(fmaf(__uint_as_float(x[1][k]), sl2, off));
-            if (c + k >= lo && c + k < rows) sum[0].x += p0;
-            if (c + k >= lo_b && c + k < rows) sum[1].x += p1;
+            if (c + k >= lo && c + k < rows) sum[0][0].x += p0;
+            if (c + k >= lo_b && c + k < rows) sum[1][0].x += p1;
           }
         }
       }
@@ -259,7 +259,10 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
     }
     unit += w.q1 - w.q0;
     // the four groups' sums (where there is no second half, its are not used)
-    float total[2] = {sum[0].x + sum[0].y, sum[1].x + sum[1].y};
+    float total[2];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+      total[half] = (sum[half][0].x + sum[half][0].y) + (sum[half][1].x + sum[half][1].y);
     all_sync();
     float (*place)[128] = side == 0 ? sh.lse : sh.sum;
     if (odd) place[0][tid] = total[0], place[1][tid] = total[1];
