@@ -16,27 +16,31 @@ __device__ __forceinline__ uint32_t unit_search(const uint64_t* off, uint32_t lo
   return lo;
 }
 
-// The requests' share of the units, and every CTA's start; blockIdx.y = 0 for
-// the tile kernel, 1 (where there is one) for the weights.  The time of a call
+// The requests' share of the units, and every CTA's (or pair's) start, for the
+// plan that blockIdx.y has in `which`.  The time of a call
 // of few units is a chain of latencies: what the lists hold is read once and
 // kept in shared memory (the first kPlanThreads requests of it), and the CTAs
 // here add it up each for itself and find 32 starts each, one a warp (one CTA
 // for all starts took 10 us, of which 8 were spent on them).
 constexpr int kPlanThreads = 1024;
-__global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
+__global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a, uint3 which) {
   asm volatile("griddepcontrol.launch_dependents;");
   grid_dep_sync();
   __shared__ uint64_t s_warp[32], s_off[kPlanThreads + 1];
   __shared__ uint32_t s_m[kPlanThreads], s_n[kPlanThreads];
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, tq = a.tq;
-  const bool weights = blockIdx.y == 1;
-  auto extra_of = [&](uint32_t m, uint32_t i) { return weights ? kMassExtra : tile_extra(m, tq, a.tq32, i); };
-  AttnPlan* plan = a.plan + blockIdx.y;
-  uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.y * (R + 1);
+  const uint32_t kind = blockIdx.y == 0 ? which.x : blockIdx.y == 1 ? which.y : which.z;
+  const bool weights = kind == 1;
+  const uint32_t span = kind == 2 ? 4 * tq : 2 * tq, ctas = kind == 2 ? a.ctas / 2 : a.ctas;
+  auto extra_of = [&](uint32_t m, uint32_t i) { return weights ? kMassExtra : tile_extra(m, span, a.tq32, i); };
+  AttnPlan* plan = a.plan + kind;
+  uint64_t* unit_off = a.unit_off + (uint64_t)kind * (R + 1);
+  // new tokens of a request, as far as they are this plan's
+  auto mine_of = [&](uint32_t m) { return weights || (m > a.pair_min) == (kind == 2) ? m : 0u; };
   // a request's first-level tiles, and the units of one of them
-  auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kMassKeys) : 0u) : query_tiles(m, tq); };
+  auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kMassKeys) : 0u) : div_up(m, span); };
   auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
-    return extra_of(m, i) + (weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, tq, i));
+    return extra_of(m, i) + (weights ? div_up(m, tq) - first_seeing(m, n, tq, i) : key_tiles(m, n, span, i));
   };
   bool bad = tid == 0 && (a.tok_off[0] != 0 || a.tok_off[R] != a.n_tok);
   uint64_t carry = 0;
@@ -50,7 +54,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
       const bool hold = pages_hold(a.kv, r, n);
       const bool wrong = (lo > hi) | (hi > a.n_tok) | (hi - lo > a.max_q_len) | !hold;
       bad |= wrong;
-      m = wrong ? 0 : (uint32_t)(hi - lo);
+      m = wrong ? 0 : mine_of((uint32_t)(hi - lo));
     }
     const uint32_t tiles = tiles_of(m, n);
     uint64_t mine = 0;
@@ -105,12 +109,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   __syncthreads();
   // 64-bit divisions are long; hardly a call needs one
   auto ratio = [](uint64_t x, uint64_t y) { return x >> 32 || y >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y); };
-  const uint64_t each = ratio(carry, a.ctas);
-  const uint32_t over = (uint32_t)(carry - each * a.ctas);
+  const uint64_t each = ratio(carry, ctas);
+  const uint32_t over = (uint32_t)(carry - each * ctas);
   const uint32_t c = blockIdx.x * 32 + warp;
-  if (c <= a.ctas) {
+  if (c <= ctas) {
     CtaStart s{};
-    s.u = each * c + over * c / a.ctas;
+    s.u = each * c + over * c / ctas;
     uint32_t m = 0, n = 0;
     if (s.u < carry) {
       uint64_t from, to;
@@ -128,7 +132,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
         to = s_off[lo + 1];
       } else {
         s.r = unit_search(unit_off, 0, R - 1, s.u);
-        m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]);
+        m = mine_of((uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]));
         n = a.kv.kv_len[s.r];
         from = ld_relaxed_u64(unit_off + s.r);
         to = ld_relaxed_u64(unit_off + s.r + 1);
@@ -152,7 +156,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
           const uint32_t at = (uint32_t)rest - __shfl_sync(kFull, incl - k, src), extra = extra_of(m, s.major);
           s.minor = at > extra ? at - extra : 0;
           const uint32_t all = __shfl_sync(kFull, k, src) - extra;
-          const uint32_t least = weights || m - s.major * 2 * tq <= a.tq32 ? 1 : kPartMin;
+          const uint32_t least = weights || m - s.major * span <= a.tq32 ? 1 : kPartMin;
           if (s.minor < least) {
             s.u -= at;
             s.minor = 0;
@@ -175,8 +179,13 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   }
 }
 
-// The query tiles that a CTA has a part in, in order, with the part.
+// The query tiles that a CTA has a part in, in order, with the part.  PAIR: of
+// a pair of CTAs, whose tiles are twice as long: the first half is the first
+// CTA's, the second the second's.
+template <bool PAIR>
 struct Walk {
+  static constexpr uint32_t kSpan = PAIR ? 4 : 2;  // in tq tokens
+
   uint64_t left, u, tok0, page0;     // units left, the part's first unit
   uint32_t r, h, qt, kv0, kv1, nkv;  // key tiles [kv0, kv1) of nkv
   uint32_t extra;                    // units before the first key tile
@@ -185,18 +194,20 @@ struct Walk {
   __device__ __forceinline__ void request(const AttnArgs& a) {
     tok0 = a.tok_off[r];
     m = (uint32_t)(a.tok_off[r + 1] - tok0);
+    if ((m > a.pair_min) != PAIR) m = 0;  // the other kernel's
     n = a.kv.kv_len[r];
     page0 = a.kv.page_off[r];
   }
+  __device__ __forceinline__ uint32_t cost(const AttnArgs& a) const { return tile_extra(m, kSpan * a.tq, a.tq32, qt); }
   __device__ __forceinline__ void part(const AttnArgs& a) {
-    nkv = key_tiles(m, n, a.tq, qt);
-    extra = kv0 ? 0 : tile_extra(m, a.tq, a.tq32, qt);
+    nkv = key_tiles(m, n, kSpan * a.tq, qt);
+    extra = kv0 ? 0 : cost(a);
     kv1 = nkv - kv0 + extra > left ? kv0 + (uint32_t)left - extra : nkv;
   }
   // The next query tile.
   __device__ __forceinline__ bool step(const AttnArgs& a) {
     kv0 = 0;
-    if (++qt * 2 * a.tq >= m) {
+    if (++qt * kSpan * a.tq >= m) {
       qt = 0;
       if (++h == a.kv.H) {
         h = 0;
@@ -210,8 +221,9 @@ struct Walk {
   }
   // False if the CTA has nothing to do.
   __device__ __forceinline__ bool begin(const AttnArgs& a) {
-    const CtaStart s = a.plan->start[blockIdx.x];
-    left = a.plan->start[blockIdx.x + 1].u - s.u;
+    const CtaStart* start = plan(a)->start + (PAIR ? blockIdx.x / 2 : blockIdx.x);
+    const CtaStart s = start[0];
+    left = start[1].u - s.u;
     if (left == 0) return false;
     u = s.u;
     first = true;
@@ -223,7 +235,7 @@ struct Walk {
     m = s.m;
     n = s.n;
     page0 = s.page0;
-    if (kv0 && kv0 == key_tiles(m, n, a.tq, qt) && !step(a)) return false;
+    if (kv0 && kv0 == key_tiles(m, n, kSpan * a.tq, qt) && !step(a)) return false;
     part(a);
     return true;
   }
@@ -236,16 +248,17 @@ struct Walk {
     part(a);
     return true;
   }
-  __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const { return qt * 2 * a.tq; }
+  static __device__ __forceinline__ AttnPlan* plan(const AttnArgs& a) { return a.plan + (PAIR ? 2 : 0); }
+  // The first token of this CTA's rows (of a pair's second CTA it may lie past the request).
+  __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const {
+    return (qt * kSpan + (PAIR ? 2 * (blockIdx.x & 1) : 0)) * a.tq;
+  }
   // The units of the whole tile.
-  __device__ __forceinline__ uint64_t from(const AttnArgs& a) const {
-    return kv0 ? u - kv0 - tile_extra(m, a.tq, a.tq32, qt) : u;
-  }
-  __device__ __forceinline__ uint64_t to(const AttnArgs& a) const {
-    return from(a) + tile_extra(m, a.tq, a.tq32, qt) + nkv;
-  }
+  __device__ __forceinline__ uint64_t from(const AttnArgs& a) const { return kv0 ? u - kv0 - cost(a) : u; }
+  __device__ __forceinline__ uint64_t to(const AttnArgs& a) const { return from(a) + cost(a) + nkv; }
   // How the two halves of the softmax share the tile.
   __device__ __forceinline__ int mode(const AttnArgs& a) const {
+    if (PAIR) return 0;
     const uint32_t tokens = m - qt * 2 * a.tq;
     return tokens > a.tq ? 0 : tokens > a.tq32 ? 1 : 2;
   }
@@ -324,14 +337,25 @@ struct TileShared {
   uint16_t slots[kMaxCtas];  // a split tile's parts, in the order of the keys
 };
 
-// FEW: every request of the call has so few rows that its tiles are all
-// kColumnsApart.  There is no second half of queries then, and the ring has
-// its place: 5 tiles of 32 KB keep more of the cache in flight than 4.
-template <int NSLAB, bool FEW>
+// Kinds of the kernel.
+//   kFew   every request of the call has so few rows that its tiles are all
+//          kColumnsApart.  There is no second half of queries then, and the
+//          ring has its place: 5 tiles of 32 KB keep more of the cache in
+//          flight than 4.
+//   kPair  pairs of CTAs, clusters of two, for requests of at least four query
+//          tiles: the two take neighbouring query tiles through the same key
+//          tiles, and each loads half of every tile into both's shared memory.
+//          A CTA by itself draws 64 KB a unit out of L2, 7.0 TB/s over the
+//          GPU, which is all that comes out of it: without any softmax and an
+//          eighth of the products, 4,096 tokens at 32K still took 1.15 of
+//          1.33 ms.
+enum { kAny = 0, kFew = 1, kPair = 2 };
+constexpr uint32_t kPairTiles = 4;
+template <int NSLAB, int KIND>
 struct TileShape {
   static constexpr int kTile = NSLAB * kSlabBytes;
-  static constexpr uint32_t kRing = NSLAB == 1 ? 8 : FEW ? 5 : 4;
-  static constexpr int kQueries = FEW ? 1 : 2;
+  static constexpr uint32_t kRing = NSLAB == 1 ? 8 : KIND == kFew ? 5 : 4;
+  static constexpr int kQueries = KIND == kFew ? 1 : 2;
   // queries, ring, stage, the rest
   static constexpr int kRest = kQueries * kTile + kRing * kTile + kStage;
   static constexpr int kSmem = kRest + sizeof(TileShared);
@@ -450,20 +474,23 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
 constexpr float kMove = 256.f;
 
 // Who has a part of the tile, and where; by one warp.
+template <bool PAIR>
 __device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, uint64_t from, uint64_t to) {
-  const uint32_t lane = threadIdx.x & 31;
-  const Sharers s = sharers(a.plan, a.ctas, from, to);
+  const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x & 1;
+  const AttnPlan* plan = Walk<PAIR>::plan(a);
+  const Sharers s = sharers(plan, PAIR ? a.ctas / 2 : a.ctas, from, to);
   uint32_t n = 0;
   for (uint32_t x0 = s.c0; x0 <= s.c1; x0 += 32) {
     const uint32_t x = x0 + lane;
-    const uint64_t u = x <= s.c1 ? a.plan->start[x].u : 0, v = x <= s.c1 ? a.plan->start[x + 1].u : 0;
+    const uint64_t u = x <= s.c1 ? plan->start[x].u : 0, v = x <= s.c1 ? plan->start[x + 1].u : 0;
     const uint32_t has = __ballot_sync(kFull, v > u);
     // a CTA's first part, or (of the tile's first CTA, where it began with another tile) its last
-    if (v > u) sh.slots[n + __popc(has & ((1u << lane) - 1))] = (uint16_t)(2 * x + (u < from ? 1 : 0));
+    if (v > u) sh.slots[n + __popc(has & ((1u << lane) - 1))] =
+          (uint16_t)(2 * (PAIR ? 2 * x + rank : x) + (u < from ? 1 : 0));
     n += __popc(has);
   }
   if (lane == 0) {
-    sh.c0 = s.c0;
+    sh.c0 = PAIR ? 2 * s.c0 + rank : s.c0;
     sh.count = s.count;
   }
   __syncwarp();
@@ -549,7 +576,7 @@ __device__ __noinline__ void join_parts(const AttnArgs& a, const TileShared& sh,
   }
 }
 
-template <typename T, int NSLAB, bool FEW>
+template <typename T, int NSLAB, int KIND>
 __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, char* stages, uint32_t half) {
   using W = Weights<T>;
   const uint32_t tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
@@ -563,9 +590,9 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
   char* stage = stages + (half * 4 + warp) * 4096;
   bool alive = true;  // a warp that has given up waiting runs on without, for the others at the barriers
   uint32_t done = 0, parted = 0;  // key tiles of this half so far, and those in two parts
-  Walk w;
+  Walk<KIND == kPair> w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const int mode = FEW ? kColumnsApart : w.mode(a);
+    const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     // the thread's row: a token of the request and a head of the group
     const uint32_t i = mode == kColumnsApart ? lane : tid;
     const uint32_t t = w.token0(a) + (mode == kRowsApart ? half * a.tq : 0) + i / G, g = i % G;
@@ -578,7 +605,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     RowState st;
     st.clear();
     const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
-    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w.from(a), w.to(a));
+    if (!whole && threadIdx.x < 32) list_sharers<KIND == kPair>(a, sh, w.from(a), w.to(a));
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
         if (alive) alive = mbar_wait(bar_s, done & 1);
@@ -846,7 +873,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
       __threadfence();
       softmax_sync();
       if (threadIdx.x == 0) {
-        sh.last = atomicAdd(&a.plan->arrived[sh.c0], 1u) + 1 == sh.count;
+        sh.last = atomicAdd(&Walk<KIND == kPair>::plan(a)->arrived[sh.c0], 1u) + 1 == sh.count;
         __threadfence();
       }
       softmax_sync();
@@ -860,9 +887,9 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
   return alive;
 }
 
-template <typename T, int NSLAB, bool FEW>
+template <typename T, int NSLAB, int KIND>
 __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, uint32_t q_smem, uint32_t ring) {
-  using Sh = TileShape<NSLAB, FEW>;
+  using Sh = TileShape<NSLAB, KIND>;
   constexpr uint32_t kQk = mma_desc(Weights<T>::kBf16, 128, kKeys, false);
   constexpr uint32_t kPv = mma_desc(Weights<T>::kBf16, 128, NSLAB * 64, true);
   const uint32_t lane = threadIdx.x & 31, tmem = sh.tmem, steps = (a.kv.D + 15) / 16;
@@ -873,6 +900,14 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   auto tile_at = [&](uint32_t i) { return ring + (i % Sh::kRing) * Sh::kTile; };
   auto commit = [&](uint64_t& bar) {
     if (elect_lane()) mma_commit(smem_u32(&bar));
+  };
+  // a ring tile is free when both CTAs of a pair are done with it
+  auto release = [&](uint32_t at) {
+    if (KIND == kPair) mma_commit_both(smem_u32(&sh.empty[at]));
+    else mma_commit(smem_u32(&sh.empty[at]));
+  };
+  auto free_tile = [&](uint32_t i) {
+    if (elect_lane()) release(i % Sh::kRing);
   };
   auto scores = [&](uint32_t half, uint32_t region, uint32_t k_item) {
     const uint64_t da = tile_desc(q_smem + region * Sh::kTile, 16), db = tile_desc(tile_at(k_item), 16);
@@ -934,7 +969,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
             mma_ts(tmem + o_col(s), tmem + p_col(s, 16 * k), desc_at(v_desc, k * 2048), kPv, j > 0 || k > 0);
           mma_commit(smem_u32(&sh.pv_done[s][part]));
         }
-        if (s == 1) mma_commit(smem_u32(&sh.empty[v_at]));
+        if (s == 1) release(v_at);
         if (more) {
           if (s == 0 && !mbar_wait_lane(smem_u32(&sh.full[k_at]), (k_next / Sh::kRing) & 1)) return false;
           // in order after the product above, which reads the weights that these scores overwrite
@@ -948,13 +983,13 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
           if (j + 2 == L) mma_commit(smem_u32(&sh.q_empty[s]));
         }
       }
-      if (more) mma_commit(smem_u32(&sh.empty[k_at]));
+      if (more) release(k_at);
     }
     return true;
   };
-  Walk w;
+  Walk<KIND == kPair> w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const int mode = FEW ? kColumnsApart : w.mode(a);
+    const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     const uint32_t L = w.kv1 - w.kv0;
     // slots that hold no token may hold NaN: zero their values (their weights are zero)
     auto clear_tail = [&](uint32_t j, uint32_t v_item) {
@@ -976,7 +1011,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
       if (!mbar_wait(smem_u32(&sh.q_full[1]), used[1]++ & 1)) return false;
       tc_fence_after();
       scores(1, 1, item);
-      commit(sh.empty[item % Sh::kRing]);
+      free_tile(item);
       if (L == 1) {
         commit(sh.q_empty[0]);
         commit(sh.q_empty[1]);
@@ -997,7 +1032,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
         clear_tail(j, v_item);
         for (uint32_t s = 0; s < 2; ++s) {
           if (!values(s, v_item, j > 0, true)) return false;
-          if (s == 1) commit(sh.empty[v_item % Sh::kRing]);
+          if (s == 1) free_tile(v_item);
           if (j + 1 < L) {
             if (s == 0 && !full(k_next)) return false;
             // in order after the product above, which reads the weights that these scores overwrite
@@ -1005,15 +1040,15 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
             if (j + 2 == L) commit(sh.q_empty[s]);
           }
         }
-        if (j + 1 < L) commit(sh.empty[k_next % Sh::kRing]);
+        if (j + 1 < L) free_tile(k_next);
       }
     } else {
-      commit(sh.empty[item % Sh::kRing]);
+      free_tile(item);
       if (L > 1) {
         if (!full(item + 2)) return false;
         tc_fence_after();
         scores(1, 0, item + 2);
-        commit(sh.empty[(item + 2) % Sh::kRing]);
+        free_tile(item + 2);
       }
       if (L <= 2) commit(sh.q_empty[0]);
       for (uint32_t j = 0; j < L; ++j) {
@@ -1021,11 +1056,11 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
         if (!full(v_item)) return false;
         clear_tail(j, v_item);
         if (!values(j & 1, v_item, j > 1, mode != kColumnsApart)) return false;
-        commit(sh.empty[v_item % Sh::kRing]);
+        free_tile(v_item);
         if (j + 2 < L) {
           if (!full(k_next)) return false;
           scores(j & 1, 0, k_next);
-          commit(sh.empty[k_next % Sh::kRing]);
+          free_tile(k_next);
           if (j + 3 == L) commit(sh.q_empty[0]);
         }
       }
@@ -1036,14 +1071,14 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
 }
 
 // Queries by tensor copies, a tile ahead of the products.
-template <int NSLAB, bool FEW>
+template <int NSLAB, int KIND>
 __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* mq,
                                            const CUtensorMap* mq32, uint32_t q_smem, uint32_t (&loads)[2]) {
-  using Sh = TileShape<NSLAB, FEW>;
+  using Sh = TileShape<NSLAB, KIND>;
   const uint32_t lane = threadIdx.x & 31;
-  Walk w;
+  Walk<KIND == kPair> w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
-    const int mode = FEW ? kColumnsApart : w.mode(a);
+    const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     const int tok = (int)(w.tok0 + w.token0(a));
     for (uint32_t s = 0; s < (mode == kRowsApart ? 2u : 1u); ++s) {
       if (loads[s] && !mbar_wait(smem_u32(&sh.q_empty[s]), (loads[s] - 1) & 1)) return false;
@@ -1069,18 +1104,20 @@ __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, co
 // of the page size and of the tile) and slab.  Stretches at or past the
 // request's end and pages that the cache does not have read as zeros: their
 // page coordinate is n_pages, which is out of range.
-template <int NSLAB, bool FEW>
+template <int NSLAB, int KIND>
 __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* mk, const CUtensorMap* mv,
                                           uint32_t ring, uint32_t& issued) {
-  using Sh = TileShape<NSLAB, FEW>;
-  const uint32_t lane = threadIdx.x & 31, boxes = kKeys / a.box;
-  Walk w;
+  using Sh = TileShape<NSLAB, KIND>;
+  // a pair's CTA loads its half of a tile, into both
+  constexpr uint32_t kMine = KIND == kPair ? kKeys / 2 : kKeys;
+  const uint32_t lane = threadIdx.x & 31, boxes = kMine / a.box, first = KIND == kPair ? cluster_rank() * kMine : 0;
+  Walk<KIND == kPair> w;
   if (!w.begin(a)) return true;
   // the page of the lane's stretch of key tile j, asked for a tile ahead
   uint32_t j = w.kv0, id = 0, slot = 0, head = 0;
   bool in = false;
   auto ask = [&] {
-    const uint32_t key = j * kKeys + lane * a.box, at = key / a.kv.B;
+    const uint32_t key = j * kKeys + first + lane * a.box, at = key / a.kv.B;
     in = lane < boxes && key < w.n;
     slot = key - at * a.kv.B;
     head = w.h;
@@ -1101,30 +1138,36 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
     for (int kv = 0; kv < 2; ++kv, ++issued) {
       const uint32_t at = issued % Sh::kRing;
       if (issued >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / Sh::kRing - 1) & 1)) return false;
-      const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + lane * a.box * 128;
+      const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + (first + lane * a.box) * 128;
       if (lane == 0) mbar_expect(bar, Sh::kTile);
       __syncwarp();
       if (lane < boxes)
 #pragma unroll
-        for (int s = 0; s < NSLAB; ++s)
-          tma_load_4d(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, s0, h0, page);
+        for (int s = 0; s < NSLAB; ++s) {
+          if (KIND == kPair) tma_load_4d_both(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, s0, h0, page);
+          else tma_load_4d(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, s0, h0, page);
+        }
     }
   }
+  // a pair's CTA stays until all arrivals that the other owes it are there
+  if (KIND == kPair)
+    for (uint32_t i = issued > Sh::kRing ? issued - Sh::kRing : 0; i < issued; ++i)
+      if (!mbar_wait(smem_u32(&sh.empty[i % Sh::kRing]), (i / Sh::kRing) & 1)) return false;
   return true;
 }
 
 // The same for page sizes that are no multiple of 8 (a swizzled tile takes
 // copies of whole groups of 8 rows): 64 threads copy 16 bytes each.
-template <int NSLAB, bool FEW>
+template <int NSLAB, int KIND>
 __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, uint32_t ring) {
-  using Sh = TileShape<NSLAB, FEW>;
+  using Sh = TileShape<NSLAB, KIND>;
   const uint32_t tid = (threadIdx.x & 31) + (threadIdx.x >= 352 ? 32 : 0);
   uint32_t issued = 0, landed = 0;
   auto land = [&](uint32_t upto) {
     fence_async_shared();
     for (; landed < upto; ++landed) mbar_arrive(smem_u32(&sh.full[landed % Sh::kRing]));
   };
-  Walk w;
+  Walk<KIND == kPair> w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const uint32_t* ids = a.kv.page_ids + w.page0;
     for (uint32_t j = w.kv0; j < w.kv1; ++j)
@@ -1158,11 +1201,11 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
   return true;
 }
 
-template <typename T, int NSLAB, bool TMA, bool FEW>
+template <typename T, int NSLAB, bool TMA, int KIND>
 __global__ void __launch_bounds__(kTileThreads, 1)
     k_attn_tiles(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                  const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mq32, const AttnArgs a) {
-  using Sh = TileShape<NSLAB, FEW>;
+  using Sh = TileShape<NSLAB, KIND>;
   extern __shared__ __align__(1024) char smem_raw[];
   TileShared& sh = *reinterpret_cast<TileShared*>(smem_raw + Sh::kRest);
   const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + Sh::kQueries * Sh::kTile;
@@ -1174,7 +1217,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < Sh::kRing; ++i) {
       mbar_init(smem_u32(&sh.full[i]), TMA ? 1 : 64);
-      mbar_init(smem_u32(&sh.empty[i]), 1);
+      mbar_init(smem_u32(&sh.empty[i]), KIND == kPair ? 2 : 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sh.q_full[i]), 1);
@@ -1190,30 +1233,31 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   }
   if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
   tc_fence_before();
-  __syncthreads();
+  if (KIND == kPair) cluster_sync();  // the other CTA's barriers are there too
+  else __syncthreads();
   tc_fence_after();
   grid_dep_sync();
-  const bool go = a.plan->ok != 0;
+  const bool go = Walk<KIND == kPair>::plan(a)->ok != 0;
   bool fine = true;
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    if (go) fine = softmax_role<T, NSLAB, FEW>(a, sh, smem_raw + Sh::kRest - kStage, warp / 4);
+    if (go) fine = softmax_role<T, NSLAB, KIND>(a, sh, smem_raw + Sh::kRest - kStage, warp / 4);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     uint32_t issued = 0, loads[2] = {0, 0};
     if (!go) {
     } else if (warp == 8) {
-      fine = product_role<T, NSLAB, FEW>(a, sh, q_smem, ring);
+      fine = product_role<T, NSLAB, KIND>(a, sh, q_smem, ring);
       // every product and every arrival it owes is done before the CTA ends
       if (elect_lane()) mma_commit(smem_u32(&sh.drain));
       __syncwarp();
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
     } else if (warp == 10) {
-      fine = query_role<NSLAB, FEW>(a, sh, &mq, &mq32, q_smem, loads);
+      fine = query_role<NSLAB, KIND>(a, sh, &mq, &mq32, q_smem, loads);
     } else if (!TMA) {
-      fine = gather_role<NSLAB, FEW>(a, sh, ring);
+      fine = gather_role<NSLAB, KIND>(a, sh, ring);
     } else if (warp == 9) {
-      fine = copy_role<NSLAB, FEW>(a, sh, &mk, &mv, ring, issued);
+      fine = copy_role<NSLAB, KIND>(a, sh, &mk, &mv, ring, issued);
     }
     if (!fine) {
       // given up: let the copies in flight land
@@ -1226,7 +1270,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   }
   if (!fine) report(a.status, PTC_ERR_TIMEOUT);
   tc_fence_before();
-  __syncthreads();
+  if (KIND == kPair) cluster_sync();  // no CTA ends while the other may still write to it
+  else __syncthreads();
   tc_fence_after();
   if (warp == 8) tmem_free(sh.tmem, 512);
 }
@@ -1258,32 +1303,59 @@ bool encode(CUtensorMap* map, bool bf16, void* base, const cuuint64_t (&dims)[4]
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int NSLAB, bool TMA, bool FEW>
+template <typename T, int NSLAB, bool TMA, int KIND>
 ptc_status launch_one(const AttnArgs& a, const CUtensorMap (&m)[4], cudaStream_t s) {
-  constexpr int smem = TileShape<NSLAB, FEW>::kSmem;
+  constexpr int smem = TileShape<NSLAB, KIND>::kSmem;
   static std::atomic<uint64_t> ready{0};
-  if (!large_smem(k_attn_tiles<T, NSLAB, TMA, FEW>, smem, ready)) return PTC_ERR_CUDA;
-  PTC_KERNEL("k_attn_tiles", s, (k_attn_tiles<T, NSLAB, TMA, FEW>), a.ctas, kTileThreads, smem, m[0], m[1], m[2], m[3], a);
+  const auto kernel = k_attn_tiles<T, NSLAB, TMA, KIND>;
+  if (!large_smem(kernel, smem, ready)) return PTC_ERR_CUDA;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = KIND == kPair ? a.ctas / 2 * 2 : a.ctas;
+  cfg.blockDim = kTileThreads;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = KIND == kPair ? 2 : 1;
+  PTC_LAUNCH("k_attn_tiles", s, (void)cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], a));
   return PTC_OK;
 }
 template <typename T, int NSLAB>
 ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], bool tma, cudaStream_t s) {
-  if (a.max_q_len <= a.tq32) return tma ? launch_one<T, NSLAB, true, true>(a, m, s) : launch_one<T, NSLAB, false, true>(a, m, s);
-  return tma ? launch_one<T, NSLAB, true, false>(a, m, s) : launch_one<T, NSLAB, false, false>(a, m, s);
+  if (a.max_q_len <= a.tq32) return tma ? launch_one<T, NSLAB, true, kFew>(a, m, s) : launch_one<T, NSLAB, false, kFew>(a, m, s);
+  if (a.pair_min != UINT32_MAX) {
+    const ptc_status st = launch_one<T, NSLAB, true, kPair>(a, m, s);
+    if (st != PTC_OK || a.kv.n_req == 1) return st;  // one request has all n_tok tokens
+  }
+  return tma ? launch_one<T, NSLAB, true, kAny>(a, m, s) : launch_one<T, NSLAB, false, kAny>(a, m, s);
 }
+
+// Requests of more new tokens are pairs' work.
+uint32_t pair_tokens(const AttnArgs& a) { return kPairTiles * 2 * a.tq; }
 
 template <typename T>
 ptc_status launch(AttnArgs& a, cudaStream_t s) {
   constexpr bool bf16 = Weights<T>::kBf16;
   const bool by_tiles = a.mass_out && !a.scores && a.n_tok;  // the weights' own tiles
-  PTC_KERNEL("k_attn_plan", s, k_attn_plan, dim3(a.ctas / 32 + 1, by_tiles ? 2 : 1), kPlanThreads, 0, a);
+  // copies of whole groups of 8 rows that neither leave a page nor a tile (a pair: half a tile)
+  const bool some_long = a.max_q_len > pair_tokens(a) && a.n_tok > pair_tokens(a);
+  a.box = some_long ? kKeys / 2 : kKeys;
+  while (a.kv.B % a.box) a.box /= 2;
+  const bool tma = a.n_tok && a.box >= 8 && a.kv.n_pages > 0;
+  a.pair_min = some_long && tma && a.ctas >= 2 ? pair_tokens(a) : UINT32_MAX;
+  uint3 which = {0, 0, 0};
+  uint32_t plans = 1;
+  if (by_tiles) (&which.x)[plans++] = 1;
+  if (a.pair_min != UINT32_MAX) (&which.x)[plans++] = 2;
+  PTC_KERNEL("k_attn_plan", s, k_attn_plan, dim3(a.ctas / 32 + 1, plans), kPlanThreads, 0, a, which);
   CUtensorMap m[4] = {};
-  bool tma = false;
   if (a.n_tok) {
-    // copies of whole groups of 8 rows that neither leave a page nor a tile
-    a.box = 128;
-    while (a.kv.B % a.box) a.box /= 2;
-    tma = a.box >= 8 && a.kv.n_pages > 0;
     if (tma && (!cache_map(&m[0], a.kv, bf16, a.kv.k, a.kv.ks_page, a.kv.ks_head, a.kv.ks_slot, a.box) ||
                 !cache_map(&m[1], a.kv, bf16, a.kv.v, a.kv.vs_page, a.kv.vs_head, a.kv.vs_slot, a.box)))
       return PTC_ERR_CUDA;
@@ -1302,8 +1374,8 @@ AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D, uint64_t scores) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   AttnWs w;
   w.plan = kKvStatusBytes;
-  w.units = w.plan + up(2 * sizeof(AttnPlan));
-  w.ml = w.units + up(2 * (size_t)(n_req + 1) * 8);
+  w.units = w.plan + up(3 * sizeof(AttnPlan));
+  w.ml = w.units + up(3 * (size_t)(n_req + 1) * 8);
   w.part = w.ml + up((size_t)2 * ctas * kRows * 8);
   w.mass = w.part + up((size_t)2 * ctas * kRows * D * 4);
   w.scores = w.mass + up((size_t)2 * ctas * kMassKeys * 4);

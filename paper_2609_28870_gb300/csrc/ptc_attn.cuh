@@ -45,14 +45,15 @@ struct AttnArgs {
   uint64_t n_tok;
   uint32_t n_q_heads, G, max_q_len;
   uint32_t tq, tq32;   // whole tokens in 128 and in 32 rows
+  uint32_t pair_min;   // requests of more new tokens are pairs of CTAs' (see k_attn_tiles)
   float scale;
   char* out;
   float* lse;
   const float* mass_in;
   float* mass_out;
   uint64_t mass_stride;
-  AttnPlan* plan;      // [0] tiles, [1] weights
-  uint64_t* unit_off;  // [0] and [1]: n_req + 1
+  AttnPlan* plan;      // [0] tiles, [1] weights, [2] tiles of pairs
+  uint64_t* unit_off;  // three times n_req + 1
   float* part;         // unnormalised rows of split tiles: [2 * ctas][kRows][D]
   float2* part_ml;     // their maxima (in powers of two) and sums
   float* part_mass;    // weights of split key tiles: [2 * ctas][kMassKeys]
@@ -94,16 +95,16 @@ __device__ __forceinline__ Sharers sharers(const AttnPlan* plan, uint32_t ctas, 
 
 __host__ __device__ __forceinline__ uint32_t div_up(uint32_t a, uint32_t b) { return (a + b - 1) / b; }
 
-// Query tiles of a request, and the key tiles that one of them sees, at least one.
-__device__ __forceinline__ uint32_t query_tiles(uint32_t m, uint32_t tq) { return div_up(m, 2 * tq); }
-__device__ __forceinline__ uint32_t key_tiles(uint32_t m, uint32_t n, uint32_t tq, uint32_t qt) {
-  const uint32_t end = (qt + 1) * 2 * tq < m ? (qt + 1) * 2 * tq : m;
+// Query tiles of `span` tokens of a request, and the key tiles that one of them
+// sees, at least one.
+__device__ __forceinline__ uint32_t key_tiles(uint32_t m, uint32_t n, uint32_t span, uint32_t qt) {
+  const uint32_t end = (qt + 1) * span < m ? (qt + 1) * span : m;
   const int64_t sees = (int64_t)n - m + end;
   return sees <= (int64_t)kKeys ? 1u : (uint32_t)((sees + kKeys - 1) / kKeys);
 }
 // What query tile qt costs by itself.
-__device__ __forceinline__ uint32_t tile_extra(uint32_t m, uint32_t tq, uint32_t tq32, uint32_t qt) {
-  return m - qt * 2 * tq <= tq32 ? kFewExtra : kTileExtra;
+__device__ __forceinline__ uint32_t tile_extra(uint32_t m, uint32_t span, uint32_t tq32, uint32_t qt) {
+  return m - qt * span <= tq32 ? kFewExtra : kTileExtra;
 }
 // The first half tile of queries that sees anything of the weights' key tile kt.
 __device__ __forceinline__ uint32_t first_seeing(uint32_t m, uint32_t n, uint32_t tq, uint32_t kt) {
