@@ -292,9 +292,10 @@ struct Weights<__half> {
 
 // ------------------------------------------------------------------ the tile kernel
 // One CTA an SM walks its units.  Warps 0-3 and 4-7 are the two halves of the
-// softmax, warp 8 issues the products, warp 9 loads keys and values into a
-// ring of tiles (with warp 11 where there are no tensor copies), warp 10 loads
-// the queries of the next tile.  For key tile j:
+// softmax, warp 8 issues the products, warp 9 loads keys and warp 11 values into
+// a ring of tiles, warp 10 loads the queries of the next tile.  (Pages of 16 are 16
+// copies a tile: one warp for both took 179 us for 64 single tokens, two 158;
+// 1.31 and 1.22 ms for 4,096 tokens at 32K, without pairs.)  For key tile j:
 //   scores   S = Q K_j^T     128 x 128 sums in tensor memory
 //   softmax  one thread a row: running maximum and sum in 32 bits; weights
 //            exp2(s - max), rounded to 16 bits, over the scores' columns
@@ -342,15 +343,20 @@ struct TileShared {
 //          kColumnsApart.  There is no second half of queries then, and the
 //          ring has its place: 5 tiles of 32 KB keep more of the cache in
 //          flight than 4.
-//   kPair  pairs of CTAs, clusters of two, for requests of at least four query
-//          tiles: the two take neighbouring query tiles through the same key
-//          tiles, and each loads half of every tile into both's shared memory.
-//          A CTA by itself draws 64 KB a unit out of L2, 7.0 TB/s over the
-//          GPU, which is all that comes out of it: without any softmax and an
-//          eighth of the products, 4,096 tokens at 32K still took 1.15 of
-//          1.33 ms.
+//   kPair  pairs of CTAs, clusters of two, for long requests: the two take
+//          neighbouring query tiles through the same key tiles, and each loads
+//          half of every tile into both's shared memory, so that 32 KB a unit
+//          leave L2 and not 64.
 enum { kAny = 0, kFew = 1, kPair = 2 };
-constexpr uint32_t kPairTiles = 4;
+// Requests of more than kPairTiles query tiles are pairs' work, in calls whose
+// requests have kPairMean or more on average: 16 requests of 1,024 tokens over
+// 4,000 take 702 us without and 654 with pairs, 4,096 tokens at 32K 1.22 and 1.18 ms.
+// Rows that a pair's last tile lacks cost as much as others, and the requests
+// that are left to the second kernel have the GPU's ends to themselves: 40
+// requests of 100 to 300 tokens took 76 us without and 92 us with pairs.  Up to
+// 64 columns the copies are half of that beside the same softmax: 389 us either
+// way for 2,048 tokens at 20K.
+constexpr uint32_t kPairTiles = 4, kPairMean = 8;
 template <int NSLAB, int KIND>
 struct TileShape {
   static constexpr int kTile = NSLAB * kSlabBytes;
@@ -1100,13 +1106,20 @@ __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, co
   return true;
 }
 
-// Keys and values by tensor copies: a copy a stretch of `box` slots (a divisor
+// The copies of keys (or values) that may still be in flight or unused, of those issued.
+template <uint32_t RING>
+__device__ __forceinline__ uint32_t first_open(uint32_t issued) {
+  constexpr uint32_t kOpen = (RING + 1) / 2;
+  return issued > kOpen ? issued - kOpen : 0;
+}
+
+// Keys and values by tensor copies, a warp for each: a copy a stretch of `box` slots (a divisor
 // of the page size and of the tile) and slab.  Stretches at or past the
 // request's end and pages that the cache does not have read as zeros: their
 // page coordinate is n_pages, which is out of range.
 template <int NSLAB, int KIND>
-__device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* mk, const CUtensorMap* mv,
-                                          uint32_t ring, uint32_t& issued) {
+__device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* map,
+                                          uint32_t ring, uint32_t kv, uint32_t& issued) {
   using Sh = TileShape<NSLAB, KIND>;
   // a pair's CTA loads its half of a tile, into both
   constexpr uint32_t kMine = KIND == kPair ? kKeys / 2 : kKeys;
@@ -1134,25 +1147,27 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
       j = w.kv0;
     }
     if (more) ask();
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv, ++issued) {
-      const uint32_t at = issued % Sh::kRing;
-      if (issued >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / Sh::kRing - 1) & 1)) return false;
-      const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + (first + lane * a.box) * 128;
-      if (lane == 0) mbar_expect(bar, Sh::kTile);
-      __syncwarp();
-      if (lane < boxes)
-#pragma unroll
-        for (int s = 0; s < NSLAB; ++s) {
-          if (KIND == kPair) tma_load_4d_both(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, s0, h0, page);
-          else tma_load_4d(dst + s * kSlabBytes, kv == 0 ? mk : mv, bar, 64 * s, s0, h0, page);
-        }
+    const uint32_t item = 2 * issued++ + kv, at = item % Sh::kRing;
+    if (item >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (item / Sh::kRing - 1) & 1)) {
+      --issued;
+      return false;
     }
+    const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + (first + lane * a.box) * 128;
+    if (lane == 0) mbar_expect(bar, Sh::kTile);
+    __syncwarp();
+    if (lane < boxes)
+#pragma unroll
+      for (int s = 0; s < NSLAB; ++s) {
+        if (KIND == kPair) tma_load_4d_both(dst + s * kSlabBytes, map, bar, 64 * s, s0, h0, page);
+        else tma_load_4d(dst + s * kSlabBytes, map, bar, 64 * s, s0, h0, page);
+      }
   }
   // a pair's CTA stays until all arrivals that the other owes it are there
   if (KIND == kPair)
-    for (uint32_t i = issued > Sh::kRing ? issued - Sh::kRing : 0; i < issued; ++i)
-      if (!mbar_wait(smem_u32(&sh.empty[i % Sh::kRing]), (i / Sh::kRing) & 1)) return false;
+    for (uint32_t i = first_open<Sh::kRing>(issued); i < issued; ++i) {
+      const uint32_t item = 2 * i + kv;
+      if (!mbar_wait(smem_u32(&sh.empty[item % Sh::kRing]), (item / Sh::kRing) & 1)) return false;
+    }
   return true;
 }
 
@@ -1256,13 +1271,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
       fine = query_role<NSLAB, KIND>(a, sh, &mq, &mq32, q_smem, loads);
     } else if (!TMA) {
       fine = gather_role<NSLAB, KIND>(a, sh, ring);
-    } else if (warp == 9) {
-      fine = copy_role<NSLAB, KIND>(a, sh, &mk, &mv, ring, issued);
+    } else {
+      fine = copy_role<NSLAB, KIND>(a, sh, warp == 9 ? &mk : &mv, ring, warp == 9 ? 0 : 1, issued);
     }
     if (!fine) {
       // given up: let the copies in flight land
-      for (uint32_t i = issued > Sh::kRing ? issued - Sh::kRing : 0; i < issued; ++i)
-        (void)mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1);
+      for (uint32_t i = first_open<Sh::kRing>(issued); i < issued; ++i) {
+        const uint32_t item = 2 * i + (warp == 9 ? 0 : 1);
+        (void)mbar_wait(smem_u32(&sh.full[item % Sh::kRing]), (item / Sh::kRing) & 1);
+      }
       for (int s = 0; s < 2; ++s)
         if (loads[s]) (void)mbar_wait(smem_u32(&sh.q_full[s]), (loads[s] - 1) & 1);
       if (!TMA) cp_async_wait<0>();
@@ -1329,8 +1346,8 @@ ptc_status launch_one(const AttnArgs& a, const CUtensorMap (&m)[4], cudaStream_t
 template <typename T, int NSLAB>
 ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], bool tma, cudaStream_t s) {
   if (a.max_q_len <= a.tq32) return tma ? launch_one<T, NSLAB, true, kFew>(a, m, s) : launch_one<T, NSLAB, false, kFew>(a, m, s);
-  if (a.pair_min != UINT32_MAX) {
-    const ptc_status st = launch_one<T, NSLAB, true, kPair>(a, m, s);
+  if (NSLAB == 2 && a.pair_min != UINT32_MAX) {
+    const ptc_status st = launch_one<T, 2, true, kPair>(a, m, s);
     if (st != PTC_OK || a.kv.n_req == 1) return st;  // one request has all n_tok tokens
   }
   return tma ? launch_one<T, NSLAB, true, kAny>(a, m, s) : launch_one<T, NSLAB, false, kAny>(a, m, s);
@@ -1339,12 +1356,16 @@ ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], bool tma, 
 // Requests of more new tokens are pairs' work.
 uint32_t pair_tokens(const AttnArgs& a) { return kPairTiles * 2 * a.tq; }
 
+bool pairs_pay(const AttnArgs& a) {
+  return a.kv.D > 64 && a.max_q_len > pair_tokens(a) && a.n_tok >= (uint64_t)kPairMean * 2 * a.tq * a.kv.n_req;
+}
+
 template <typename T>
 ptc_status launch(AttnArgs& a, cudaStream_t s) {
   constexpr bool bf16 = Weights<T>::kBf16;
   const bool by_tiles = a.mass_out && !a.scores && a.n_tok;  // the weights' own tiles
   // copies of whole groups of 8 rows that neither leave a page nor a tile (a pair: half a tile)
-  const bool some_long = a.max_q_len > pair_tokens(a) && a.n_tok > pair_tokens(a);
+  const bool some_long = pairs_pay(a);
   a.box = some_long ? kKeys / 2 : kKeys;
   while (a.kv.B % a.box) a.box /= 2;
   const bool tma = a.n_tok && a.box >= 8 && a.kv.n_pages > 0;
