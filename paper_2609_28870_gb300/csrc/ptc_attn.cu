@@ -317,12 +317,12 @@ struct Weights<__half> {
 // hardly happens (2.02 -> 1.38 ms for 4,096 tokens at 32K, with the products'
 // descriptors made outside the issuing lane).
 //
-// Bounds.  Single tokens: HBM; 12 contexts of 32K to 131K, 1.81 GB, take 277 us,
-// 6.5 TB/s.  Chunks: a unit of 256 rows and 128 keys is 2,048 cycles of products
-// at D = 128.  It takes 3,030 (4,096 tokens at 32K: 1.32 ms, 1.56 PFLOP/s, the
-// tensor pipe 68% active): the products read 192 KB of shared memory and the
-// copies write 64, 2,048 cycles at 128 bytes a cycle too, and a half's own
-// chain (softmax 1,260, its two products 1,024, four hand-overs) is 2,600.
+// Bounds.  Single tokens: HBM; 12 contexts of 32K to 131K, 1.81 GB, take 275 us,
+// 6.6 TB/s.  Chunks: the tensor cores; a unit of 256 rows and 128 keys is 2,048
+// cycles of products at D = 128 and takes 2,700 (4,096 tokens at 32K: 1.18 ms,
+// 1.75 PFLOP/s, the tensor pipe 75% active).  A half's own chain (softmax 1,260,
+// its two products 1,024, four hand-overs) is 2,600, and what the products and
+// copies move through shared memory, 256 KB, 2,048 cycles at 128 bytes a cycle.
 enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
 constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns

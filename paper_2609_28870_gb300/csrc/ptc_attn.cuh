@@ -66,8 +66,9 @@ struct AttnArgs {
 // Units that a tile costs by itself (the softmax's first steps, the sums' way
 // out).  A step of mixed chunks took 549, 494, 489 and 500 us with 1, 2, 3 and 5
 // for every tile, 64 single tokens 179, 182, 185 and 191 us: a tile of few rows
-// costs one key tile, any other three.  A key tile's sum of weights costs about
-// one query tile.
+// costs one key tile, any other three.  (A key tile counts the same under a short
+// query tile: counted as half of one, the mixed chunks took 524 us, not 468.)  A
+// key tile's sum of weights costs about one query tile.
 constexpr uint32_t kTileExtra = 3, kFewExtra = 1, kMassExtra = 1;
 // Fewest key tiles of a part.  A part of up to 256 rows costs their sums' way
 // through memory (6 us for two parts of 256 rows); one of few rows hardly any.

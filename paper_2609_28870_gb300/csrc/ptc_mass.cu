@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
 // KB, its queries are 32 KB, the lse 32 KB (at D = 128), 1,540 cycles for 1,024
 // of products and as many of exponentials.  (With 128 keys a unit the queries'
 // stream out of L2, 7.4 TB/s, was the bound.)  A unit takes 2,270 cycles: 4
-// chunks of 300 to 2,048 tokens over up to 8K, 205 us beside 310 for the
+// chunks of 300 to 2,048 tokens over up to 8K, 212 us beside 296 for the
 // attention itself.
 constexpr int kMassThreads = 640;
 constexpr int kSlab = 128 * 128;
