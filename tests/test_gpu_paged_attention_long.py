@@ -103,3 +103,83 @@ def test_captured_and_replayed():
         close(out, want[0], want[3])
         close(lse, want[1], want[4])
     ptc.check_status(status, "attention")
+
+
+# From here on the requests have at least eight query tiles (of 256 rows) on
+# average and more than 64 columns, without which no pair is formed.
+
+
+@pytest.mark.parametrize("m", [1, 63, 64, 65, 127, 128, 129, 191, 192, 193])
+def test_ends_of_a_pairs_last_tile(m):
+    """Four heads a group: a pair's tile is 128 tokens."""
+    check([(1024 + m, 1024 + m)], Hq=4, Hkv=1, D=128)
+    check([(512 + m, 512 + m + 1000)], Hq=8, Hkv=2, D=96, dtype="fp16")
+
+
+@pytest.mark.parametrize("group,m", [(1, 2100), (2, 1100), (3, 700), (5, 450), (7, 300), (16, 140), (31, 70), (64, 37),
+                                     (100, 20), (128, 17), (128, 40)])
+def test_pairs_by_head_groups(group, m):
+    check([(m, m + 300), (m + 1, m + 1)], Hq=2 * group, Hkv=2, D=128)
+
+
+@pytest.mark.parametrize("lens", [
+    [(1500, 1500), (1, 500), (255, 300), (256, 256), (257, 900), (1100, 1101)],
+    [(0, 0), (1400, 3000), (0, 10), (200, 200)],
+    [(1, 1000), (2000, 2000), (3, 4)],
+    [(1300, 100), (900, 0), (700, 701), (60, 400)],
+    [(600, 600)] * 7,
+])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_pairs_beside_other_requests(lens, dtype):
+    """Requests of up to four query tiles, empty ones and rows that see no key."""
+    check(lens, Hq=8, Hkv=2, D=128, dtype=dtype)
+
+
+@pytest.mark.parametrize("B", [8, 16, 24, 32, 40, 48, 64, 96, 128, 192, 256, 512])
+@pytest.mark.parametrize("layout", ["head", "token"])
+def test_pairs_by_page_sizes(B, layout):
+    check([(700, 1777), (520, 520)], Hq=4, Hkv=1, D=128, B=B, layout=layout)
+
+
+@pytest.mark.parametrize("B", [7, 12, 100])
+def test_pages_without_tensor_copies(B):
+    check([(700, 1777)], Hq=4, Hkv=1, D=128, B=B)
+
+
+@pytest.mark.parametrize("D", [72, 80, 104, 120])
+def test_pairs_by_widths(D):
+    check([(600, 1000), (520, 4000)], Hq=4, Hkv=1, D=D)
+
+
+def test_pairs_over_many_requests():
+    """More requests than the plan keeps in shared memory, all of them pairs';
+    every 37th and the last are compared."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv_util import Cache, close, reference
+    c = Cache([(17 + r % 5, 20 + r % 40) for r in range(1200)], Hq=128, Hkv=1, D=72)
+    out, lse = ptc.ptc_paged_attention(c.q, *c.table(), c.tok_off, c.kv_len, 21)
+    assert torch.isfinite(out).all() and not torch.isnan(lse).any()
+    some = [r for r in range(1200) if r % 37 == 0 or r == 1199]
+    c.lens = [x if r in some else (0, 0) for r, x in enumerate(c.lens)]
+    want = reference(c)
+    rows = torch.cat([torch.arange(int(c.tok_off[r]), int(c.tok_off[r + 1])) for r in some]).cuda()
+    close(out[rows], want[0][rows], want[3][rows])
+    close(lse[rows], want[1][rows], want[4][rows])
+
+
+def test_pairs_with_pages_that_the_cache_does_not_have():
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv_util import Cache
+    c = Cache([(600, 900)], Hq=4, Hkv=1, D=128)
+    ids = c.page_ids.clone()
+    ids[3] = c.n_pages
+    with pytest.raises(ptc.PtcError):
+        ptc.ptc_paged_attention(c.q, c.k, c.v, ids, c.page_off, c.tok_off, c.kv_len, 600)
+    short = c.tok_off.clone()
+    short[0] = 1
+    with pytest.raises(ptc.PtcError):
+        ptc.ptc_paged_attention(c.q, *c.table()[:2], c.page_ids, c.page_off, short, c.kv_len, 600)
+    out, _ = ptc.ptc_paged_attention(c.q, *c.table(), c.tok_off, c.kv_len, 600)
+    assert torch.isfinite(out).all()
