@@ -16,27 +16,24 @@ __device__ __forceinline__ uint32_t unit_search(const uint64_t* off, uint32_t lo
   return lo;
 }
 
-// The requests' share of the units, and every CTA's (or pair's) start, for the
-// plan that blockIdx.y has in `which`.  The time of a call
-// of few units is a chain of latencies: what the lists hold is read once and
-// kept in shared memory (the first kPlanThreads requests of it), and the CTAs
-// here add it up each for itself and find 32 starts each, one a warp (one CTA
-// for all starts took 10 us, of which 8 were spent on them).
+// The requests' share of the units, and every CTA's start, for the tiles
+// (blockIdx.y = 0) or the weights (1).  The time of a call of few units is a
+// chain of latencies: what the lists hold is read once and kept in shared
+// memory (the first kPlanThreads requests of it), and the CTAs here add it up
+// each for itself and find 32 starts each, one a warp (one CTA for all starts
+// took 10 us, of which 8 were spent on them).
 constexpr int kPlanThreads = 1024;
-__global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a, uint3 which) {
+__global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
   asm volatile("griddepcontrol.launch_dependents;");
   grid_dep_sync();
   __shared__ uint64_t s_warp[32], s_off[kPlanThreads + 1];
   __shared__ uint32_t s_m[kPlanThreads], s_n[kPlanThreads];
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, R = a.kv.n_req, tq = a.tq;
-  const uint32_t kind = blockIdx.y == 0 ? which.x : blockIdx.y == 1 ? which.y : which.z;
-  const bool weights = kind == 1;
-  const uint32_t span = kind == 2 ? 4 * tq : 2 * tq, ctas = kind == 2 ? a.ctas / 2 : a.ctas;
+  const bool weights = blockIdx.y == 1;
+  const uint32_t span = 2 * tq, ctas = a.ctas;
   auto extra_of = [&](uint32_t m, uint32_t i) { return weights ? kMassExtra : tile_extra(m, span, a.tq32, i); };
-  AttnPlan* plan = a.plan + kind;
-  uint64_t* unit_off = a.unit_off + (uint64_t)kind * (R + 1);
-  // new tokens of a request, as far as they are this plan's
-  auto mine_of = [&](uint32_t m) { return weights || (m > a.pair_min) == (kind == 2) ? m : 0u; };
+  AttnPlan* plan = a.plan + blockIdx.y;
+  uint64_t* unit_off = a.unit_off + (uint64_t)blockIdx.y * (R + 1);
   // a request's first-level tiles, and the units of one of them
   auto tiles_of = [&](uint32_t m, uint32_t n) { return weights ? (m ? div_up(n, kMassKeys) : 0u) : div_up(m, span); };
   auto units_of = [&](uint32_t m, uint32_t n, uint32_t i) {
@@ -54,7 +51,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a, uint3 wh
       const bool hold = pages_hold(a.kv, r, n);
       const bool wrong = (lo > hi) | (hi > a.n_tok) | (hi - lo > a.max_q_len) | !hold;
       bad |= wrong;
-      m = wrong ? 0 : mine_of((uint32_t)(hi - lo));
+      m = wrong ? 0 : (uint32_t)(hi - lo);
     }
     const uint32_t tiles = tiles_of(m, n);
     uint64_t mine = 0;
@@ -132,7 +129,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a, uint3 wh
         to = s_off[lo + 1];
       } else {
         s.r = unit_search(unit_off, 0, R - 1, s.u);
-        m = mine_of((uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]));
+        m = (uint32_t)(a.tok_off[s.r + 1] - a.tok_off[s.r]);
         n = a.kv.kv_len[s.r];
         from = ld_relaxed_u64(unit_off + s.r);
         to = ld_relaxed_u64(unit_off + s.r + 1);
@@ -179,13 +176,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a, uint3 wh
   }
 }
 
-// The query tiles that a CTA has a part in, in order, with the part.  PAIR: of
-// a pair of CTAs, whose tiles are twice as long: the first half is the first
-// CTA's, the second the second's.
-template <bool PAIR>
+// The query tiles that a CTA has a part in, in order, with the part.
 struct Walk {
-  static constexpr uint32_t kSpan = PAIR ? 4 : 2;  // in tq tokens
-
   uint64_t left, u, tok0, page0;     // units left, the part's first unit
   uint32_t r, h, qt, kv0, kv1, nkv;  // key tiles [kv0, kv1) of nkv
   uint32_t extra;                    // units before the first key tile
@@ -194,20 +186,19 @@ struct Walk {
   __device__ __forceinline__ void request(const AttnArgs& a) {
     tok0 = a.tok_off[r];
     m = (uint32_t)(a.tok_off[r + 1] - tok0);
-    if ((m > a.pair_min) != PAIR) m = 0;  // the other kernel's
     n = a.kv.kv_len[r];
     page0 = a.kv.page_off[r];
   }
-  __device__ __forceinline__ uint32_t cost(const AttnArgs& a) const { return tile_extra(m, kSpan * a.tq, a.tq32, qt); }
+  __device__ __forceinline__ uint32_t cost(const AttnArgs& a) const { return tile_extra(m, 2 * a.tq, a.tq32, qt); }
   __device__ __forceinline__ void part(const AttnArgs& a) {
-    nkv = key_tiles(m, n, kSpan * a.tq, qt);
+    nkv = key_tiles(m, n, 2 * a.tq, qt);
     extra = kv0 ? 0 : cost(a);
     kv1 = nkv - kv0 + extra > left ? kv0 + (uint32_t)left - extra : nkv;
   }
   // The next query tile.
   __device__ __forceinline__ bool step(const AttnArgs& a) {
     kv0 = 0;
-    if (++qt * kSpan * a.tq >= m) {
+    if (++qt * 2 * a.tq >= m) {
       qt = 0;
       if (++h == a.kv.H) {
         h = 0;
@@ -221,7 +212,7 @@ struct Walk {
   }
   // False if the CTA has nothing to do.
   __device__ __forceinline__ bool begin(const AttnArgs& a) {
-    const CtaStart* start = plan(a)->start + (PAIR ? blockIdx.x / 2 : blockIdx.x);
+    const CtaStart* start = a.plan->start + blockIdx.x;
     const CtaStart s = start[0];
     left = start[1].u - s.u;
     if (left == 0) return false;
@@ -235,7 +226,7 @@ struct Walk {
     m = s.m;
     n = s.n;
     page0 = s.page0;
-    if (kv0 && kv0 == key_tiles(m, n, kSpan * a.tq, qt) && !step(a)) return false;
+    if (kv0 && kv0 == key_tiles(m, n, 2 * a.tq, qt) && !step(a)) return false;
     part(a);
     return true;
   }
@@ -248,18 +239,14 @@ struct Walk {
     part(a);
     return true;
   }
-  static __device__ __forceinline__ AttnPlan* plan(const AttnArgs& a) { return a.plan + (PAIR ? 2 : 0); }
-  // The first token of this CTA's rows (of a pair's second CTA it may lie past the request).
-  __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const {
-    return (qt * kSpan + (PAIR ? 2 * (blockIdx.x & 1) : 0)) * a.tq;
-  }
+  // The tile's first token.
+  __device__ __forceinline__ uint32_t token0(const AttnArgs& a) const { return qt * 2 * a.tq; }
   // The units of the whole tile.
   __device__ __forceinline__ uint64_t from(const AttnArgs& a) const { return kv0 ? u - kv0 - cost(a) : u; }
   __device__ __forceinline__ uint64_t to(const AttnArgs& a) const { return from(a) + cost(a) + nkv; }
   // How the two halves of the softmax share the tile.
   __device__ __forceinline__ int mode(const AttnArgs& a) const {
-    if (PAIR) return 0;
-    const uint32_t tokens = m - qt * 2 * a.tq;
+    const uint32_t tokens = m - token0(a);
     return tokens > a.tq ? 0 : tokens > a.tq32 ? 1 : 2;
   }
 };
@@ -295,7 +282,7 @@ struct Weights<__half> {
 // softmax, warp 8 issues the products, warp 9 loads keys and warp 11 values into
 // a ring of tiles, warp 10 loads the queries of the next tile.  (Pages of 16 are 16
 // copies a tile: one warp for both took 179 us for 64 single tokens, two 158;
-// 1.31 and 1.22 ms for 4,096 tokens at 32K, without pairs.)  For key tile j:
+// 1.31 and 1.23 ms for 4,096 tokens at 32K.)  For key tile j:
 //   scores   S = Q K_j^T     128 x 128 sums in tensor memory
 //   softmax  one thread a row: running maximum and sum in 32 bits; weights
 //            exp2(s - max), rounded to 16 bits, over the scores' columns
@@ -319,8 +306,8 @@ struct Weights<__half> {
 //
 // Bounds.  Single tokens: HBM; 12 contexts of 32K to 131K, 1.81 GB, take 275 us,
 // 6.6 TB/s.  Chunks: the tensor cores; a unit of 256 rows and 128 keys is 2,048
-// cycles of products at D = 128 and takes 2,700 (4,096 tokens at 32K: 1.18 ms,
-// 1.75 PFLOP/s, the tensor pipe 75% active).  A half's own chain (softmax 1,260,
+// cycles of products at D = 128 and takes 2,800 (4,096 tokens at 32K: 1.23 ms,
+// 1.67 PFLOP/s).  A half's own chain (softmax 1,260,
 // its two products 1,024, four hand-overs) is 2,600, and what the products and
 // copies move through shared memory, 256 KB, 2,048 cycles at 128 bytes a cycle.
 enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
@@ -343,20 +330,7 @@ struct TileShared {
 //          kColumnsApart.  There is no second half of queries then, and the
 //          ring has its place: 5 tiles of 32 KB keep more of the cache in
 //          flight than 4.
-//   kPair  pairs of CTAs, clusters of two, for long requests: the two take
-//          neighbouring query tiles through the same key tiles, and each loads
-//          half of every tile into both's shared memory, so that 32 KB a unit
-//          leave L2 and not 64.
-enum { kAny = 0, kFew = 1, kPair = 2 };
-// Requests of more than kPairTiles query tiles are pairs' work, in calls whose
-// requests have kPairMean or more on average: 16 requests of 1,024 tokens over
-// 4,000 take 702 us without and 654 with pairs, 4,096 tokens at 32K 1.22 and 1.18 ms.
-// Rows that a pair's last tile lacks cost as much as others, and the requests
-// that are left to the second kernel have the GPU's ends to themselves: 40
-// requests of 100 to 300 tokens took 76 us without and 92 us with pairs.  Up to
-// 64 columns the copies are half of that beside the same softmax: 389 us either
-// way for 2,048 tokens at 20K.
-constexpr uint32_t kPairTiles = 4, kPairMean = 8;
+enum { kAny = 0, kFew = 1 };
 template <int NSLAB, int KIND>
 struct TileShape {
   static constexpr int kTile = NSLAB * kSlabBytes;
@@ -480,11 +454,10 @@ __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl2, float 
 constexpr float kMove = 256.f;
 
 // Who has a part of the tile, and where; by one warp.
-template <bool PAIR>
 __device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, uint64_t from, uint64_t to) {
-  const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x & 1;
-  const AttnPlan* plan = Walk<PAIR>::plan(a);
-  const Sharers s = sharers(plan, PAIR ? a.ctas / 2 : a.ctas, from, to);
+  const uint32_t lane = threadIdx.x & 31;
+  const AttnPlan* plan = a.plan;
+  const Sharers s = sharers(plan, a.ctas, from, to);
   uint32_t n = 0;
   for (uint32_t x0 = s.c0; x0 <= s.c1; x0 += 32) {
     const uint32_t x = x0 + lane;
@@ -492,11 +465,11 @@ __device__ __noinline__ void list_sharers(const AttnArgs& a, TileShared& sh, uin
     const uint32_t has = __ballot_sync(kFull, v > u);
     // a CTA's first part, or (of the tile's first CTA, where it began with another tile) its last
     if (v > u) sh.slots[n + __popc(has & ((1u << lane) - 1))] =
-          (uint16_t)(2 * (PAIR ? 2 * x + rank : x) + (u < from ? 1 : 0));
+          (uint16_t)(2 * x + (u < from ? 1 : 0));
     n += __popc(has);
   }
   if (lane == 0) {
-    sh.c0 = PAIR ? 2 * s.c0 + rank : s.c0;
+    sh.c0 = s.c0;
     sh.count = s.count;
   }
   __syncwarp();
@@ -596,7 +569,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
   char* stage = stages + (half * 4 + warp) * 4096;
   bool alive = true;  // a warp that has given up waiting runs on without, for the others at the barriers
   uint32_t done = 0, parted = 0;  // key tiles of this half so far, and those in two parts
-  Walk<KIND == kPair> w;
+  Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     // the thread's row: a token of the request and a head of the group
@@ -611,7 +584,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     RowState st;
     st.clear();
     const bool whole = w.kv0 == 0 && w.kv1 == w.nkv;
-    if (!whole && threadIdx.x < 32) list_sharers<KIND == kPair>(a, sh, w.from(a), w.to(a));
+    if (!whole && threadIdx.x < 32) list_sharers(a, sh, w.from(a), w.to(a));
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
         if (alive) alive = mbar_wait(bar_s, done & 1);
@@ -879,7 +852,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
       __threadfence();
       softmax_sync();
       if (threadIdx.x == 0) {
-        sh.last = atomicAdd(&Walk<KIND == kPair>::plan(a)->arrived[sh.c0], 1u) + 1 == sh.count;
+        sh.last = atomicAdd(&a.plan->arrived[sh.c0], 1u) + 1 == sh.count;
         __threadfence();
       }
       softmax_sync();
@@ -907,11 +880,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   auto commit = [&](uint64_t& bar) {
     if (elect_lane()) mma_commit(smem_u32(&bar));
   };
-  // a ring tile is free when both CTAs of a pair are done with it
-  auto release = [&](uint32_t at) {
-    if (KIND == kPair) mma_commit_both(smem_u32(&sh.empty[at]));
-    else mma_commit(smem_u32(&sh.empty[at]));
-  };
+  auto release = [&](uint32_t at) { mma_commit(smem_u32(&sh.empty[at])); };
   auto free_tile = [&](uint32_t i) {
     if (elect_lane()) release(i % Sh::kRing);
   };
@@ -993,7 +962,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
     }
     return true;
   };
-  Walk<KIND == kPair> w;
+  Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     const uint32_t L = w.kv1 - w.kv0;
@@ -1082,7 +1051,7 @@ __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, co
                                            const CUtensorMap* mq32, uint32_t q_smem, uint32_t (&loads)[2]) {
   using Sh = TileShape<NSLAB, KIND>;
   const uint32_t lane = threadIdx.x & 31;
-  Walk<KIND == kPair> w;
+  Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     const int tok = (int)(w.tok0 + w.token0(a));
@@ -1121,16 +1090,14 @@ template <int NSLAB, int KIND>
 __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* map,
                                           uint32_t ring, uint32_t kv, uint32_t& issued) {
   using Sh = TileShape<NSLAB, KIND>;
-  // a pair's CTA loads its half of a tile, into both
-  constexpr uint32_t kMine = KIND == kPair ? kKeys / 2 : kKeys;
-  const uint32_t lane = threadIdx.x & 31, boxes = kMine / a.box, first = KIND == kPair ? cluster_rank() * kMine : 0;
-  Walk<KIND == kPair> w;
+  const uint32_t lane = threadIdx.x & 31, boxes = kKeys / a.box;
+  Walk w;
   if (!w.begin(a)) return true;
   // the page of the lane's stretch of key tile j, asked for a tile ahead
   uint32_t j = w.kv0, id = 0, slot = 0, head = 0;
   bool in = false;
   auto ask = [&] {
-    const uint32_t key = j * kKeys + first + lane * a.box, at = key / a.kv.B;
+    const uint32_t key = j * kKeys + lane * a.box, at = key / a.kv.B;
     in = lane < boxes && key < w.n;
     slot = key - at * a.kv.B;
     head = w.h;
@@ -1152,22 +1119,13 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
       --issued;
       return false;
     }
-    const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + (first + lane * a.box) * 128;
+    const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + lane * a.box * 128;
     if (lane == 0) mbar_expect(bar, Sh::kTile);
     __syncwarp();
     if (lane < boxes)
 #pragma unroll
-      for (int s = 0; s < NSLAB; ++s) {
-        if (KIND == kPair) tma_load_4d_both(dst + s * kSlabBytes, map, bar, 64 * s, s0, h0, page);
-        else tma_load_4d(dst + s * kSlabBytes, map, bar, 64 * s, s0, h0, page);
-      }
+      for (int s = 0; s < NSLAB; ++s) tma_load_4d(dst + s * kSlabBytes, map, bar, 64 * s, s0, h0, page);
   }
-  // a pair's CTA stays until all arrivals that the other owes it are there
-  if (KIND == kPair)
-    for (uint32_t i = first_open<Sh::kRing>(issued); i < issued; ++i) {
-      const uint32_t item = 2 * i + kv;
-      if (!mbar_wait(smem_u32(&sh.empty[item % Sh::kRing]), (item / Sh::kRing) & 1)) return false;
-    }
   return true;
 }
 
@@ -1182,7 +1140,7 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
     fence_async_shared();
     for (; landed < upto; ++landed) mbar_arrive(smem_u32(&sh.full[landed % Sh::kRing]));
   };
-  Walk<KIND == kPair> w;
+  Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const uint32_t* ids = a.kv.page_ids + w.page0;
     for (uint32_t j = w.kv0; j < w.kv1; ++j)
@@ -1232,7 +1190,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < Sh::kRing; ++i) {
       mbar_init(smem_u32(&sh.full[i]), TMA ? 1 : 64);
-      mbar_init(smem_u32(&sh.empty[i]), KIND == kPair ? 2 : 1);
+      mbar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sh.q_full[i]), 1);
@@ -1248,11 +1206,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   }
   if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
   tc_fence_before();
-  if (KIND == kPair) cluster_sync();  // the other CTA's barriers are there too
-  else __syncthreads();
+  __syncthreads();
   tc_fence_after();
   grid_dep_sync();
-  const bool go = Walk<KIND == kPair>::plan(a)->ok != 0;
+  const bool go = a.plan->ok != 0;
   bool fine = true;
   if (warp < 8) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
@@ -1287,8 +1244,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   }
   if (!fine) report(a.status, PTC_ERR_TIMEOUT);
   tc_fence_before();
-  if (KIND == kPair) cluster_sync();  // no CTA ends while the other may still write to it
-  else __syncthreads();
+  __syncthreads();
   tc_fence_after();
   if (warp == 8) tmem_free(sh.tmem, 512);
 }
@@ -1326,55 +1282,24 @@ ptc_status launch_one(const AttnArgs& a, const CUtensorMap (&m)[4], cudaStream_t
   static std::atomic<uint64_t> ready{0};
   const auto kernel = k_attn_tiles<T, NSLAB, TMA, KIND>;
   if (!large_smem(kernel, smem, ready)) return PTC_ERR_CUDA;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = KIND == kPair ? a.ctas / 2 * 2 : a.ctas;
-  cfg.blockDim = kTileThreads;
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cfg.attrs = attr;
-  cfg.numAttrs = KIND == kPair ? 2 : 1;
-  PTC_LAUNCH("k_attn_tiles", s, (void)cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], a));
+  PTC_KERNEL("k_attn_tiles", s, kernel, a.ctas, kTileThreads, smem, m[0], m[1], m[2], m[3], a);
   return PTC_OK;
 }
 template <typename T, int NSLAB>
 ptc_status launch_tiles(const AttnArgs& a, const CUtensorMap (&m)[4], bool tma, cudaStream_t s) {
   if (a.max_q_len <= a.tq32) return tma ? launch_one<T, NSLAB, true, kFew>(a, m, s) : launch_one<T, NSLAB, false, kFew>(a, m, s);
-  if (NSLAB == 2 && a.pair_min != UINT32_MAX) {
-    const ptc_status st = launch_one<T, 2, true, kPair>(a, m, s);
-    if (st != PTC_OK || a.kv.n_req == 1) return st;  // one request has all n_tok tokens
-  }
   return tma ? launch_one<T, NSLAB, true, kAny>(a, m, s) : launch_one<T, NSLAB, false, kAny>(a, m, s);
-}
-
-// Requests of more new tokens are pairs' work.
-uint32_t pair_tokens(const AttnArgs& a) { return kPairTiles * 2 * a.tq; }
-
-bool pairs_pay(const AttnArgs& a) {
-  return a.kv.D > 64 && a.max_q_len > pair_tokens(a) && a.n_tok >= (uint64_t)kPairMean * 2 * a.tq * a.kv.n_req;
 }
 
 template <typename T>
 ptc_status launch(AttnArgs& a, cudaStream_t s) {
   constexpr bool bf16 = Weights<T>::kBf16;
   const bool by_tiles = a.mass_out && !a.scores && a.n_tok;  // the weights' own tiles
-  // copies of whole groups of 8 rows that neither leave a page nor a tile (a pair: half a tile)
-  const bool some_long = pairs_pay(a);
-  a.box = some_long ? kKeys / 2 : kKeys;
+  // copies of whole groups of 8 rows that neither leave a page nor a tile
+  a.box = kKeys;
   while (a.kv.B % a.box) a.box /= 2;
   const bool tma = a.n_tok && a.box >= 8 && a.kv.n_pages > 0;
-  a.pair_min = some_long && tma && a.ctas >= 2 ? pair_tokens(a) : UINT32_MAX;
-  uint3 which = {0, 0, 0};
-  uint32_t plans = 1;
-  if (by_tiles) (&which.x)[plans++] = 1;
-  if (a.pair_min != UINT32_MAX) (&which.x)[plans++] = 2;
-  PTC_KERNEL("k_attn_plan", s, k_attn_plan, dim3(a.ctas / 32 + 1, plans), kPlanThreads, 0, a, which);
+  PTC_KERNEL("k_attn_plan", s, k_attn_plan, dim3(a.ctas / 32 + 1, by_tiles ? 2 : 1), kPlanThreads, 0, a);
   CUtensorMap m[4] = {};
   if (a.n_tok) {
     if (tma && (!cache_map(&m[0], a.kv, bf16, a.kv.k, a.kv.ks_page, a.kv.ks_head, a.kv.ks_slot, a.box) ||
@@ -1395,8 +1320,8 @@ AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D, uint64_t scores) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   AttnWs w;
   w.plan = kKvStatusBytes;
-  w.units = w.plan + up(3 * sizeof(AttnPlan));
-  w.ml = w.units + up(3 * (size_t)(n_req + 1) * 8);
+  w.units = w.plan + up(2 * sizeof(AttnPlan));
+  w.ml = w.units + up(2 * (size_t)(n_req + 1) * 8);
   w.part = w.ml + up((size_t)2 * ctas * kRows * 8);
   w.mass = w.part + up((size_t)2 * ctas * kRows * D * 4);
   w.scores = w.mass + up((size_t)2 * ctas * kMassKeys * 4);

@@ -45,15 +45,14 @@ struct AttnArgs {
   uint64_t n_tok;
   uint32_t n_q_heads, G, max_q_len;
   uint32_t tq, tq32;   // whole tokens in 128 and in 32 rows
-  uint32_t pair_min;   // requests of more new tokens are pairs of CTAs' (see k_attn_tiles)
   float scale;
   char* out;
   float* lse;
   const float* mass_in;
   float* mass_out;
   uint64_t mass_stride;
-  AttnPlan* plan;      // [0] tiles, [1] weights, [2] tiles of pairs
-  uint64_t* unit_off;  // three times n_req + 1
+  AttnPlan* plan;      // [0] tiles, [1] weights
+  uint64_t* unit_off;  // twice n_req + 1
   float* part;         // unnormalised rows of split tiles: [2 * ctas][kRows][D]
   float2* part_ml;     // their maxima (in powers of two) and sums
   float* part_mass;    // weights of split key tiles: [2 * ctas][kMassKeys]
