@@ -23,7 +23,9 @@
  *                                                              Sec. 4.1-4.3, App. B
  *
  * Conventions shared by every call
- *   - Pointers are caller-owned DEVICE memory unless the name ends in _host.
+ *   - Pointers are caller-owned DEVICE memory unless the name ends in _host,
+ *     memory of the calling thread's current device, as `stream` is: kernels
+ *     are launched there (the Python binding refuses tensors of another).
  *     The library allocates no device memory: each call takes a device
  *     workspace `ws` of at least ptc_<call>_workspace_bytes(...) bytes,
  *     256-byte aligned.  The workspace holds no state between calls.

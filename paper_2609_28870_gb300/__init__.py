@@ -14,7 +14,8 @@ CUDA kernels.  PyTorch provides device memory and the current CUDA stream.
 and for the cached state itself (keys and values in pages, see ``kv``):
 ptc_kv_append, ptc_paged_attention, ptc_kv_evict.
 
-Arrays are torch CUDA tensors.  Unsigned 32/64-bit arrays travel as int32 /
+Arrays are torch CUDA tensors, on the current device (a call on another
+device's is refused).  Unsigned 32/64-bit arrays travel as int32 /
 int64 tensors holding the same bits (``u32()`` / ``u64()`` give numpy views).
 There is no CPU fallback: without the built library every call raises.
 """
@@ -220,7 +221,14 @@ def _dev(t: torch.Tensor) -> torch.device:
     return t.device
 
 
+def _on_current(index: int, now: int) -> None:
+    if index != now:
+        raise ValueError(f"the tensors lie on cuda:{index}, the current device is cuda:{now}: kernels are launched there")
+
+
 def _stream(device) -> int:
+    """The current stream of the tensors' device, which has to be the current device."""
+    _on_current(device.index, torch.cuda.current_device())
     return torch.cuda.current_stream(device).cuda_stream
 
 
@@ -489,7 +497,7 @@ class TraceStatsPlan:
     def __init__(self, ids: torch.Tensor, prev: torch.Tensor, nxt: torch.Tensor, n_distinct: int,
                  req_blk_off: torch.Tensor, req_ts_us: torch.Tensor, req_session: torch.Tensor, n_session: int,
                  dist: torch.Tensor | None = None, caps=None, ws: torch.Tensor | None = None):
-        dev = _dev(req_blk_off)
+        dev = self.device = _dev(req_blk_off)
         n = ids.numel()
         n_req = req_blk_off.numel() - 1
         self.caps = np.ascontiguousarray([] if caps is None else caps, dtype=np.uint64)
@@ -505,6 +513,7 @@ class TraceStatsPlan:
                       _stream(dev))
 
     def run(self) -> "TraceStatsPlan":
+        _on_current(self.device.index, torch.cuda.current_device())
         rc = self._fn(*self._args)
         if rc != 0:
             raise PtcError("ptc_trace_stats", rc)
@@ -579,7 +588,7 @@ class PipelinePlan:
     def __init__(self, tokens, req_tok_off, req_ts_us, block_size: int, caps, kind: int = PTC_COST_MEASURED,
                  seed: int = 0, f_lin: int = F_LIN, f_attn: int = F_ATTN, ws: torch.Tensor | None = None,
                  outputs: dict | None = None, req_session: torch.Tensor | None = None, n_session: int = 0):
-        dev = _dev(req_tok_off)
+        dev = self.device = _dev(req_tok_off)
         n_req = req_tok_off.numel() - 1
         n_tok = tokens.numel()
         self.caps = np.ascontiguousarray(caps, dtype=np.uint64)
@@ -601,6 +610,7 @@ class PipelinePlan:
                       self.saved.ctypes.data, ctypes.byref(self.total), _ptr(self.ws), self.ws.numel(), _stream(dev))
 
     def run(self) -> "PipelinePlan":
+        _on_current(self.device.index, torch.cuda.current_device())
         rc = self._fn(*self._args)
         if rc != 0:
             raise PtcError("ptc_pipeline", rc)
@@ -627,6 +637,7 @@ class HostPipelinePlan:
         dev = torch.device(device)
         if dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
+        self.device = dev
 
         def host_ptr(a, dt):
             if a is None:
@@ -659,6 +670,7 @@ class HostPipelinePlan:
                       self.saved.ctypes.data, ctypes.byref(self.total), _ptr(self.ws), self.ws.numel(), _stream(dev))
 
     def run(self) -> "HostPipelinePlan":
+        _on_current(self.device.index, torch.cuda.current_device())
         rc = self._fn(*self._args)
         if rc != 0:
             raise PtcError("ptc_pipeline_host", rc)

@@ -123,6 +123,7 @@ def _place(w):
 
 
 def _stream(dev: int) -> int:
+    _pkg()._on_current(dev, torch._C._cuda_getDevice())
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
