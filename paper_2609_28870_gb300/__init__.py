@@ -238,7 +238,7 @@ def _ptr(t) -> int | None:
 
 def _workspace(nbytes: int, device, ws: torch.Tensor | None = None) -> torch.Tensor:
     nbytes = max(int(nbytes), 256)
-    if ws is not None and ws.numel() >= nbytes and ws.device == device:
+    if ws is not None and ws.numel() >= nbytes and ws.is_contiguous() and ws.device == device:
         return ws
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 

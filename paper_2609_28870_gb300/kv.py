@@ -113,7 +113,7 @@ def _status(status, dev: int):
 
 
 def _room(k, need: int, dev: int, ws):
-    if ws is not None and ws.numel() >= need and ws.get_device() == dev:
+    if ws is not None and ws.numel() >= need and ws.is_contiguous() and ws.get_device() == dev:
         return ws
     return torch.empty(max(need, 256), dtype=torch.uint8, device=k.device)
 
