@@ -676,8 +676,9 @@ ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* 
  * the new tokens and over the query heads of its key head, for ptc_kv_evict:
  *   mass_out[h][S] = mass_in[h][S] + sum exp(s_j - lse),  S = page_off[r] * block_size + j
  * for j < n, and 0 for the rest of request r's slots.  mass_in and mass_out are
- * f32[n_kv_heads, mass_stride], mass_stride >= n_page_ids * block_size; mass_in
- * may be NULL (zeros) or mass_out itself.
+ * f32[n_kv_heads, mass_stride], mass_stride >= n_page_ids * block_size and at
+ * most 2^40; mass_in may be NULL (zeros) or mass_out itself.  More than 2^38
+ * slots in page_ids, or 2^31 query rows, are PTC_ERR_OVERFLOW.
  */
 size_t ptc_paged_attention_workspace_bytes(uint32_t n_req, uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t head_dim,
                                            uint32_t max_q_len, uint64_t mass_stride /* 0 without mass_out */);

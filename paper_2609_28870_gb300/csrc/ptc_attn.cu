@@ -1382,7 +1382,9 @@ extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q,
   if (n_q_heads / kv->n_kv_heads > kMaxGroup) return PTC_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale) || (n_tok && !kv->n_req)) return PTC_ERR_INVALID_ARG;
   if (!std::isfinite(scale * kLog2e)) return PTC_ERR_INVALID_ARG;
-  if (n_tok > 0x7FFFFFFFu || n_tok * n_q_heads > (uint64_t(1) << 31) || kv->n_page_ids * kv->block_size > (uint64_t(1) << 38))
+  // (a stride of up to 2^40 times the scores' rows, at most kFewRows a key head, stays below 2^64 bytes)
+  if (n_tok > 0x7FFFFFFFu || n_tok * n_q_heads > (uint64_t(1) << 31) ||
+      kv->n_page_ids > (uint64_t(1) << 38) / kv->block_size || (mass_out && mass_stride > uint64_t(1) << 40))
     return PTC_ERR_OVERFLOW;
   if (mass_out ? mass_stride / kv->block_size < kv->n_page_ids : mass_in != nullptr) return PTC_ERR_INVALID_ARG;
   if (kv->n_pages > 0x7FFFFFFFu) return PTC_ERR_OVERFLOW;  // tensor copies have signed coordinates
