@@ -16,6 +16,9 @@ ptc_assign_ids and the offsets of ptc_hash_blocks, or any other page lists.
 With ``status`` (an int32 CUDA tensor of one zero) a call returns without
 waiting, for loops over layers and for graph capture; check_status(status)
 waits and raises what went wrong.  Without it a call waits and raises itself.
+
+The calls have no backward pass: inputs that ask for gradients are refused,
+unless under torch.no_grad().
 """
 from __future__ import annotations
 
@@ -98,6 +101,14 @@ def _tokens(x, name: str, k, dev: int, head_dim: int, heads: int | None = None) 
     return _STRIDES.pack(a, b)
 
 
+def _no_backward(*tensors) -> None:
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("the calls on paged keys and values have no backward pass: expected inputs that do not "
+                                 "require gradients, or torch.no_grad()")
+
+
 def _off(tok_off, kv_len, dev: int) -> None:
     _want(tok_off, torch.int64, "tok_off", dev)
     if tok_off.shape[0] != kv_len.shape[0] + 1:
@@ -146,6 +157,7 @@ def ptc_kv_append(k_new, v_new, k, v, page_ids, page_off, tok_off, kv_len, ws: t
     ks, vs = _tokens(k_new, "k_new", k, dev, shape[3], shape[1]), _tokens(v_new, "v_new", k, dev, shape[3], shape[1])
     if v_new.shape != k_new.shape:
         raise ValueError("v_new: expected k_new's shape")
+    _no_backward(k_new, v_new, k, v)
     L = p.lib()
     w = _room(k, L.ptc_kv_append_workspace_bytes(kv_len.shape[0]), dev, ws) if status is None else None
     rc = L.ptc_kv_append(kv, k_new.data_ptr(), v_new.data_ptr(), ks, vs, tok_off.data_ptr(), k_new.shape[0],
@@ -168,6 +180,7 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
     D = shape[3]
     qs = _tokens(q, "q", k, dev, D)
     T, Hq, _ = q.shape
+    _no_backward(q, k, v, mass, mass_out, out, lse)
     if out is None:
         out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
     elif out.shape != q.shape:
@@ -220,6 +233,7 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
         raise ValueError("mass: expected one row a key head")
     if min(n_keep, n_sink, n_recent, max_kv_len) < 0:
         raise ValueError("n_keep, n_sink, n_recent and max_kv_len: expected no negative numbers")
+    _no_backward(k, v, mass)
     keep = torch.empty((n_req, heads, n_keep), dtype=torch.int32, device=k.device)
     new_len = torch.empty(n_req, dtype=torch.int32, device=k.device)
     slots = dst_page_ids.shape[0] * shape[2]
