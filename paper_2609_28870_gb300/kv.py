@@ -30,6 +30,7 @@ import torch
 
 PTC_DTYPE_BF16, PTC_DTYPE_FP16 = 0, 1
 MAX_HEAD_DIM, MAX_GROUP = 128, 128
+_U32 = 0xFFFFFFFF
 _DTYPES = {torch.bfloat16: PTC_DTYPE_BF16, torch.float16: PTC_DTYPE_FP16}
 
 # ptc_paged_kv and two strides, as the C compiler lays them out.  A decode step
@@ -177,6 +178,8 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
     p, dev, shape = _pkg(), k.get_device(), k.shape
     kv = _paged(k, v, page_ids, page_off, kv_len, shape, dev)
     _off(tok_off, kv_len, dev)
+    if not 0 <= max_q_len <= _U32:
+        raise ValueError("max_q_len: expected a number of 32 bits, not negative")
     D = shape[3]
     qs = _tokens(q, "q", k, dev, D)
     T, Hq, _ = q.shape
@@ -231,8 +234,8 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
         raise ValueError("dst_page_off: expected one entry more than kv_len")
     if mass.shape[0] != heads:
         raise ValueError("mass: expected one row a key head")
-    if min(n_keep, n_sink, n_recent, max_kv_len) < 0:
-        raise ValueError("n_keep, n_sink, n_recent and max_kv_len: expected no negative numbers")
+    if min(n_keep, n_sink, n_recent, max_kv_len) < 0 or max(n_keep, n_sink, n_recent, max_kv_len) > _U32:
+        raise ValueError("n_keep, n_sink, n_recent and max_kv_len: expected numbers of 32 bits, none negative")
     _no_backward(k, v, mass)
     keep = torch.empty((n_req, heads, n_keep), dtype=torch.int32, device=k.device)
     new_len = torch.empty(n_req, dtype=torch.int32, device=k.device)
