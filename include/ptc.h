@@ -735,10 +735,14 @@ void ptc_release_host_staging(void);
  * polls, so a test can drive the give-up path: the call must return
  * PTC_ERR_TIMEOUT and leave the device usable.  With
  * PTC_TEST_WAIT_PIECES + polls it is stage c's wait that gives up (a call with
- * fewer than 2,049 pieces has none).  0 restores normal waits.  Process-wide;
- * not for production use.
+ * fewer than 2,049 pieces has none).  With PTC_TEST_WAIT_ATTENTION + polls it is
+ * the roles of ptc_paged_attention's CTAs, which wait for one another for about
+ * two seconds at most: no queries are loaded, and the waits for them, and for
+ * what depends on them, give up after `polls` times 1,024 clock cycles.  0
+ * restores normal waits.  Process-wide; not for production use.
  */
 #define PTC_TEST_WAIT_PIECES 0x80000000u
+#define PTC_TEST_WAIT_ATTENTION 0x40000000u
 void ptc_test_wait_polls(uint32_t polls);
 
 /*

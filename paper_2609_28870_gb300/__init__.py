@@ -40,6 +40,7 @@ PTC_REUSE_AUTO, PTC_REUSE_SORT, PTC_REUSE_RUNS = 0, 1, 2
 PTC_IDS_AUTO, PTC_IDS_TABLE, PTC_IDS_PARTITIONED = 0, 1, 2
 PTC_TOUCH_ROOT_FIRST, PTC_TOUCH_LEAF_FIRST = 0, 1
 PTC_RESIDENCY_BLOCK, PTC_RESIDENCY_REQUEST = 0, 1
+PTC_TEST_WAIT_PIECES, PTC_TEST_WAIT_ATTENTION = 0x80000000, 0x40000000
 F_LIN = 6_600_000_000          # 2 x 3.3e9 active parameters, FLOPs per token
 F_ATTN = 4 * 48 * 32 * 128     # per attended position: 4 x layers x heads x head_dim
 MAX_CAPACITIES = 1024

@@ -390,9 +390,10 @@ namespace {
 std::atomic<uint32_t> g_wait_polls{0};
 }  // namespace
 
-uint32_t ptc::test_wait_polls(bool pieces) {
+uint32_t ptc::test_wait_polls(uint32_t which) {
+  constexpr uint32_t kWhich = PTC_TEST_WAIT_PIECES | PTC_TEST_WAIT_ATTENTION;
   const uint32_t v = g_wait_polls.load(std::memory_order_relaxed);
-  return ((v & PTC_TEST_WAIT_PIECES) != 0) == pieces ? v & ~PTC_TEST_WAIT_PIECES : 0u;
+  return (v & kWhich) == which ? v & ~kWhich : 0u;
 }
 
 void ptc::release_host_stage() {

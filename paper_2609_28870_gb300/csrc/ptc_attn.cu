@@ -322,6 +322,7 @@ struct TileShared {
   uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2][2], drain;
   float2 ml[256];
   uint32_t tmem, last, count, c0;
+  uint32_t issued[2], loads[2];  // tensor copies of keys and of values, loads of either half's queries
   uint16_t slots[kMaxCtas];  // a split tile's parts, in the order of the keys
 };
 
@@ -387,14 +388,14 @@ struct RowState {
 // and what was summed so far shrink with it.
 template <int NSLAB>
 __device__ __forceinline__ void raise_top(RowState& st, float mx, float sl2, uint32_t o_at, bool first,
-                                          uint32_t bar_o, uint32_t parity, bool& alive) {
+                                          uint32_t bar_o, uint32_t parity, long long limit, bool& alive) {
   if (!__any_sync(kFull, mx > st.top)) return;
   const float nt = fmaxf(st.top, mx);
   const float f = st.top == -INFINITY ? 0.f : exp2_approx((st.top - nt) * sl2);
   st.l *= f;
   st.top = nt;
   if (first) return;
-  if (alive) alive = mbar_wait(bar_o, parity);
+  if (alive) alive = mbar_wait(bar_o, parity, limit);
   tc_fence_after();
 #pragma unroll 1
   for (int c = 0; c < NSLAB * 2; ++c) {
@@ -587,7 +588,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     if (!whole && threadIdx.x < 32) list_sharers(a, sh, w.from(a), w.to(a));
     if (mode != kColumnsApart) {
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, ++parted, see_all -= step * kKeys) {
-        if (alive) alive = mbar_wait(bar_s, done & 1);
+        if (alive) alive = mbar_wait(bar_s, done & 1, a.limit);
         tc_fence_after();
         const int see = see_all >= (int64_t)kKeys ? (int)kKeys : see_all > 0 ? (int)see_all : 0;
         const bool masked = __any_sync(kFull, see < (int)kKeys);
@@ -631,7 +632,8 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
             }
             if (move) {
               const float mx = valid ? fmaxf(max32(x[2 * part]), max32(x[2 * part + 1])) : -INFINITY;
-              raise_top<NSLAB>(st, mx, sl2, o_at, first, bar_o[1 - part], (part ? parted : done - 1) & 1, alive);
+              raise_top<NSLAB>(st, mx, sl2, o_at, first, bar_o[1 - part], (part ? parted : done - 1) & 1, a.limit,
+                               alive);
               sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
               sum.clear();
 #pragma unroll
@@ -650,7 +652,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     } else {
       see_all -= 32 * warp;
       for (uint32_t j = j0; j < w.kv1; j += step, ++done, see_all -= step * kKeys) {
-        if (alive) alive = mbar_wait(bar_s, done & 1);
+        if (alive) alive = mbar_wait(bar_s, done & 1, a.limit);
         tc_fence_after();
         uint32_t x[32], y[16], zero[16];
         tmem_ld32(x, s_at + 32 * warp);
@@ -680,7 +682,8 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
         weigh<T>(x, sl2, sub, sum, y);
         float total = sum.total();
         if (__any_sync(kFull, j == j0 || (valid && !(total <= kMove * W::kScale)))) {
-          raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o[1], (done - 1) & 1, alive);
+          raise_top<NSLAB>(st, valid ? max32(x) : -INFINITY, sl2, o_at, j == j0, bar_o[1], (done - 1) & 1, a.limit,
+                             alive);
           sub = (st.top == -INFINITY ? 0.f : st.top * sl2) - W::kShift;
           sum.clear();
           weigh<T>(x, sl2, sub, sum, y);
@@ -701,7 +704,7 @@ __device__ __forceinline__ bool softmax_role(const AttnArgs& a, TileShared& sh, 
     }
     // the sums of the rows
     const bool some = j0 < w.kv1;  // this half had a key tile
-    if (some && alive) alive = mbar_wait(bar_o[1], (done - 1) & 1);
+    if (some && alive) alive = mbar_wait(bar_o[1], (done - 1) & 1, a.limit);
     tc_fence_after();
     const uint64_t prow0 = (uint64_t)(2 * blockIdx.x + (w.first ? 0 : 1)) * kRows;
     const uint64_t orow0 = w.tok0 * a.n_q_heads + w.h * G;  // row (t, g) is orow0 + t * n_q_heads + g
@@ -875,7 +878,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
   uint32_t item = 0;           // ring tiles before this query tile
   uint32_t used[2] = {0, 0};   // query tiles of each region
   uint32_t weights[2][2] = {};  // of each half: weights by part
-  auto full = [&](uint32_t i) { return mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1); };
+  auto full = [&](uint32_t i) { return mbar_wait(smem_u32(&sh.full[i % Sh::kRing]), (i / Sh::kRing) & 1, a.limit); };
   auto tile_at = [&](uint32_t i) { return ring + (i % Sh::kRing) * Sh::kTile; };
   auto commit = [&](uint64_t& bar) {
     if (elect_lane()) mma_commit(smem_u32(&bar));
@@ -904,7 +907,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
     const uint64_t db = tile_desc(tile_at(v_item), kSlabBytes);
 #pragma unroll
     for (uint32_t part = 0; part < 2; ++part) {
-      if ((part || apart) && !mbar_wait(smem_u32(&sh.p_full[half][part]), weights[half][part]++ & 1)) return false;
+      if ((part || apart) && !mbar_wait(smem_u32(&sh.p_full[half][part]), weights[half][part]++ & 1, a.limit)) return false;
       if (!part && !apart) continue;
       tc_fence_after();
       if (elect_lane()) {
@@ -932,12 +935,12 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
       const uint32_t v_at = v_item % Sh::kRing, k_at = k_next % Sh::kRing;
       const uint64_t v_desc = desc_at(v_base, v_at * Sh::kTile), k_desc = desc_at(k_base, k_at * Sh::kTile);
       const bool more = j + 1 < L;
-      if (!mbar_wait_lane(smem_u32(&sh.full[v_at]), (v_item / Sh::kRing) & 1)) return false;
+      if (!mbar_wait_lane(smem_u32(&sh.full[v_at]), (v_item / Sh::kRing) & 1, a.limit)) return false;
 #pragma unroll
       for (uint32_t s = 0; s < 2; ++s) {
 #pragma unroll
         for (uint32_t part = 0; part < 2; ++part) {
-          if (!mbar_wait_lane(smem_u32(&sh.p_full[s][part]), (before[s][part] + j) & 1)) return false;
+          if (!mbar_wait_lane(smem_u32(&sh.p_full[s][part]), (before[s][part] + j) & 1, a.limit)) return false;
           tc_fence_after();
 #pragma unroll
           for (uint32_t k = 4 * part; k < 4 * part + 4; ++k)
@@ -946,7 +949,7 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
         }
         if (s == 1) release(v_at);
         if (more) {
-          if (s == 0 && !mbar_wait_lane(smem_u32(&sh.full[k_at]), (k_next / Sh::kRing) & 1)) return false;
+          if (s == 0 && !mbar_wait_lane(smem_u32(&sh.full[k_at]), (k_next / Sh::kRing) & 1, a.limit)) return false;
           // in order after the product above, which reads the weights that these scores overwrite
           mma_ss<false>(tmem + s_col(s), q_desc[s], k_desc, kQk);
 #pragma unroll
@@ -979,11 +982,11 @@ __device__ __forceinline__ bool product_role(const AttnArgs& a, TileShared& sh, 
       fence_async_shared();
       __syncwarp();
     };
-    if (!mbar_wait(smem_u32(&sh.q_full[0]), used[0]++ & 1) || !full(item)) return false;
+    if (!mbar_wait(smem_u32(&sh.q_full[0]), used[0]++ & 1, a.limit) || !full(item)) return false;
     tc_fence_after();
     scores(0, 0, item);
     if (mode == kRowsApart) {
-      if (!mbar_wait(smem_u32(&sh.q_full[1]), used[1]++ & 1)) return false;
+      if (!mbar_wait(smem_u32(&sh.q_full[1]), used[1]++ & 1, a.limit)) return false;
       tc_fence_after();
       scores(1, 1, item);
       free_tile(item);
@@ -1051,14 +1054,16 @@ __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, co
                                            const CUtensorMap* mq32, uint32_t q_smem, uint32_t (&loads)[2]) {
   using Sh = TileShape<NSLAB, KIND>;
   const uint32_t lane = threadIdx.x & 31;
+  if (a.withhold) return true;
   Walk w;
   for (bool more = w.begin(a); more; more = w.next(a)) {
     const int mode = KIND == kFew ? kColumnsApart : w.mode(a);
     const int tok = (int)(w.tok0 + w.token0(a));
     for (uint32_t s = 0; s < (mode == kRowsApart ? 2u : 1u); ++s) {
-      if (loads[s] && !mbar_wait(smem_u32(&sh.q_empty[s]), (loads[s] - 1) & 1)) return false;
+      if (loads[s] && !mbar_wait(smem_u32(&sh.q_empty[s]), (loads[s] - 1) & 1, a.limit)) return false;
       ++loads[s];
       const uint32_t bar = smem_u32(&sh.q_full[s]), dst = q_smem + s * Sh::kTile;
+      if (lane == 0) sh.loads[s] = loads[s];
       if (lane == 0 && mode != kColumnsApart) {
         mbar_expect(bar, NSLAB * a.tq * a.G * 128);
 #pragma unroll
@@ -1075,26 +1080,19 @@ __device__ __forceinline__ bool query_role(const AttnArgs& a, TileShared& sh, co
   return true;
 }
 
-// The copies of keys (or values) that may still be in flight or unused, of those issued.
-template <uint32_t RING>
-__device__ __forceinline__ uint32_t first_open(uint32_t issued) {
-  constexpr uint32_t kOpen = (RING + 1) / 2;
-  return issued > kOpen ? issued - kOpen : 0;
-}
-
 // Keys and values by tensor copies, a warp for each: a copy a stretch of `box` slots (a divisor
 // of the page size and of the tile) and slab.  Stretches at or past the
 // request's end and pages that the cache does not have read as zeros: their
 // page coordinate is n_pages, which is out of range.
 template <int NSLAB, int KIND>
 __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, const CUtensorMap* map,
-                                          uint32_t ring, uint32_t kv, uint32_t& issued) {
+                                          uint32_t ring, uint32_t kv) {
   using Sh = TileShape<NSLAB, KIND>;
   const uint32_t lane = threadIdx.x & 31, boxes = kKeys / a.box;
   Walk w;
   if (!w.begin(a)) return true;
   // the page of the lane's stretch of key tile j, asked for a tile ahead
-  uint32_t j = w.kv0, id = 0, slot = 0, head = 0;
+  uint32_t issued = 0, j = w.kv0, id = 0, slot = 0, head = 0;
   bool in = false;
   auto ask = [&] {
     const uint32_t key = j * kKeys + lane * a.box, at = key / a.kv.B;
@@ -1115,12 +1113,12 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
     }
     if (more) ask();
     const uint32_t item = 2 * issued++ + kv, at = item % Sh::kRing;
-    if (item >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (item / Sh::kRing - 1) & 1)) {
-      --issued;
-      return false;
-    }
+    if (item >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (item / Sh::kRing - 1) & 1, a.limit)) return false;
     const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * Sh::kTile + lane * a.box * 128;
-    if (lane == 0) mbar_expect(bar, Sh::kTile);
+    if (lane == 0) {
+      sh.issued[kv] = issued;
+      mbar_expect(bar, Sh::kTile);
+    }
     __syncwarp();
     if (lane < boxes)
 #pragma unroll
@@ -1146,7 +1144,10 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
     for (uint32_t j = w.kv0; j < w.kv1; ++j)
       for (int kv = 0; kv < 2; ++kv) {
         const uint32_t at = issued % Sh::kRing;
-        if (issued >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / Sh::kRing - 1) & 1)) return false;
+        if (issued >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / Sh::kRing - 1) & 1, a.limit)) {
+          cp_async_wait<0>();
+          return false;
+        }
         const char* src = kv == 0 ? a.kv.k : a.kv.v;
         const int64_t sp = kv == 0 ? a.kv.ks_page : a.kv.vs_page, ss = kv == 0 ? a.kv.ks_slot : a.kv.vs_slot;
         const int64_t head = w.h * (kv == 0 ? a.kv.ks_head : a.kv.vs_head);
@@ -1172,6 +1173,27 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
   cp_async_wait<0>();
   land(issued);
   return true;
+}
+
+// Where a role has given up: all tensor copies that were issued land before the
+// CTA ends, also those of a role that has issued all of its own.  A place of the
+// ring was taken again only after its products, so its last copy is the one
+// that may be in flight.  By one warp.
+template <uint32_t RING>
+__device__ __noinline__ void land_copies(TileShared& sh) {
+  for (uint32_t at = 0; at < RING; ++at) {
+    uint32_t next = 0;  // the place's last copy, and one
+    for (uint32_t kv = 0; kv < 2; ++kv)
+      for (uint32_t i = sh.issued[kv], k = 0; i > 0 && k < RING; --i, ++k) {
+        const uint32_t item = 2 * (i - 1) + kv;
+        if (item % RING != at) continue;
+        if (item + 1 > next) next = item + 1;
+        break;
+      }
+    if (next) (void)mbar_wait(smem_u32(&sh.full[at]), ((next - 1) / RING) & 1);
+  }
+  for (int s = 0; s < 2; ++s)
+    if (sh.loads[s]) (void)mbar_wait(smem_u32(&sh.q_full[s]), (sh.loads[s] - 1) & 1);
 }
 
 template <typename T, int NSLAB, bool TMA, int KIND>
@@ -1203,6 +1225,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
     mbar_init(smem_u32(&sh.drain), 1);
     fence_mbar_init();
+    for (int i = 0; i < 2; ++i) sh.issued[i] = sh.loads[i] = 0;
   }
   if (warp == 8) tmem_alloc(smem_u32(&sh.tmem), 512);
   tc_fence_before();
@@ -1216,7 +1239,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     if (go) fine = softmax_role<T, NSLAB, KIND>(a, sh, smem_raw + Sh::kRest - kStage, warp / 4);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    uint32_t issued = 0, loads[2] = {0, 0};
+    // (declared inside query_role, the registers fall so that the softmax spills: 1.23 -> 1.6 ms for 4,096 tokens at 32K)
+    uint32_t loads[2] = {0, 0};
     if (!go) {
     } else if (warp == 8) {
       fine = product_role<T, NSLAB, KIND>(a, sh, q_smem, ring);
@@ -1229,22 +1253,15 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     } else if (!TMA) {
       fine = gather_role<NSLAB, KIND>(a, sh, ring);
     } else {
-      fine = copy_role<NSLAB, KIND>(a, sh, warp == 9 ? &mk : &mv, ring, warp == 9 ? 0 : 1, issued);
-    }
-    if (!fine) {
-      // given up: let the copies in flight land
-      for (uint32_t i = first_open<Sh::kRing>(issued); i < issued; ++i) {
-        const uint32_t item = 2 * i + (warp == 9 ? 0 : 1);
-        (void)mbar_wait(smem_u32(&sh.full[item % Sh::kRing]), (item / Sh::kRing) & 1);
-      }
-      for (int s = 0; s < 2; ++s)
-        if (loads[s]) (void)mbar_wait(smem_u32(&sh.q_full[s]), (loads[s] - 1) & 1);
-      if (!TMA) cp_async_wait<0>();
+      fine = copy_role<NSLAB, KIND>(a, sh, warp == 9 ? &mk : &mv, ring, warp == 9 ? 0 : 1);
     }
   }
   if (!fine) report(a.status, PTC_ERR_TIMEOUT);
   tc_fence_before();
-  __syncthreads();
+  if (__syncthreads_or(!fine)) {
+    if (warp == 9) land_copies<Sh::kRing>(sh);
+    __syncthreads();
+  }
   tc_fence_after();
   if (warp == 8) tmem_free(sh.tmem, 512);
 }
@@ -1422,6 +1439,9 @@ extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q,
   a.part_mass = reinterpret_cast<float*>(w + at.mass);
   a.scores = scores && n_tok ? reinterpret_cast<float*>(w + at.scores) : nullptr;
   a.few = max_q_len * a.G;
+  const uint32_t wait_test = test_wait_polls(PTC_TEST_WAIT_ATTENTION);
+  a.withhold = wait_test != 0;
+  a.limit = wait_test ? 1024ll * wait_test : kMbarCycles;
   if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
   const ptc_status run = kv->dtype == PTC_DTYPE_BF16 ? launch<__nv_bfloat16>(a, s) : launch<__half>(a, s);
   if (run != PTC_OK) return run;

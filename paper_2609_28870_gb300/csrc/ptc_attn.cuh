@@ -59,6 +59,8 @@ struct AttnArgs {
   float* scores;       // scores of few rows, [n_kv_heads][few][slots], or null
   uint32_t few;
   uint32_t ctas, box;  // box: rows of a tensor copy of keys or values
+  uint32_t withhold;   // test of the bounded waits: no queries are loaded
+  long long limit;     // cycles after which a wait for another role gives up
   uint32_t* status;
 };
 

@@ -224,8 +224,8 @@ __device__ __forceinline__ bool mass_sums(const AttnArgs& a, MassShared& sh, uin
       if (side == 0) sh.lse[odd][tid] = ahead;
       odd_sync();
       if (side == 0 && q + 2 < w.q1) ahead = lse_of(q + 2);
-      if (alive) alive = mbar_wait(smem_u32(&sh.s_full[2 * odd]), uses[0]++ & 1);
-      if (two && alive) alive = mbar_wait(smem_u32(&sh.s_full[2 * odd + 1]), uses[1]++ & 1);
+      if (alive) alive = mbar_wait(smem_u32(&sh.s_full[2 * odd]), uses[0]++ & 1, a.limit);
+      if (two && alive) alive = mbar_wait(smem_u32(&sh.s_full[2 * odd + 1]), uses[1]++ & 1, a.limit);
       tc_fence_after();
       // the rows that see either key, from `lo` on
       const int64_t lo64 = (t_first - (int64_t)q * a.tq) * a.G, lo64b = lo64 + (int64_t)kKeys * a.G;
@@ -299,10 +299,10 @@ __device__ __forceinline__ bool mass_products(const AttnArgs& a, MassShared& sh,
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
     const uint32_t k_at = smem + (seg & 1) * 2 * Sh::kTile, halves = w.two() ? 2 : 1;
-    if (!mbar_wait(smem_u32(&sh.k_full[seg & 1]), (seg >> 1) & 1)) return false;
+    if (!mbar_wait(smem_u32(&sh.k_full[seg & 1]), (seg >> 1) & 1, a.limit)) return false;
     for (uint32_t q = w.q0; q < w.q1; ++q, ++unit) {
       const uint32_t ring = unit % kQueryRing, q_at = smem + Sh::kQueries + ring * Sh::kTile;
-      if (!mbar_wait(smem_u32(&sh.q_full[ring]), (unit / kQueryRing) & 1)) return false;
+      if (!mbar_wait(smem_u32(&sh.q_full[ring]), (unit / kQueryRing) & 1, a.limit)) return false;
       const uint32_t desc = mma_desc(bf16, 128, (w.rows(a, q) + 15) & ~15u, false);
       const uint64_t db = tile_desc(q_at, 16);
 #pragma unroll
@@ -310,7 +310,7 @@ __device__ __forceinline__ bool mass_products(const AttnArgs& a, MassShared& sh,
         if (half >= halves) break;
         const uint32_t buf = (unit & 1) * 2 + half;
         uint32_t& n = (unit & 1) ? used[2 + half] : used[half];
-        if (n && !mbar_wait(smem_u32(&sh.s_empty[buf]), (n - 1) & 1)) return false;
+        if (n && !mbar_wait(smem_u32(&sh.s_empty[buf]), (n - 1) & 1, a.limit)) return false;
         ++n;
         tc_fence_after();
         const uint64_t da = tile_desc(k_at + half * Sh::kTile, 16);
@@ -339,11 +339,12 @@ __device__ __forceinline__ bool mass_queries(const AttnArgs& a, MassShared& sh, 
                                              uint32_t& unit) {
   using Sh = MassShape<NSLAB>;
   const uint32_t lane = threadIdx.x & 31;
+  if (a.withhold) return true;
   MassWalk w;
   for (bool more = w.begin(a); more; more = w.next(a))
     for (uint32_t q = w.q0; q < w.q1; ++q, ++unit) {
       const uint32_t at = unit % kQueryRing, bar = smem_u32(&sh.q_full[at]), dst = smem + Sh::kQueries + at * Sh::kTile;
-      if (unit >= kQueryRing && !mbar_wait(smem_u32(&sh.q_empty[at]), (unit / kQueryRing - 1) & 1)) return false;
+      if (unit >= kQueryRing && !mbar_wait(smem_u32(&sh.q_empty[at]), (unit / kQueryRing - 1) & 1, a.limit)) return false;
       if (lane == 0) {
         mbar_expect(bar, NSLAB * a.tq * a.G * 128);
 #pragma unroll
@@ -367,7 +368,7 @@ __device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, con
   for (bool more = w.begin(a); more; more = w.next(a), ++seg) {
     const uint32_t at = seg & 1, bar = smem_u32(&sh.k_full[at]), halves = w.two() ? 2 : 1;
     const uint32_t* ids = a.kv.page_ids + w.page0;
-    if (seg >= 2 && !mbar_wait(smem_u32(&sh.k_empty[at]), ((seg >> 1) - 1) & 1)) return false;
+    if (seg >= 2 && !mbar_wait(smem_u32(&sh.k_empty[at]), ((seg >> 1) - 1) & 1, a.limit)) return false;
     if constexpr (TMA) {
       const uint32_t boxes = kKeys / a.box;
       if (lane == 0) mbar_expect(bar, halves * Sh::kTile);
@@ -455,12 +456,12 @@ __global__ void __launch_bounds__(kMassThreads, 1)
       fine &= mbar_wait(smem_u32(&sh.drain), 0);
     } else if (warp == 18) {
       fine = mass_queries<NSLAB>(a, sh, &mq, smem, units);
-      if (!fine)  // given up: let the copies in flight land
-        for (uint32_t u = units > kQueryRing ? units - kQueryRing : 0; u < units; ++u)
-          (void)mbar_wait(smem_u32(&sh.q_full[u % kQueryRing]), (u / kQueryRing) & 1);
+      // copies in flight land before the CTA ends, whoever has given up
+      for (uint32_t u = units > kQueryRing ? units - kQueryRing : 0; u < units; ++u)
+        (void)mbar_wait(smem_u32(&sh.q_full[u % kQueryRing]), (u / kQueryRing) & 1);
     } else if (warp == 17 || !TMA) {
       fine = mass_keys<NSLAB, TMA>(a, sh, &mk, smem, segs);
-      if (!fine && TMA)
+      if (TMA)
         for (uint32_t k = segs > 2 ? segs - 2 : 0; k < segs; ++k)
           (void)mbar_wait(smem_u32(&sh.k_full[k & 1]), (k >> 1) & 1);
     }

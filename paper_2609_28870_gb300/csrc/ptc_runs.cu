@@ -952,7 +952,7 @@ ptc_status stack_distance_runs(const uint32_t* prev, uint64_t n, uint32_t* dist_
   const uint64_t K = pieces.K;
   const bool by_pieces = lent && K > 0 && reinterpret_cast<const char*>(M.sd) <= reinterpret_cast<const char*>(pieces.ipos);
   if (by_pieces) {
-    const uint32_t wait_test = test_wait_polls(true);
+    const uint32_t wait_test = test_wait_polls(PTC_TEST_WAIT_PIECES);
     if (wait_test && fill_async(&M.st->wait_test, wait_test, sizeof(uint32_t), s) != PTC_OK) return PTC_ERR_CUDA;
     const PieceArgs pa{pieces, (uint32_t)n, M.bits, M.kbits, M.rec_s, M.rec_a, lent->lb, M.st};
     PTC_KERNEL("k_runs_pieces", s, k_runs_pieces, ceil_div_u32(K, kPieceTile), kPT, 0, pa);

@@ -1,7 +1,7 @@
 // Fifth-generation tensor cores, tensor memory, tensor copies and the shared
 // memory barriers between them (sm_103a), as the attention kernels use them.
 //
-//  * Waits on barriers are bounded: mbar_wait gives up after kMbarCycles.
+//  * Waits on barriers are bounded: mbar_wait gives up after `limit` cycles.
 //  * Tiles in shared memory are slabs of 64 16-bit columns: a row is 128
 //    bytes, and the 16-byte pieces of row i are permuted by i % 8 (the
 //    128-byte swizzle of tensor copies and of matrix operands).
@@ -44,25 +44,25 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 // Waits for the phase of `parity` with the whole warp, which comes out
 // converged.  False if the phase did not complete in time: the caller gives up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long long limit = kMbarCycles) {
   bool ok = mbar_try(bar, parity);
   if (!ok) {
     const long long began = clock64();
 #pragma unroll 1
     do ok = mbar_try(bar, parity);
-    while (!ok && clock64() - began < kMbarCycles);
+    while (!ok && clock64() - began < limit);
   }
   return __all_sync(0xFFFFFFFFu, ok);
 }
 
 // The same by one lane.
-__device__ __forceinline__ bool mbar_wait_lane(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait_lane(uint32_t bar, uint32_t parity, long long limit) {
   if (mbar_try(bar, parity)) return true;
   const long long began = clock64();
 #pragma unroll 1
   do {
     if (mbar_try(bar, parity)) return true;
-  } while (clock64() - began < kMbarCycles);
+  } while (clock64() - began < limit);
   return false;
 }
 
