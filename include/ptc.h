@@ -675,7 +675,10 @@ ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* 
  * With mass_out the weights that each cached token receives are added up over
  * the new tokens and over the query heads of its key head, for ptc_kv_evict:
  *   mass_out[h][S] = mass_in[h][S] + sum exp(s_j - lse),  S = page_off[r] * block_size + j
- * for j < n, and 0 for the rest of request r's slots.  mass_in and mass_out are
+ * for j < n, and 0 for the rest of request r's slots.  Slots of page_ids before
+ * page_off[0] and from page_off[n_req] on are no request's: there mass_out takes
+ * mass_in's values, and so stays as it is where it is mass_in (n_req = 0 writes
+ * nothing).  mass_in and mass_out are
  * f32[n_kv_heads, mass_stride], mass_stride >= n_page_ids * block_size and at
  * most 2^40; mass_in may be NULL (zeros) or mass_out itself.  More than 2^38
  * slots in page_ids, or 2^31 query rows, are PTC_ERR_OVERFLOW.
@@ -711,7 +714,8 @@ ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q, const int6
  *   new_len_out   u32[n_req]: b
  *   new_mass_out  f32[n_kv_heads, new_mass_stride], new_mass_stride >=
  *                 n_dst_page_ids * block_size: the kept tokens' weights at their
- *                 new slots, 0 in the requests' other slots; not mass itself
+ *                 new slots, 0 in all other slots of dst_page_ids (n_req = 0
+ *                 writes nothing); not mass itself
  */
 size_t ptc_kv_evict_workspace_bytes(uint32_t n_req, uint32_t n_kv_heads, uint32_t max_kv_len);
 ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, uint64_t mass_stride, uint32_t n_keep,

@@ -158,6 +158,12 @@ __global__ void __launch_bounds__(kSelThreads, 2) k_evict_select(const EvictArgs
     a.new_len[r] = b;
     if (!ok) report(a.status, PTC_ERR_INVALID_ARG);
   }
+  if (r == 0) {  // slots of no request
+    const uint64_t lo = a.dst_off[0] * a.kv.B, hi = a.dst_off[a.kv.n_req] * a.kv.B, end = a.n_dst_ids * a.kv.B;
+    if (lo <= hi && hi <= end)
+      for (uint64_t i = rank * kSelThreads + tid; i < lo + (end - hi); i += clusters * kSelThreads)
+        a.new_mass[h * a.new_mass_stride + (i < lo ? i : hi + i - lo)] = 0.f;
+  }
   if (!ok) return;  // the whole cluster
   uint32_t* keep = a.keep + ((uint64_t)r * a.kv.H + h) * a.n_keep;
   const float* w = a.mass + h * a.mass_stride + a.kv.page_off[r] * a.kv.B;

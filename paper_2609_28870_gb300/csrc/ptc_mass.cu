@@ -18,6 +18,11 @@
 namespace ptc {
 namespace {
 
+// A slot of no request.
+__device__ __forceinline__ void copy_weight(const AttnArgs& a, uint64_t at) {
+  if (a.mass_in != a.mass_out) a.mass_out[at] = a.mass_in ? a.mass_in[at] : 0.f;
+}
+
 // ------------------------------------------------------------------ few rows
 constexpr int kRowThreads = 256;
 constexpr uint32_t kRowSlots = 4 * kRowThreads;
@@ -28,8 +33,8 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
   __shared__ uint32_t s_r;
   const uint32_t R = a.kv.n_req, B = a.kv.B, h = blockIdx.y;
   const uint64_t first = a.kv.page_off[0] * B, end = a.kv.page_off[R] * B;
-  const uint64_t s0 = first + (uint64_t)blockIdx.x * kRowSlots;
-  if (s0 >= end) return;
+  const uint64_t s0 = (uint64_t)blockIdx.x * kRowSlots, slots = a.kv.n_page_ids * B;
+  if ((s0 + kRowSlots <= first || s0 >= end) && a.mass_in == a.mass_out) return;  // no request's, and in place
   if (threadIdx.x == 0) s_r = req_search(a.kv.page_off, 0, R - 1, s0 / B);
   __syncthreads();
   uint32_t r = s_r;
@@ -37,7 +42,11 @@ __global__ void __launch_bounds__(kRowThreads) k_mass_rows(const AttnArgs a) {
   const uint32_t width = four ? 4 : 1;
   for (uint32_t pass = 0; pass < 4 / width; ++pass) {
     const uint64_t slot = s0 + ((uint64_t)pass * kRowThreads + threadIdx.x) * width;
-    if (slot >= end) return;
+    if (slot >= slots) return;
+    if (slot < first || slot >= end) {
+      for (uint32_t k = 0; k < width; ++k) copy_weight(a, h * a.mass_stride + slot + k);
+      continue;
+    }
     while (r + 1 < R && a.kv.page_off[r + 1] * B <= slot) ++r;
     const int64_t j = (int64_t)(slot - a.kv.page_off[r] * B), n = a.kv.kv_len[r];
     const uint64_t tok0 = a.tok_off[r];
@@ -475,7 +484,8 @@ __global__ void __launch_bounds__(kMassThreads, 1)
 
 // blockIdx.y = 0: the key tiles that CTAs of the kernel above share, as
 // the tile kernel does it for query tiles.  1: what no unit covers, the slots
-// past every request's tokens and the requests without queries.
+// past every request's tokens, the requests without queries and the slots of
+// no request.
 __global__ void __launch_bounds__(kMassKeys) k_mass_join(const AttnArgs a) {
   grid_dep_sync();
   const AttnPlan* plan = a.plan + 1;
@@ -488,6 +498,12 @@ __global__ void __launch_bounds__(kMassKeys) k_mass_join(const AttnArgs a) {
       const uint64_t room = (a.kv.page_off[r + 1] - a.kv.page_off[r]) * a.kv.B;
       for (uint64_t j = (a.tok_off[r] == a.tok_off[r + 1] ? 0 : n) + tid; j < room; j += kMassKeys)
         a.mass_out[at + j] = j < n && a.mass_in ? a.mass_in[at + j] : 0.f;
+    }
+    const uint64_t lo = a.kv.page_off[0] * a.kv.B, hi = a.kv.page_off[a.kv.n_req] * a.kv.B;
+    const uint64_t none = lo + a.kv.n_page_ids * a.kv.B - hi;  // slots of no request
+    for (uint64_t i = (uint64_t)c * kMassKeys + tid; i < none * a.kv.H; i += (uint64_t)gridDim.x * kMassKeys) {
+      const uint64_t h = i / none, x = i - h * none;
+      copy_weight(a, h * a.mass_stride + (x < lo ? x : hi + x - lo));
     }
     return;
   }

@@ -173,7 +173,8 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
     """Causal attention of new tokens ``q`` [tokens, query heads, head_dim] over
     their requests' pages.  Returns (out, lse), with ``mass`` (the weights
     accumulated so far, float32 [key heads, slots]) or ``mass_out`` (where the
-    new sums go; may be ``mass`` itself) also the accumulated weights.  ``scale``
+    new sums go; may be ``mass`` itself) also the accumulated weights, which in
+    slots of no request are what they were (zero without ``mass``).  ``scale``
     defaults to head_dim ** -0.5."""
     p, dev, shape = _pkg(), k.get_device(), k.shape
     kv = _paged(k, v, page_ids, page_off, kv_len, shape, dev)
@@ -209,6 +210,10 @@ def ptc_paged_attention(q, k, v, page_ids, page_off, tok_off, kv_len, max_q_len:
         if mass_out.shape[0] != shape[1]:
             raise ValueError("mass: expected one row a key head")
         slots, m_out = mass_out.shape[1], mass_out.data_ptr()
+        # the call writes the slots of page_ids, and without requests none
+        first = page_ids.shape[0] * shape[2] if kv_len.shape[0] else 0
+        if slots > first and m_in != m_out:
+            mass_out[:, first:] = 0 if mass is None else mass[:, first:]
     L = p.lib()
     w = _room(k, L.ptc_paged_attention_workspace_bytes(kv_len.shape[0], Hq, shape[1], D, max_q_len, slots), dev, ws)
     rc = L.ptc_paged_attention(kv, q.data_ptr(), qs, tok_off.data_ptr(), T, Hq, max_q_len,
@@ -223,7 +228,8 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
     """Cuts every request to n_keep tokens a key head (the first n_sink, the
     last n_recent and the heaviest others) and moves them to the destination
     pages.  Returns (keep int32 [requests, key heads, n_keep], new_len int32,
-    new_mass float32 [key heads, destination slots])."""
+    new_mass float32 [key heads, destination slots], zero where no token was
+    moved)."""
     p, dev, shape = _pkg(), k.get_device(), k.shape
     kv = _paged(k, v, page_ids, page_off, kv_len, shape, dev)
     _want(mass, torch.float32, "mass", dev, 2)
@@ -241,6 +247,8 @@ def ptc_kv_evict(k, v, page_ids, page_off, kv_len, mass, dst_page_ids, dst_page_
     new_len = torch.empty(n_req, dtype=torch.int32, device=k.device)
     slots = dst_page_ids.shape[0] * shape[2]
     new_mass = torch.empty((heads, slots), dtype=torch.float32, device=k.device)
+    if n_req == 0:
+        new_mass.zero_()  # the call has nothing to do
     L = p.lib()
     w = _room(k, L.ptc_kv_evict_workspace_bytes(n_req, heads, max_kv_len), dev, ws) if status is None else None
     rc = L.ptc_kv_evict(kv, mass.data_ptr(), mass.shape[1], n_keep, n_sink, n_recent, max_kv_len,
