@@ -662,7 +662,8 @@ ptc_status ptc_kv_append(const ptc_paged_kv* kv, const void* k_new, const void* 
  * of which at most PTC_MAX_GROUP share one.
  *   s_j = scale * <q, k_j>,  lse = log sum_j exp(s_j),  out = sum_j exp(s_j - lse) v_j
  * A token that sees no key (i < m - n) gets out = 0 and lse = -infinity.
- * Products are summed in 32 bits; the weights are rounded to the cache's dtype
+ * Products are summed in 32 bits; exponentials and logarithms are the
+ * hardware's, good to about 2^-21; the weights are rounded to the cache's dtype
  * before they meet the values (their sum is not).  Slots at or after kv_len[r]
  * may hold anything, NaN included; a NaN or infinite value before that may
  * reach any new token of its request, also one that does not see it.

@@ -306,10 +306,15 @@ struct Weights<__half> {
 //
 // Bounds.  Single tokens: HBM; 12 contexts of 32K to 131K, 1.81 GB, take 275 us,
 // 6.6 TB/s.  Chunks: the tensor cores; a unit of 256 rows and 128 keys is 2,048
-// cycles of products at D = 128 and takes 2,800 (4,096 tokens at 32K: 1.23 ms,
-// 1.67 PFLOP/s).  A half's own chain (softmax 1,260,
-// its two products 1,024, four hand-overs) is 2,600, and what the products and
-// copies move through shared memory, 256 KB, 2,048 cycles at 128 bytes a cycle.
+// cycles of products at D = 128 and takes 2,700 (4,096 tokens at 32K: 1.22 ms in
+// a few calls, 1.69 PFLOP/s, the tensor pipe 75% active at 1.84 GHz; 1.37 ms,
+// 1.50 PFLOP/s, in many, where the power cap takes the clock down).  A half's own
+// chain (softmax 1,260, its two products 1,024, four hand-overs) is 2,600, and
+// what the products and copies move through shared memory, 256 KB, 2,048 cycles
+// at 128 bytes a cycle.  At D <= 64 a unit takes 2,600 cycles for 1,024 of
+// products and 1,024 of exponentials: the softmax's chain alone (2,048 tokens at
+// 20K, 32 heads of 64: 387 us for 182 of products).  Short query tiles: their
+// way out and the joins (40 prompts of 100 to 300 tokens 75 us for 23).
 enum { kRowsApart = 0, kTilesApart = 1, kColumnsApart = 2 };
 constexpr int kTileThreads = 384;
 constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
@@ -1128,7 +1133,10 @@ __device__ __forceinline__ bool copy_role(const AttnArgs& a, TileShared& sh, con
 }
 
 // The same for page sizes that are no multiple of 8 (a swizzled tile takes
-// copies of whole groups of 8 rows): 64 threads copy 16 bytes each.
+// copies of whole groups of 8 rows): 64 threads copy 16 bytes each.  Ten times
+// slower, and bound by these threads' own steps, two divisions and a page id for
+// every 16 bytes: with pages of 12, 64 single tokens (0.89 GB) take 1.56 ms for
+// 0.16 with pages of 16, 4,096 tokens at 32K 10.8 ms for 1.22.
 template <int NSLAB, int KIND>
 __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, uint32_t ring) {
   using Sh = TileShape<NSLAB, KIND>;

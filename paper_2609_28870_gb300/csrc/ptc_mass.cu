@@ -365,8 +365,9 @@ __device__ __forceinline__ bool mass_queries(const AttnArgs& a, MassShared& sh, 
   return true;
 }
 
-// Key tiles, by tensor copies (one warp) or 16 bytes at a time (two).  Pages
-// that the cache does not have were reported by the tile kernel.
+// Key tiles, by tensor copies (one warp) or 16 bytes at a time (two, each tile
+// waited for: pages of 12 take the call of 4 chunks above from 508 us to 2.5 ms).
+// Pages that the cache does not have were reported by the tile kernel.
 template <int NSLAB, bool TMA>
 __device__ __forceinline__ bool mass_keys(const AttnArgs& a, MassShared& sh, const CUtensorMap* mk, uint32_t smem,
                                           uint32_t& seg) {
