@@ -725,6 +725,107 @@ ptc_status ptc_kv_evict(const ptc_paged_kv* kv, const float* mass, uint64_t mass
                         uint32_t* new_len_out, float* new_mass_out, uint64_t new_mass_stride, void* ws,
                         size_t ws_bytes, uint32_t* status, void* stream);
 
+/*
+ * Rotary positions.  A head's first 2 n_freq channels are n_freq pairs, pair i
+ * of a token at position p turned by the angle p * freq[i]:
+ *   x' = x cos - y sin,  y' = y cos + x sin
+ * Pair i is channels (2 i, 2 i + 1) where interleaved, (i, n_freq + i) where not;
+ * channels from 2 n_freq on stay as they are.
+ *   table         f32[n_pos][2][n_freq], 16-byte aligned: the cosines of position
+ *                 p's angles, then their sines, as ptc_rope_table makes it or with
+ *                 any other values
+ *   pos           u32[n_tok]: every new token's position, or NULL: a token's
+ *                 position is its place among its request's kv_len tokens.  (After
+ *                 an eviction the two differ.)  A position at or above n_pos is
+ *                 PTC_ERR_INVALID_ARG, and nothing is written for its token
+ * A turned channel is rounded once to 16 bits (products and sum are as good as
+ * exact before that).
+ */
+typedef struct {
+  const float* table;
+  const uint32_t* pos;
+  uint32_t n_pos, n_freq;
+  int32_t interleaved;
+} ptc_rope;
+
+/*
+ * ptc_rope_table — table[p][0][i] = factor * cos(p * freq[i]) and table[p][1][i] =
+ * factor * sin(p * freq[i]) for p < n_pos, to 2^-22 * factor up to angles of 2^24:
+ * they are reduced in 64 bits.  freq: f64[n_freq] in device memory,
+ * radians, finite (others give NaN), 1 <= n_freq <= PTC_MAX_HEAD_DIM / 2; factor
+ * finite.  Returns when its work is enqueued.
+ */
+ptc_status ptc_rope_table(const double* freq, uint32_t n_freq, uint32_t n_pos, float factor, float* table, void* stream);
+
+/*
+ * ptc_kv_append_rope — ptc_kv_append with the new keys turned on the way, and the
+ * new tokens' queries with them.
+ *   q, q_out      [n_tok, n_q_heads, head_dim], the cache's dtype; token and head
+ *                 strides in elements, as for the cache; 16-byte aligned.  q_out
+ *                 may be q itself, with q's strides, but not overlap it otherwise.
+ *                 n_q_heads = 0: no queries, and q, q_out and their strides are
+ *                 not used
+ */
+size_t ptc_kv_append_rope_workspace_bytes(uint32_t n_req);
+ptc_status ptc_kv_append_rope(const ptc_paged_kv* kv, const ptc_rope* rope, const void* q, const int64_t q_stride[2],
+                              void* q_out, const int64_t q_out_stride[2], uint32_t n_q_heads, const void* k_new,
+                              const void* v_new, const int64_t k_new_stride[2], const int64_t v_new_stride[2],
+                              const uint64_t* tok_off, uint64_t n_tok, void* ws, size_t ws_bytes, uint32_t* status,
+                              void* stream);
+
+/*
+ * Pages of 4 bits.  A ptc_paged_kv whose k and v are rows of ptc_kv4_row_bytes
+ * bytes, a row a (page, head, slot) at page * stride[0] + head * stride[1] + slot *
+ * stride[2], strides in bytes and positive multiples of 16; dtype is the 16-bit
+ * type that the rows stand for.  32 channels of a row (the last group of a head
+ * may have fewer) share a scale s and a base b of that type, and code c of a
+ * channel stands for
+ *   (16 + c) * s + b, rounded to 16 bits.
+ * The calls that write rows take, of a group with the extremes lo and hi,
+ *   s = (hi - lo) / 15,  b = lo - 16 s,  c = floor((x - b) / s - 15.5) in [0, 15]
+ * (0 where s = 0), s and b rounded to 16 bits before they are used; the arithmetic
+ * is as good as exact.  A group that holds a NaN or an infinity, or a range that
+ * makes s or b infinite (for fp16: values from about 20,000 on), reads as NaN.
+ * Row layout: words of 32 bits; word i holds the codes of channels 8 i .. 8 i + 7,
+ * the even ones in its low half and the odd ones in its high half, from the lowest
+ * bits; then, from byte 32 (64 for head_dim > 64), a word for each group, s in the
+ * low half and b in the high half; zeros.
+ */
+uint32_t ptc_kv4_row_bytes(uint32_t head_dim); /* 48 up to head_dim 64, 80 up to 128 */
+
+/*
+ * ptc_kv4_append — ptc_kv_append into pages of 4 bits.  rope (may be NULL) turns
+ * the new keys, and the queries with them, as in ptc_kv_append_rope, before they
+ * are quantised; without it n_q_heads must be 0.
+ */
+size_t ptc_kv4_append_workspace_bytes(uint32_t n_req);
+ptc_status ptc_kv4_append(const ptc_paged_kv* kv, const ptc_rope* rope, const void* q, const int64_t q_stride[2],
+                          void* q_out, const int64_t q_out_stride[2], uint32_t n_q_heads, const void* k_new,
+                          const void* v_new, const int64_t k_new_stride[2], const int64_t v_new_stride[2],
+                          const uint64_t* tok_off, uint64_t n_tok, void* ws, size_t ws_bytes, uint32_t* status,
+                          void* stream);
+
+/*
+ * ptc_kv4_read — the values of the last tok_off[r+1] - tok_off[r] tokens of every
+ * request (all of them, where that is kv_len[r]): k_out, v_out [n_tok, n_kv_heads,
+ * head_dim], the cache's dtype, contiguous, 16-byte aligned.  Nothing is written for
+ * a request that ptc_kv_append would not write.
+ */
+size_t ptc_kv4_read_workspace_bytes(uint32_t n_req);
+ptc_status ptc_kv4_read(const ptc_paged_kv* kv, const uint64_t* tok_off, uint64_t n_tok, void* k_out, void* v_out,
+                        void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
+/*
+ * ptc_kv4_attention — ptc_paged_attention, without accumulated weights, over pages
+ * of 4 bits: the same arguments, masks, roundings and refusals.  A tensor of
+ * queries and its outputs have the cache's dtype.
+ */
+size_t ptc_kv4_attention_workspace_bytes(uint32_t n_req, uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t head_dim,
+                                         uint32_t max_q_len);
+ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, const int64_t q_stride[2], const uint64_t* tok_off,
+                             uint64_t n_tok, uint32_t n_q_heads, uint32_t max_q_len, float scale, void* out, float* lse,
+                             void* ws, size_t ws_bytes, uint32_t* status, void* stream);
+
 /* Frees the calling thread's page-locked staging block (see the
  * conventions above); safe to call at any time between calls. */
 void ptc_release_host_staging(void);

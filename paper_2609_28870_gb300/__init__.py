@@ -12,7 +12,9 @@ CUDA kernels.  PyTorch provides device memory and the current CUDA stream.
     curves               = ptc_curves(dist, req_blk_off, 16, caps, PTC_COST_MEASURED)
 
 and for the cached state itself (keys and values in pages, see ``kv``):
-ptc_kv_append, ptc_paged_attention, ptc_kv_evict.
+ptc_kv_append, ptc_paged_attention, ptc_kv_evict; with rotary positions (see
+``rope``): ptc_rope_table, ptc_kv_append_rope; with pages of 4 bits (see ``kv4``):
+ptc_kv4_append, ptc_kv4_read, ptc_kv4_attention.
 
 Arrays are torch CUDA tensors, on the current device (a call on another
 device's is refused).  Unsigned 32/64-bit arrays travel as int32 /
@@ -30,8 +32,12 @@ import torch
 
 from . import build as _build
 from . import kv as _kv
+from . import kv4 as _kv4
+from . import rope as _rope
 from .kv import (MAX_GROUP, MAX_HEAD_DIM, PTC_DTYPE_BF16, PTC_DTYPE_FP16, check_status, ptc_kv_append,  # noqa: F401
                  ptc_kv_evict, ptc_paged_attention)
+from .kv4 import kv4_row_bytes, ptc_kv4_append, ptc_kv4_attention, ptc_kv4_read  # noqa: F401
+from .rope import ptc_kv_append_rope, ptc_rope_table, rope_frequencies  # noqa: F401
 
 PTC_NONE = 0xFFFFFFFF
 PTC_COST_UNIFORM, PTC_COST_MEASURED, PTC_COST_LINEAR = 0, 1, 2
@@ -202,6 +208,8 @@ def lib():
                 L.ptc_launch_count.restype = u64
                 L.ptc_launch_count.argtypes = []
                 _kv.declare(L)
+                _rope.declare(L)
+                _kv4.declare(L)
                 del i64
                 _lib = L
     return _lib

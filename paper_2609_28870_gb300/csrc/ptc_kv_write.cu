@@ -1,0 +1,419 @@
+// New tokens on their way into the pages, turned and quantised
+// (ptc_kv_append_rope, ptc_kv4_append), and back (ptc_kv4_read).
+#include "ptc_kv4.cuh"
+
+namespace ptc {
+namespace {
+
+constexpr int kWrThreads = 256;
+constexpr int kWrRows = 4;  // rows of a token that a thread has in flight
+
+struct WriteArgs {
+  KvView kv;
+  RopeView rope;
+  const char* q;
+  char* q_out;
+  int64_t q_tok, q_head, o_tok, o_head;
+  const char* kn;
+  const char* vn;
+  int64_t kn_tok, kn_head, vn_tok, vn_head;
+  char* k_out;  // of ptc_kv4_read
+  char* v_out;
+  const uint64_t* tok_off;
+  uint64_t n_tok;
+  uint32_t n_q_heads, slice, rows;  // rows of a token, and those that a CTA takes
+  uint32_t* status;
+};
+
+// Where a token's row of head 0 lies in the pages, or k = -1, and its position.
+struct Place {
+  int64_t k, v;
+  uint32_t pos;
+};
+
+// The first CTA of a call looks whether the offsets are in order.
+__device__ __forceinline__ void check_offsets(const WriteArgs& a) {
+  if (blockIdx.x || blockIdx.y) return;
+  bool bad = threadIdx.x == 0 && (a.tok_off[0] != 0 || a.tok_off[a.kv.n_req] != a.n_tok);
+  for (uint32_t r = threadIdx.x; r < a.kv.n_req; r += kWrThreads) bad |= a.tok_off[r] > a.tok_off[r + 1];
+  if (bad) report(a.status, PTC_ERR_INVALID_ARG);
+}
+
+__device__ __forceinline__ Place find_place(const WriteArgs& a, uint64_t t) {
+  Place at{-1, -1, 0};
+  const uint32_t r = req_search(a.tok_off, 0, a.kv.n_req - 1, t);
+  const uint64_t lo = a.tok_off[r], hi = a.tok_off[r + 1];
+  const uint64_t n = a.kv.kv_len[r];
+  if (lo <= t && t < hi && hi <= a.n_tok && hi - lo <= n && pages_hold(a.kv, r, n)) {
+    const uint64_t j = n - (hi - t);
+    const uint32_t page = a.kv.page_ids[a.kv.page_off[r] + j / a.kv.B];
+    const int64_t slot = (int64_t)(j % a.kv.B);
+    at.pos = a.rope.pos ? a.rope.pos[t] : (uint32_t)j;
+    if (page < a.kv.n_pages && (!a.rope.table || at.pos < a.rope.n_pos)) {
+      at.k = (int64_t)page * a.kv.ks_page + slot * a.kv.ks_slot;
+      at.v = (int64_t)page * a.kv.vs_page + slot * a.kv.vs_slot;
+    }
+  }
+  if (at.k < 0) report(a.status, PTC_ERR_INVALID_ARG);
+  return at;
+}
+
+// How a thread's eight channels are turned: by the same angles for all heads of
+// a token, so they are kept.  sn has its sign: channel e becomes
+// x[e] cs[e] - partner sn[e].
+struct Turn {
+  float cs[8], sn[8];
+  uint32_t which;  // the channels that are turned, a bit each
+};
+
+__device__ __forceinline__ void load_turn(const RopeView& rope, uint32_t pos, uint32_t c, Turn& o) {
+  const uint32_t F = rope.n_freq;
+  const float* row = rope.table + (uint64_t)pos * 2 * F;
+  o.which = 0;
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    const uint32_t d = 8 * c + e;
+    const uint32_t i = rope.interleaved ? d / 2 : d < F ? d : d - F;
+    const bool second = rope.interleaved ? d & 1 : d >= F;
+    o.cs[e] = 1.f;
+    o.sn[e] = 0.f;
+    if (d < 2 * F) {
+      o.which |= 1u << e;
+      o.cs[e] = __ldg(row + i);
+      const float s = __ldg(row + F + i);
+      o.sn[e] = second ? -s : s;
+    }
+  }
+}
+
+// A row's channels turned; x: the thread's eight, row: all of them in global
+// memory.  By all lanes of the row (c: the lane's place among them).
+template <typename T, int LANES>
+__device__ __forceinline__ uint4 turn_row(const RopeView& rope, const Turn& t, const uint4& x, const char* row, uint32_t c,
+                                          bool live) {
+  const uint32_t F = rope.n_freq;
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t p[4] = {x.x, x.y, x.z, x.w};
+  if (!rope.interleaved) {
+    if (F % 8 == 0) {
+      const uint32_t f = F / 8, other = c < f ? c + f : c < 2 * f ? c - f : c;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(kFull, w[k], other, LANES);
+    } else if (live) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t d = 8 * c + e;
+        if (t.which >> e & 1) {
+          const uint32_t y = *reinterpret_cast<const uint16_t*>(row + 2 * (d < F ? d + F : d - F));
+          p[e / 2] = e & 1 ? (p[e / 2] & 0xFFFFu) | y << 16 : (p[e / 2] & 0xFFFF0000u) | y;
+        }
+      }
+    }
+  }
+  uint32_t o[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 a = Half16<T>::get2(w[k]), b = Half16<T>::get2(p[k]);
+    const float px = rope.interleaved ? b.y : b.x, py = rope.interleaved ? b.x : b.y;
+    const uint32_t lo = t.which >> (2 * k) & 1 ? turn<T>(a.x, t.cs[2 * k], px, t.sn[2 * k]) : w[k] & 0xFFFFu;
+    const uint32_t hi = t.which >> (2 * k + 1) & 1 ? turn<T>(a.y, t.cs[2 * k + 1], py, t.sn[2 * k + 1]) : w[k] >> 16;
+    o[k] = lo | hi << 16;
+  }
+  return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// What 32 bits do not settle of a group's scale, its base and a code.  (Inlined,
+// these were computed for every group and picked from afterwards, at the 64-bit
+// unit's sixtieth of the rate.)
+template <typename T>
+__device__ __noinline__ T scale_wide(float lo, float hi) {
+  return Half16<T>::put(((double)hi - (double)lo) / 15.0);
+}
+template <typename T>
+__device__ __noinline__ T base_wide(float lo, float s) {
+  return Half16<T>::put((double)lo - 16.0 * (double)s);
+}
+__device__ __noinline__ float code_wide(float v, float b, float s) {
+  return (float)floor(((double)v - (double)b) / (double)s - 15.5);
+}
+
+// The codes of eight channels, and their group's scale and base.  A group is
+// four threads' channels; a thread without channels (real = false) takes part.
+template <typename T>
+__device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t& words) {
+  using Two = typename Half16<T>::Two;
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  auto two = [](uint32_t v) { return *reinterpret_cast<const Two*>(&v); };
+  auto raw = [](Two v) { return *reinterpret_cast<const uint32_t*>(&v); };
+  constexpr uint32_t kInf2 = Half16<T>::kBf16 ? 0x7F807F80u : 0x7C007C00u;
+  // the smallest and the largest with its sign changed, in one word; NaN stays
+  const Two small = __hmin2_nan(__hmin2_nan(two(w[0]), two(w[1])), __hmin2_nan(two(w[2]), two(w[3])));
+  const Two large = __hmax2_nan(__hmax2_nan(two(w[0]), two(w[1])), __hmax2_nan(two(w[2]), two(w[3])));
+  const uint32_t a = raw(small), b = raw(large) ^ 0x80008000u;
+  uint32_t m = raw(__hmin2_nan(two(__byte_perm(a, b, 0x5410)), two(__byte_perm(a, b, 0x7632))));
+  if (!real) m = kInf2;
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) m = raw(__hmin2_nan(two(m), two(__shfl_xor_sync(kFull, m, o))));
+  const float2 ends = Half16<T>::get2(m);
+  const float lo = ends.x, hi = -ends.y;
+  words = 0;
+  if (m == kInf2) return 0;  // no channel in the group (an infinity among them makes the other end finite or -infinity)
+  const float d = hi - lo, s32 = d / 15.f;
+  const T s = Half16<T>::unsure(s32) || !(d < INFINITY) ? scale_wide<T>(lo, hi) : Half16<T>::put(s32);
+  const float sf = Half16<T>::get(s), s16 = 16.f * sf, b32 = lo - s16, back = b32 - lo;
+  const float left = (lo - (b32 - back)) + (-s16 - back);  // what the subtraction lost
+  const T base = (left != 0.f && Half16<T>::unsure(b32)) || !(s16 < INFINITY) ? base_wide<T>(lo, sf) : Half16<T>::put(b32);
+  const float bf = Half16<T>::get(base);
+  if (!(sf < INFINITY) || !(fabsf(bf) < INFINITY)) {
+    words = Half16<T>::kBf16 ? 0x7FC07FC0u : 0x7E007E00u;
+    return 0;
+  }
+  words = bits16(s) | bits16(base) << 16;
+  if (sf == 0.f || !real) return 0;
+  uint32_t code = 0;
+  const float inv = 1.f / sf, half = 0.5f * sf;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float2 pair = Half16<T>::get2(w[e / 2]);
+    const float v = e & 1 ? pair.y : pair.x, y = v - bf;
+    float k = fminf(fmaxf(rintf(fmaf(y, inv, -16.f)), 0.f), 15.f);
+    const float r = fmaf(-(k + 16.f), sf, y);  // exact within a step
+    // k is the nearest code or, by the division's rounding, beside it; a value
+    // half way goes up, and on that border what y's subtraction lost decides
+    float lost = 0.f;
+    if (fabsf(r) == half) {
+      const float z = y - v;
+      lost = (v - (y - z)) + (-bf - z);
+    }
+    k += (r > half || (r == half && lost >= 0.f) ? 1.f : 0.f) - (r < -half || (r == -half && lost < 0.f) ? 1.f : 0.f);
+    if (sf < 0x1p-100f) k = code_wide(v, bf, sf);
+    k = fminf(fmaxf(k, 0.f), 15.f);
+    code |= (uint32_t)k << (4 * (e / 2) + 16 * (e & 1));
+  }
+  return code;
+}
+
+// The rows of tokens: queries, keys and values, LANES threads a row with eight
+// channels each (so that a row stays within a warp: it may be turned in place).
+// A group of LANES threads stays with its token and takes `slice` of its rows;
+// each row is read and written once, so HBM bounds it.
+template <typename T, int LANES, bool FOUR>
+__global__ void __launch_bounds__(kWrThreads) k_kv_write(const __grid_constant__ WriteArgs a) {
+  grid_dep_sync();
+  constexpr uint32_t kTok = kWrThreads / LANES;
+  __shared__ Place s_at[kTok];
+  const uint64_t t0 = (uint64_t)blockIdx.x * kTok;
+  check_offsets(a);
+  if (threadIdx.x < kTok) s_at[threadIdx.x] = t0 + threadIdx.x < a.n_tok ? find_place(a, t0 + threadIdx.x) : Place{-1, -1, 0};
+  __syncthreads();
+  const Place at = s_at[threadIdx.x / LANES];
+  const int64_t t = (int64_t)t0 + threadIdx.x / LANES;
+  const uint32_t c = threadIdx.x % LANES, D = a.kv.D, Hq = a.n_q_heads, H = a.kv.H;
+  const bool live = at.k >= 0, real = 8 * c < D;
+  const bool turned = a.rope.table != nullptr;
+  Turn angles;
+  if (turned && live && real) load_turn(a.rope, at.pos, c, angles);
+  else angles.which = 0;
+  const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
+  auto source = [&](uint32_t r) {
+    if (r < Hq) return a.q + 2 * (t * a.q_tok + r * a.q_head);
+    if (r < Hq + H) return a.kn + 2 * (t * a.kn_tok + (r - Hq) * a.kn_head);
+    return a.vn + 2 * (t * a.vn_tok + (r - Hq - H) * a.vn_head);
+  };
+  for (uint32_t r0 = first; r0 < end; r0 += kWrRows) {
+    uint4 x[kWrRows];
+#pragma unroll
+    for (int u = 0; u < kWrRows; ++u) {
+      x[u] = make_uint4(0, 0, 0, 0);
+      if (r0 + u < end && live && real) x[u] = *reinterpret_cast<const uint4*>(source(r0 + u) + 16 * c);
+    }
+#pragma unroll
+    for (int u = 0; u < kWrRows; ++u) {
+      const uint32_t r = r0 + u;
+      if (r >= end) break;  // the whole CTA
+      uint4 y = x[u];
+      if (turned && r < Hq + H) y = turn_row<T, LANES>(a.rope, angles, x[u], source(r), c, live);
+      __syncwarp();  // a row is written after all of it was read
+      if (r < Hq) {
+        if (live && real) *reinterpret_cast<uint4*>(a.q_out + 2 * (t * a.o_tok + r * a.o_head) + 16 * c) = y;
+        continue;
+      }
+      const bool key = r < Hq + H;
+      const int64_t head = r - Hq - (key ? 0 : H);
+      char* to = key ? a.kv.k : a.kv.v;
+      const int64_t place = (key ? at.k : at.v) + head * (key ? a.kv.ks_head : a.kv.vs_head);
+      if (!FOUR) {
+        if (live && real) *reinterpret_cast<uint4*>(to + 2 * place + 16 * c) = y;
+      } else {
+        uint32_t words;
+        const uint32_t code = quantise<T>(y, live && real, words);
+        if (!live) continue;
+        uint32_t* row = reinterpret_cast<uint32_t*>(to + place);
+        row[c] = code;
+        if (c % 4 == 0) row[LANES + c / 4] = words;
+        if (LANES == 8 && c % 4 == 1) row[10 + c / 4] = 0;
+      }
+    }
+  }
+}
+
+template <typename T, int LANES>
+__global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__ WriteArgs a) {
+  grid_dep_sync();
+  constexpr uint32_t kTok = kWrThreads / LANES;
+  __shared__ Place s_at[kTok];
+  const uint64_t t0 = (uint64_t)blockIdx.x * kTok;
+  check_offsets(a);
+  if (threadIdx.x < kTok) s_at[threadIdx.x] = t0 + threadIdx.x < a.n_tok ? find_place(a, t0 + threadIdx.x) : Place{-1, -1, 0};
+  __syncthreads();
+  const Place at = s_at[threadIdx.x / LANES];
+  const uint64_t t = t0 + threadIdx.x / LANES;
+  const uint32_t c = threadIdx.x % LANES, D = a.kv.D, H = a.kv.H;
+  if (at.k < 0 || 8 * c >= D) return;
+  const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
+  for (uint32_t r0 = first; r0 < end; r0 += kWrRows) {
+    uint32_t w[kWrRows], p[kWrRows];
+#pragma unroll
+    for (int u = 0; u < kWrRows; ++u) {
+      const uint32_t r = r0 + u < end ? r0 + u : end - 1;
+      const bool key = r < H;
+      const char* row = key ? a.kv.k + at.k + r * a.kv.ks_head : a.kv.v + at.v + (r - H) * a.kv.vs_head;
+      w[u] = *reinterpret_cast<const uint32_t*>(row + 4 * c);
+      p[u] = *reinterpret_cast<const uint32_t*>(row + 4 * (LANES + c / 4));
+    }
+#pragma unroll
+    for (int u = 0; u < kWrRows; ++u) {
+      const uint32_t r = r0 + u;
+      if (r >= end) break;
+      const uint32_t s = both_low(p[u]), b = both_high(p[u]);
+      const uint4 y = make_uint4(fma16x2<T>(pair4<T>(w[u], 0), s, b), fma16x2<T>(pair4<T>(w[u], 1), s, b),
+                                 fma16x2<T>(pair4<T>(w[u], 2), s, b), fma16x2<T>(pair4<T>(w[u], 3), s, b));
+      char* to = r < H ? a.k_out : a.v_out;
+      *reinterpret_cast<uint4*>(to + 2 * ((t * H + (r < H ? r : r - H)) * D + 8 * c)) = y;
+    }
+  }
+}
+
+// Rows of a CTA: as few as leave four CTAs for every SM, so that a call of few
+// tokens is spread, and at most 8, so that a token's place and angles serve
+// several rows.
+dim3 write_grid(WriteArgs& a, uint32_t tok) {
+  const uint64_t blocks = (a.n_tok + tok - 1) / tok;
+  uint64_t slice = blocks * a.rows / (4 * (uint64_t)num_sms());
+  a.slice = (uint32_t)(slice < 1 ? 1 : slice > 8 ? 8 : slice);
+  if ((a.rows + a.slice - 1) / a.slice > 65535) a.slice = (a.rows + 65534) / 65535;
+  return dim3((uint32_t)blocks, (a.rows + a.slice - 1) / a.slice);
+}
+
+template <typename T, bool FOUR>
+void launch_write(WriteArgs& a, cudaStream_t s) {
+  const char* name = FOUR ? "k_kv4_append" : "k_kv_append_rope";
+  if (a.kv.D <= 64) PTC_KERNEL(name, s, (k_kv_write<T, 8, FOUR>), write_grid(a, kWrThreads / 8), kWrThreads, 0, a);
+  else PTC_KERNEL(name, s, (k_kv_write<T, 16, FOUR>), write_grid(a, kWrThreads / 16), kWrThreads, 0, a);
+}
+template <typename T>
+void launch_read(WriteArgs& a, cudaStream_t s) {
+  if (a.kv.D <= 64) PTC_KERNEL("k_kv4_read", s, (k_kv4_read<T, 8>), write_grid(a, kWrThreads / 8), kWrThreads, 0, a);
+  else PTC_KERNEL("k_kv4_read", s, (k_kv4_read<T, 16>), write_grid(a, kWrThreads / 16), kWrThreads, 0, a);
+}
+
+// What ptc_kv_append_rope and ptc_kv4_append have in common.
+template <bool FOUR>
+ptc_status write_tokens(const ptc_paged_kv* kv, const ptc_rope* rope, const void* q, const int64_t q_stride[2], void* q_out,
+                        const int64_t q_out_stride[2], uint32_t n_q_heads, const void* k_new, const void* v_new,
+                        const int64_t k_new_stride[2], const int64_t v_new_stride[2], const uint64_t* tok_off, uint64_t n_tok,
+                        void* ws, size_t ws_bytes, uint32_t* status, void* stream) {
+  WriteArgs a{};
+  ptc_status st = FOUR ? kv4_view(kv, &a.kv) : kv_view(kv, &a.kv);
+  if (st == PTC_OK && rope) st = rope_view(rope, kv->head_dim, &a.rope);
+  if (st != PTC_OK) return st;
+  if (!tok_off || !k_new_stride || !v_new_stride || (n_tok && !kv->n_req) || (n_q_heads && (!rope || !q_stride || !q_out_stride)))
+    return PTC_ERR_INVALID_ARG;
+  if (n_q_heads > 65535u * PTC_MAX_GROUP) return PTC_ERR_INVALID_ARG;
+  if (n_tok > (uint64_t(1) << 31)) return PTC_ERR_OVERFLOW;
+  if (!status && !ws_ok(ws, ws_bytes, kKvStatusBytes)) return PTC_ERR_WORKSPACE;
+  if (n_tok == 0) return PTC_OK;
+  if (!aligned16(k_new) || !aligned16(v_new) || (n_q_heads && (!aligned16(q) || !aligned16(q_out)))) return PTC_ERR_INVALID_ARG;
+  const uint32_t ext[2] = {(uint32_t)n_tok, kv->n_kv_heads}, q_ext[2] = {(uint32_t)n_tok, n_q_heads};
+  for (int i = 0; i < 2; ++i) {
+    if (!stride_ok(k_new_stride[i], ext[i]) || !stride_ok(v_new_stride[i], ext[i])) return PTC_ERR_INVALID_ARG;
+    if (n_q_heads && (!stride_ok(q_stride[i], q_ext[i]) || !stride_ok(q_out_stride[i], q_ext[i]))) return PTC_ERR_INVALID_ARG;
+    if (n_q_heads && q == q_out && q_ext[i] > 1 && q_stride[i] != q_out_stride[i]) return PTC_ERR_INVALID_ARG;
+  }
+  if (rope && !rope->n_pos) return PTC_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  a.n_q_heads = n_q_heads;
+  if (n_q_heads) {
+    a.q = static_cast<const char*>(q);
+    a.q_out = static_cast<char*>(q_out);
+    a.q_tok = stride_of(q_stride[0], q_ext[0]);
+    a.q_head = stride_of(q_stride[1], q_ext[1]);
+    a.o_tok = stride_of(q_out_stride[0], q_ext[0]);
+    a.o_head = stride_of(q_out_stride[1], q_ext[1]);
+  }
+  a.kn = static_cast<const char*>(k_new);
+  a.vn = static_cast<const char*>(v_new);
+  a.kn_tok = stride_of(k_new_stride[0], ext[0]);
+  a.kn_head = stride_of(k_new_stride[1], ext[1]);
+  a.vn_tok = stride_of(v_new_stride[0], ext[0]);
+  a.vn_head = stride_of(v_new_stride[1], ext[1]);
+  a.tok_off = tok_off;
+  a.n_tok = n_tok;
+  a.rows = n_q_heads + 2 * kv->n_kv_heads;
+  if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
+  if (kv->dtype == PTC_DTYPE_BF16) launch_write<__nv_bfloat16, FOUR>(a, s);
+  else launch_write<__half, FOUR>(a, s);
+  return kv_end(status, a.status, s);
+}
+
+}  // namespace
+}  // namespace ptc
+
+using namespace ptc;
+
+extern "C" uint32_t ptc_kv4_row_bytes(uint32_t head_dim) { return row4_bytes(head_dim); }
+extern "C" size_t ptc_kv_append_rope_workspace_bytes(uint32_t) { return kKvStatusBytes; }
+extern "C" size_t ptc_kv4_append_workspace_bytes(uint32_t) { return kKvStatusBytes; }
+extern "C" size_t ptc_kv4_read_workspace_bytes(uint32_t) { return kKvStatusBytes; }
+
+extern "C" ptc_status ptc_kv_append_rope(const ptc_paged_kv* kv, const ptc_rope* rope, const void* q,
+                                         const int64_t q_stride[2], void* q_out, const int64_t q_out_stride[2],
+                                         uint32_t n_q_heads, const void* k_new, const void* v_new,
+                                         const int64_t k_new_stride[2], const int64_t v_new_stride[2],
+                                         const uint64_t* tok_off, uint64_t n_tok, void* ws, size_t ws_bytes,
+                                         uint32_t* status, void* stream) {
+  if (!rope) return PTC_ERR_INVALID_ARG;
+  return write_tokens<false>(kv, rope, q, q_stride, q_out, q_out_stride, n_q_heads, k_new, v_new, k_new_stride, v_new_stride,
+                             tok_off, n_tok, ws, ws_bytes, status, stream);
+}
+
+extern "C" ptc_status ptc_kv4_append(const ptc_paged_kv* kv, const ptc_rope* rope, const void* q, const int64_t q_stride[2],
+                                     void* q_out, const int64_t q_out_stride[2], uint32_t n_q_heads, const void* k_new,
+                                     const void* v_new, const int64_t k_new_stride[2], const int64_t v_new_stride[2],
+                                     const uint64_t* tok_off, uint64_t n_tok, void* ws, size_t ws_bytes,
+                                     uint32_t* status, void* stream) {
+  return write_tokens<true>(kv, rope, q, q_stride, q_out, q_out_stride, n_q_heads, k_new, v_new, k_new_stride, v_new_stride,
+                            tok_off, n_tok, ws, ws_bytes, status, stream);
+}
+
+extern "C" ptc_status ptc_kv4_read(const ptc_paged_kv* kv, const uint64_t* tok_off, uint64_t n_tok, void* k_out, void* v_out,
+                                   void* ws, size_t ws_bytes, uint32_t* status, void* stream) {
+  WriteArgs a{};
+  const ptc_status st = kv4_view(kv, &a.kv);
+  if (st != PTC_OK) return st;
+  if (!tok_off || (n_tok && !kv->n_req)) return PTC_ERR_INVALID_ARG;
+  if (n_tok > (uint64_t(1) << 31)) return PTC_ERR_OVERFLOW;
+  if (!status && !ws_ok(ws, ws_bytes, kKvStatusBytes)) return PTC_ERR_WORKSPACE;
+  if (n_tok == 0) return PTC_OK;
+  if (!aligned16(k_out) || !aligned16(v_out)) return PTC_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  a.k_out = static_cast<char*>(k_out);
+  a.v_out = static_cast<char*>(v_out);
+  a.tok_off = tok_off;
+  a.n_tok = n_tok;
+  a.rows = 2 * kv->n_kv_heads;
+  if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
+  if (kv->dtype == PTC_DTYPE_BF16) launch_read<__nv_bfloat16>(a, s);
+  else launch_read<__half>(a, s);
+  return kv_end(status, a.status, s);
+}

@@ -1,0 +1,77 @@
+// The table of rotary angles (ptc_rope_table).
+#include <cmath>
+
+#include "ptc_rope.cuh"
+
+namespace ptc {
+namespace {
+
+// Angles are kept as fractions of a turn in 64-bit integers: a frequency f is
+// round(f / 2 pi * 2^64) of them a position (its error, 2^-53 of it, grows with
+// the position to 2^-32 of a turn at most), a position's angle the product modulo
+// 2^64, exact.  The two upper bits after rounding to the nearest quarter are the
+// quarter; the rest, within an eighth of a turn, becomes 32-bit radians with a
+// relative error of 2^-23, and the Taylor series about 0 give both functions (next
+// terms: 1.7e-9 and 2.4e-9).  Bound by what it writes: a thread has a frequency and
+// goes down the positions, a warp writes 128 bytes in a row.
+constexpr int kTableThreads = 256;
+
+struct TableArgs {
+  const double* freq;
+  float* table;
+  uint32_t n_freq, n_pos;
+  float factor;
+};
+
+__global__ void __launch_bounds__(kTableThreads) k_rope_table(TableArgs a) {
+  grid_dep_sync();
+  const uint32_t F = a.n_freq, across = kTableThreads / F, i = threadIdx.x % F, row = threadIdx.x / F;
+  if (row >= across) return;
+  const double f = a.freq[i];
+  // the fraction of a turn; only its last bits are lost to the division
+  double t = f / 6.283185307179586476925;
+  t -= floor(t);
+  const bool fine = t >= 0.0 && t <= 1.0;  // not of an infinity or NaN
+  const uint64_t step = fine && t < 1.0 ? (uint64_t)(t * 18446744073709551616.0) : 0;
+  for (uint64_t p = (uint64_t)blockIdx.x * across + row; p < a.n_pos; p += (uint64_t)gridDim.x * across) {
+    const uint64_t at = p * step + (uint64_t(1) << 61);
+    const uint32_t quarter = (uint32_t)(at >> 62);
+    const int64_t rest = (int64_t)(at & ((uint64_t(1) << 62) - 1)) - (int64_t(1) << 61);
+    // 2 pi / 2^32 times the rest's upper half, and 2^-32 of that times the lower
+    const float hi = (float)(int32_t)(rest >> 32), lo = (float)(uint32_t)rest;
+    const float x = fmaf(lo, 0x1p-32f, hi) * 1.4629180792671596e-9f, z = x * x;
+    float s = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), 0.f);
+    s = fmaf(x, s, x);
+    float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.f / 3628800.f, 1.f / 40320.f), -1.f / 720.f), 1.f / 24.f), -0.5f);
+    c = fmaf(z, c, 1.f);
+    if (quarter & 1) {
+      const float y = s;
+      s = c;
+      c = -y;
+    }
+    if (quarter & 2) {
+      s = -s;
+      c = -c;
+    }
+    if (!fine) s = c = __int_as_float(0x7FC00000);
+    float* to = a.table + p * 2 * F + i;
+    to[0] = a.factor * c;
+    to[F] = a.factor * s;
+  }
+}
+
+}  // namespace
+}  // namespace ptc
+
+using namespace ptc;
+
+extern "C" ptc_status ptc_rope_table(const double* freq, uint32_t n_freq, uint32_t n_pos, float factor, float* table,
+                                     void* stream) {
+  if (n_freq < 1 || n_freq > PTC_MAX_HEAD_DIM / 2 || !std::isfinite(factor)) return PTC_ERR_INVALID_ARG;
+  if (n_pos == 0) return PTC_OK;
+  if (!freq || ((uintptr_t)freq & 7) || !aligned16(table)) return PTC_ERR_INVALID_ARG;
+  const TableArgs a{freq, table, n_freq, n_pos, factor};
+  const uint32_t across = kTableThreads / n_freq, rows = (n_pos - 1) / across + 1, most = 8 * num_sms();
+  PTC_KERNEL("k_rope_table", static_cast<cudaStream_t>(stream), k_rope_table, rows < most ? rows : most, kTableThreads, 0, a);
+  return cudaGetLastError() == cudaSuccess ? PTC_OK : PTC_ERR_CUDA;
+}
