@@ -1,7 +1,7 @@
 // Attention of new tokens over paged keys and values (ptc_paged_attention).
 #include <cmath>
 
-#include "ptc_attn.cuh"
+#include "ptc_attn4.cuh"
 
 namespace ptc {
 namespace {
@@ -1292,13 +1292,17 @@ EncodeFn encoder() {
   return fn;
 }
 
-bool encode(CUtensorMap* map, bool bf16, void* base, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3],
-            const cuuint32_t (&boxes)[4]) {
+bool encode(CUtensorMap* map, CUtensorMapDataType type, CUtensorMapSwizzle swizzle, void* base,
+            const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3], const cuuint32_t (&boxes)[4]) {
   const cuuint32_t steps[4] = {1, 1, 1, 1};
   const EncodeFn fn = encoder();
-  return fn && fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides,
-                  boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  return fn && fn(map, type, 4, base, dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode(CUtensorMap* map, bool bf16, void* base, const cuuint64_t (&dims)[4], const cuuint64_t (&strides)[3],
+            const cuuint32_t (&boxes)[4]) {
+  return encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, CU_TENSOR_MAP_SWIZZLE_128B,
+                base, dims, strides, boxes);
 }
 
 template <typename T, int NSLAB, bool TMA, int KIND>
@@ -1375,6 +1379,13 @@ bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_
   const cuuint64_t strides[3] = {2 * (cuuint64_t)slot, 2 * (cuuint64_t)head, 2 * (cuuint64_t)page};
   const cuuint32_t boxes[4] = {64, box, 1, 1};
   return encode(map, bf16, base, dims, strides, boxes);
+}
+
+bool cache4_map(CUtensorMap* map, const KvView& kv, char* base, int64_t page, int64_t head, int64_t slot, uint32_t box) {
+  const cuuint64_t dims[4] = {row4_bytes(kv.D), kv.B, kv.H, kv.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)slot, (cuuint64_t)head, (cuuint64_t)page};
+  const cuuint32_t boxes[4] = {row4_bytes(kv.D), box, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, CU_TENSOR_MAP_SWIZZLE_NONE, base, dims, strides, boxes);
 }
 
 // The queries as [token][key head][head of the group][d], read 64 columns by

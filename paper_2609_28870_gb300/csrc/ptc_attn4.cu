@@ -1,8 +1,7 @@
 // Attention of new tokens over pages of 4 bits (ptc_kv4_attention).
 #include <cmath>
 
-#include "ptc_attn.cuh"
-#include "ptc_kv4.cuh"
+#include "ptc_attn4.cuh"
 
 namespace ptc {
 namespace {
@@ -105,7 +104,19 @@ __global__ void __launch_bounds__(32 * kOneWarps) k_attn4_rows(const Attn4Args a
 
 using namespace ptc;
 
-extern "C" size_t ptc_kv4_attention_workspace_bytes(uint32_t, uint32_t, uint32_t, uint32_t, uint32_t) { return kKvStatusBytes; }
+namespace {
+// Query rows of a request, or none of k_attn4_few's where there may be more than it takes.
+uint32_t few_rows(uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t max_q_len) {
+  const uint64_t rows = (uint64_t)max_q_len * (n_kv_heads ? n_q_heads / n_kv_heads : 0);
+  return rows <= kFew4Rows ? (uint32_t)rows : 0;
+}
+}  // namespace
+
+extern "C" size_t ptc_kv4_attention_workspace_bytes(uint32_t, uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t head_dim,
+                                                    uint32_t max_q_len) {
+  const uint32_t rows = few_rows(n_q_heads, n_kv_heads, max_q_len);
+  return kKvStatusBytes + (rows ? few4_ws(head_dim, rows) : 0);
+}
 
 extern "C" ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, const int64_t q_stride[2],
                                         const uint64_t* tok_off, uint64_t n_tok, uint32_t n_q_heads, uint32_t max_q_len,
@@ -122,7 +133,8 @@ extern "C" ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, c
       kv->n_page_ids > (uint64_t(1) << 38) / kv->block_size)
     return PTC_ERR_OVERFLOW;
   if (kv->n_pages > 0x7FFFFFFFu) return PTC_ERR_OVERFLOW;
-  if (!ws_ok(ws, ws_bytes, kKvStatusBytes)) return PTC_ERR_WORKSPACE;
+  if (!ws_ok(ws, ws_bytes, ptc_kv4_attention_workspace_bytes(kv->n_req, n_q_heads, kv->n_kv_heads, kv->head_dim, max_q_len)))
+    return PTC_ERR_WORKSPACE;
   if (kv->n_req == 0) return PTC_OK;
   if (n_tok && (!aligned16(q) || !aligned16(out) || !lse)) return PTC_ERR_INVALID_ARG;
   const uint32_t ext[2] = {(uint32_t)n_tok, n_q_heads};
@@ -141,6 +153,28 @@ extern "C" ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, c
   a.out = static_cast<char*>(out);
   a.lse = lse;
   if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
+  if (const uint32_t few = few_rows(n_q_heads, kv->n_kv_heads, max_q_len)) {
+    Few4Args f{};
+    f.kv = a.kv;
+    f.q = a.q;
+    f.q_tok = a.q_tok;
+    f.q_head = a.q_head;
+    f.tok_off = a.tok_off;
+    f.n_tok = a.n_tok;
+    f.n_q_heads = a.n_q_heads;
+    f.G = a.G;
+    f.max_q_len = max_q_len;
+    f.scale = scale;
+    f.out = a.out;
+    f.lse = a.lse;
+    f.status = a.status;
+    const uint32_t wait_test = test_wait_polls(PTC_TEST_WAIT_ATTENTION);
+    f.withhold = wait_test != 0;
+    f.limit = wait_test ? 1024ll * wait_test : kMbarCycles;
+    few4_place(f, few, static_cast<char*>(ws) + kKvStatusBytes);
+    const ptc_status run = launch_few4(f, few, kv->dtype == PTC_DTYPE_BF16, s);
+    return run != PTC_OK ? run : kv_end(status, a.status, s);
+  }
   const uint64_t rows = n_tok * n_q_heads;
   const uint32_t ctas = rows ? (uint32_t)((rows + kOneWarps - 1) / kOneWarps) : 1;
   if (kv->dtype == PTC_DTYPE_BF16) PTC_KERNEL("k_attn4_rows", s, k_attn4_rows<__nv_bfloat16>, ctas, 32 * kOneWarps, 0, a);
