@@ -168,9 +168,6 @@ extern "C" ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, c
     f.out = a.out;
     f.lse = a.lse;
     f.status = a.status;
-    const uint32_t wait_test = test_wait_polls(PTC_TEST_WAIT_ATTENTION);
-    f.withhold = wait_test != 0;
-    f.limit = wait_test ? 1024ll * wait_test : kMbarCycles;
     few4_place(f, few, static_cast<char*>(ws) + kKvStatusBytes);
     const ptc_status run = launch_few4(f, few, kv->dtype == PTC_DTYPE_BF16, s);
     return run != PTC_OK ? run : kv_end(status, a.status, s);

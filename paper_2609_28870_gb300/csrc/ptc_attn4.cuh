@@ -26,9 +26,8 @@ struct Few4Args {
   uint32_t* arrived;  // parts of the split tile that begins in CTA c
   float* part;        // unnormalised rows of split tiles: [2 * ctas][rows][64 or 128]
   float2* part_ml;    // their maxima (in powers of two) and sums
-  uint32_t ctas, box;
-  uint32_t withhold;  // test of the bounded waits: nothing is loaded
-  long long limit;    // cycles after which a wait for another role gives up
+  uint32_t ctas;
+  uint32_t div_mul, div_shift;  // key / B
   uint32_t* status;
 };
 
@@ -37,8 +36,5 @@ uint32_t few4_ctas(uint32_t head_dim, uint32_t rows);
 size_t few4_ws(uint32_t head_dim, uint32_t rows);
 void few4_place(Few4Args& a, uint32_t rows, char* ws);
 ptc_status launch_few4(Few4Args& a, uint32_t rows, bool bf16, cudaStream_t s);
-
-// The cache as bytes [page][head][slot][row], read `box` slots at a time (ptc_attn.cu).
-bool cache4_map(CUtensorMap* map, const KvView& kv, char* base, int64_t page, int64_t head, int64_t slot, uint32_t box);
 
 }  // namespace ptc

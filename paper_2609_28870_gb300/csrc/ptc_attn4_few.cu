@@ -17,18 +17,19 @@
 // A call's units are 128 keys of a request's key head, and `kExtra` for what a
 // head's tile costs by itself.  CTA c of C has the units from U c / C on, so where
 // a cut lies, and which CTAs share a tile, is arithmetic that every CTA does for
-// itself from the requests' lengths; there is no plan to wait for.  Warp 8 copies
-// units into a ring, warps 0-7 take 16 keys of each; at the tile's end they put
-// their rows together, and of a split tile the last CTA that is done does so with
-// the parts.
+// itself from the requests' lengths; there is no plan to wait for.  A warp takes
+// 32 keys of every 256 and copies its next ones into a ring of its own meanwhile, so
+// no warp waits for another until the tile's end, where they put their rows together;
+// of a split tile the last CTA that is done does so with the parts.
 #include "ptc_attn4.cuh"
 
 namespace ptc {
 namespace {
 
-constexpr uint32_t kUnit = 128, kWarps = 8, kThreads = 32 * (kWarps + 1);
+constexpr uint32_t kUnit = 128, kChunk = 32, kWarps = 8, kTeam = 4, kThreads = 32 * kWarps;
 constexpr uint32_t kExtra = 2;
 constexpr float kMove4 = 256.f;  // the maximum moves when a weight passes this
+constexpr float kNoTop = -3e38f;  // the maximum of no score: any score's weight passes kMove4 by it
 
 template <typename T>
 struct Mma16;
@@ -39,11 +40,12 @@ struct Mma16<__nv_bfloat16> {
     const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
   }
+  // d = A B + c
   static __device__ __forceinline__ void run(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                             uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                                             uint32_t b1, float c0, float c1, float c2, float c3) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
   }
 };
 // (weights of fp16 caches are scaled by 2^7: small ones would fall among fp16's subnormals)
@@ -55,10 +57,10 @@ struct Mma16<__half> {
     return *reinterpret_cast<const uint32_t*>(&x);
   }
   static __device__ __forceinline__ void run(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                             uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                                             uint32_t b1, float c0, float c1, float c2, float c3) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
   }
 };
 // An 8 x 8 matrix of 16-bit numbers over a warp, transposed.
@@ -67,27 +69,26 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// The eight warps of the products.
-__device__ __forceinline__ void warps_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
 // NS: rows of 64 or 128 channels.  NT: eight or sixteen query rows.
 template <int NS, int NT>
 struct Shape {
   static constexpr uint32_t kDim = 64 * NS, kRow = NS == 1 ? 48 : 80, kQRows = 8 * NT;
-  static constexpr uint32_t kTensor = kUnit * kRow, kStage = 2 * kTensor;
+  static constexpr uint32_t kTensor = kChunk * kRow, kStage = 2 * kTensor;  // a warp's chunk
   static constexpr uint32_t kCtas = NS * NT <= 2 ? 2 : 1;  // of an SM: by their registers
-  static constexpr uint32_t kRing = NS == 1 ? 4 : NT == 1 ? 3 : 6;
+  static constexpr uint32_t kRing = kCtas == 1 ? 4 : NS == 1 ? 3 : 2;
   static constexpr uint32_t kORow = kDim + 4;  // 32-bit words of a row on its way to the other warps
-  static constexpr uint32_t kBytes = kRing * kStage + kWarps * kQRows * kORow * 4;
+  static constexpr uint32_t kRegion = NT * 512 * (4 * NS + 1);  // a warp's rows, as lanes hold them or row by row
+  static constexpr uint32_t kBytes = kWarps * kRing * kStage + kTeam * kRegion;
+  static_assert(kQRows * kORow * 4 <= kRegion, "a warp's rows");
 };
 
 struct Shared {
-  uint64_t full[8], empty[8];
   uint64_t off[257];  // units before a block of requests
   uint64_t tok0[256], page0[256];
   uint32_t m[256], n[256];
   uint64_t warp_sum[8];
-  float2 ml[kWarps][kFew4Rows];
+  float2 ml[kTeam][kFew4Rows];
+  uint4 q[8][32];  // the queries' operand: 16 bytes a lane, 4 NS NT of them; see product_warps
   uint32_t last;
 };
 
@@ -220,85 +221,105 @@ __device__ __forceinline__ bool add_up(const Few4Args& a, Shared& sh, uint64_t& 
   return !bad;
 }
 
-// Units into the ring, by tensor copies of `box` slots (a divisor of the page
-// size and of a unit).  Slots of no page read as zeros: their page's coordinate is
-// n_pages, out of range.  The pages of the unit after are asked for meanwhile.
-template <int NS, int NT>
-__device__ __forceinline__ bool copy_units(const Few4Args& a, Shared& sh, Way& w, bool more, uint32_t ring,
-                                           const CUtensorMap* mk, const CUtensorMap* mv, uint32_t& issued) {
+// A warp's copies, chunk by chunk, a chunk or more ahead of its products: 16 bytes a
+// lane (cp.async: a tensor or bulk copy of the 1,280 bytes that a head has in a page
+// of 16 takes 90 cycles of the SM's one copy engine, 4.1 TB/s; this took 12 contexts
+// of 32K to 131K from 140 to XXX us).  BLOCKS: 16 keys lie in a row in one page, else
+// every lane finds a key's row.  The pages of the chunk after are asked for
+// meanwhile, as a page list comes from HBM too.  Slots of no token read as zeros.
+template <int NS, int NT, bool BLOCKS>
+struct Feed {
   using S = Shape<NS, NT>;
-  const uint32_t lane = threadIdx.x & 31, boxes = kUnit / a.box;
-  uint32_t j = w.kv0, id = 0, slot = 0, head = 0;
-  bool in = false;
-  auto ask = [&] {
-    const uint32_t key = j * kUnit + lane * a.box, at = key / a.kv.B;
-    in = lane < boxes && key < w.n;
-    slot = key - at * a.kv.B;
-    head = w.h;
-    id = in ? __ldg(a.kv.page_ids + w.page0 + at) : 0;
-  };
-  if (more) ask();
-  while (more) {
-    int page = (int)a.kv.n_pages;
-    if (in && id < a.kv.n_pages) page = (int)id;
-    else if (in) report(a.status, PTC_ERR_INVALID_ARG);
-    const int s0 = in ? (int)slot : 0, h0 = (int)head;
-    if (++j == w.kv1) {
-      more = w.next(a, sh);
-      j = w.kv0;
-    }
-    if (more) ask();
-    const uint32_t at = issued % S::kRing;
-    if (issued >= S::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / S::kRing - 1) & 1, a.limit)) return false;
-    ++issued;
-    const uint32_t bar = smem_u32(&sh.full[at]), dst = ring + at * S::kStage + lane * a.box * S::kRow;
-    if (lane == 0) mbar_expect(bar, S::kStage);
-    __syncwarp();
-    if (lane < boxes) {
-      tma_load_4d(dst, mk, bar, 0, s0, h0, page);
-      tma_load_4d(dst + S::kTensor, mv, bar, 0, s0, h0, page);
+  static constexpr uint32_t kPieces = kChunk * S::kRow / 16;  // of keys, and of values
+  Way w;
+  const char *kb, *vb;  // the key head's rows of page 0
+  uint32_t chunk, id[2], slot[2], issued;
+  bool more;
+
+  __device__ __forceinline__ void head(const Few4Args& a) {
+    kb = a.kv.k + w.h * a.kv.ks_head;
+    vb = a.kv.v + w.h * a.kv.vs_head;
+  }
+
+  // The chunk at hand's pages, of both blocks of 16 or of the lane's key.
+  __device__ __forceinline__ void ask(const Few4Args& a) {
+    const uint32_t lane = threadIdx.x & 31, key = w.kv0 * kUnit + chunk * kChunk + (BLOCKS ? 0 : lane);
+    const uint32_t at = a.kv.B == 1 ? key : __umulhi(key, a.div_mul) >> a.div_shift;
+    const uint32_t* ids = a.kv.page_ids + w.page0;
+    slot[0] = key - at * a.kv.B;
+    id[0] = key < w.n ? __ldg(ids + at) : kNone;
+    if (BLOCKS) {
+      const bool over = slot[0] + 16 == a.kv.B;
+      slot[1] = over ? 0 : slot[0] + 16;
+      id[1] = key + 16 < w.n ? __ldg(ids + at + (over ? 1 : 0)) : kNone;
     }
   }
-  return true;
-}
-
-// The same for page sizes that are no multiple of 8, 16 bytes a copy.
-template <int NS, int NT>
-__device__ __forceinline__ bool gather_units(const Few4Args& a, Shared& sh, Way& w, bool more, uint32_t ring, uint32_t& issued) {
-  using S = Shape<NS, NT>;
-  constexpr uint32_t kPieces = S::kRow / 16;
-  const uint32_t lane = threadIdx.x & 31;
-  for (; more; more = w.next(a, sh)) {
-    const uint32_t* ids = a.kv.page_ids + w.page0;
-    for (uint32_t j = w.kv0; j < w.kv1; ++j) {
-      const uint32_t at = issued % S::kRing;
-      if (issued >= S::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (issued / S::kRing - 1) & 1, a.limit)) return false;
+  // The warp's first chunk of the part at hand or of a later one.
+  __device__ __forceinline__ void find(const Few4Args& a, const Shared& sh) {
+    const uint32_t warp = threadIdx.x >> 5;
+    while (more && chunk >= (w.kv1 - w.kv0) * (kUnit / kChunk)) {
+      more = w.next(a, sh);
+      chunk = warp;
+      head(a);
+    }
+    if (more) ask(a);
+  }
+  __device__ __forceinline__ void begin(const Few4Args& a, const Shared& sh, const Way& start, bool some) {
+    w = start;
+    head(a);
+    more = some;
+    chunk = threadIdx.x >> 5;
+    issued = 0;
+    find(a, sh);
+  }
+  // Copies the chunk at hand to its place; a group of copies in any case.
+  __device__ __forceinline__ void issue(const Few4Args& a, const Shared& sh, uint32_t ring) {
+    if (more) {
+      const uint32_t lane = threadIdx.x & 31, dst = ring + issued % S::kRing * S::kStage + 16 * lane;
       ++issued;
-      for (uint32_t x = 0; x < kUnit; x += 32) {
-        const uint32_t row = x + lane, key = j * kUnit + row, page = key / a.kv.B, slot = key - page * a.kv.B;
-        bool in = key < w.n;
-        uint32_t id = 0;
-        if (in) {
-          id = __ldg(ids + page);
-          if (id >= a.kv.n_pages) {
-            report(a.status, PTC_ERR_INVALID_ARG);
-            in = false;
-          }
-        }
-        const char* k = in ? a.kv.k + id * a.kv.ks_page + w.h * a.kv.ks_head + slot * a.kv.ks_slot : a.kv.k;
-        const char* v = in ? a.kv.v + id * a.kv.vs_page + w.h * a.kv.vs_head + slot * a.kv.vs_slot : a.kv.v;
-        const uint32_t dst = ring + at * S::kStage + row * S::kRow;
+      bool on[2];
+      const char *k[2], *v[2];
 #pragma unroll
-        for (uint32_t p = 0; p < kPieces; ++p) {
-          cp_async16(dst + 16 * p, k + 16 * p, in);
-          cp_async16(dst + S::kTensor + 16 * p, v + 16 * p, in);
+      for (int x = 0; x < (BLOCKS ? 2 : 1); ++x) {
+        on[x] = id[x] < a.kv.n_pages;
+        if (!on[x] && id[x] != kNone) report(a.status, PTC_ERR_INVALID_ARG);
+        if (!on[x]) id[x] = slot[x] = 0;
+        if (BLOCKS) {
+          const uint32_t in = slot[x] * S::kRow;
+          k[x] = kb + id[x] * a.kv.ks_page + in;
+          v[x] = vb + id[x] * a.kv.vs_page + in;
+        } else {
+          k[x] = kb + id[x] * a.kv.ks_page + slot[x] * a.kv.ks_slot;
+          v[x] = vb + id[x] * a.kv.vs_page + slot[x] * a.kv.vs_slot;
         }
       }
-      asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&sh.full[at])) : "memory");
+      if (BLOCKS) {
+#pragma unroll
+        for (uint32_t i = 0; i < kPieces / 32; ++i) {
+          const uint32_t p = lane + 32 * i;
+          const bool up = p >= kPieces / 2;
+          const uint32_t off = 16 * (up ? p - kPieces / 2 : p);
+          cp_async16(dst + 512 * i, (up ? k[1] : k[0]) + off, up ? on[1] : on[0]);
+          cp_async16(dst + S::kTensor + 512 * i, (up ? v[1] : v[0]) + off, up ? on[1] : on[0]);
+        }
+      } else {
+        const uint32_t rows = __ballot_sync(kFull, on[0]);
+#pragma unroll
+        for (uint32_t i = 0; i < kPieces / 32; ++i) {
+          const uint32_t p = lane + 32 * i, row = p / (S::kRow / 16), off = 16 * (p % (S::kRow / 16));
+          const char* ks = reinterpret_cast<const char*>(__shfl_sync(kFull, reinterpret_cast<uint64_t>(k[0]), row));
+          const char* vs = reinterpret_cast<const char*>(__shfl_sync(kFull, reinterpret_cast<uint64_t>(v[0]), row));
+          const bool in = rows >> row & 1;
+          cp_async16(dst + 512 * i, ks + off, in);
+          cp_async16(dst + S::kTensor + 512 * i, vs + off, in);
+        }
+      }
+      chunk += kWarps;
+      find(a, sh);
     }
+    cp_async_commit();
   }
-  return true;
-}
+};
 
 __device__ __forceinline__ uint32_t lds32(uint32_t at) {
   uint32_t x;
@@ -328,69 +349,83 @@ struct Rows {
   float top[NT][2], l[NT][2], o[NT][4 * NS][4];
 };
 
-// 16 keys of a unit.  Row i of the matrices is key (2 (i % 8 / 2) + 4 (i % 2)) % 8 +
-// 8 (i % 2) + i / 8: rows of 80 (48) bytes in that order meet no bank twice, neither
-// where four lanes read K's rows whole nor where eight read a piece of V's each.
+// 32 keys of a unit, as two blocks of 16.  Row i of a block's matrices is key (2 (i %
+// 8 / 2) + 4 (i % 2)) % 8 + 8 (i % 2) + i / 8: rows of 80 (48) bytes in that order meet
+// no bank twice, neither where four lanes read K's rows whole nor where eight read a
+// piece of V's each.
 template <typename T, int NS, int NT>
 __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n, const int32_t (&see)[NT][2], int32_t least,
-                                          float sl2, const uint32_t (&q)[NT][8 * NS], Rows<NS, NT>& st) {
+                                          float sl2, uint32_t q_at, Rows<NS, NT>& st) {
   using S = Shape<NS, NT>;
   using M = Mma16<T>;
   const uint32_t lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  // scores
-  const uint32_t kg = ((g & 6) + 4 * (g & 1) & 7) + 8 * (g & 1);
-  const uint32_t k_at = at + kg * S::kRow;
-  uint32_t wa[2 * NS], wb[2 * NS];
-  lds_words<NS>(wa, k_at + 8 * NS * t);
-  lds_words<NS>(wb, k_at + S::kRow + 8 * NS * t);
-  const uint32_t group = NS == 2 ? t : t >> 1;
-  const uint32_t pa = lds32(k_at + 32 * NS + 4 * group), pb = lds32(k_at + S::kRow + 32 * NS + 4 * group);
-  const uint32_t sa = both_low(pa), ba = both_high(pa), sb = both_low(pb), bb = both_high(pb);
-  float s[NT][4];
+  // scores, in two strands where there are only two blocks' to keep the products apart
+  constexpr int kStrands = NT == 1 ? 2 : 1;
+  const uint32_t kg = ((g & 6) + 4 * (g & 1) & 7) + 8 * (g & 1), group = NS == 2 ? t : t >> 1;
+  float s[2][NT][4];
 #pragma unroll
-  for (int x = 0; x < NT; ++x)
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t k_at = at + (16 * u + kg) * S::kRow;
+    uint32_t wa[2 * NS], wb[2 * NS];
+    lds_words<NS>(wa, k_at + 8 * NS * t);
+    lds_words<NS>(wb, k_at + S::kRow + 8 * NS * t);
+    const uint32_t pa = lds32(k_at + 32 * NS + 4 * group), pb = lds32(k_at + S::kRow + 32 * NS + 4 * group);
+    const uint32_t sa = both_low(pa), ba = both_high(pa), sb = both_low(pb), bb = both_high(pb);
+    float sum[kStrands][NT][4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[x][k] = 0.f;
+    for (int i = 0; i < 2 * NS; ++i) {
+      uint32_t q[NT][4];
 #pragma unroll
-  for (int i = 0; i < 2 * NS; ++i)
+      for (int x = 0; x < NT; ++x) lds_words<2>(q[x], q_at + (x * 2 * NS + i) * 512);
 #pragma unroll
-    for (int j = 0; j < 4; j += 2) {
-      const uint32_t a0 = fma16x2<T>(pair4<T>(wa[i], j), sa, ba), a1 = fma16x2<T>(pair4<T>(wb[i], j), sb, bb);
-      const uint32_t a2 = fma16x2<T>(pair4<T>(wa[i], j + 1), sa, ba), a3 = fma16x2<T>(pair4<T>(wb[i], j + 1), sb, bb);
+      for (int j = 0; j < 4; j += 2) {
+        const uint32_t a0 = fma16x2<T>(pair4<T>(wa[i], j), sa, ba), a1 = fma16x2<T>(pair4<T>(wb[i], j), sb, bb);
+        const uint32_t a2 = fma16x2<T>(pair4<T>(wa[i], j + 1), sa, ba), a3 = fma16x2<T>(pair4<T>(wb[i], j + 1), sb, bb);
 #pragma unroll
-      for (int x = 0; x < NT; ++x) M::run(s[x], a0, a1, a2, a3, q[x][4 * i + j], q[x][4 * i + j + 1]);
+        for (int x = 0; x < NT; ++x) {
+          float(&d)[4] = sum[i % kStrands][x];
+          if (i < kStrands && j == 0) M::run(d, a0, a1, a2, a3, q[x][j], q[x][j + 1], 0.f, 0.f, 0.f, 0.f);
+          else M::run(d, a0, a1, a2, a3, q[x][j], q[x][j + 1], d[0], d[1], d[2], d[3]);
+        }
+      }
     }
-  // weights; s[x][0], s[x][1]: key kg of query rows 2 t and 2 t + 1, [2], [3]: the key after
-  if ((int32_t)(key0 + 16) > least) {
-    const int32_t key = (int32_t)(key0 + kg);
 #pragma unroll
     for (int x = 0; x < NT; ++x)
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (key + (k >> 1) >= see[x][k & 1]) s[x][k] = -INFINITY;
+      for (int k = 0; k < 4; ++k) s[u][x][k] = kStrands == 2 ? sum[0][x][k] + sum[kStrands - 1][x][k] : sum[0][x][k];
   }
-  float p[NT][4];
-  bool move = false;
+  // weights; s[u][x][0], [1]: key kg of query rows 2 t and 2 t + 1, [2], [3]: the key after
+  if ((int32_t)(key0 + 32) > least) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if ((int32_t)(key0 + 16 * u + kg + (k >> 1)) >= see[x][k & 1]) s[u][x][k] = -INFINITY;
+  }
+  float p[2][NT][4], most = 0.f;
   auto weigh = [&] {
 #pragma unroll
-    for (int x = 0; x < NT; ++x)
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float sub = (st.top[x][k & 1] == -INFINITY ? 0.f : st.top[x][k & 1]) - M::kShift;
-        p[x][k] = exp2_approx(fmaf(s[x][k], sl2, -sub));
-        move |= !(p[x][k] <= kMove4 * M::kScale) | (st.top[x][k & 1] == -INFINITY && s[x][k] != -INFINITY);
-      }
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          p[u][x][k] = exp2_approx(fmaf(s[u][x][k], sl2, M::kShift - st.top[x][k & 1]));
+          most = fmaxf(most, p[u][x][k]);
+        }
   };
   weigh();
-  if (__any_sync(kFull, move)) {
+  if (__any_sync(kFull, most > kMove4 * M::kScale)) {
 #pragma unroll
     for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        float mx = fmaxf(s[x][y], s[x][y + 2]) * sl2;
+        float mx = fmaxf(fmaxf(s[0][x][y], s[0][x][y + 2]), fmaxf(s[1][x][y], s[1][x][y + 2])) * sl2;
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
-        const float top = st.top[x][y], up = fmaxf(top, mx), f = top == -INFINITY ? 0.f : exp2_approx(top - up);
+        const float top = st.top[x][y], up = fmaxf(top, mx), f = exp2_approx(top - up);
         st.top[x][y] = up;
         st.l[x][y] *= f;
 #pragma unroll
@@ -401,42 +436,47 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
       }
     weigh();
   }
-  uint32_t b[NT][2];
+  const uint32_t r0 = 2 * t, r1 = ((2 * t + 4) & 7) + 8, v_group = NS == 2 ? g >> 1 : g >> 2;
 #pragma unroll
-  for (int x = 0; x < NT; ++x) {
-    st.l[x][0] += p[x][0] + p[x][2];
-    st.l[x][1] += p[x][1] + p[x][3];
-    b[x][0] = transposed(M::pack(p[x][0], p[x][1]));
-    b[x][1] = transposed(M::pack(p[x][2], p[x][3]));
-  }
-  // values: keys 2 t and 2 t + 1 of the matrix's order, and the two 8 rows on
-  const uint32_t r0 = 2 * t, r1 = ((2 * t + 4) & 7) + 8;
-  const uint32_t v0 = at + S::kTensor + r0 * S::kRow, v1 = at + S::kTensor + r1 * S::kRow;
-  uint32_t w[4][NS], par[4];
-  const uint32_t v_group = NS == 2 ? g >> 1 : g >> 2;
+  for (int u = 0; u < 2; ++u) {
+    uint32_t b[NT][2];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t row = (k & 1 ? v1 : v0) + (k >> 1) * S::kRow;
-    lds_half<NS>(w[k], row + 4 * NS * g);
-    par[k] = lds32(row + 32 * NS + 4 * v_group);
-  }
-  if (key0 + 16 > n) {  // slots that hold no token may hold anything: values of 0
+    for (int x = 0; x < NT; ++x) {
+      st.l[x][0] += p[u][x][0] + p[u][x][2];
+      st.l[x][1] += p[u][x][1] + p[u][x][3];
+      b[x][0] = transposed(M::pack(p[u][x][0], p[u][x][1]));
+      b[x][1] = transposed(M::pack(p[u][x][2], p[u][x][3]));
+    }
+    // values: keys 2 t and 2 t + 1 of the matrix's order, and the two 8 rows on
+    const uint32_t v0 = at + S::kTensor + (16 * u + r0) * S::kRow, v1 = at + S::kTensor + (16 * u + r1) * S::kRow;
+    uint32_t w[4][NS], par[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (key0 + (k & 1 ? r1 : r0) + (k >> 1) >= n) par[k] = 0;
-  }
-  const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), b0 = __byte_perm(par[0], par[1], 0x7632);
-  const uint32_t s1 = __byte_perm(par[2], par[3], 0x5410), b1 = __byte_perm(par[2], par[3], 0x7632);
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t row = (k & 1 ? v1 : v0) + (k >> 1) * S::kRow;
+      lds_half<NS>(w[k], row + 4 * NS * g);
+      par[k] = lds32(row + 32 * NS + 4 * v_group);
+    }
+    if (key0 + 16 * u + 16 > n) {  // slots that hold no token may hold anything: values of 0
 #pragma unroll
-  for (int i = 0; i < NS; ++i) {
-    const uint32_t e0 = __byte_perm(w[0][i], w[1][i], 0x5410), d0 = __byte_perm(w[0][i], w[1][i], 0x7632);
-    const uint32_t e1 = __byte_perm(w[2][i], w[3][i], 0x5410), d1 = __byte_perm(w[2][i], w[3][i], 0x7632);
+      for (int k = 0; k < 4; ++k)
+        if (key0 + 16 * u + (k & 1 ? r1 : r0) + (k >> 1) >= n) par[k] = 0;
+    }
+    const uint32_t s0 = __byte_perm(par[0], par[1], 0x5410), b0 = __byte_perm(par[0], par[1], 0x7632);
+    const uint32_t s1 = __byte_perm(par[2], par[3], 0x5410), b1 = __byte_perm(par[2], par[3], 0x7632);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t a0 = fma16x2<T>(pair4<T>(e0, j), s0, b0), a1 = fma16x2<T>(pair4<T>(d0, j), s0, b0);
-      const uint32_t a2 = fma16x2<T>(pair4<T>(e1, j), s1, b1), a3 = fma16x2<T>(pair4<T>(d1, j), s1, b1);
+    for (int i = 0; i < NS; ++i) {
+      const uint32_t e0 = __byte_perm(w[0][i], w[1][i], 0x5410), d0 = __byte_perm(w[0][i], w[1][i], 0x7632);
+      const uint32_t e1 = __byte_perm(w[2][i], w[3][i], 0x5410), d1 = __byte_perm(w[2][i], w[3][i], 0x7632);
 #pragma unroll
-      for (int x = 0; x < NT; ++x) M::run(st.o[x][4 * i + j], a0, a1, a2, a3, b[x][0], b[x][1]);
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t a0 = fma16x2<T>(pair4<T>(e0, j), s0, b0), a1 = fma16x2<T>(pair4<T>(d0, j), s0, b0);
+        const uint32_t a2 = fma16x2<T>(pair4<T>(e1, j), s1, b1), a3 = fma16x2<T>(pair4<T>(d1, j), s1, b1);
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+          float(&d)[4] = st.o[x][4 * i + j];
+          M::run(d, a0, a1, a2, a3, b[x][0], b[x][1], d[0], d[1], d[2], d[3]);
+        }
+      }
     }
   }
 }
@@ -483,75 +523,114 @@ __device__ __noinline__ void join_row(const Few4Args& a, uint32_t c0, uint32_t c
   if (lane == 0) a.lse[at] = none ? -INFINITY : (top + log2_approx(l)) * kLn2;
 }
 
-template <typename T, int NS, int NT>
-__device__ __forceinline__ bool product_warps(const Few4Args& a, Shared& sh, Way& w, bool more, uint32_t ring, float* rows,
-                                              uint64_t all, uint32_t ctas) {
+template <typename T, int NS, int NT, bool BLOCKS>
+__device__ __forceinline__ void take_units(const Few4Args& a, Shared& sh, Way& w, bool more, uint32_t ring, char* rows,
+                                           uint64_t all, uint32_t ctas) {
   using S = Shape<NS, NT>;
   using M = Mma16<T>;
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, team = warp / kTeam;
   const uint32_t D = a.kv.D, G = a.G;
   const float sl2 = a.scale * kLog2e;
-  bool alive = true;  // a warp that has given up waiting runs on without, for the others at the barriers
+  const uint32_t q_at = smem_u32(&sh.q[0][lane]);
+  ring += warp * S::kRing * S::kStage;
+  Feed<NS, NT, BLOCKS> feed;
+  feed.begin(a, sh, w, more);
+#pragma unroll
+  for (uint32_t i = 0; i + 1 < S::kRing; ++i) feed.issue(a, sh, ring);
   uint32_t item = 0;
   for (; more; more = w.next(a, sh)) {
-    // the queries' operand: row 8 x + g, channels 16 NS t on
-    uint32_t q[NT][8 * NS];
-    int32_t see[NT][2], least = (int32_t)w.n;
+    // the queries' operand, once for all warps: lane (g, t) of it has, of row 8 x + g,
+    // channels 16 NS t on, eight a piece
+    if (warp < 2 * NS * NT) {
+      const uint32_t i = 8 * (warp / (2 * NS)) + g, d = 16 * NS * t + 8 * (warp % (2 * NS)), tok = i / G;
+      uint4 y = make_uint4(0, 0, 0, 0);
+      if (tok < w.m && d < D)
+        y = *reinterpret_cast<const uint4*>(a.q + 2 * ((int64_t)(w.tok0 + tok) * a.q_tok + (int64_t)(w.h * G + i % G) * a.q_head + d));
+      sh.q[warp][lane] = y;
+    }
+    int32_t see[NT][2];
 #pragma unroll
-    for (int x = 0; x < NT; ++x) {
-      const uint32_t i = 8 * x + g, tok = i / G, head = w.h * G + i % G;
-      const char* row = a.q + 2 * ((int64_t)(w.tok0 + tok) * a.q_tok + (int64_t)head * a.q_head);
-#pragma unroll
-      for (uint32_t k = 0; k < 2 * NS; ++k) {
-        const uint32_t d = 16 * NS * t + 8 * k;
-        uint4 y = make_uint4(0, 0, 0, 0);
-        if (tok < w.m && d < D) y = *reinterpret_cast<const uint4*>(row + 2 * d);
-        q[x][4 * k] = y.x;
-        q[x][4 * k + 1] = y.y;
-        q[x][4 * k + 2] = y.z;
-        q[x][4 * k + 3] = y.w;
-      }
+    for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (uint32_t y = 0; y < 2; ++y) {  // keys that query row 8 x + 2 t + y sees (rows that are none: all)
         const uint32_t mine = (8 * x + 2 * t + y) / G;
         const int64_t last = (int64_t)w.n - w.m + mine + 1;
         see[x][y] = mine >= w.m ? (int32_t)w.n : last > 0 ? (int32_t)last : 0;
       }
-      const int64_t first = (int64_t)w.n - w.m + 1;
-      least = first > 0 ? (int32_t)first : 0;
-    }
+    const int32_t least = w.n >= w.m ? (int32_t)(w.n - w.m + 1) : 0;
+    __syncthreads();
     Rows<NS, NT> st;
 #pragma unroll
     for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        st.top[x][y] = -INFINITY;
+        st.top[x][y] = kNoTop;
         st.l[x][y] = 0.f;
 #pragma unroll
         for (int i = 0; i < 4 * NS; ++i) st.o[x][i][y] = st.o[x][i][y + 2] = 0.f;
       }
-    for (uint32_t j = w.kv0; j < w.kv1; ++j, ++item) {
-      const uint32_t at = item % S::kRing, key0 = j * kUnit + 16 * warp;
-      if (alive) alive = mbar_wait(smem_u32(&sh.full[at]), (item / S::kRing) & 1, a.limit);
-      if (key0 < w.n) take_keys<T, NS, NT>(ring + at * S::kStage + 16 * warp * S::kRow, key0, w.n, see, least, sl2, q, st);
-      mbar_arrive_warp(smem_u32(&sh.empty[at]));
+    const uint32_t chunks = (w.kv1 - w.kv0) * (kUnit / kChunk);
+    for (uint32_t c = warp; c < chunks; c += kWarps, ++item) {
+      const uint32_t key0 = w.kv0 * kUnit + c * kChunk;
+      cp_async_wait<S::kRing - 2>();
+      __syncwarp();  // the chunk is there for all lanes, and all are through with the one before
+      feed.issue(a, sh, ring);
+      if (key0 < w.n) take_keys<T, NS, NT>(ring + item % S::kRing * S::kStage, key0, w.n, see, least, sl2, q_at, st);
     }
-    // the warps' rows
+    // the warps' rows: the second team's are added to the first's
+    char* region = rows + (warp % kTeam) * S::kRegion;
 #pragma unroll
     for (int x = 0; x < NT; ++x)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        float l = st.l[x][y];
+      for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(kFull, l, o);
-        const uint32_t i = 8 * x + 2 * t + y;
-        if (g == 0) sh.ml[warp][i] = make_float2(l != 0.f ? st.top[x][y] - M::kShift : -INFINITY, l);
-        float4* to = reinterpret_cast<float4*>(rows + (warp * S::kQRows + i) * S::kORow + 8 * NS * g);
+        for (int o = 4; o < 32; o <<= 1) st.l[x][y] += __shfl_xor_sync(kFull, st.l[x][y], o);
+    float4* mine = reinterpret_cast<float4*>(region) + lane;
+    if (team == 1) {
 #pragma unroll
-        for (int k = 0; k < 2 * NS; ++k)
-          to[k] = make_float4(st.o[x][2 * k][y], st.o[x][2 * k][y + 2], st.o[x][2 * k + 1][y], st.o[x][2 * k + 1][y + 2]);
+      for (int x = 0; x < NT; ++x) {
+#pragma unroll
+        for (int i = 0; i < 4 * NS; ++i)
+          mine[32 * (x * (4 * NS + 1) + i)] = make_float4(st.o[x][i][0], st.o[x][i][1], st.o[x][i][2], st.o[x][i][3]);
+        mine[32 * (x * (4 * NS + 1) + 4 * NS)] = make_float4(st.top[x][0], st.top[x][1], st.l[x][0], st.l[x][1]);
       }
-    warps_sync();
+    }
+    __syncthreads();
+    if (team == 0) {
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        const float4 o = mine[32 * (x * (4 * NS + 1) + 4 * NS)];
+        const float top[2] = {fmaxf(st.top[x][0], o.x), fmaxf(st.top[x][1], o.y)};
+        const float f[2] = {exp2_approx(st.top[x][0] - top[0]), exp2_approx(st.top[x][1] - top[1])};
+        const float h[2] = {exp2_approx(o.x - top[0]), exp2_approx(o.y - top[1])};
+        st.l[x][0] = st.l[x][0] * f[0] + o.z * h[0];
+        st.l[x][1] = st.l[x][1] * f[1] + o.w * h[1];
+        st.top[x][0] = top[0];
+        st.top[x][1] = top[1];
+#pragma unroll
+        for (int i = 0; i < 4 * NS; ++i) {
+          const float4 y = mine[32 * (x * (4 * NS + 1) + i)];
+          st.o[x][i][0] = fmaf(st.o[x][i][0], f[0], y.x * h[0]);
+          st.o[x][i][1] = fmaf(st.o[x][i][1], f[1], y.y * h[1]);
+          st.o[x][i][2] = fmaf(st.o[x][i][2], f[0], y.z * h[0]);
+          st.o[x][i][3] = fmaf(st.o[x][i][3], f[1], y.w * h[1]);
+        }
+      }
+      __syncwarp();  // the region is the warp's own from here on
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t i = 8 * x + 2 * t + y;
+          const float l = st.l[x][y];
+          if (g == 0) sh.ml[warp][i] = make_float2(l != 0.f ? st.top[x][y] - M::kShift : -INFINITY, l);
+          float4* to = reinterpret_cast<float4*>(reinterpret_cast<float*>(region) + i * S::kORow + 8 * NS * g);
+#pragma unroll
+          for (int k = 0; k < 2 * NS; ++k)
+            to[k] = make_float4(st.o[x][2 * k][y], st.o[x][2 * k][y + 2], st.o[x][2 * k + 1][y], st.o[x][2 * k + 1][y + 2]);
+        }
+    }
+    __syncthreads();
     const bool whole = w.kv0 == 0 && w.kv1 == w.tiles;
     const uint32_t used = w.m * G;
     const uint64_t out0 = w.tok0 * a.n_q_heads + w.h * G;  // of row 0; row i is token i / G, head i % G
@@ -562,14 +641,14 @@ __device__ __forceinline__ bool product_warps(const Few4Args& a, Shared& sh, Way
       if (i >= used) break;
       float top = -INFINITY, l = 0.f;
 #pragma unroll
-      for (uint32_t x = 0; x < kWarps; ++x) top = fmaxf(top, sh.ml[x][i].x);
+      for (uint32_t x = 0; x < kTeam; ++x) top = fmaxf(top, sh.ml[x][i].x);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (uint32_t x = 0; x < kWarps; ++x) {
+      for (uint32_t x = 0; x < kTeam; ++x) {
         const float2 ml = sh.ml[x][i];
         if (ml.x == -INFINITY) continue;
         const float f = exp2_approx(ml.x - top);
-        const float4 y = *reinterpret_cast<const float4*>(rows + (x * S::kQRows + i) * S::kORow + c);
+        const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(rows + x * S::kRegion) + i * S::kORow + c);
         l = fmaf(ml.y, f, l);
         o.x = fmaf(y.x, f, o.x);
         o.y = fmaf(y.y, f, o.y);
@@ -595,39 +674,25 @@ __device__ __forceinline__ bool product_warps(const Few4Args& a, Shared& sh, Way
       const uint32_t c0 = (uint32_t)(((first + 1) * ctas + all - 1) / all - 1);
       const uint32_t c1 = (uint32_t)(((first + w.tiles) * ctas + all - 1) / all - 1);
       __threadfence();
-      warps_sync();
+      __syncthreads();
       if (tid == 0) sh.last = atomicAdd(a.arrived + c0, 1u) == c1 - c0;
-      warps_sync();
+      __syncthreads();
       if (sh.last) {
         __threadfence();
         for (uint32_t i = warp; i < used; i += kWarps)
           join_row<T, NS, NT>(a, c0, c1 - c0 + 1, i, out0 + (uint64_t)(i / G) * a.n_q_heads + i % G);
       }
     }
-    warps_sync();
+    __syncthreads();
   }
-  return alive;
+  cp_async_wait<0>();
 }
 
-template <typename T, int NS, int NT, bool TMA>
-__global__ void __launch_bounds__(kThreads, Shape<NS, NT>::kCtas)
-    k_attn4_few(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const __grid_constant__ Few4Args a) {
+template <typename T, int NS, int NT, bool BLOCKS>
+__global__ void __launch_bounds__(kThreads, Shape<NS, NT>::kCtas) k_attn4_few(const __grid_constant__ Few4Args a) {
   using S = Shape<NS, NT>;
-  extern __shared__ __align__(1024) char smem_raw[];
+  extern __shared__ __align__(128) char smem_raw[];
   __shared__ Shared sh;
-  const uint32_t ring = smem_u32(smem_raw), warp = threadIdx.x >> 5;
-  float* rows = reinterpret_cast<float*>(smem_raw + S::kRing * S::kStage);
-  if (ring & 127) {  // tensor copies land on whole lines
-    if (threadIdx.x == 0) report(a.status, PTC_ERR_CUDA);
-    return;
-  }
-  if (threadIdx.x == 0) {
-    for (uint32_t i = 0; i < S::kRing; ++i) {
-      mbar_init(smem_u32(&sh.full[i]), TMA ? 1 : 32);
-      mbar_init(smem_u32(&sh.empty[i]), kWarps);
-    }
-    fence_mbar_init();
-  }
   grid_dep_sync();
   uint64_t all;
   if (!add_up(a, sh, all)) return;
@@ -635,37 +700,22 @@ __global__ void __launch_bounds__(kThreads, Shape<NS, NT>::kCtas)
   if (blockIdx.x >= ctas) return;
   Way w;
   const bool more = w.begin(a, sh, all, blockIdx.x, ctas);
-  bool fine = true;
-  uint32_t issued = 0;
-  if (warp < kWarps) {
-    fine = product_warps<T, NS, NT>(a, sh, w, more, ring, rows, all, ctas);
-  } else if (!a.withhold) {
-    fine = TMA ? copy_units<NS, NT>(a, sh, w, more, ring, &mk, &mv, issued) : gather_units<NS, NT>(a, sh, w, more, ring, issued);
-    if (!TMA) {
-      cp_async_commit();
-      cp_async_wait<0>();
-    }
-  }
-  if (!fine) report(a.status, PTC_ERR_TIMEOUT);
-  // Where a role has given up, the copies that were issued land before the CTA ends.
-  if (__syncthreads_or(!fine) && warp == kWarps && TMA)
-    for (uint32_t i = issued > S::kRing ? issued - S::kRing : 0; i < issued; ++i)
-      (void)mbar_wait(smem_u32(&sh.full[i % S::kRing]), (i / S::kRing) & 1);
+  take_units<T, NS, NT, BLOCKS>(a, sh, w, more, smem_u32(smem_raw), smem_raw + kWarps * S::kRing * S::kStage, all, ctas);
 }
 
-template <typename T, int NS, int NT, bool TMA>
-ptc_status launch_one(const Few4Args& a, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
+template <typename T, int NS, int NT, bool BLOCKS>
+ptc_status launch_one(const Few4Args& a, cudaStream_t s) {
   constexpr int smem = Shape<NS, NT>::kBytes;
   static std::atomic<uint64_t> ready{0};
-  const auto kernel = k_attn4_few<T, NS, NT, TMA>;
+  const auto kernel = k_attn4_few<T, NS, NT, BLOCKS>;
   if (!large_smem(kernel, smem, ready)) return PTC_ERR_CUDA;
-  PTC_KERNEL("k_attn4_few", s, kernel, a.ctas, kThreads, smem, mk, mv, a);
+  PTC_KERNEL("k_attn4_few", s, kernel, a.ctas, kThreads, smem, a);
   return PTC_OK;
 }
 template <typename T>
-ptc_status launch_some(const Few4Args& a, uint32_t rows, bool tma, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t s) {
+ptc_status launch_some(const Few4Args& a, uint32_t rows, bool blocks, cudaStream_t s) {
   const bool wide = a.kv.D > 64, two = rows > 8;
-#define PTC_FEW4(NS, NT) (tma ? launch_one<T, NS, NT, true>(a, mk, mv, s) : launch_one<T, NS, NT, false>(a, mk, mv, s))
+#define PTC_FEW4(NS, NT) (blocks ? launch_one<T, NS, NT, true>(a, s) : launch_one<T, NS, NT, false>(a, s))
   return wide ? two ? PTC_FEW4(2, 2) : PTC_FEW4(2, 1) : two ? PTC_FEW4(1, 2) : PTC_FEW4(1, 1);
 #undef PTC_FEW4
 }
@@ -694,16 +744,15 @@ void few4_place(Few4Args& a, uint32_t rows, char* ws) {
 }
 
 ptc_status launch_few4(Few4Args& a, uint32_t rows, bool bf16, cudaStream_t s) {
-  a.box = kUnit;
-  while (a.kv.B % a.box) a.box /= 2;
-  const bool tma = a.box >= 8 && a.kv.n_pages > 0;
-  CUtensorMap mk = {}, mv = {};
-  if (tma && (!cache4_map(&mk, a.kv, a.kv.k, a.kv.ks_page, a.kv.ks_head, a.kv.ks_slot, a.box) ||
-              !cache4_map(&mv, a.kv, a.kv.v, a.kv.vs_page, a.kv.vs_head, a.kv.vs_slot, a.box)))
-    return PTC_ERR_CUDA;
+  const int64_t row = row4_bytes(a.kv.D);
+  const bool blocks = a.kv.B % 16 == 0 && a.kv.ks_slot == row && a.kv.vs_slot == row;
+  // key / B as a product: exact below 2^31
+  a.div_shift = 0;
+  while (a.kv.B > 2u << a.div_shift) ++a.div_shift;
+  a.div_mul = a.kv.B > 1 ? (uint32_t)(((uint64_t(1) << (32 + a.div_shift)) + a.kv.B - 1) / a.kv.B) : 0;
   const ptc_status st = fill_async(a.arrived, 0u, 4 * a.ctas, s);
   if (st != PTC_OK) return st;
-  return bf16 ? launch_some<__nv_bfloat16>(a, rows, tma, mk, mv, s) : launch_some<__half>(a, rows, tma, mk, mv, s);
+  return bf16 ? launch_some<__nv_bfloat16>(a, rows, blocks, s) : launch_some<__half>(a, rows, blocks, s);
 }
 
 }  // namespace ptc

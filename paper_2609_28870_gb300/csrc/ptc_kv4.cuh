@@ -30,7 +30,10 @@ __device__ __forceinline__ uint32_t pair4(uint32_t w, int j) {
   constexpr int at = Half16<T>::kBf16 ? 3 : 6;  // the code's place among the mantissa bits
   constexpr uint32_t mask = 0xFu << at | 0xFu << (at + 16), one = Half16<T>::kBf16 ? 0x41804180u : 0x4C004C00u;
   const int up = at - 4 * j;
-  return ((up >= 0 ? w << up : w >> -up) & mask) | one;
+  // (one instruction: left to itself the compiler takes two, each with a constant of its own)
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(up >= 0 ? w << up : w >> -up), "r"(mask), "r"(one));
+  return y;
 }
 template <typename T>
 __device__ __forceinline__ uint32_t fma16x2(uint32_t a, uint32_t b, uint32_t c) {
