@@ -115,6 +115,18 @@ __device__ __forceinline__ uint32_t first_seeing(uint32_t m, uint32_t n, uint32_
 }
 
 // Host side (ptc_attn.cu, ptc_mass.cu).
+// Workspace: the status word, the plans, the unit offsets, the parts, the scores.
+struct AttnWs {
+  size_t plan, units, ml, part, mass, scores, total;
+};
+AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D, uint64_t scores);
+uint32_t tile_ctas();
+void attn_place(AttnArgs& a, const AttnWs& at, char* ws);
+// What a call says of its queries: checks, and what follows from them.
+ptc_status attn_call(AttnArgs& a, const ptc_paged_kv* kv, const uint64_t* tok_off, uint64_t n_tok, const int64_t* q_stride,
+                     uint32_t n_q_heads, float scale);
+ptc_status attn_rows(AttnArgs& a, const void* q, const int64_t* q_stride, uint32_t max_q_len, void* out, float* lse);
+void launch_plan(const AttnArgs& a, bool weights, cudaStream_t s);
 bool tokens_map(CUtensorMap* map, const AttnArgs& a, bool bf16, uint32_t tokens);
 bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_t page, int64_t head, int64_t slot,
                uint32_t box);

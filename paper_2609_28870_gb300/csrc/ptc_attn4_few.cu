@@ -28,6 +28,24 @@ namespace {
 
 constexpr uint32_t kUnit = 128, kChunk = 32, kWarps = 8, kTeam = 4, kThreads = 32 * kWarps;
 constexpr uint32_t kExtra = 2;
+struct Few4Args {
+  KvView kv;
+  const char* q;
+  int64_t q_tok, q_head;
+  const uint64_t* tok_off;
+  uint64_t n_tok;
+  uint32_t n_q_heads, G, max_q_len;
+  float scale;
+  char* out;
+  float* lse;
+  uint32_t* arrived;  // parts of the split tile that begins in CTA c
+  float* part;        // unnormalised rows of split tiles: [2 * ctas][rows][64 or 128]
+  float2* part_ml;    // their maxima (in powers of two) and sums
+  uint32_t ctas;
+  uint32_t div_mul, div_shift;  // key / B
+  uint32_t* status;
+};
+
 constexpr float kMove4 = 256.f;  // the maximum moves when a weight passes this
 constexpr float kNoTop = -3e38f;  // the maximum of no score: any score's weight passes kMove4 by it
 
@@ -722,32 +740,30 @@ ptc_status launch_some(const Few4Args& a, uint32_t rows, bool blocks, cudaStream
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-}  // namespace
-
 uint32_t few4_ctas(uint32_t head_dim, uint32_t rows) {
   const uint32_t n = (uint32_t)num_sms() * (head_dim > 64 && rows > 8 ? 1 : 2);
   return n < kFew4MaxCtas ? n : kFew4MaxCtas;
 }
+
+}  // namespace
 
 size_t few4_ws(uint32_t head_dim, uint32_t rows) {
   const size_t places = 2 * (size_t)few4_ctas(head_dim, rows) * (rows > 8 ? 16 : 8);
   return up256(4 * kFew4MaxCtas) + up256(8 * places) + up256(4 * places * padded4(head_dim));
 }
 
-void few4_place(Few4Args& a, uint32_t rows, char* ws) {
+ptc_status launch_few4(const AttnArgs& c, uint32_t rows, char* ws, bool bf16, cudaStream_t s) {
+  Few4Args a{c.kv, c.q, c.q_tok, c.q_head, c.tok_off, c.n_tok, c.n_q_heads, c.G, c.max_q_len, c.scale, c.out, c.lse};
+  a.status = c.status;
   a.ctas = few4_ctas(a.kv.D, rows);
   const size_t places = 2 * (size_t)a.ctas * (rows > 8 ? 16 : 8);
   a.arrived = reinterpret_cast<uint32_t*>(ws);
   ws += up256(4 * kFew4MaxCtas);
   a.part_ml = reinterpret_cast<float2*>(ws);
   a.part = reinterpret_cast<float*>(ws + up256(8 * places));
-}
-
-ptc_status launch_few4(Few4Args& a, uint32_t rows, bool bf16, cudaStream_t s) {
   const int64_t row = row4_bytes(a.kv.D);
   const bool blocks = a.kv.B % 16 == 0 && a.kv.ks_slot == row && a.kv.vs_slot == row;
   // key / B as a product: exact below 2^31
-  a.div_shift = 0;
   while (a.kv.B > 2u << a.div_shift) ++a.div_shift;
   a.div_mul = a.kv.B > 1 ? (uint32_t)(((uint64_t(1) << (32 + a.div_shift)) + a.kv.B - 1) / a.kv.B) : 0;
   const ptc_status st = fill_async(a.arrived, 0u, 4 * a.ctas, s);
