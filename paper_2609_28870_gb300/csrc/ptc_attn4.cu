@@ -69,6 +69,7 @@ extern "C" ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, c
   if (const uint32_t few = few_rows(n_q_heads, kv->n_kv_heads, max_q_len)) {
     run = launch_few4(a, few, static_cast<char*>(ws) + kKvStatusBytes, bf16, s);
   } else {
+    page_division(a.kv.B, &a.div_mul, &a.div_shift);
     attn_place(a, attn_ws(kv->n_req, tile_ctas(), kv->head_dim, 0), static_cast<char*>(ws));
     run = bf16 ? launch4<__nv_bfloat16>(a, s) : launch4<__half>(a, s);
   }

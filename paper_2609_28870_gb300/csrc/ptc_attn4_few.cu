@@ -763,9 +763,7 @@ ptc_status launch_few4(const AttnArgs& c, uint32_t rows, char* ws, bool bf16, cu
   a.part = reinterpret_cast<float*>(ws + up256(8 * places));
   const int64_t row = row4_bytes(a.kv.D);
   const bool blocks = a.kv.B % 16 == 0 && a.kv.ks_slot == row && a.kv.vs_slot == row;
-  // key / B as a product: exact below 2^31
-  while (a.kv.B > 2u << a.div_shift) ++a.div_shift;
-  a.div_mul = a.kv.B > 1 ? (uint32_t)(((uint64_t(1) << (32 + a.div_shift)) + a.kv.B - 1) / a.kv.B) : 0;
+  page_division(a.kv.B, &a.div_mul, &a.div_shift);
   const ptc_status st = fill_async(a.arrived, 0u, 4 * a.ctas, s);
   if (st != PTC_OK) return st;
   return bf16 ? launch_some<__nv_bfloat16>(a, rows, blocks, s) : launch_some<__half>(a, rows, blocks, s);

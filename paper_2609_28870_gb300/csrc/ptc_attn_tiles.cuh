@@ -153,8 +153,8 @@ constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
 // 4 KB a softmax warp: rows on their way out; the sums of 8 warps, 32 rows and 32 columns.
 constexpr int kStage = 8 * 4096;
 // Registers a thread: 2 * 128 * 200 + 128 * 104 = 384 * 168, what the block has at launch.
-// With four warps more: 256 * 200 + 256 * 56 = 512 * 128.
-constexpr int kSoftmaxRegs = 200, kOtherRegs = 104, kOtherRegs4 = 56;
+// With four warps more: 256 * 184 + 256 * 72 = 512 * 128 (4,096 tokens at 32K: 1.47 ms; with 200, 56 and 56 2.0 ms, the copies' state in local memory).
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 104, kSoftmaxRegs4 = 184, kOtherRegs4 = 72, kQuantRegs4 = 72;
 
 struct TileShared {
   uint64_t full[8], empty[8], q_full[2], q_empty[2], s_full[2], p_full[2][2], pv_done[2][2], drain;
@@ -183,10 +183,10 @@ struct TileShape {
   static constexpr int kTiles4 = KIND == kFour ? kRing4 * 128 * kRow4 : 0;
   // A role's warps, and registers a thread: the softmax's and the others'.
   static constexpr int kThreads = KIND == kFour ? 512 : kTileThreads;
-  static constexpr int kOther = KIND == kFour ? kOtherRegs4 : kOtherRegs;
+  static constexpr int kSoftmax = KIND == kFour ? kSoftmaxRegs4 : kSoftmaxRegs, kOther = KIND == kFour ? kOtherRegs4 : kOtherRegs;
   // queries, ring, tiles of 4 bits, stage, the rest
   static constexpr int kRest = kQueries * kTile + kRing * kTile + kTiles4 + kStage;
-  static constexpr int kSmem = kRest + sizeof(TileShared);
+  static constexpr int kSmem = kRest + sizeof(TileShared) + (KIND == kFour ? 4 * sizeof(Walk) : 0);
   static_assert(kSmem <= 227 * 1024, "shared memory of a block");
 };
 
@@ -1034,93 +1034,110 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
 template <typename T, int NSLAB>
 __device__ __forceinline__ bool quant_role(const AttnArgs& a, TileShared& sh, uint32_t ring, uint32_t tiles4) {
   using Sh = TileShape<NSLAB, kFour>;
-  constexpr uint32_t kRow = Sh::kRow4, kPer = kRow / 16, kCopies = kPer;  // pieces of a row, and copies of a lane
+  constexpr uint32_t kLanes = 2 * NSLAB, kSteps = kLanes;  // lanes of a row, rows of a lane
   constexpr uint32_t kCodes = 32 * NSLAB;                               // bytes of a row's codes
-  constexpr uint32_t kMine = 32 * kRow;                                 // bytes of the warp's part of a tile
+  constexpr uint32_t kMine = 32 * Sh::kRow4;                            // bytes of the warp's part of a tile
   const uint32_t lane = threadIdx.x & 31, row0 = 32 * (threadIdx.x / 32 - 12);
   const uint32_t mine = tiles4 + row0 / 32 * Sh::kRing4 * kMine;
-  // copies: every lane finds a row; item 2 j + 1, a tile's values, follows item 2 j, its keys
-  Walk w;
-  bool more = w.begin(a), values = false;
-  uint32_t j = more ? w.kv0 : 0, id = kNone, slot = 0, rows = 0, issued = 0;
-  const char *k = nullptr, *v = nullptr;
-  auto ask = [&] {
-    const uint32_t key = j * kKeys + row0 + lane, at = key / a.kv.B;
-    slot = key - at * a.kv.B;
-    id = key < w.n ? __ldg(a.kv.page_ids + w.page0 + at) : kNone;
+  // copies: every lane finds a row; item 2 j + 1, a tile's values, follows item 2 j, its keys.
+  // The walk waits in shared memory from one part to the next: 56 registers are few.
+  Walk& rest = reinterpret_cast<Walk*>(&sh + 1)[row0 / 32];
+  bool more, values = false;
+  uint32_t j = 0, end = 0, n = 0, id = kNone, slot = 0, rows = 0, issued = 0;
+  const char *kb = nullptr, *vb = nullptr, *k = nullptr, *v = nullptr;  // the head's rows of page 0; the lane's rows
+  const uint32_t* ids = nullptr;
+  auto part = [&](const Walk& w) {
+    j = w.kv0;
+    end = w.kv1;
+    n = w.n;
+    ids = a.kv.page_ids + w.page0;
+    kb = a.kv.k + w.h * a.kv.ks_head;
+    vb = a.kv.v + w.h * a.kv.vs_head;
+    __syncwarp();
+    if (lane == 0) rest = w;
+    __syncwarp();
   };
-  if (more) ask();
+  auto ask = [&] {
+    const uint32_t key = j * kKeys + row0 + lane, at = a.kv.B == 1 ? key : __umulhi(key, a.div_mul) >> a.div_shift;
+    slot = key - at * a.kv.B;
+    id = key < n ? __ldg(ids + at) : kNone;
+  };
+  {
+    Walk w;
+    more = w.begin(a);
+    if (more) {
+      part(w);
+      ask();
+    }
+  }
   auto issue = [&] {
     if (!values && more) {
       const bool on = id < a.kv.n_pages;
       if (!on && id != kNone) report(a.status, PTC_ERR_INVALID_ARG);
       rows = __ballot_sync(kFull, on);
       const uint32_t page = on ? id : 0, s = on ? slot : 0;
-      k = a.kv.k + page * a.kv.ks_page + w.h * a.kv.ks_head + s * a.kv.ks_slot;
-      v = a.kv.v + page * a.kv.vs_page + w.h * a.kv.vs_head + s * a.kv.vs_slot;
-      if (++j == w.kv1) {
+      k = kb + page * a.kv.ks_page + s * a.kv.ks_slot;
+      v = vb + page * a.kv.vs_page + s * a.kv.vs_slot;
+      if (++j == end) {
+        Walk w = rest;
         more = w.next(a);
-        j = w.kv0;
+        if (more) part(w);
       }
       if (more) ask();
     } else if (!values) {
       cp_async_commit();
       return;
     }
-    const uint32_t dst = mine + issued % Sh::kRing4 * kMine;
+    // all rows' codes, then all rows' scales and bases
+    const uint32_t dst = mine + issued % Sh::kRing4 * kMine + 16 * lane;
+    const char* from = values ? v : k;
 #pragma unroll
-    for (uint32_t i = 0; i < kCopies; ++i) {
-      const uint32_t p = lane + 32 * i, row = p / kPer, x = p % kPer;
-      const char* from = reinterpret_cast<const char*>(__shfl_sync(kFull, reinterpret_cast<uint64_t>(values ? v : k), row));
-      // all rows' codes, then all rows' scales and bases: neither meets a bank twice when it is read
-      cp_async16(dst + (16 * x < kCodes ? row * kCodes + 16 * x : 32 * kCodes + 16 * row), from + 16 * x, rows >> row & 1);
+    for (uint32_t i = 0; i < kSteps; ++i) {
+      const uint32_t row = 32 / kLanes * i + lane / kLanes;
+      const char* x = reinterpret_cast<const char*>(__shfl_sync(kFull, reinterpret_cast<uint64_t>(from), row));
+      cp_async16(dst + 512 * i, x + 16 * (lane % kLanes), rows >> row & 1);
     }
+    cp_async16(dst + 32 * kCodes, from + kCodes, rows >> lane & 1);
     cp_async_commit();
     ++issued;
     values = !values;
   };
 #pragma unroll 1
   for (uint32_t i = 0; i + 1 < Sh::kRing4; ++i) issue();
-  constexpr uint32_t kLanes = 2 * NSLAB;  // of a row
-  const uint32_t r0 = lane / kLanes, group = lane % kLanes;
+  // The lane's rows are first, first + 32 / kLanes and so on.  (The second slab's
+  // rows are two off: the loads and the stores of eight lanes meet no bank twice.)
+  const uint32_t group = lane % kLanes, first = (lane / kLanes) ^ (group & 2);
+  const uint32_t codes_at = mine + first * kCodes + 16 * group, pars_at = mine + 32 * kCodes + 16 * first + 4 * group;
+  const uint32_t piece0 = (4 * (group & 1)) ^ (first & 7);
+  const uint32_t tile_at = ring + group / 2 * kSlabBytes + (row0 + first) * 128;
   for (uint32_t item = 0; item < issued; ++item) {
     cp_async_wait<Sh::kRing4 - 2>();
     __syncwarp();  // the rows are there for all lanes, and all are through with the tile before
     issue();
-    const uint32_t at = item % Sh::kRing, src = mine + item % Sh::kRing4 * kMine;
+    const uint32_t at = item % Sh::kRing, src = item % Sh::kRing4 * kMine;
+    uint32_t c[kSteps][4], par[kSteps];
+#pragma unroll
+    for (uint32_t i = 0; i < kSteps; ++i) {
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(c[i][0]), "=r"(c[i][1]), "=r"(c[i][2]), "=r"(c[i][3])
+                   : "r"(codes_at + src + 512 * i)
+                   : "memory");
+      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(par[i]) : "r"(pars_at + src + 512 / kLanes * i) : "memory");
+    }
     if (item >= Sh::kRing && !mbar_wait(smem_u32(&sh.empty[at]), (item / Sh::kRing - 1) & 1, a.limit)) {
       cp_async_wait<0>();
       return false;
     }
-    const uint32_t tile = ring + at * Sh::kTile + group / 2 * kSlabBytes;
-#pragma unroll 2
-    for (uint32_t i = 0; i < 32; i += 32 / kLanes) {
-      const uint32_t row = i + r0;
-      uint32_t c[4], par;
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3])
-                   : "r"(src + row * kCodes + 16 * group)
-                   : "memory");
-      asm volatile("ld.shared.b32 %0, [%1];" : "=r"(par) : "r"(src + 32 * kCodes + 16 * row + 4 * group) : "memory");
-      const uint32_t s = both_low(par), b = both_high(par);
-      // lanes of the second slab begin with their third word: the stores of two rows' eight lanes meet no bank twice
-      const uint32_t turn = group & 2;
-      if (NSLAB == 2 && turn) {
-        const uint32_t x = c[0], y = c[1];
-        c[0] = c[2];
-        c[1] = c[3];
-        c[2] = x;
-        c[3] = y;
-      }
-      const uint32_t to = tile + (row0 + row) * 128;
+    const uint32_t to = tile_at + at * Sh::kTile;
 #pragma unroll
-      for (uint32_t x = 0; x < 4; ++x) {
-        const uint32_t piece = (4 * (group & 1) + (x ^ (NSLAB == 2 ? turn : 0))) ^ (row & 7);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16 * piece), "r"(fma16x2<T>(pair4<T>(c[x], 0), s, b)),
-                     "r"(fma16x2<T>(pair4<T>(c[x], 1), s, b)), "r"(fma16x2<T>(pair4<T>(c[x], 2), s, b)),
-                     "r"(fma16x2<T>(pair4<T>(c[x], 3), s, b))
+    for (uint32_t i = 0; i < kSteps; ++i) {
+      const uint32_t s = both_low(par[i]), b = both_high(par[i]);
+#pragma unroll
+      for (uint32_t x = 0; x < 4; ++x)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16 * (piece0 ^ x) + 4096 / kLanes * i),
+                     "r"(fma16x2<T>(pair4<T>(c[i][x], 0), s, b)), "r"(fma16x2<T>(pair4<T>(c[i][x], 1), s, b)),
+                     "r"(fma16x2<T>(pair4<T>(c[i][x], 2), s, b)), "r"(fma16x2<T>(pair4<T>(c[i][x], 3), s, b))
                      : "memory");
-      }
     }
     fence_async_shared();
     mbar_arrive_warp(smem_u32(&sh.full[at]));
@@ -1189,8 +1206,11 @@ __global__ void __launch_bounds__(TileShape<NSLAB, KIND>::kThreads, 1)
   const bool go = a.plan->ok != 0;
   bool fine = true;
   if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(Sh::kSoftmax));
     if (go) fine = softmax_role<T, NSLAB, KIND>(a, sh, smem_raw + Sh::kRest - kStage, warp / 4);
+  } else if (KIND == kFour && warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kQuantRegs4));
+    if (go) fine = quant_role<T, NSLAB>(a, sh, ring, ring + Sh::kRing * Sh::kTile);
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(Sh::kOther));
     // (declared inside query_role, the registers fall so that the softmax spills: 1.23 -> 1.6 ms for 4,096 tokens at 32K)
@@ -1205,7 +1225,6 @@ __global__ void __launch_bounds__(TileShape<NSLAB, KIND>::kThreads, 1)
     } else if (warp == 10) {
       fine = query_role<NSLAB, KIND>(a, sh, &mq, &mq32, q_smem, loads);
     } else if (KIND == kFour) {
-      if (warp >= 12) fine = quant_role<T, NSLAB>(a, sh, ring, ring + Sh::kRing * Sh::kTile);
     } else if (!TMA) {
       fine = gather_role<NSLAB, KIND>(a, sh, ring);
     } else {

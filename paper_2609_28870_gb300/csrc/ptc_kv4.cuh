@@ -44,6 +44,14 @@ __device__ __forceinline__ uint32_t fma16x2(uint32_t a, uint32_t b, uint32_t c) 
 __device__ __forceinline__ uint32_t both_low(uint32_t x) { return __byte_perm(x, x, 0x1010); }
 __device__ __forceinline__ uint32_t both_high(uint32_t x) { return __byte_perm(x, x, 0x3232); }
 
+// key / B as (key * mul >> 32) >> shift, exact for keys below 2^31 and B > 1: mul's
+// error, below B, times key is below 2^32 << shift, as B <= 2 << shift.
+inline void page_division(uint32_t B, uint32_t* mul, uint32_t* shift) {
+  *shift = 0;
+  while (B > 2u << *shift) ++*shift;
+  *mul = B > 1 ? (uint32_t)(((uint64_t(1) << (32 + *shift)) + B - 1) / B) : 0;
+}
+
 // The host-side checks of a ptc_paged_kv whose pages are 4-bit rows, and its
 // device view; strides in bytes.
 inline ptc_status kv4_view(const ptc_paged_kv* kv, KvView* o) {
