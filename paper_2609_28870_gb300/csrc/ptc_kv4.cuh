@@ -37,9 +37,7 @@ __device__ __forceinline__ uint32_t pair4(uint32_t w, int j) {
 }
 template <typename T>
 __device__ __forceinline__ uint32_t fma16x2(uint32_t a, uint32_t b, uint32_t c) {
-  using Two = typename Half16<T>::Two;
-  const Two d = __hfma2(*reinterpret_cast<const Two*>(&a), *reinterpret_cast<const Two*>(&b), *reinterpret_cast<const Two*>(&c));
-  return *reinterpret_cast<const uint32_t*>(&d);
+  return fma_bits<typename Half16<T>::Two>(a, b, c);
 }
 __device__ __forceinline__ uint32_t both_low(uint32_t x) { return __byte_perm(x, x, 0x1010); }
 __device__ __forceinline__ uint32_t both_high(uint32_t x) { return __byte_perm(x, x, 0x3232); }

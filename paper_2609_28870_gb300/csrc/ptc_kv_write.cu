@@ -6,7 +6,8 @@ namespace ptc {
 namespace {
 
 constexpr int kWrThreads = 256;
-constexpr int kWrRows = 4;  // rows of a token that a thread has in flight
+constexpr int kRdRows = 4;  // rows of a token that a thread has in flight, of those that are read back
+constexpr uint32_t kWrSlice = 24;
 
 struct WriteArgs {
   KvView kv;
@@ -58,30 +59,65 @@ __device__ __forceinline__ Place find_place(const WriteArgs& a, uint64_t t) {
   return at;
 }
 
+template <uint32_t TOKENS>
+__device__ __forceinline__ void find_places(const WriteArgs& a, uint64_t t0, Place (&at)[TOKENS]) {
+  check_offsets(a);
+  if (threadIdx.x < TOKENS) at[threadIdx.x] = t0 + threadIdx.x < a.n_tok ? find_place(a, t0 + threadIdx.x) : Place{-1, -1, 0};
+  __syncthreads();
+}
+
 // How a thread's eight channels are turned: by the same angles for all heads of
 // a token, so they are kept.  sn has its sign: channel e becomes
-// x[e] cs[e] - partner sn[e].
+// x[e] cs[e] + partner sn[e].
 struct Turn {
-  float cs[8], sn[8];
-  uint32_t which;  // the channels that are turned, a bit each
+  float2 cs[4], sn[4];
+  uint32_t mask[4];  // the channels that are turned, where not all are
+  bool any, all;
 };
 
 __device__ __forceinline__ void load_turn(const RopeView& rope, uint32_t pos, uint32_t c, Turn& o) {
-  const uint32_t F = rope.n_freq;
+  const uint32_t F = rope.n_freq, d0 = 8 * c;
   const float* row = rope.table + (uint64_t)pos * 2 * F;
-  o.which = 0;
+  o.any = d0 < 2 * F;
+  o.all = rope.interleaved ? F % 4 == 0 : F % 8 == 0;
+  if (!o.any) return;
+  if (rope.interleaved && F % 4 == 0) {  // 2 F is a multiple of 8: all eight are turned
+    const float4 x = __ldg(reinterpret_cast<const float4*>(row + 4 * c)), y = __ldg(reinterpret_cast<const float4*>(row + F + 4 * c));
+    const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-  for (uint32_t e = 0; e < 8; ++e) {
-    const uint32_t d = 8 * c + e;
-    const uint32_t i = rope.interleaved ? d / 2 : d < F ? d : d - F;
-    const bool second = rope.interleaved ? d & 1 : d >= F;
-    o.cs[e] = 1.f;
-    o.sn[e] = 0.f;
-    if (d < 2 * F) {
-      o.which |= 1u << e;
-      o.cs[e] = __ldg(row + i);
-      const float s = __ldg(row + F + i);
-      o.sn[e] = second ? -s : s;
+    for (int k = 0; k < 4; ++k) {
+      o.cs[k] = make_float2(xs[k], xs[k]);
+      o.sn[k] = make_float2(-ys[k], ys[k]);
+    }
+  } else if (!rope.interleaved && F % 8 == 0) {
+    const uint32_t i = d0 < F ? d0 : d0 - F;
+    const float sign = d0 < F ? -1.f : 1.f;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float4 x = __ldg(reinterpret_cast<const float4*>(row + i) + k), y = __ldg(reinterpret_cast<const float4*>(row + F + i) + k);
+      o.cs[2 * k] = make_float2(x.x, x.y);
+      o.cs[2 * k + 1] = make_float2(x.z, x.w);
+      o.sn[2 * k] = make_float2(sign * y.x, sign * y.y);
+      o.sn[2 * k + 1] = make_float2(sign * y.z, sign * y.w);
+    }
+  } else {
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+      float cs[2] = {1.f, 1.f}, sn[2] = {0.f, 0.f};
+      o.mask[k] = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < 2; ++e) {
+        const uint32_t d = d0 + 2 * k + e;
+        if (d >= 2 * F) continue;
+        const uint32_t i = rope.interleaved ? d / 2 : d < F ? d : d - F;
+        const bool second = rope.interleaved ? d & 1 : d >= F;
+        o.mask[k] |= 0xFFFFu << (16 * e);
+        cs[e] = __ldg(row + i);
+        const float s = __ldg(row + F + i);
+        sn[e] = second ? s : -s;
+      }
+      o.cs[k] = make_float2(cs[0], cs[1]);
+      o.sn[k] = make_float2(sn[0], sn[1]);
     }
   }
 }
@@ -94,30 +130,29 @@ __device__ __forceinline__ uint4 turn_row(const RopeView& rope, const Turn& t, c
   const uint32_t F = rope.n_freq;
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t p[4] = {x.x, x.y, x.z, x.w};
-  if (!rope.interleaved) {
-    if (F % 8 == 0) {
-      const uint32_t f = F / 8, other = c < f ? c + f : c < 2 * f ? c - f : c;
+  if (rope.interleaved) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(kFull, w[k], other, LANES);
-    } else if (live) {
+    for (int k = 0; k < 4; ++k) p[k] = __byte_perm(w[k], w[k], 0x1032);
+  } else if (F % 8 == 0) {
+    const uint32_t f = F / 8, other = c < f ? c + f : c < 2 * f ? c - f : c;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t d = 8 * c + e;
-        if (t.which >> e & 1) {
-          const uint32_t y = *reinterpret_cast<const uint16_t*>(row + 2 * (d < F ? d + F : d - F));
-          p[e / 2] = e & 1 ? (p[e / 2] & 0xFFFFu) | y << 16 : (p[e / 2] & 0xFFFF0000u) | y;
-        }
+    for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(kFull, w[k], other, LANES);
+  } else if (live && t.any) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t d = 8 * c + e;
+      if (d < 2 * F) {
+        const uint32_t y = *reinterpret_cast<const uint16_t*>(row + 2 * (d < F ? d + F : d - F));
+        p[e / 2] = e & 1 ? (p[e / 2] & 0xFFFFu) | y << 16 : (p[e / 2] & 0xFFFF0000u) | y;
       }
     }
   }
-  uint32_t o[4];
+  if (!t.any) return x;
+  uint32_t o[4] = {w[0], w[1], w[2], w[3]};
+  turn8<T>(o, p, t.cs, t.sn);
+  if (!t.all) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float2 a = Half16<T>::get2(w[k]), b = Half16<T>::get2(p[k]);
-    const float px = rope.interleaved ? b.y : b.x, py = rope.interleaved ? b.x : b.y;
-    const uint32_t lo = t.which >> (2 * k) & 1 ? turn<T>(a.x, t.cs[2 * k], px, t.sn[2 * k]) : w[k] & 0xFFFFu;
-    const uint32_t hi = t.which >> (2 * k + 1) & 1 ? turn<T>(a.y, t.cs[2 * k + 1], py, t.sn[2 * k + 1]) : w[k] >> 16;
-    o[k] = lo | hi << 16;
+    for (int k = 0; k < 4; ++k) o[k] = (o[k] & t.mask[k]) | (w[k] & ~t.mask[k]);
   }
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
@@ -133,8 +168,24 @@ template <typename T>
 __device__ __noinline__ T base_wide(float lo, float s) {
   return Half16<T>::put((double)lo - 16.0 * (double)s);
 }
-__device__ __noinline__ float code_wide(float v, float b, float s) {
-  return (float)floor(((double)v - (double)b) / (double)s - 15.5);
+// Eight codes, where 32 bits do not hold what is taken from b.
+template <typename T>
+__device__ __noinline__ uint32_t codes_wide(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, float b, float s) {
+  const uint32_t w[4] = {w0, w1, w2, w3};
+  const float inv = 1.f / s, half = 0.5f * s;
+  uint32_t code = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float2 pair = Half16<T>::get2(w[e / 2]);
+    const float v = e & 1 ? pair.y : pair.x, y = v - b, z = y - v;
+    const float lost = (v - (y - z)) + (-b - z);  // of y by its rounding
+    float k = fminf(fmaxf(rintf(fmaf(y, inv, -16.f)), 0.f), 15.f);
+    const float r = fmaf(-(k + 16.f), s, y);
+    k += (r > half || (r == half && lost >= 0.f) ? 1.f : 0.f) - (r < -half || (r == -half && lost < 0.f) ? 1.f : 0.f);
+    if (s < 0x1p-100f) k = (float)floor(((double)v - (double)b) / (double)s - 15.5);
+    code |= (uint32_t)fminf(fmaxf(k, 0.f), 15.f) << (4 * (e / 2) + 16 * (e & 1));
+  }
+  return code;
 }
 
 // The codes of eight channels, and their group's scale and base.  A group is
@@ -172,24 +223,25 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
   if (sf == 0.f || !real) return 0;
   uint32_t code = 0;
   const float inv = 1.f / sf, half = 0.5f * sf;
+  // Whether what is taken from b is exact in 32 bits for all eight: then a value on
+  // a code's border is seen to be there (and goes up).
+  const float most = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), fabsf(bf));
+  bool fine = sf >= 0x1p-100f && (bf == 0.f || fabsf(bf) >= Half16<T>::kExact * most);
+  const float least = Half16<T>::kExact * most;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float2 pair = Half16<T>::get2(w[e / 2]);
-    const float v = e & 1 ? pair.y : pair.x, y = v - bf;
-    float k = fminf(fmaxf(rintf(fmaf(y, inv, -16.f)), 0.f), 15.f);
-    const float r = fmaf(-(k + 16.f), sf, y);  // exact within a step
-    // k is the nearest code or, by the division's rounding, beside it; a value
-    // half way goes up, and on that border what y's subtraction lost decides
-    float lost = 0.f;
-    if (fabsf(r) == half) {
-      const float z = y - v;
-      lost = (v - (y - z)) + (-bf - z);
-    }
-    k += (r > half || (r == half && lost >= 0.f) ? 1.f : 0.f) - (r < -half || (r == -half && lost < 0.f) ? 1.f : 0.f);
-    if (sf < 0x1p-100f) k = code_wide(v, bf, sf);
-    k = fminf(fmaxf(k, 0.f), 15.f);
-    code |= (uint32_t)k << (4 * (e / 2) + 16 * (e & 1));
+  for (int i = 0; i < 4; ++i) {
+    const float2 v = Half16<T>::get2(w[i]), y = add2(v, both(-bf));
+    fine &= fminf(fabsf(v.x), fabsf(v.y)) >= least;
+    // y / s to the nearest whole number, in the sum's last bits; y less that many s,
+    // exact, tells whether it is the nearest or, by the reciprocal's rounding, beside it
+    const float2 z = fma2(y, both(inv), both(12582912.f)), k = add2(z, both(-12582912.f)), r = fma2(k, both(-sf), y);
+    int k0 = __float_as_int(z.x) - 0x4B400010 + (r.x >= half ? 1 : 0) - (r.x < -half ? 1 : 0);
+    int k1 = __float_as_int(z.y) - 0x4B400010 + (r.y >= half ? 1 : 0) - (r.y < -half ? 1 : 0);
+    k0 = min(max(k0, 0), 15);
+    k1 = min(max(k1, 0), 15);
+    code |= (uint32_t)k0 << (4 * i) | (uint32_t)k1 << (4 * i + 16);
   }
+  if (!fine) code = codes_wide<T>(w[0], w[1], w[2], w[3], bf, sf);
   return code;
 }
 
@@ -198,34 +250,39 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // A group of LANES threads stays with its token and takes `slice` of its rows;
 // each row is read and written once, so HBM bounds it.
 template <typename T, int LANES, bool FOUR>
-__global__ void __launch_bounds__(kWrThreads) k_kv_write(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWrThreads, FOUR ? 4 : 3) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
   constexpr uint32_t kTok = kWrThreads / LANES;
+  constexpr int kWrRows = FOUR ? 1 : 2;  // rows of a token that a thread works on while it loads as many
   __shared__ Place s_at[kTok];
   const uint64_t t0 = (uint64_t)blockIdx.x * kTok;
-  check_offsets(a);
-  if (threadIdx.x < kTok) s_at[threadIdx.x] = t0 + threadIdx.x < a.n_tok ? find_place(a, t0 + threadIdx.x) : Place{-1, -1, 0};
-  __syncthreads();
+  find_places(a, t0, s_at);
   const Place at = s_at[threadIdx.x / LANES];
   const int64_t t = (int64_t)t0 + threadIdx.x / LANES;
   const uint32_t c = threadIdx.x % LANES, D = a.kv.D, Hq = a.n_q_heads, H = a.kv.H;
   const bool live = at.k >= 0, real = 8 * c < D;
   const bool turned = a.rope.table != nullptr;
   Turn angles;
+  angles.any = false;
   if (turned && live && real) load_turn(a.rope, at.pos, c, angles);
-  else angles.which = 0;
   const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
   auto source = [&](uint32_t r) {
     if (r < Hq) return a.q + 2 * (t * a.q_tok + r * a.q_head);
     if (r < Hq + H) return a.kn + 2 * (t * a.kn_tok + (r - Hq) * a.kn_head);
     return a.vn + 2 * (t * a.vn_tok + (r - Hq - H) * a.vn_head);
   };
+  auto load = [&](uint32_t r) {
+    return r < end && live && real ? *reinterpret_cast<const uint4*>(source(r) + 16 * c) : make_uint4(0, 0, 0, 0);
+  };
+  uint4 x[kWrRows], next[kWrRows];
+#pragma unroll
+  for (int u = 0; u < kWrRows; ++u) next[u] = load(first + u);
+#pragma unroll 1
   for (uint32_t r0 = first; r0 < end; r0 += kWrRows) {
-    uint4 x[kWrRows];
 #pragma unroll
     for (int u = 0; u < kWrRows; ++u) {
-      x[u] = make_uint4(0, 0, 0, 0);
-      if (r0 + u < end && live && real) x[u] = *reinterpret_cast<const uint4*>(source(r0 + u) + 16 * c);
+      x[u] = next[u];
+      next[u] = load(r0 + kWrRows + u);
     }
 #pragma unroll
     for (int u = 0; u < kWrRows; ++u) {
@@ -263,18 +320,16 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
   constexpr uint32_t kTok = kWrThreads / LANES;
   __shared__ Place s_at[kTok];
   const uint64_t t0 = (uint64_t)blockIdx.x * kTok;
-  check_offsets(a);
-  if (threadIdx.x < kTok) s_at[threadIdx.x] = t0 + threadIdx.x < a.n_tok ? find_place(a, t0 + threadIdx.x) : Place{-1, -1, 0};
-  __syncthreads();
+  find_places(a, t0, s_at);
   const Place at = s_at[threadIdx.x / LANES];
   const uint64_t t = t0 + threadIdx.x / LANES;
   const uint32_t c = threadIdx.x % LANES, D = a.kv.D, H = a.kv.H;
   if (at.k < 0 || 8 * c >= D) return;
   const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
-  for (uint32_t r0 = first; r0 < end; r0 += kWrRows) {
-    uint32_t w[kWrRows], p[kWrRows];
+  for (uint32_t r0 = first; r0 < end; r0 += kRdRows) {
+    uint32_t w[kRdRows], p[kRdRows];
 #pragma unroll
-    for (int u = 0; u < kWrRows; ++u) {
+    for (int u = 0; u < kRdRows; ++u) {
       const uint32_t r = r0 + u < end ? r0 + u : end - 1;
       const bool key = r < H;
       const char* row = key ? a.kv.k + at.k + r * a.kv.ks_head : a.kv.v + at.v + (r - H) * a.kv.vs_head;
@@ -282,7 +337,7 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
       p[u] = *reinterpret_cast<const uint32_t*>(row + 4 * (LANES + c / 4));
     }
 #pragma unroll
-    for (int u = 0; u < kWrRows; ++u) {
+    for (int u = 0; u < kRdRows; ++u) {
       const uint32_t r = r0 + u;
       if (r >= end) break;
       const uint32_t s = both_low(p[u]), b = both_high(p[u]);
@@ -300,7 +355,7 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
 dim3 write_grid(WriteArgs& a, uint32_t tok) {
   const uint64_t blocks = (a.n_tok + tok - 1) / tok;
   uint64_t slice = blocks * a.rows / (4 * (uint64_t)num_sms());
-  a.slice = (uint32_t)(slice < 1 ? 1 : slice > 8 ? 8 : slice);
+  a.slice = (uint32_t)(slice < 1 ? 1 : slice > kWrSlice ? kWrSlice : slice);
   if ((a.rows + a.slice - 1) / a.slice > 65535) a.slice = (a.rows + 65534) / 65535;
   return dim3((uint32_t)blocks, (a.rows + a.slice - 1) / a.slice);
 }
