@@ -817,11 +817,13 @@ ptc_status ptc_kv4_read(const ptc_paged_kv* kv, const uint64_t* tok_off, uint64_
 
 /*
  * ptc_kv4_attention — ptc_paged_attention, without accumulated weights, over pages
- * of 4 bits: the same arguments, masks, roundings and refusals.  A tensor of
- * queries and its outputs have the cache's dtype.
+ * of 4 bits: the same arguments, masks, roundings and refusals, and no request of
+ * 2^31 - 256 tokens or more.  A tensor of queries and its outputs have the cache's
+ * dtype.  Where requests have thousands of query rows a key head the workspace has
+ * room for the listed pages in 16 bits, up to 1 GB.
  */
 size_t ptc_kv4_attention_workspace_bytes(uint32_t n_req, uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t head_dim,
-                                         uint32_t max_q_len);
+                                         uint32_t max_q_len, uint64_t n_tok, uint64_t n_page_ids, uint32_t block_size);
 ptc_status ptc_kv4_attention(const ptc_paged_kv* kv, const void* q, const int64_t q_stride[2], const uint64_t* tok_off,
                              uint64_t n_tok, uint32_t n_q_heads, uint32_t max_q_len, float scale, void* out, float* lse,
                              void* ws, size_t ws_bytes, uint32_t* status, void* stream);

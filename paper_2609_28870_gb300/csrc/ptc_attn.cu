@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan(AttnArgs a) {
       const uint64_t lo = a.tok_off[r], hi = a.tok_off[r + 1];
       n = a.kv.kv_len[r];
       const bool hold = pages_hold(a.kv, r, n);
-      const bool wrong = (lo > hi) | (hi > a.n_tok) | (hi - lo > a.max_q_len) | !hold;
+      const bool wrong = (lo > hi) | (hi > a.n_tok) | (hi - lo > a.max_q_len) | (n > a.most) | !hold;
       bad |= wrong;
       m = wrong ? 0 : (uint32_t)(hi - lo);
     }
@@ -255,6 +255,10 @@ uint64_t kept_scores(uint32_t n_q_heads, uint32_t n_kv_heads, uint32_t max_q_len
 
 }  // namespace
 
+ptc_status launch_attention(AttnArgs& a, bool bf16, cudaStream_t s) {
+  return bf16 ? launch<__nv_bfloat16>(a, s) : launch<__half>(a, s);
+}
+
 AttnWs attn_ws(uint32_t n_req, uint32_t ctas, uint32_t D, uint64_t scores) {
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   AttnWs w;
@@ -295,6 +299,7 @@ ptc_status attn_call(AttnArgs& a, const ptc_paged_kv* kv, const uint64_t* tok_of
   a.tq = 128 / a.G;
   a.tq32 = 32 / a.G;
   a.scale = scale;
+  a.most = 0xFFFFFFFFu;
   return PTC_OK;
 }
 ptc_status attn_rows(AttnArgs& a, const void* q, const int64_t* q_stride, uint32_t max_q_len, void* out, float* lse) {
@@ -372,7 +377,7 @@ extern "C" ptc_status ptc_paged_attention(const ptc_paged_kv* kv, const void* q,
   a.scores = scores && n_tok ? reinterpret_cast<float*>(w + at.scores) : nullptr;
   a.few = max_q_len * a.G;
   if (kv_begin(status, ws, s, &a.status) != PTC_OK) return PTC_ERR_CUDA;
-  const ptc_status run = kv->dtype == PTC_DTYPE_BF16 ? launch<__nv_bfloat16>(a, s) : launch<__half>(a, s);
+  const ptc_status run = launch_attention(a, kv->dtype == PTC_DTYPE_BF16, s);
   if (run != PTC_OK) return run;
   return kv_end(status, a.status, s);
 }

@@ -59,6 +59,7 @@ struct AttnArgs {
   float* scores;       // scores of few rows, [n_kv_heads][few][slots], or null
   uint32_t few;
   uint32_t ctas, box;  // box: rows of a tensor copy of keys or values
+  uint32_t most;       // tokens of a request
   uint32_t div_mul, div_shift;  // key / B for pages of 4 bits; see page_division
   uint32_t withhold;   // test of the bounded waits: no queries are loaded
   long long limit;     // cycles after which a wait for another role gives up
@@ -128,6 +129,8 @@ ptc_status attn_call(AttnArgs& a, const ptc_paged_kv* kv, const uint64_t* tok_of
                      uint32_t n_q_heads, float scale);
 ptc_status attn_rows(AttnArgs& a, const void* q, const int64_t* q_stride, uint32_t max_q_len, void* out, float* lse);
 void launch_plan(const AttnArgs& a, bool weights, cudaStream_t s);
+// The whole call over pages of 16 bits, after its checks.
+ptc_status launch_attention(AttnArgs& a, bool bf16, cudaStream_t s);
 bool tokens_map(CUtensorMap* map, const AttnArgs& a, bool bf16, uint32_t tokens);
 bool cache_map(CUtensorMap* map, const KvView& kv, bool bf16, char* base, int64_t page, int64_t head, int64_t slot,
                uint32_t box);

@@ -42,7 +42,7 @@ def declare(L) -> None:
     L.ptc_kv4_read.restype = st
     L.ptc_kv4_read.argtypes = [packed, vp, u64, vp, vp, vp, sz, vp, vp]
     L.ptc_kv4_attention_workspace_bytes.restype = sz
-    L.ptc_kv4_attention_workspace_bytes.argtypes = [u32, u32, u32, u32, u32]
+    L.ptc_kv4_attention_workspace_bytes.argtypes = [u32, u32, u32, u32, u32, u64, u64, u32]
     L.ptc_kv4_attention.restype = st
     L.ptc_kv4_attention.argtypes = [packed, vp, packed, vp, u64, u32, u32, ctypes.c_float, vp, vp, vp, sz, vp, vp]
 
@@ -165,7 +165,8 @@ def ptc_kv4_attention(q, k4, v4, page_ids, page_off, tok_off, kv_len, max_q_len:
     else:
         _want(lse, torch.float32, "lse", dev, 2)
     L = p.lib()
-    w = _room(k4, L.ptc_kv4_attention_workspace_bytes(kv_len.shape[0], Hq, shape[1], D, max_q_len), dev, ws)
+    w = _room(k4, L.ptc_kv4_attention_workspace_bytes(kv_len.shape[0], Hq, shape[1], D, max_q_len, T, page_ids.shape[0],
+                                                      shape[2]), dev, ws)
     rc = L.ptc_kv4_attention(kv, q.data_ptr(), qs, tok_off.data_ptr(), T, Hq, max_q_len,
                              D ** -0.5 if scale is None else scale, out.data_ptr(), lse.data_ptr(), w.data_ptr(),
                              w.numel(), _status(status, dev), _stream(dev))

@@ -229,6 +229,27 @@ def test_many_requests():
     check_attention4(Cache4([(1 + r % 3, 5 + 7 * r % 190) for r in range(1200)], Hq=2, Hkv=1, D=64))
 
 
+@pytest.mark.parametrize("B,D,layout,dtype", [(16, 128, "head", "bf16"), (24, 64, "token", "fp16"), (8, 80, "token", "bf16"),
+                                              (12, 128, "head", "bf16"), (256, 120, "head", "fp16")])
+def test_attention_of_many_rows(B, D, layout, dtype):
+    """Requests of thousands of rows: over a copy of the pages in 16 bits
+    (where pages have a multiple of 8 slots).  List entries behind a request's
+    tokens may name no page; one that is needed may not."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4, check_attention4
+    c = Cache4([(40, 700), (33, 33), (90, 2000)], Hq=128, Hkv=1, D=D, B=B, layout=layout, dtype=dtype, spare=2)
+    for r, n in enumerate(c.total):
+        c.page_ids[int(c.page_off[r + 1]) - 1] = -1
+    check_attention4(c)
+    c.page_ids[int(c.page_off[1])] = c.n_pages
+    with pytest.raises(ptc.PtcError) as e:
+        ptc.ptc_kv4_attention(c.q, *c.table(), c.tok_off, c.kv_len, 90)
+    assert e.value.status == 1
+    c = Cache4([(128, 40), (64, 0), (200, 130)], Hq=64, Hkv=1, D=D, B=B, layout=layout, dtype=dtype)
+    check_attention4(c)  # tokens that see no key
+
+
 def test_attention_refusals():
     import torch
     import paper_2609_28870_gb300 as ptc

@@ -136,7 +136,12 @@ def test_read_and_attention_refusals(L):
     assert call(n_page_ids=1 << 38) == OVERFLOW
     assert call(ws=None) == WORKSPACE and call(ws_bytes=0) == WORKSPACE
     assert call(n_req=0, n_tok=0) == 0
-    assert L.ptc_kv4_attention_workspace_bytes(3, 8, 8, 64, 5) % 256 == 0
+    assert L.ptc_kv4_attention_workspace_bytes(3, 8, 8, 64, 5, 15, 20, 16) % 256 == 0
+    # many rows a request: room for the pages in 16 bits, unless they are no multiple of 8 slots or more than 1 GB
+    plain = L.ptc_kv4_attention_workspace_bytes(1, 8, 2, 128, 4096, 50, 300, 16)
+    assert L.ptc_kv4_attention_workspace_bytes(1, 8, 2, 128, 4096, 4096, 300, 16) >= plain + 300 * 16 * 2 * 128 * 4
+    assert L.ptc_kv4_attention_workspace_bytes(1, 8, 2, 128, 4096, 4096, 400, 12) == plain
+    assert L.ptc_kv4_attention_workspace_bytes(1, 8, 2, 128, 4096, 4096, 1 << 17, 16) == plain
 
 
 def cached():
