@@ -43,6 +43,7 @@ struct Few4Args {
   float2* part_ml;    // their maxima (in powers of two) and sums
   uint32_t ctas;
   uint32_t div_mul, div_shift;  // key / B
+  uint32_t k_page16, v_page16;  // BLOCKS: a page's stride by 16
   uint32_t* status;
 };
 
@@ -242,7 +243,7 @@ __device__ __forceinline__ bool add_up(const Few4Args& a, Shared& sh, uint64_t& 
 // A warp's copies, chunk by chunk, a chunk or more ahead of its products: 16 bytes a
 // lane (cp.async: a tensor or bulk copy of the 1,280 bytes that a head has in a page
 // of 16 takes 90 cycles of the SM's one copy engine, 4.1 TB/s; this took 12 contexts
-// of 32K to 131K from 140 to XXX us).  BLOCKS: 16 keys lie in a row in one page, else
+// of 32K to 131K from 140 to 125 us).  BLOCKS: 16 keys lie in a row in one page, else
 // every lane finds a key's row.  The pages of the chunk after are asked for
 // meanwhile, as a page list comes from HBM too.  Slots of no token read as zeros.
 template <int NS, int NT, bool BLOCKS>
@@ -303,9 +304,9 @@ struct Feed {
         if (!on[x] && id[x] != kNone) report(a.status, PTC_ERR_INVALID_ARG);
         if (!on[x]) id[x] = slot[x] = 0;
         if (BLOCKS) {
-          const uint32_t in = slot[x] * S::kRow;
-          k[x] = kb + id[x] * a.kv.ks_page + in;
-          v[x] = vb + id[x] * a.kv.vs_page + in;
+          const uint32_t in = slot[x] * (S::kRow / 16);
+          k[x] = kb + 16 * (uint64_t)(id[x] * a.k_page16 + in);
+          v[x] = vb + 16 * (uint64_t)(id[x] * a.v_page16 + in);
         } else {
           k[x] = kb + id[x] * a.kv.ks_page + slot[x] * a.kv.ks_slot;
           v[x] = vb + id[x] * a.kv.vs_page + slot[x] * a.kv.vs_slot;
@@ -377,40 +378,40 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
   using S = Shape<NS, NT>;
   using M = Mma16<T>;
   const uint32_t lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  // scores, in two strands where there are only two blocks' to keep the products apart
-  constexpr int kStrands = NT == 1 ? 2 : 1;
+  // scores
   const uint32_t kg = ((g & 6) + 4 * (g & 1) & 7) + 8 * (g & 1), group = NS == 2 ? t : t >> 1;
   float s[2][NT][4];
+  uint32_t wa[2][2 * NS], wb[2][2 * NS], sa[2], ba[2], sb[2], bb[2];
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const uint32_t k_at = at + (16 * u + kg) * S::kRow;
-    uint32_t wa[2 * NS], wb[2 * NS];
-    lds_words<NS>(wa, k_at + 8 * NS * t);
-    lds_words<NS>(wb, k_at + S::kRow + 8 * NS * t);
+    lds_words<NS>(wa[u], k_at + 8 * NS * t);
+    lds_words<NS>(wb[u], k_at + S::kRow + 8 * NS * t);
     const uint32_t pa = lds32(k_at + 32 * NS + 4 * group), pb = lds32(k_at + S::kRow + 32 * NS + 4 * group);
-    const uint32_t sa = both_low(pa), ba = both_high(pa), sb = both_low(pb), bb = both_high(pb);
-    float sum[kStrands][NT][4];
+    sa[u] = both_low(pa);
+    ba[u] = both_high(pa);
+    sb[u] = both_low(pb);
+    bb[u] = both_high(pb);
+  }
 #pragma unroll
-    for (int i = 0; i < 2 * NS; ++i) {
-      uint32_t q[NT][4];
+  for (int i = 0; i < 2 * NS; ++i) {
+    uint32_t q[NT][4];
 #pragma unroll
-      for (int x = 0; x < NT; ++x) lds_words<2>(q[x], q_at + (x * 2 * NS + i) * 512);
+    for (int x = 0; x < NT; ++x) lds_words<2>(q[x], q_at + (x * 2 * NS + i) * 512);
 #pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        const uint32_t a0 = fma16x2<T>(pair4<T>(wa[i], j), sa, ba), a1 = fma16x2<T>(pair4<T>(wb[i], j), sb, bb);
-        const uint32_t a2 = fma16x2<T>(pair4<T>(wa[i], j + 1), sa, ba), a3 = fma16x2<T>(pair4<T>(wb[i], j + 1), sb, bb);
+    for (int j = 0; j < 4; j += 2)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const uint32_t a0 = fma16x2<T>(pair4<T>(wa[u][i], j), sa[u], ba[u]), a1 = fma16x2<T>(pair4<T>(wb[u][i], j), sb[u], bb[u]);
+        const uint32_t a2 = fma16x2<T>(pair4<T>(wa[u][i], j + 1), sa[u], ba[u]);
+        const uint32_t a3 = fma16x2<T>(pair4<T>(wb[u][i], j + 1), sb[u], bb[u]);
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-          float(&d)[4] = sum[i % kStrands][x];
-          if (i < kStrands && j == 0) M::run(d, a0, a1, a2, a3, q[x][j], q[x][j + 1], 0.f, 0.f, 0.f, 0.f);
+          float(&d)[4] = s[u][x];
+          if (i == 0 && j == 0) M::run(d, a0, a1, a2, a3, q[x][j], q[x][j + 1], 0.f, 0.f, 0.f, 0.f);
           else M::run(d, a0, a1, a2, a3, q[x][j], q[x][j + 1], d[0], d[1], d[2], d[3]);
         }
       }
-    }
-#pragma unroll
-    for (int x = 0; x < NT; ++x)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s[u][x][k] = kStrands == 2 ? sum[0][x][k] + sum[kStrands - 1][x][k] : sum[0][x][k];
   }
   // weights; s[u][x][0], [1]: key kg of query rows 2 t and 2 t + 1, [2], [3]: the key after
   if ((int32_t)(key0 + 32) > least) {
@@ -762,7 +763,12 @@ ptc_status launch_few4(const AttnArgs& c, uint32_t rows, char* ws, bool bf16, cu
   a.part_ml = reinterpret_cast<float2*>(ws);
   a.part = reinterpret_cast<float*>(ws + up256(8 * places));
   const int64_t row = row4_bytes(a.kv.D);
-  const bool blocks = a.kv.B % 16 == 0 && a.kv.ks_slot == row && a.kv.vs_slot == row;
+  // (places in the cache by 16 are numbers of 32 bits then)
+  const int64_t most = a.kv.ks_page > a.kv.vs_page ? a.kv.ks_page : a.kv.vs_page;
+  const bool blocks = a.kv.B % 16 == 0 && a.kv.ks_slot == row && a.kv.vs_slot == row &&
+                      most <= (int64_t(1) << 36) / ((int64_t)a.kv.n_pages + 1);
+  a.k_page16 = (uint32_t)(a.kv.ks_page / 16);
+  a.v_page16 = (uint32_t)(a.kv.vs_page / 16);
   page_division(a.kv.B, &a.div_mul, &a.div_shift);
   const ptc_status st = fill_async(a.arrived, 0u, 4 * a.ctas, s);
   if (st != PTC_OK) return st;
