@@ -250,6 +250,91 @@ def test_attention_of_many_rows(B, D, layout, dtype):
     check_attention4(c)  # tokens that see no key
 
 
+def joined(c):
+    """The cache's keys and values in one buffer, a page's keys before its values."""
+    import torch
+    both = torch.stack([c.k, c.v], 1).contiguous()
+    c.k, c.v = both[:, 0], both[:, 1]
+    return c
+
+
+@pytest.mark.parametrize("lens", [[(1, 700), (3, 41)], [(200, 900), (1, 30)], [(700, 700)]])
+@pytest.mark.parametrize("B,D,Hq", [(16, 128, 8), (12, 64, 8)])
+def test_keys_and_values_in_one_buffer(lens, B, D, Hq):
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4, check_attention4
+    c = joined(Cache4(lens, Hq=Hq, Hkv=2, D=D, B=B))
+    check_attention4(c)
+    T = sum(c.new)
+    k, v = ptc.ptc_kv4_read(*c.table(), c.tok_off, c.kv_len, T, D, c.dt)
+    assert torch.equal(k, torch.cat([x[n - m:] for x, (m, n) in zip(c.keys, lens)]))
+    assert torch.equal(v, torch.cat([x[n - m:] for x, (m, n) in zip(c.vals, lens)]))
+    was = c.k.clone(), c.v.clone()
+    ptc.ptc_kv4_append(k, v, *c.table(), c.tok_off, c.kv_len)  # values, quantised again, are other values near them
+    again = ptc.ptc_kv4_read(*c.table(), c.tok_off, c.kv_len, T, D, c.dt)
+    step = 2 / 15 * k.abs().amax()
+    assert float((again[0] - k).abs().max()) <= step and float((again[1] - v).abs().max()) <= 2 / 15 * v.abs().amax()
+    rest = torch.ones(c.n_pages, B, dtype=torch.bool, device="cuda")
+    for r, (m, n) in enumerate(lens):
+        page, slot = c.where(r, n)
+        rest[page[n - m:], slot[n - m:]] = False
+    for now, before in zip((c.k, c.v), was):
+        assert torch.equal(now.transpose(1, 2)[rest], before.transpose(1, 2)[rest])
+
+
+def test_two_calls_at_once():
+    """On two streams, each with its own workspace; and one workspace for calls in turn."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4
+    cs = [Cache4([(1, 5000), (1, 900)], Hq=8, Hkv=2, D=128, seed=1), Cache4([(300, 2000), (5, 70)], Hq=8, Hkv=2, D=128, seed=2)]
+    call = lambda c, **k: ptc.ptc_kv4_attention(c.q, *c.table(), c.tok_off, c.kv_len, max(c.new), **k)
+    want = [call(c) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    status = [torch.zeros(1, dtype=torch.int32, device="cuda") for _ in cs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, c in enumerate(cs):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(call(c, status=status[i]))
+    torch.cuda.synchronize()
+    ws = torch.full((1 << 27,), 255, dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        for i, c in enumerate(cs):
+            got[i].append(call(c, ws=ws))
+    for w, g, s in zip(want, got, status):
+        ptc.check_status(s)
+        for x in g:
+            assert torch.equal(x[0], w[0]) and torch.equal(x[1], w[1])
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(300, 900), (1, 77), (130, 130)], 4, 2), ([(600, 3000)], 8, 1), ([(24, 400)], 8, 8)])
+@pytest.mark.parametrize("D,B", [(128, 16), (64, 12)])
+def test_given_up_waits_then_right_results(lens, Hq, Hkv, D, B):
+    """The tile kernel's waits give up where nothing comes, without a fault; the
+    calls after that are right.  (Requests of few rows wait for nothing.)"""
+    import time
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4, check_attention4
+    c = Cache4(lens, Hq=Hq, Hkv=Hkv, D=D, B=B)
+    check_attention4(c)
+    torch.cuda.synchronize()
+    L = ptc.lib()
+    L.ptc_test_wait_polls(ptc.PTC_TEST_WAIT_ATTENTION + 2000)
+    try:
+        began = time.perf_counter()
+        with pytest.raises(ptc.PtcError) as e:
+            ptc.ptc_kv4_attention(c.q, *c.table(), c.tok_off, c.kv_len, max(c.new))
+        assert e.value.name == "PTC_ERR_TIMEOUT" and time.perf_counter() - began < 1.0
+    finally:
+        L.ptc_test_wait_polls(0)
+    for _ in range(2):
+        check_attention4(c)
+
+
 def test_attention_refusals():
     import torch
     import paper_2609_28870_gb300 as ptc
