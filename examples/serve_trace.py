@@ -13,11 +13,17 @@ requests come in trace order:
 3. eviction  every request is cut to a budget a head by those weights
              (ptc_kv_evict) and decodes on over what is left.
 
+With --bits 4 the pages hold 4 bits a channel, and positions are turned into
+queries and keys on their way (ptc_kv4_append with a table of ptc_rope_table,
+ptc_kv4_attention); prefill and decode only, as evictions go by weights that the
+attention over such pages does not add up.  A shared prefix has the same positions
+in all its requests, so its turned and quantised keys are the same too.
+
 The layer's projections are random tables by token; there are no weights to
 load.  --check repeats every step densely in 64 bits: outputs, accumulated
 weights and the tokens that the eviction keeps.
 
-    python examples/serve_trace.py [--requests N] [--steps S] [--budget TOKENS] [--check]
+    python examples/serve_trace.py [--requests N] [--steps S] [--budget TOKENS] [--bits 16 | 4] [--check]
 """
 import argparse
 import os
@@ -101,15 +107,84 @@ def main():
     ap.add_argument("--requests", type=int, default=48)
     ap.add_argument("--steps", type=int, default=8, help="tokens decoded before and after the eviction")
     ap.add_argument("--budget", type=int, default=512, help="tokens a head that the eviction keeps")
+    ap.add_argument("--bits", type=int, choices=(16, 4), default=16, help="of a cached channel")
     ap.add_argument("--check", action="store_true")
     o = ap.parse_args()
-    tr = tracegen.make(0, max_requests=o.requests)
-    R = tr.n_req
+    serve4(o) if o.bits == 4 else serve16(o)
+
+
+def trace(requests):
+    """The trace's requests as page lists: token offsets, blocks and their
+    offsets, the number of distinct ones, previous uses, and the tokens' words."""
+    tr = tracegen.make(0, max_requests=requests)
     tokens = ptc.to_device_u32(tr.tokens)
     keys, blk_off, _ = ptc.ptc_hash_blocks(tokens, ptc.to_device_u64(tr.req_tok_off), None, B, 0)
     ids, n_blocks = ptc.ptc_assign_ids(keys)
     prev, _ = ptc.ptc_reuse_indices(ids, n_blocks)
-    word = (tokens % VOCAB).long()
+    return (tr.req_tok_off.astype(np.int64), ids, ptc.u64(blk_off).astype(np.int64), n_blocks, ptc.u32(prev),
+            (tokens % VOCAB).long())
+
+
+def found(seen, off, r, n):
+    """Tokens of request r (of n) that an earlier request left in the cache; one at least is computed."""
+    first = np.flatnonzero(seen[off[r]:off[r + 1]] == ptc.PTC_NONE)
+    return min(B * int(first[0] if first.size else off[r + 1] - off[r]), n - 1)
+
+
+def serve4(o):
+    tok_off, ids, off, n_blocks, seen, word = trace(o.requests)
+    R = len(tok_off) - 1
+    tail = (o.steps + B - 1) // B + 1
+    pages, layer = n_blocks + R * tail, Layer()
+    k, v = (torch.zeros(pages, HKV, B, ptc.kv4_row_bytes(D), dtype=torch.uint8, device="cuda") for _ in range(2))
+    freq, factor = ptc.rope_frequencies(D, scaling="parts", factor=4, original=8192)
+    rope = ptc.ptc_rope_table(freq.cuda(), int(np.diff(tok_off).max()) + o.steps, factor)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lists = [torch.cat([ids[off[r]:off[r + 1]], i32(list(range(n_blocks + r * tail, n_blocks + (r + 1) * tail)))])
+             for r in range(R)]
+
+    def check(what, q, out, table, n):
+        """out against dense attention over what the pages stand for."""
+        K, V = ptc.ptc_kv4_read(k, v, *table, offsets([n]), i32([n]), n, D)
+        compare(what, out, *dense(q, K, V)[:2])
+
+    torch.cuda.synchronize()
+    began, reused = time.perf_counter(), 0
+    for r in range(R):
+        n = int(tok_off[r + 1] - tok_off[r])
+        hit = found(seen, off, r, n)
+        reused += hit
+        new, table = word[tok_off[r] + hit:tok_off[r + 1]], (lists[r], offsets([lists[r].numel()]))
+        call = (offsets([n - hit]), i32([n]))
+        q = ptc.ptc_kv4_append(layer.k[new], layer.v[new], k, v, *table, *call, q=layer.q[new], rope=rope, status=status)
+        out, _ = ptc.ptc_kv4_attention(q, k, v, *table, *call, max_q_len=n - hit, status=status)
+        if o.check:
+            check("prefill", q, out, table, n)
+    ptc.check_status(status, "prefill")
+    total = int(tok_off[-1])
+    print(f"prefill: {R} requests, {total} tokens, {reused} of them ({reused / total:.0%}) out of the cache, "
+          f"{(time.perf_counter() - began) * 1e3:.1f} ms")
+
+    g = torch.Generator(device="cuda").manual_seed(1)
+    table = (torch.cat(lists), offsets([x.numel() for x in lists]))
+    lens, one = i32(np.diff(tok_off).tolist()), offsets([1] * R)
+    for _ in range(o.steps):
+        lens += 1
+        new = torch.randint(VOCAB, (R,), generator=g, device="cuda")
+        q = ptc.ptc_kv4_append(layer.k[new], layer.v[new], k, v, *table, one, lens, q=layer.q[new], rope=rope, status=status)
+        out, _ = ptc.ptc_kv4_attention(q, k, v, *table, one, lens, max_q_len=1, status=status)
+        if o.check:
+            for r in range(R):
+                check("decode", q[r:r + 1], out[r:r + 1], (lists[r], offsets([lists[r].numel()])), int(lens[r]))
+    ptc.check_status(status, "decode")
+    size = lambda row: 2 * pages * HKV * B * row / 1e6
+    print(f"decode: {o.steps} steps of {R} requests; {size(k.shape[3]):.1f} MB of pages, {size(2 * D):.1f} MB in 16 bits")
+    print("every step checked against 64 bits" if o.check else "done")
+
+
+def serve16(o):
+    tok_off, ids, off, n_blocks, seen, word = trace(o.requests)
+    R = len(tok_off) - 1
 
     # pages: one a distinct block, then private ones for what follows the full blocks
     tail = (2 * o.steps + B - 1) // B + 1
@@ -118,7 +193,6 @@ def main():
     k = torch.zeros(pages, HKV, B, D, dtype=torch.bfloat16, device="cuda")
     v = torch.zeros_like(k)
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
-    tok_off, off, seen = tr.req_tok_off.astype(np.int64), ptc.u64(blk_off).astype(np.int64), ptc.u32(prev)
     lists = [torch.cat([ids[off[r]:off[r + 1]], i32(list(range(n_blocks + r * tail, n_blocks + (r + 1) * tail)))])
              for r in range(R)]
 
@@ -127,8 +201,7 @@ def main():
     began, reused = time.perf_counter(), 0
     for r in range(R):
         n = int(tok_off[r + 1] - tok_off[r])
-        first = np.flatnonzero(seen[off[r]:off[r + 1]] == ptc.PTC_NONE)
-        hit = min(B * int(first[0] if first.size else off[r + 1] - off[r]), n - 1)  # a token at least is computed
+        hit = found(seen, off, r, n)
         reused += hit
         new = word[tok_off[r] + hit:tok_off[r + 1]]
         table = (k, v, lists[r], offsets([lists[r].numel()]))

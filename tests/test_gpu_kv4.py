@@ -425,3 +425,14 @@ def test_a_captured_decode_loop(dtype):
     stream.synchronize()
     ptc.check_status(status)
     assert c.kv_len.tolist() == [n + steps for n in prompts]
+
+
+def test_example_over_pages_of_4_bits():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "examples", "serve_trace.py"), "--requests", "12", "--steps", "3",
+                        "--bits", "4", "--check"], capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout + r.stderr
+    assert "every step checked against 64 bits" in r.stdout
