@@ -209,11 +209,12 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
   const float lo = ends.x, hi = -ends.y;
   words = 0;
   if (m == kInf2) return 0;  // no channel in the group (an infinity among them makes the other end finite or -infinity)
-  const float d = hi - lo, s32 = d / 15.f;
+  // (three roundings of half a unit: within 3 units in the last place)
+  const float d = hi - lo, s32 = d * (1.f / 15.f);
   const T s = Half16<T>::unsure(s32) || !(d < INFINITY) ? scale_wide<T>(lo, hi) : Half16<T>::put(s32);
-  const float sf = Half16<T>::get(s), s16 = 16.f * sf, b32 = lo - s16, back = b32 - lo;
-  const float left = (lo - (b32 - back)) + (-s16 - back);  // what the subtraction lost
-  const T base = (left != 0.f && Half16<T>::unsure(b32)) || !(s16 < INFINITY) ? base_wide<T>(lo, sf) : Half16<T>::put(b32);
+  const float sf = Half16<T>::get(s), s16 = 16.f * sf;
+  const bool near = lo == 0.f || (fabsf(lo) >= Half16<T>::kExact * s16 && s16 >= Half16<T>::kExact * fabsf(lo));
+  const T base = near && s16 < INFINITY ? Half16<T>::put(lo - s16) : base_wide<T>(lo, sf);
   const float bf = Half16<T>::get(base);
   if (!(sf < INFINITY) || !(fabsf(bf) < INFINITY)) {
     words = Half16<T>::kBf16 ? 0x7FC07FC0u : 0x7E007E00u;
@@ -222,7 +223,9 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
   words = bits16(s) | bits16(base) << 16;
   if (sf == 0.f || !real) return 0;
   uint32_t code = 0;
-  const float inv = 1.f / sf, half = 0.5f * sf;
+  float inv;  // (within a unit or two: what is left of a value after a code tells)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sf));
+  const float half = 0.5f * sf;
   // Whether what is taken from b is exact in 32 bits for all eight: then a value on
   // a code's border is seen to be there (and goes up).
   const float most = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), fabsf(bf));
@@ -235,11 +238,9 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
     // y / s to the nearest whole number, in the sum's last bits; y less that many s,
     // exact, tells whether it is the nearest or, by the reciprocal's rounding, beside it
     const float2 z = fma2(y, both(inv), both(12582912.f)), k = add2(z, both(-12582912.f)), r = fma2(k, both(-sf), y);
-    int k0 = __float_as_int(z.x) - 0x4B400010 + (r.x >= half ? 1 : 0) - (r.x < -half ? 1 : 0);
-    int k1 = __float_as_int(z.y) - 0x4B400010 + (r.y >= half ? 1 : 0) - (r.y < -half ? 1 : 0);
-    k0 = min(max(k0, 0), 15);
-    k1 = min(max(k1, 0), 15);
-    code |= (uint32_t)k0 << (4 * i) | (uint32_t)k1 << (4 * i + 16);
+    const int k0 = __float_as_int(z.x) - 0x4B400010 + (r.x >= half ? 1 : 0) - (r.x < -half ? 1 : 0);
+    const int k1 = __float_as_int(z.y) - 0x4B400010 + (r.y >= half ? 1 : 0) - (r.y < -half ? 1 : 0);
+    code |= __vimin_s16x2_relu(__byte_perm(k0, k1, 0x5410), 0x000F000F) << (4 * i);
   }
   if (!fine) code = codes_wide<T>(w[0], w[1], w[2], w[3], bf, sf);
   return code;
@@ -250,7 +251,7 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // A group of LANES threads stays with its token and takes `slice` of its rows;
 // each row is read and written once, so HBM bounds it.
 template <typename T, int LANES, bool FOUR>
-__global__ void __launch_bounds__(kWrThreads, FOUR ? 4 : 3) k_kv_write(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
   constexpr uint32_t kTok = kWrThreads / LANES;
   constexpr int kWrRows = FOUR ? 1 : 2;  // rows of a token that a thread works on while it loads as many
@@ -266,49 +267,77 @@ __global__ void __launch_bounds__(kWrThreads, FOUR ? 4 : 3) k_kv_write(const __g
   angles.any = false;
   if (turned && live && real) load_turn(a.rope, at.pos, c, angles);
   const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
-  auto source = [&](uint32_t r) {
-    if (r < Hq) return a.q + 2 * (t * a.q_tok + r * a.q_head);
-    if (r < Hq + H) return a.kn + 2 * (t * a.kn_tok + (r - Hq) * a.kn_head);
-    return a.vn + 2 * (t * a.vn_tok + (r - Hq - H) * a.vn_head);
+  // Where row r comes from and where it goes: queries, keys and values each lie a
+  // stride apart, so a place is found once for all rows of a kind.
+  auto source = [&](uint32_t r, int64_t& step, uint32_t& last) {
+    if (r < Hq) {
+      step = 2 * a.q_head;
+      last = Hq;
+      return a.q + 2 * t * a.q_tok + r * step;
+    }
+    const bool key = r < Hq + H;
+    step = 2 * (key ? a.kn_head : a.vn_head);
+    last = key ? Hq + H : a.rows;
+    return (key ? a.kn + 2 * t * a.kn_tok : a.vn + 2 * t * a.vn_tok) + (r - Hq - (key ? 0 : H)) * step;
   };
-  auto load = [&](uint32_t r) {
-    return r < end && live && real ? *reinterpret_cast<const uint4*>(source(r) + 16 * c) : make_uint4(0, 0, 0, 0);
+  auto target = [&](uint32_t r, int64_t& step) {
+    if (r < Hq) {
+      step = 2 * a.o_head;
+      return a.q_out + 2 * t * a.o_tok + r * step;
+    }
+    const bool key = r < Hq + H;
+    constexpr int kUnit = FOUR ? 1 : 2;  // bytes of a stride's unit
+    step = kUnit * (key ? a.kv.ks_head : a.kv.vs_head);
+    return (key ? a.kv.k + kUnit * at.k : a.kv.v + kUnit * at.v) + (r - Hq - (key ? 0 : H)) * step;
+  };
+  uint32_t ahead = first, ahead_last, last;
+  int64_t ahead_step, from_step, step;
+  const char* ahead_at = source(first, ahead_step, ahead_last);
+  const char* from = source(first, from_step, last);
+  char* to = target(first, step);
+  auto load = [&] {
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (ahead < end) {
+      if (live && real) x = *reinterpret_cast<const uint4*>(ahead_at + 16 * c);
+      ahead_at += ahead_step;
+      if (++ahead == ahead_last && ahead < end) ahead_at = source(ahead, ahead_step, ahead_last);
+    }
+    return x;
   };
   uint4 x[kWrRows], next[kWrRows];
 #pragma unroll
-  for (int u = 0; u < kWrRows; ++u) next[u] = load(first + u);
+  for (int u = 0; u < kWrRows; ++u) next[u] = load();
 #pragma unroll 1
   for (uint32_t r0 = first; r0 < end; r0 += kWrRows) {
 #pragma unroll
     for (int u = 0; u < kWrRows; ++u) {
       x[u] = next[u];
-      next[u] = load(r0 + kWrRows + u);
+      next[u] = load();
     }
 #pragma unroll
     for (int u = 0; u < kWrRows; ++u) {
       const uint32_t r = r0 + u;
       if (r >= end) break;  // the whole CTA
       uint4 y = x[u];
-      if (turned && r < Hq + H) y = turn_row<T, LANES>(a.rope, angles, x[u], source(r), c, live);
+      if (turned && r < Hq + H) y = turn_row<T, LANES>(a.rope, angles, x[u], from, c, live);
       __syncwarp();  // a row is written after all of it was read
-      if (r < Hq) {
-        if (live && real) *reinterpret_cast<uint4*>(a.q_out + 2 * (t * a.o_tok + r * a.o_head) + 16 * c) = y;
-        continue;
-      }
-      const bool key = r < Hq + H;
-      const int64_t head = r - Hq - (key ? 0 : H);
-      char* to = key ? a.kv.k : a.kv.v;
-      const int64_t place = (key ? at.k : at.v) + head * (key ? a.kv.ks_head : a.kv.vs_head);
-      if (!FOUR) {
-        if (live && real) *reinterpret_cast<uint4*>(to + 2 * place + 16 * c) = y;
+      if (!FOUR || r < Hq) {
+        if (live && real) *reinterpret_cast<uint4*>(to + 16 * c) = y;
       } else {
         uint32_t words;
         const uint32_t code = quantise<T>(y, live && real, words);
-        if (!live) continue;
-        uint32_t* row = reinterpret_cast<uint32_t*>(to + place);
-        row[c] = code;
-        if (c % 4 == 0) row[LANES + c / 4] = words;
-        if (LANES == 8 && c % 4 == 1) row[10 + c / 4] = 0;
+        if (live) {
+          uint32_t* row = reinterpret_cast<uint32_t*>(to);
+          row[c] = code;
+          if (c % 4 == 0) row[LANES + c / 4] = words;
+          if (LANES == 8 && c % 4 == 1) row[10 + c / 4] = 0;
+        }
+      }
+      from += from_step;
+      to += step;
+      if (r + 1 == last && r + 1 < end) {
+        from = source(r + 1, from_step, last);
+        to = target(r + 1, step);
       }
     }
   }

@@ -23,12 +23,12 @@ struct Half16<__nv_bfloat16> {
     const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
   }
-  static constexpr float kExact = 0x1p-14f;  // sums of numbers whose sizes are no further apart are exact in 32 bits
-  // Whether 32 bits that are within 2 units in their last place may lie on the
+  static constexpr float kExact = 0x1p-15f;  // sums of numbers whose sizes are no further apart are exact in 32 bits
+  // Whether 32 bits that are within 4 units in their last place may lie on the
   // other side of a rounding's border, or are too small for such a bound.
   static __device__ __forceinline__ bool unsure(float x) {
     const uint32_t u = __float_as_uint(x);
-    return ((u & 0xFFFFu) - 0x7FFEu <= 4u) | (fabsf(x) < 0x1p-90f && x != 0.f);
+    return ((u & 0xFFFFu) - 0x7FFCu <= 8u) | (fabsf(x) < 0x1p-90f && x != 0.f);
   }
 };
 template <>
@@ -43,11 +43,11 @@ struct Half16<__half> {
     const __half2 x = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
   }
-  static constexpr float kExact = 0x1p-11f;
+  static constexpr float kExact = 0x1p-12f;
   // (among fp16's subnormals the border lies elsewhere)
   static __device__ __forceinline__ bool unsure(float x) {
     const uint32_t u = __float_as_uint(x);
-    return ((u & 0x1FFFu) - 0xFFEu <= 4u) | (fabsf(x) < 0x1p-13f && x != 0.f);
+    return ((u & 0x1FFFu) - 0xFFCu <= 8u) | (fabsf(x) < 0x1p-13f && x != 0.f);
   }
 };
 
