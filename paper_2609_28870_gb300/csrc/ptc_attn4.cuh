@@ -9,7 +9,7 @@ namespace ptc {
 
 // Most query rows (new tokens times query heads of a key head) of a request that
 // k_attn4_few takes.
-constexpr uint32_t kFew4Rows = 16;
+constexpr uint32_t kFew4Rows = 32;
 constexpr uint32_t kFew4MaxCtas = 512;
 constexpr uint32_t kMost4 = 0x7FFFFF00u;  // tokens of a request: positions are signed 32-bit numbers
 

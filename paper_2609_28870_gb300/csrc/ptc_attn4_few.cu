@@ -88,16 +88,19 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// NS: rows of 64 or 128 channels.  NT: eight or sixteen query rows.
+// NS: rows of 64 or 128 channels.  NT: 8, 16 or 32 query rows.
 template <int NS, int NT>
 struct Shape {
   static constexpr uint32_t kDim = 64 * NS, kRow = NS == 1 ? 48 : 80, kQRows = 8 * NT;
   static constexpr uint32_t kTensor = kChunk * kRow, kStage = 2 * kTensor;  // a warp's chunk
   static constexpr uint32_t kCtas = NS * NT <= 2 ? 2 : 1;  // of an SM: by their registers
-  static constexpr uint32_t kRing = kCtas == 1 ? 4 : NS == 1 ? 3 : 2;
+  static constexpr uint32_t kRing = kCtas == 1 ? (NT == 4 ? 3 : 4) : NS == 1 ? 3 : 2;
+  static constexpr int kBlocks = NS * NT == 8 ? 1 : 2;     // of 16 keys at a time: by the registers again
   static constexpr uint32_t kORow = kDim + 4;  // 32-bit words of a row on its way to the other warps
   static constexpr uint32_t kRegion = NT * 512 * (4 * NS + 1);  // a warp's rows, as lanes hold them or row by row
-  static constexpr uint32_t kBytes = kWarps * kRing * kStage + kTeam * kRegion;
+  static constexpr uint32_t kQueries = 2 * NS * NT * 512;         // the queries' operand; see take_units
+  static constexpr uint32_t kRows0 = kWarps * kRing * kStage, kQueries0 = kRows0 + kTeam * kRegion;
+  static constexpr uint32_t kBytes = kQueries0 + kQueries;
   static_assert(kQRows * kORow * 4 <= kRegion, "a warp's rows");
 };
 
@@ -107,7 +110,6 @@ struct Shared {
   uint32_t m[256], n[256];
   uint64_t warp_sum[8];
   float2 ml[kTeam][kFew4Rows];
-  uint4 q[8][32];  // the queries' operand: 16 bytes a lane, 4 NS NT of them; see product_warps
   uint32_t last;
 };
 
@@ -368,11 +370,11 @@ struct Rows {
   float top[NT][2], l[NT][2], o[NT][4 * NS][4];
 };
 
-// 32 keys of a unit, as two blocks of 16.  Row i of a block's matrices is key (2 (i %
+// Up to 32 keys of a unit, as blocks of 16.  Row i of a block's matrices is key (2 (i %
 // 8 / 2) + 4 (i % 2)) % 8 + 8 (i % 2) + i / 8: rows of 80 (48) bytes in that order meet
 // no bank twice, neither where four lanes read K's rows whole nor where eight read a
 // piece of V's each.
-template <typename T, int NS, int NT>
+template <typename T, int NS, int NT, int U>
 __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n, const int32_t (&see)[NT][2], int32_t least,
                                           float sl2, uint32_t q_at, Rows<NS, NT>& st) {
   using S = Shape<NS, NT>;
@@ -380,10 +382,10 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
   const uint32_t lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   // scores
   const uint32_t kg = ((g & 6) + 4 * (g & 1) & 7) + 8 * (g & 1), group = NS == 2 ? t : t >> 1;
-  float s[2][NT][4];
-  uint32_t wa[2][2 * NS], wb[2][2 * NS], sa[2], ba[2], sb[2], bb[2];
+  float s[U][NT][4];
+  uint32_t wa[U][2 * NS], wb[U][2 * NS], sa[U], ba[U], sb[U], bb[U];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
+  for (int u = 0; u < U; ++u) {
     const uint32_t k_at = at + (16 * u + kg) * S::kRow;
     lds_words<NS>(wa[u], k_at + 8 * NS * t);
     lds_words<NS>(wb[u], k_at + S::kRow + 8 * NS * t);
@@ -401,7 +403,7 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
 #pragma unroll
     for (int j = 0; j < 4; j += 2)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int u = 0; u < U; ++u) {
         const uint32_t a0 = fma16x2<T>(pair4<T>(wa[u][i], j), sa[u], ba[u]), a1 = fma16x2<T>(pair4<T>(wb[u][i], j), sb[u], bb[u]);
         const uint32_t a2 = fma16x2<T>(pair4<T>(wa[u][i], j + 1), sa[u], ba[u]);
         const uint32_t a3 = fma16x2<T>(pair4<T>(wb[u][i], j + 1), sb[u], bb[u]);
@@ -414,19 +416,19 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
       }
   }
   // weights; s[u][x][0], [1]: key kg of query rows 2 t and 2 t + 1, [2], [3]: the key after
-  if ((int32_t)(key0 + 32) > least) {
+  if ((int32_t)(key0 + 16 * U) > least) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           if ((int32_t)(key0 + 16 * u + kg + (k >> 1)) >= see[x][k & 1]) s[u][x][k] = -INFINITY;
   }
-  float p[2][NT][4], most = 0.f;
+  float p[U][NT][4], most = 0.f;
   auto weigh = [&] {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int x = 0; x < NT; ++x)
 #pragma unroll
@@ -441,7 +443,7 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
     for (int x = 0; x < NT; ++x)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        float mx = fmaxf(fmaxf(s[0][x][y], s[0][x][y + 2]), fmaxf(s[1][x][y], s[1][x][y + 2])) * sl2;
+        float mx = fmaxf(fmaxf(s[0][x][y], s[0][x][y + 2]), fmaxf(s[U - 1][x][y], s[U - 1][x][y + 2])) * sl2;
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, o));
         const float top = st.top[x][y], up = fmaxf(top, mx), f = exp2_approx(top - up);
@@ -457,7 +459,7 @@ __device__ __forceinline__ void take_keys(uint32_t at, uint32_t key0, uint32_t n
   }
   const uint32_t r0 = 2 * t, r1 = ((2 * t + 4) & 7) + 8, v_group = NS == 2 ? g >> 1 : g >> 2;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
+  for (int u = 0; u < U; ++u) {
     uint32_t b[NT][2];
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
@@ -543,15 +545,17 @@ __device__ __noinline__ void join_row(const Few4Args& a, uint32_t c0, uint32_t c
 }
 
 template <typename T, int NS, int NT, bool BLOCKS>
-__device__ __forceinline__ void take_units(const Few4Args& a, Shared& sh, Way& w, bool more, uint32_t ring, char* rows,
-                                           uint64_t all, uint32_t ctas) {
+__device__ __forceinline__ void take_units(const Few4Args& a, Shared& sh, Way& w, bool more, char* smem, uint64_t all,
+                                           uint32_t ctas) {
   using S = Shape<NS, NT>;
   using M = Mma16<T>;
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, team = warp / kTeam;
   const uint32_t D = a.kv.D, G = a.G;
   const float sl2 = a.scale * kLog2e;
-  const uint32_t q_at = smem_u32(&sh.q[0][lane]);
-  ring += warp * S::kRing * S::kStage;
+  const uint32_t ring = smem_u32(smem) + warp * S::kRing * S::kStage;
+  char* rows = smem + S::kRows0;
+  uint4* queries = reinterpret_cast<uint4*>(smem + S::kQueries0);
+  const uint32_t q_at = smem_u32(queries + lane);
   Feed<NS, NT, BLOCKS> feed;
   feed.begin(a, sh, w, more);
 #pragma unroll
@@ -560,12 +564,12 @@ __device__ __forceinline__ void take_units(const Few4Args& a, Shared& sh, Way& w
   for (; more; more = w.next(a, sh)) {
     // the queries' operand, once for all warps: lane (g, t) of it has, of row 8 x + g,
     // channels 16 NS t on, eight a piece
-    if (warp < 2 * NS * NT) {
-      const uint32_t i = 8 * (warp / (2 * NS)) + g, d = 16 * NS * t + 8 * (warp % (2 * NS)), tok = i / G;
+    for (uint32_t x = warp; x < 2 * NS * NT; x += kWarps) {
+      const uint32_t i = 8 * (x / (2 * NS)) + g, d = 16 * NS * t + 8 * (x % (2 * NS)), tok = i / G;
       uint4 y = make_uint4(0, 0, 0, 0);
       if (tok < w.m && d < D)
         y = *reinterpret_cast<const uint4*>(a.q + 2 * ((int64_t)(w.tok0 + tok) * a.q_tok + (int64_t)(w.h * G + i % G) * a.q_head + d));
-      sh.q[warp][lane] = y;
+      queries[x * 32 + lane] = y;
     }
     int32_t see[NT][2];
 #pragma unroll
@@ -594,7 +598,11 @@ __device__ __forceinline__ void take_units(const Few4Args& a, Shared& sh, Way& w
       cp_async_wait<S::kRing - 2>();
       __syncwarp();  // the chunk is there for all lanes, and all are through with the one before
       feed.issue(a, sh, ring);
-      if (key0 < w.n) take_keys<T, NS, NT>(ring + item % S::kRing * S::kStage, key0, w.n, see, least, sl2, q_at, st);
+      const uint32_t at = ring + item % S::kRing * S::kStage;
+#pragma unroll
+      for (uint32_t u = 0; u < 2; u += S::kBlocks)
+        if (key0 + 16 * u < w.n)
+          take_keys<T, NS, NT, S::kBlocks>(at + 16 * u * S::kRow, key0 + 16 * u, w.n, see, least, sl2, q_at, st);
     }
     // the warps' rows: the second team's are added to the first's
     char* region = rows + (warp % kTeam) * S::kRegion;
@@ -719,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, Shape<NS, NT>::kCtas) k_attn4_few(co
   if (blockIdx.x >= ctas) return;
   Way w;
   const bool more = w.begin(a, sh, all, blockIdx.x, ctas);
-  take_units<T, NS, NT, BLOCKS>(a, sh, w, more, smem_u32(smem_raw), smem_raw + kWarps * S::kRing * S::kStage, all, ctas);
+  take_units<T, NS, NT, BLOCKS>(a, sh, w, more, smem_raw, all, ctas);
 }
 
 template <typename T, int NS, int NT, bool BLOCKS>
@@ -733,23 +741,24 @@ ptc_status launch_one(const Few4Args& a, cudaStream_t s) {
 }
 template <typename T>
 ptc_status launch_some(const Few4Args& a, uint32_t rows, bool blocks, cudaStream_t s) {
-  const bool wide = a.kv.D > 64, two = rows > 8;
 #define PTC_FEW4(NS, NT) (blocks ? launch_one<T, NS, NT, true>(a, s) : launch_one<T, NS, NT, false>(a, s))
-  return wide ? two ? PTC_FEW4(2, 2) : PTC_FEW4(2, 1) : two ? PTC_FEW4(1, 2) : PTC_FEW4(1, 1);
+  if (a.kv.D > 64) return rows > 16 ? PTC_FEW4(2, 4) : rows > 8 ? PTC_FEW4(2, 2) : PTC_FEW4(2, 1);
+  return rows > 16 ? PTC_FEW4(1, 4) : rows > 8 ? PTC_FEW4(1, 2) : PTC_FEW4(1, 1);
 #undef PTC_FEW4
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
+uint32_t padded_rows(uint32_t rows) { return rows > 16 ? 32 : rows > 8 ? 16 : 8; }
 uint32_t few4_ctas(uint32_t head_dim, uint32_t rows) {
-  const uint32_t n = (uint32_t)num_sms() * (head_dim > 64 && rows > 8 ? 1 : 2);
+  const uint32_t n = (uint32_t)num_sms() * (padded4(head_dim) / 64 * padded_rows(rows) <= 16 ? 2 : 1);
   return n < kFew4MaxCtas ? n : kFew4MaxCtas;
 }
 
 }  // namespace
 
 size_t few4_ws(uint32_t head_dim, uint32_t rows) {
-  const size_t places = 2 * (size_t)few4_ctas(head_dim, rows) * (rows > 8 ? 16 : 8);
+  const size_t places = 2 * (size_t)few4_ctas(head_dim, rows) * padded_rows(rows);
   return up256(4 * kFew4MaxCtas) + up256(8 * places) + up256(4 * places * padded4(head_dim));
 }
 
@@ -757,7 +766,7 @@ ptc_status launch_few4(const AttnArgs& c, uint32_t rows, char* ws, bool bf16, cu
   Few4Args a{c.kv, c.q, c.q_tok, c.q_head, c.tok_off, c.n_tok, c.n_q_heads, c.G, c.max_q_len, c.scale, c.out, c.lse};
   a.status = c.status;
   a.ctas = few4_ctas(a.kv.D, rows);
-  const size_t places = 2 * (size_t)a.ctas * (rows > 8 ? 16 : 8);
+  const size_t places = 2 * (size_t)a.ctas * padded_rows(rows);
   a.arrived = reinterpret_cast<uint32_t*>(ws);
   ws += up256(4 * kFew4MaxCtas);
   a.part_ml = reinterpret_cast<float2*>(ws);
