@@ -12,15 +12,29 @@
 // A word of codes is eight neighbouring channels of a key, even ones in its low
 // half, so a shifted and masked word is two channels as K's operand wants them;
 // the low (high) halves of two keys' words together are one channel of both, as
-// V^T's operand does.  Eight query rows are all that an instruction's N asks for.
+// V^T's operand does.  Eight query rows are what an instruction's N asks for; 16 and
+// 32 take two and four for the same operand.
 //
 // A call's units are 128 keys of a request's key head, and `kExtra` for what a
-// head's tile costs by itself.  CTA c of C has the units from U c / C on, so where
-// a cut lies, and which CTAs share a tile, is arithmetic that every CTA does for
-// itself from the requests' lengths; there is no plan to wait for.  A warp takes
-// 32 keys of every 256 and copies its next ones into a ring of its own meanwhile, so
-// no warp waits for another until the tile's end, where they put their rows together;
-// of a split tile the last CTA that is done does so with the parts.
+// head's tile costs by itself (1, 2, 3, 4: 85, 84, 84, 85 us for 64 single tokens).
+// CTA c of C has the units from U c / C on, so where a cut lies, and which CTAs share
+// a tile, is arithmetic that every CTA does for itself from the requests' lengths;
+// there is no plan to wait for.  A warp takes 32 keys of every 256 and copies its next
+// ones into a ring of its own meanwhile, so no warp waits for another until the
+// tile's end, where they put their rows together; of a split tile the last CTA that
+// is done does so with the parts.
+//
+// Bounds.  At 128 channels and up to 8 rows 16 keys are 360 instructions of a warp,
+// of which the codes take 230 (shift, mask and multiply-add for two values, the
+// products, their loads): 12 single tokens over 32K to 131K, 0.57 GB, take 115 us, 4.9
+// TB/s, with 63% of the issue slots and 60% of the ALUs' in use at 1.8 GHz; what is
+// left waits for fixed latencies, which four warps a scheduler, 128 registers each, do
+// not hide.  (165 us with a warp of its own for the copies and 16 keys at a time; 132
+// with a mask and an or in one instruction; 125 with the warps' own copies; 119 with
+// places in the cache kept a tile; 115 with both blocks' products side by side.)  Two
+// and four instructions an operand: 149 and 219 us, at 8 warps an SM.  64 single tokens
+// over 1.1K to 12K 81 us, one over 1,012 9 us, a chain of latencies: a launch that
+// clears the counts, lengths, pages, keys, parts.
 #include "ptc_attn4.cuh"
 
 namespace ptc {

@@ -153,7 +153,8 @@ constexpr int kSlabBytes = 128 * 128;  // 128 rows of 64 columns
 // 4 KB a softmax warp: rows on their way out; the sums of 8 warps, 32 rows and 32 columns.
 constexpr int kStage = 8 * 4096;
 // Registers a thread: 2 * 128 * 200 + 128 * 104 = 384 * 168, what the block has at launch.
-// With four warps more: 256 * 184 + 256 * 72 = 512 * 128 (4,096 tokens at 32K: 1.47 ms; with 200, 56 and 56 2.0 ms, the copies' state in local memory).
+// With four warps more: 256 * 184 + 256 * 72 = 512 * 128 (4,096 tokens at 32K: 1.47 ms;
+// with 200, 56 and 56 2.0 ms, the copies' state in local memory).
 constexpr int kSoftmaxRegs = 200, kOtherRegs = 104, kSoftmaxRegs4 = 184, kOtherRegs4 = 72, kQuantRegs4 = 72;
 
 struct TileShared {
@@ -1031,6 +1032,12 @@ __device__ __forceinline__ bool gather_role(const AttnArgs& a, TileShared& sh, u
 // ring of tiles, swizzled as the products want them: four (two) lanes a row, 32
 // channels each, three instructions and half a store for two values.  Slots of no
 // token, or of a page that the cache does not have, are zeros.
+//
+// Bounds.  Shared memory: the products read 192 KB a pair of tiles, these warps write
+// 64, and 20 of codes go in and out, 2,520 cycles at 128 bytes a cycle of the 3,240
+// that a pair takes (without any of these warps' traffic 2,700, as over 16-bit pages;
+// without their arithmetic no less).  Loading the codes into registers instead took
+// 1.68 to 3.19 ms for the 1.47 of 4,096 tokens at 32K.
 template <typename T, int NSLAB>
 __device__ __forceinline__ bool quant_role(const AttnArgs& a, TileShared& sh, uint32_t ring, uint32_t tiles4) {
   using Sh = TileShape<NSLAB, kFour>;

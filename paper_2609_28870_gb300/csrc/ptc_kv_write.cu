@@ -248,8 +248,13 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 
 // The rows of tokens: queries, keys and values, LANES threads a row with eight
 // channels each (so that a row stays within a warp: it may be turned in place).
-// A group of LANES threads stays with its token and takes `slice` of its rows;
-// each row is read and written once, so HBM bounds it.
+// A group of LANES threads stays with its token and takes `slice` of its rows, so that
+// the token's place and angles are found once for them; a row or two are loaded while
+// as many are worked on.  Each row is read and written once, 0.86 GB for 34,692 tokens
+// of 32 query and 8 key heads of 128: 152 us, 5.6 TB/s; one of 4 bits 213 us, 3.6 TB/s,
+// bound by its 420 instructions for 512 values (the group's ends, scale and base, and
+// 13 a value), at 79% of the issue slots.  64 tokens 4.4 us, a launch and four
+// dependent reads.
 template <typename T, int LANES, bool FOUR>
 __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
@@ -343,6 +348,7 @@ __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constan
   }
 }
 
+// Tokens back out of their pages: 0.46 GB in 73 us, 6.3 TB/s, at HBM's rate.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
@@ -379,8 +385,7 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
 }
 
 // Rows of a CTA: as few as leave four CTAs for every SM, so that a call of few
-// tokens is spread, and at most 8, so that a token's place and angles serve
-// several rows.
+// tokens is spread, and at most kWrSlice (8: 210 us for what 24 take 189).
 dim3 write_grid(WriteArgs& a, uint32_t tok) {
   const uint64_t blocks = (a.n_tok + tok - 1) / tok;
   uint64_t slice = blocks * a.rows / (4 * (uint64_t)num_sms());
