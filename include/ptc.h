@@ -844,7 +844,8 @@ void ptc_release_host_staging(void);
  * PTC_ERR_TIMEOUT and leave the device usable.  With
  * PTC_TEST_WAIT_PIECES + polls it is stage c's wait that gives up (a call with
  * fewer than 2,049 pieces has none).  With PTC_TEST_WAIT_ATTENTION + polls it is
- * the roles of ptc_paged_attention's CTAs, which wait for one another for about
+ * the roles of ptc_paged_attention's CTAs (and of ptc_kv4_attention's where
+ * requests have more than 32 query rows), which wait for one another for about
  * two seconds at most: no queries are loaded, and the waits for them, and for
  * what depends on them, give up after `polls` times 1,024 clock cycles.  0
  * restores normal waits.  Process-wide; not for production use.

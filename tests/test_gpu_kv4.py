@@ -310,7 +310,7 @@ def test_two_calls_at_once():
             assert torch.equal(x[0], w[0]) and torch.equal(x[1], w[1])
 
 
-@pytest.mark.parametrize("lens,Hq,Hkv", [([(300, 900), (1, 77), (130, 130)], 4, 2), ([(600, 3000)], 8, 1), ([(24, 400)], 8, 8)])
+@pytest.mark.parametrize("lens,Hq,Hkv", [([(300, 900), (1, 77), (130, 130)], 4, 2), ([(600, 3000)], 8, 1), ([(40, 400)], 8, 8)])
 @pytest.mark.parametrize("D,B", [(128, 16), (64, 12)])
 def test_given_up_waits_then_right_results(lens, Hq, Hkv, D, B):
     """The tile kernel's waits give up where nothing comes, without a fault; the
