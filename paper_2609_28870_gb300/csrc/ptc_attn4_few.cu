@@ -102,6 +102,10 @@ __device__ __forceinline__ uint32_t transposed(uint32_t x) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// The warp's number, as one value for the warp: what follows from it is left to the
+// uniform unit.
+__device__ __forceinline__ uint32_t warp_index() { return __shfl_sync(kFull, threadIdx.x >> 5, 0); }
+
 // NS: rows of 64 or 128 channels.  NT: 8, 16 or 32 query rows.
 template <int NS, int NT>
 struct Shape {
@@ -291,7 +295,7 @@ struct Feed {
   }
   // The warp's first chunk of the part at hand or of a later one.
   __device__ __forceinline__ void find(const Few4Args& a, const Shared& sh) {
-    const uint32_t warp = threadIdx.x >> 5;
+    const uint32_t warp = warp_index();
     while (more && chunk >= (w.kv1 - w.kv0) * (kUnit / kChunk)) {
       more = w.next(a, sh);
       chunk = warp;
@@ -303,7 +307,7 @@ struct Feed {
     w = start;
     head(a);
     more = some;
-    chunk = threadIdx.x >> 5;
+    chunk = warp_index();
     issued = 0;
     find(a, sh);
   }
@@ -563,7 +567,7 @@ __device__ __forceinline__ void take_units(const Few4Args& a, Shared& sh, Way& w
                                            uint32_t ctas) {
   using S = Shape<NS, NT>;
   using M = Mma16<T>;
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3, team = warp / kTeam;
+  const uint32_t tid = threadIdx.x, warp = warp_index(), lane = tid & 31, g = lane >> 2, t = lane & 3, team = warp / kTeam;
   const uint32_t D = a.kv.D, G = a.G;
   const float sl2 = a.scale * kLog2e;
   const uint32_t ring = smem_u32(smem) + warp * S::kRing * S::kStage;
