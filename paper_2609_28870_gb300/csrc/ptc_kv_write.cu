@@ -226,18 +226,17 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
   float inv;  // (within a unit or two: what is left of a value after a code tells)
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sf));
   const float half = 0.5f * sf;
-  // Whether what is taken from b is exact in 32 bits for all eight: then a value on
-  // a code's border is seen to be there (and goes up).
-  const float most = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), fabsf(bf));
-  bool fine = sf >= 0x1p-100f && (bf == 0.f || fabsf(bf) >= Half16<T>::kExact * most);
-  const float least = Half16<T>::kExact * most;
+  // Whether what a value's subtraction of b loses in 32 bits may matter: on a code's
+  // border (a value there goes up), where value and b are far apart in size.
+  const float most = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), fabsf(bf)), least = Half16<T>::kExact * most;
+  bool fine = sf >= 0x1p-100f && (bf == 0.f || fabsf(bf) >= least);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 v = Half16<T>::get2(w[i]), y = add2(v, both(-bf));
-    fine &= fminf(fabsf(v.x), fabsf(v.y)) >= least;
     // y / s to the nearest whole number, in the sum's last bits; y less that many s,
     // exact, tells whether it is the nearest or, by the reciprocal's rounding, beside it
     const float2 z = fma2(y, both(inv), both(12582912.f)), k = add2(z, both(-12582912.f)), r = fma2(k, both(-sf), y);
+    fine &= !((fabsf(v.x) < least & fabsf(r.x) == half) | (fabsf(v.y) < least & fabsf(r.y) == half));
     const int k0 = __float_as_int(z.x) - 0x4B400010 + (r.x >= half ? 1 : 0) - (r.x < -half ? 1 : 0);
     const int k1 = __float_as_int(z.y) - 0x4B400010 + (r.y >= half ? 1 : 0) - (r.y < -half ? 1 : 0);
     code |= __vimin_s16x2_relu(__byte_perm(k0, k1, 0x5410), 0x000F000F) << (4 * i);
