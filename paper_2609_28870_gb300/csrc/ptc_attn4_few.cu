@@ -26,13 +26,13 @@
 //
 // Bounds.  At 128 channels and up to 8 rows 16 keys are 360 instructions of a warp,
 // of which the codes take 230 (shift, mask and multiply-add for two values, the
-// products, their loads): 12 single tokens over 32K to 131K, 0.57 GB, take 115 us, 4.9
+// products, their loads): 12 single tokens over 32K to 131K, 0.57 GB, take 113 us, 5.0
 // TB/s, with 63% of the issue slots and 60% of the ALUs' in use at 1.8 GHz; what is
 // left waits for fixed latencies, which four warps a scheduler, 128 registers each, do
 // not hide.  (165 us with a warp of its own for the copies and 16 keys at a time; 132
 // with a mask and an or in one instruction; 125 with the warps' own copies; 119 with
 // places in the cache kept a tile; 115 with both blocks' products side by side.)  Two
-// and four instructions an operand: 149 and 219 us, at 8 warps an SM.  64 single tokens
+// and four instructions an operand: 152 and 219 us, at 8 warps an SM.  64 single tokens
 // over 1.1K to 12K 81 us, one over 1,012 9 us, a chain of latencies: a launch that
 // clears the counts, lengths, pages, keys, parts.
 #include "ptc_attn4.cuh"

@@ -250,7 +250,7 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // A group of LANES threads stays with its token and takes `slice` of its rows, so that
 // the token's place and angles are found once for them; a row or two are loaded while
 // as many are worked on.  Each row is read and written once, 0.86 GB for 34,692 tokens
-// of 32 query and 8 key heads of 128: 152 us, 5.6 TB/s; one of 4 bits 213 us, 3.6 TB/s,
+// of 32 query and 8 key heads of 128: 152 us, 5.6 TB/s; one of 4 bits 211 us, 3.7 TB/s,
 // bound by its 420 instructions for 512 values (the group's ends, scale and base, and
 // 13 a value), at 79% of the issue slots.  64 tokens 4.4 us, a launch and four
 // dependent reads.
