@@ -6,6 +6,12 @@ namespace ptc {
 namespace {
 
 constexpr int kWrThreads = 256;
+// CTAs an SM.  The products of bf16 values fit 64 registers; those of fp16, which take
+// more to round, spill there, and a row's loads wait for the spills: 4 against 3 CTAs,
+// 34,692 tokens of 32 query and 8 key heads of 128: bf16 152 and 163 us (4 bits, with
+// the read, 237 and 249), fp16 228 and 169 us (299 and 263).
+template <typename T>
+constexpr int kWrCtas = Half16<T>::kBf16 ? 4 : 3;
 constexpr int kRdRows = 4;  // rows of a token that a thread has in flight, of those that are read back
 constexpr uint32_t kWrSlice = 24;
 
@@ -255,7 +261,7 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // 13 a value), at 79% of the issue slots.  64 tokens 4.4 us, a launch and four
 // dependent reads.
 template <typename T, int LANES, bool FOUR>
-__global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWrThreads, kWrCtas<T>) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
   constexpr uint32_t kTok = kWrThreads / LANES;
   constexpr int kWrRows = FOUR ? 1 : 2;  // rows of a token that a thread works on while it loads as many
