@@ -174,6 +174,11 @@ template <typename T>
 __device__ __noinline__ T base_wide(float lo, float s) {
   return Half16<T>::put((double)lo - 16.0 * (double)s);
 }
+// Whether 32-bit numbers divided by s stay clear of the ends of their range: 31 s,
+// the most that a value is above its base, is not infinite, nor 1 / s cut off.
+__device__ __forceinline__ bool plain_scale(float s) {
+  return __float_as_uint(s) - __float_as_uint(0x1p-100f) <= __float_as_uint(0x1p100f) - __float_as_uint(0x1p-100f);
+}
 // Eight codes, where 32 bits do not hold what is taken from b.
 template <typename T>
 __device__ __noinline__ uint32_t codes_wide(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, float b, float s) {
@@ -188,7 +193,7 @@ __device__ __noinline__ uint32_t codes_wide(uint32_t w0, uint32_t w1, uint32_t w
     float k = fminf(fmaxf(rintf(fmaf(y, inv, -16.f)), 0.f), 15.f);
     const float r = fmaf(-(k + 16.f), s, y);
     k += (r > half || (r == half && lost >= 0.f) ? 1.f : 0.f) - (r < -half || (r == -half && lost < 0.f) ? 1.f : 0.f);
-    if (s < 0x1p-100f) k = (float)floor(((double)v - (double)b) / (double)s - 15.5);
+    if (!plain_scale(s)) k = (float)floor(((double)v - (double)b) / (double)s - 15.5);
     code |= (uint32_t)fminf(fmaxf(k, 0.f), 15.f) << (4 * (e / 2) + 16 * (e & 1));
   }
   return code;
@@ -235,7 +240,7 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
   // Whether what a value's subtraction of b loses in 32 bits may matter: on a code's
   // border (a value there goes up), where value and b are far apart in size.
   const float most = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), fabsf(bf)), least = Half16<T>::kExact * most;
-  bool fine = sf >= 0x1p-100f && (bf == 0.f || fabsf(bf) >= least);
+  bool fine = plain_scale(sf) && (bf == 0.f || fabsf(bf) >= least);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 v = Half16<T>::get2(w[i]), y = add2(v, both(-bf));

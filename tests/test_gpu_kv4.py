@@ -136,6 +136,32 @@ def test_groups_that_are_not_finite_read_as_nan(dtype):
     assert torch.equal(gone.all(-1), want) and torch.equal(gone.any(-1), want) and torch.equal(k.isnan(), v.isnan())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_groups_next_to_the_largest_number(dtype):
+    """Scale and base are finite, while a value less the base may pass 32 bits."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4, rows_of
+    c = Cache4([(64, 64)], Hq=1, Hkv=1, D=128, dtype=dtype)
+    top = torch.finfo(c.dt).max
+    ends = [(a, b) for a in (0.0, 0.01, 0.25, 0.5) for b in (0.52, 0.53, 0.8, 0.92) if b - 16 * (b - a) / 15 > -0.9]
+    gen = torch.Generator().manual_seed(4)
+    x = torch.rand(64, 4, 32, generator=gen, dtype=torch.float64)
+    for t in range(64):
+        for i in range(4):
+            lo, hi = ends[(4 * t + i) % len(ends)]
+            x[t, i, 0], x[t, i, 1] = 0, 1
+            x[t, i] = (lo + (hi - lo) * x[t, i]) * top
+    x = x.to(c.dt).view(64, 1, 128).cuda()
+    ptc.ptc_kv4_append(x, x, *c.table(), c.tok_off, c.kv_len)
+    want = rows_of(x)
+    for kept in c.table()[:2]:
+        got = kept[c.lists[0][:4].long()].transpose(1, 2).reshape(64, 1, 80)
+        assert torch.equal(got.cpu(), want.cpu())
+    k, _ = ptc.ptc_kv4_read(*c.table(), c.tok_off, c.kv_len, 64, 128, c.dt)
+    assert torch.isfinite(k).all()
+
+
 def test_append_and_read_refusals():
     import torch
     import paper_2609_28870_gb300 as ptc
