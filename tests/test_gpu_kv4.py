@@ -162,6 +162,37 @@ def test_groups_next_to_the_largest_number(dtype):
     assert torch.isfinite(k).all()
 
 
+@pytest.mark.parametrize("D", [64, 120])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_reading_rows_of_any_bytes(dtype, D):
+    """Scales and bases of every size and sign, subnormal and infinite ones, NaN."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4, once
+    c = Cache4([(300, 300)], Hq=2, Hkv=2, D=D, dtype=dtype)
+    c.k.copy_(torch.randint(0, 256, c.k.shape, generator=torch.Generator().manual_seed(9), dtype=torch.uint8))
+    k, _ = ptc.ptc_kv4_read(*c.table(), c.tok_off, c.kv_len, 300, D, c.dt)
+    page, slot = c.where(0, 300)
+    row = c.k[page, :, slot].cpu()
+    word = row[..., :D // 2].contiguous().view(torch.int32).long()
+    e = torch.arange(8)
+    code = (word[..., None] >> (4 * (e // 2) + 16 * (e % 2)) & 15).flatten(-2)
+    Dp = 64 if D <= 64 else 128
+    p = row[..., Dp // 2:Dp // 2 + Dp // 8].contiguous().view(c.dt).double()[..., torch.arange(D)[:, None] // 32 * 2 + torch.arange(2)]
+    x, y = (16 + code) * p[..., 0], p[..., 1]  # x is exact
+    z = x + y
+    u = z - x
+    lost = (x - (z - u)) + (y - u)
+    # a bit that 64 bits lose makes the last one odd, so that the rounding to 16 still sees it
+    odd = (z.view(torch.int64) & 1) == 1
+    z = torch.where((lost != 0) & ~odd, torch.nextafter(z, torch.copysign(torch.full_like(z, math.inf), lost)), z)
+    fine = torch.isfinite(p).all(-1)
+    want = torch.where(fine, once(torch.where(fine, z, 0.0), c.dt).double(), x + y)
+    got = k.cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and int(fine.sum()) > 0.8 * fine.numel()
+    assert torch.equal(got.nan_to_num(1.0, math.inf, -math.inf), want.nan_to_num(1.0, math.inf, -math.inf))
+
+
 def test_append_and_read_refusals():
     import torch
     import paper_2609_28870_gb300 as ptc
