@@ -233,26 +233,29 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
   }
   words = bits16(s) | bits16(base) << 16;
   if (sf == 0.f || !real) return 0;
+  // y / s, of y = v - b, to the nearest whole number in a sum's last bits, with a
+  // reciprocal a few units too large: so what lies on a code's border goes up, as it
+  // should.  y less that many s, exact, tells of a value that lies so close below a border
+  // that it went up too (more than half an s away), and of one on it: there what y's
+  // subtraction lost in 32 bits matters, where value and base are far apart in size.
   uint32_t code = 0;
-  float inv;  // (within a unit or two: what is left of a value after a code tells)
+  float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(sf));
+  inv = fmaf(inv, 0x1p-21f, inv);
+  constexpr float kSum = 12582912.f - 16.f;  // 1.5 * 2^23: whole numbers; the base absorbs 16
   const float half = 0.5f * sf;
-  // Whether what a value's subtraction of b loses in 32 bits may matter: on a code's
-  // border (a value there goes up), where value and b are far apart in size.
   const float most = fmaxf(fmaxf(fabsf(lo), fabsf(hi)), fabsf(bf)), least = Half16<T>::kExact * most;
-  bool fine = plain_scale(sf) && (bf == 0.f || fabsf(bf) >= least);
+  const bool fine = plain_scale(sf) && (bf == 0.f || fabsf(bf) >= least);
+  float away = 0.f, small_v = INFINITY;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 v = Half16<T>::get2(w[i]), y = add2(v, both(-bf));
-    // y / s to the nearest whole number, in the sum's last bits; y less that many s,
-    // exact, tells whether it is the nearest or, by the reciprocal's rounding, beside it
-    const float2 z = fma2(y, both(inv), both(12582912.f)), k = add2(z, both(-12582912.f)), r = fma2(k, both(-sf), y);
-    fine &= !((fabsf(v.x) < least & fabsf(r.x) == half) | (fabsf(v.y) < least & fabsf(r.y) == half));
-    const int k0 = __float_as_int(z.x) - 0x4B400010 + (r.x >= half ? 1 : 0) - (r.x < -half ? 1 : 0);
-    const int k1 = __float_as_int(z.y) - 0x4B400010 + (r.y >= half ? 1 : 0) - (r.y < -half ? 1 : 0);
-    code |= __vimin_s16x2_relu(__byte_perm(k0, k1, 0x5410), 0x000F000F) << (4 * i);
+    const float2 z = fma2(y, both(inv), both(kSum)), k = add2(z, both(-kSum)), r = fma2(k, both(-sf), y);
+    away = fmaxf(away, fmaxf(fabsf(r.x), fabsf(r.y)));
+    small_v = fminf(small_v, fminf(fabsf(v.x), fabsf(v.y)));
+    code |= __vimin_s16x2_relu(__byte_perm(__float_as_uint(z.x), __float_as_uint(z.y), 0x5410), 0x000F000F) << (4 * i);
   }
-  if (!fine) code = codes_wide<T>(w[0], w[1], w[2], w[3], bf, sf);
+  if (!fine || away > half || (away == half && small_v < least)) code = codes_wide<T>(w[0], w[1], w[2], w[3], bf, sf);
   return code;
 }
 
