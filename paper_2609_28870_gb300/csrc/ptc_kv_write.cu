@@ -1,19 +1,15 @@
 // New tokens on their way into the pages, turned and quantised
 // (ptc_kv_append_rope, ptc_kv4_append), and back (ptc_kv4_read).
+#include <type_traits>
+
 #include "ptc_kv4.cuh"
 
 namespace ptc {
 namespace {
 
 constexpr int kWrThreads = 256;
-// CTAs an SM.  The products of bf16 values fit 64 registers; those of fp16, which take
-// more to round, spill there, and a row's loads wait for the spills: 4 against 3 CTAs,
-// 34,692 tokens of 32 query and 8 key heads of 128: bf16 152 and 163 us (4 bits, with
-// the read, 237 and 249), fp16 228 and 169 us (299 and 263).
-template <typename T>
-constexpr int kWrCtas = Half16<T>::kBf16 ? 4 : 3;
 constexpr int kRdRows = 4;  // rows of a token that a thread has in flight, of those that are read back
-constexpr uint32_t kWrSlice = 24;
+constexpr uint32_t kWrSlice = 32;
 
 struct WriteArgs {
   KvView kv;
@@ -262,17 +258,17 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // The rows of tokens: queries, keys and values, LANES threads a row with eight
 // channels each (so that a row stays within a warp: it may be turned in place).
 // A group of LANES threads stays with its token and takes `slice` of its rows, so that
-// the token's place and angles are found once for them; a row or two are loaded while
-// as many are worked on.  Each row is read and written once, 0.86 GB for 34,692 tokens
-// of 32 query and 8 key heads of 128: 152 us, 5.6 TB/s; one of 4 bits 211 us, 3.7 TB/s,
-// bound by its 420 instructions for 512 values (the group's ends, scale and base, and
-// 13 a value), at 79% of the issue slots.  64 tokens 4.4 us, a launch and four
-// dependent reads.
+// the token's place and angles are found once for them; queries, keys and values in a
+// loop each, with what it needs in registers and no more (a loop over rows of all
+// kinds: 152 and 223 us, in fp16 169 and 253).  Each row is read and written once,
+// 0.86 GB for 34,692 tokens of 32 query and 8 key heads of 128: 140 us, 6.1 TB/s (fp16
+// 160 us); into pages of 4 bits 176 us (200 us), bound by a quantised row's 250
+// instructions for two times 256 values, 130 of them its group's ends, scale and base.
+// 64 tokens 4.3 us, a launch and four dependent reads.
 template <typename T, int LANES, bool FOUR>
-__global__ void __launch_bounds__(kWrThreads, kWrCtas<T>) k_kv_write(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
   constexpr uint32_t kTok = kWrThreads / LANES;
-  constexpr int kWrRows = FOUR ? 1 : 2;  // rows of a token that a thread works on while it loads as many
   __shared__ Place s_at[kTok];
   const uint64_t t0 = (uint64_t)blockIdx.x * kTok;
   find_places(a, t0, s_at);
@@ -285,80 +281,66 @@ __global__ void __launch_bounds__(kWrThreads, kWrCtas<T>) k_kv_write(const __gri
   angles.any = false;
   if (turned && live && real) load_turn(a.rope, at.pos, c, angles);
   const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
-  // Where row r comes from and where it goes: queries, keys and values each lie a
-  // stride apart, so a place is found once for all rows of a kind.
-  auto source = [&](uint32_t r, int64_t& step, uint32_t& last) {
-    if (r < Hq) {
-      step = 2 * a.q_head;
-      last = Hq;
-      return a.q + 2 * t * a.q_tok + r * step;
-    }
-    const bool key = r < Hq + H;
-    step = 2 * (key ? a.kn_head : a.vn_head);
-    last = key ? Hq + H : a.rows;
-    return (key ? a.kn + 2 * t * a.kn_tok : a.vn + 2 * t * a.vn_tok) + (r - Hq - (key ? 0 : H)) * step;
-  };
-  auto target = [&](uint32_t r, int64_t& step) {
-    if (r < Hq) {
-      step = 2 * a.o_head;
-      return a.q_out + 2 * t * a.o_tok + r * step;
-    }
-    const bool key = r < Hq + H;
-    constexpr int kUnit = FOUR ? 1 : 2;  // bytes of a stride's unit
-    step = kUnit * (key ? a.kv.ks_head : a.kv.vs_head);
-    return (key ? a.kv.k + kUnit * at.k : a.kv.v + kUnit * at.v) + (r - Hq - (key ? 0 : H)) * step;
-  };
-  uint32_t ahead = first, ahead_last, last;
-  int64_t ahead_step, from_step, step;
-  const char* ahead_at = source(first, ahead_step, ahead_last);
-  const char* from = source(first, from_step, last);
-  char* to = target(first, step);
-  auto load = [&] {
-    uint4 x = make_uint4(0, 0, 0, 0);
-    if (ahead < end) {
-      if (live && real) x = *reinterpret_cast<const uint4*>(ahead_at + 16 * c);
-      ahead_at += ahead_step;
-      if (++ahead == ahead_last && ahead < end) ahead_at = source(ahead, ahead_step, ahead_last);
-    }
-    return x;
-  };
-  uint4 x[kWrRows], next[kWrRows];
+  // n rows, a stride apart where they come from and where they go to; ROWS of them are
+  // worked on while as many are loaded.
+  auto take = [&](auto rows_at_once, auto quantised, bool turn, const char* from, int64_t from_step, char* to, int64_t step,
+                  uint32_t n) {
+    constexpr uint32_t ROWS = decltype(rows_at_once)::value;
+    constexpr bool QUANT = decltype(quantised)::value;
+    uint4 x[ROWS], next[ROWS];
+    auto load = [&](uint32_t r, uint32_t ahead) {
+      return r < n && live && real ? *reinterpret_cast<const uint4*>(from + ahead * from_step + 16 * c) : make_uint4(0, 0, 0, 0);
+    };
 #pragma unroll
-  for (int u = 0; u < kWrRows; ++u) next[u] = load();
+    for (uint32_t u = 0; u < ROWS; ++u) next[u] = load(u, u);
 #pragma unroll 1
-  for (uint32_t r0 = first; r0 < end; r0 += kWrRows) {
+    for (uint32_t r0 = 0; r0 < n; r0 += ROWS) {
 #pragma unroll
-    for (int u = 0; u < kWrRows; ++u) {
-      x[u] = next[u];
-      next[u] = load();
-    }
+      for (uint32_t u = 0; u < ROWS; ++u) {
+        x[u] = next[u];
+        next[u] = load(r0 + ROWS + u, ROWS + u);
+      }
 #pragma unroll
-    for (int u = 0; u < kWrRows; ++u) {
-      const uint32_t r = r0 + u;
-      if (r >= end) break;  // the whole CTA
-      uint4 y = x[u];
-      if (turned && r < Hq + H) y = turn_row<T, LANES>(a.rope, angles, x[u], from, c, live);
-      __syncwarp();  // a row is written after all of it was read
-      if (!FOUR || r < Hq) {
-        if (live && real) *reinterpret_cast<uint4*>(to + 16 * c) = y;
-      } else {
-        uint32_t words;
-        const uint32_t code = quantise<T>(y, live && real, words);
-        if (live) {
-          uint32_t* row = reinterpret_cast<uint32_t*>(to);
-          row[c] = code;
-          if (c % 4 == 0) row[LANES + c / 4] = words;
-          if (LANES == 8 && c % 4 == 1) row[10 + c / 4] = 0;
+      for (uint32_t u = 0; u < ROWS; ++u) {
+        if (r0 + u >= n) break;  // the whole CTA
+        uint4 y = x[u];
+        if (turn) y = turn_row<T, LANES>(a.rope, angles, x[u], from, c, live);
+        __syncwarp();  // a row is written after all of it was read
+        if (!QUANT) {
+          if (live && real) *reinterpret_cast<uint4*>(to + 16 * c) = y;
+        } else {
+          uint32_t words;
+          const uint32_t code = quantise<T>(y, live && real, words);
+          if (live) {
+            uint32_t* row = reinterpret_cast<uint32_t*>(to);
+            row[c] = code;
+            if (c % 4 == 0) row[LANES + c / 4] = words;
+            if (LANES == 8 && c % 4 == 1) row[10 + c / 4] = 0;
+          }
         }
-      }
-      from += from_step;
-      to += step;
-      if (r + 1 == last && r + 1 < end) {
-        from = source(r + 1, from_step, last);
-        to = target(r + 1, step);
+        from += from_step;
+        to += step;
       }
     }
-  }
+  };
+  // The CTA's rows of a kind, of which `before` rows are of others.
+  constexpr int64_t kUnit = FOUR ? 1 : 2;  // bytes of a stride's unit in the pages
+  using Now = std::integral_constant<uint32_t, FOUR ? 1 : 2>;
+  auto part = [&](uint32_t before, uint32_t rows, uint32_t& r) {
+    const uint32_t lo = first > before ? first - before : 0, hi = end > before ? end - before : 0;
+    r = lo < rows ? lo : rows;
+    return (hi < rows ? hi : rows) - r;
+  };
+  uint32_t r, n;
+  if ((n = part(0, Hq, r)) > 0)
+    take(std::integral_constant<uint32_t, 2>{}, std::false_type{}, turned, a.q + 2 * (t * a.q_tok + r * a.q_head), 2 * a.q_head,
+         a.q_out + 2 * (t * a.o_tok + r * a.o_head), 2 * a.o_head, n);
+  if ((n = part(Hq, H, r)) > 0)
+    take(Now{}, std::integral_constant<bool, FOUR>{}, turned, a.kn + 2 * (t * a.kn_tok + r * a.kn_head), 2 * a.kn_head,
+         a.kv.k + kUnit * (at.k + r * a.kv.ks_head), kUnit * a.kv.ks_head, n);
+  if ((n = part(Hq + H, H, r)) > 0)
+    take(std::integral_constant<uint32_t, FOUR ? 1 : 4>{}, std::integral_constant<bool, FOUR>{}, false, a.vn + 2 * (t * a.vn_tok + r * a.vn_head), 2 * a.vn_head,
+         a.kv.v + kUnit * (at.v + r * a.kv.vs_head), kUnit * a.kv.vs_head, n);
 }
 
 // Tokens back out of their pages: 0.46 GB in 73 us, 6.3 TB/s, at HBM's rate.
@@ -398,7 +380,7 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
 }
 
 // Rows of a CTA: as few as leave four CTAs for every SM, so that a call of few
-// tokens is spread, and at most kWrSlice (8: 210 us for what 24 take 189).
+// tokens is spread, and at most kWrSlice (12; 16; 24; 32; 48 for 48 rows: 153, 146, 145, 140, 140 us).
 dim3 write_grid(WriteArgs& a, uint32_t tok) {
   const uint64_t blocks = (a.n_tok + tok - 1) / tok;
   uint64_t slice = blocks * a.rows / (4 * (uint64_t)num_sms());
