@@ -262,9 +262,10 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // loop each, with what it needs in registers and no more (a loop over rows of all
 // kinds: 152 and 223 us, in fp16 169 and 253).  Each row is read and written once,
 // 0.86 GB for 34,692 tokens of 32 query and 8 key heads of 128: 140 us, 6.1 TB/s (fp16
-// 160 us); into pages of 4 bits 176 us (200 us), bound by a quantised row's 250
-// instructions for two times 256 values, 130 of them its group's ends, scale and base.
-// 64 tokens 4.3 us, a launch and four dependent reads.
+// 160 us); into pages of 4 bits 176 us (200 us), bound by its instructions, 187 for two
+// rows on average, at 73% of the issue slots.  (Several batches of tokens a CTA, to
+// wait for places less often: 157 and 216 us for 140 and 203.)  64 tokens 4.3 us, a
+// launch and four dependent reads.
 template <typename T, int LANES, bool FOUR>
 __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
