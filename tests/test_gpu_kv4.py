@@ -484,6 +484,65 @@ def test_a_captured_decode_loop(dtype):
     assert c.kv_len.tolist() == [n + steps for n in prompts]
 
 
+@pytest.mark.parametrize("new", [96, 512])
+def test_captured_chunks_share_a_workspace(new):
+    """Graphs of a chunk (over codes; over the copy in 16 bits) and of single tokens, with one
+    workspace, replayed in turn while lengths, offsets and pages change under them; offsets that are
+    not sound are refused by the replay and leave the outputs; the next one works again."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4
+    big = Cache4([(new, 1500), (new, new)], Hq=8, Hkv=2, D=128, seed=1)
+    small = Cache4([(1, 700), (1, 33), (0, 5)], Hq=8, Hkv=2, D=128, seed=2)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    outs = [(torch.empty_like(c.q), torch.empty(c.q.shape[:2], device="cuda")) for c in (big, small)]
+    need = ptc.lib().ptc_kv4_attention_workspace_bytes(2, 8, 2, 128, new, 2 * new, big.page_ids.shape[0], 16)
+    plain = ptc.lib().ptc_kv4_attention_workspace_bytes(2, 8, 2, 128, new, 2 * new, big.page_ids.shape[0], 12)
+    assert (need > plain) == (new == 512)
+
+    def call(c, o, **kw):
+        return ptc.ptc_kv4_attention(c.q, *c.table(), c.tok_off, c.kv_len, new if c is big else 1, out=o[0], lse=o[1], **kw)
+
+    stream, graphs = torch.cuda.Stream(), []
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for c, o in zip((big, small), outs):
+            call(c, o, ws=ws, status=status)
+            graphs.append(torch.cuda.CUDAGraph())
+            with torch.cuda.graph(graphs[-1], stream=stream):
+                call(c, o, ws=ws, status=status)
+        turns = [([new, new], [1500, new]), ([new - 31, new], [1469, new]), ([new, 0], [1111, 9]), ([new, new], [new, 1500])]
+        for m, n in turns:
+            lens = big.kv_len
+            off = torch.tensor([0, m[0], m[0] + m[1]], dtype=torch.int64)
+            if m[0] + m[1] != 2 * new:  # rows behind the last sequence: not sound
+                big.tok_off.copy_(off)
+                for o in outs[0]:
+                    o.fill_(7.0)
+                graphs[0].replay()
+                stream.synchronize()
+                assert int(status) != 0 and all(bool((o == 7.0).all()) for o in outs[0])
+                status.zero_()
+                off = torch.tensor([0, new, 2 * new], dtype=torch.int64)
+                m, n = [new, new], [1500, new]
+            big.tok_off.copy_(off)
+            if n[1] > new:  # the lists swapped: the first has few tokens, the second many
+                c0, c1 = (x.clone() for x in big.lists)
+                both = torch.cat([c1, c0])
+                big.page_ids.copy_(both)
+                big.page_off.copy_(torch.tensor([0, len(c1), len(c1) + len(c0)]))
+            lens.copy_(torch.tensor(n, dtype=torch.int32))
+            for g in (0, 1, 0):
+                graphs[g].replay()
+            got = [[x.clone() for x in o] for o in outs]
+            want = [call(c, (torch.empty_like(c.q), torch.empty(c.q.shape[:2], device="cuda"))) for c in (big, small)]
+            stream.synchronize()
+            for x, y in zip(got, want):
+                assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1]) and bool(torch.isfinite(x[0]).all())
+            ptc.check_status(status)
+
+
 def test_example_over_pages_of_4_bits():
     import os
     import subprocess
