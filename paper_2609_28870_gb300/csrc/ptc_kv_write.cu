@@ -9,7 +9,7 @@ namespace {
 
 constexpr int kWrThreads = 256;
 constexpr int kRdRows = 4;  // rows of a token that a thread has in flight, of those that are read back
-constexpr uint32_t kWrSlice = 32;
+constexpr uint32_t kWrSlice = 48;
 
 struct WriteArgs {
   KvView kv;
@@ -68,6 +68,12 @@ __device__ __forceinline__ void find_places(const WriteArgs& a, uint64_t t0, Pla
   __syncthreads();
 }
 
+// How a call turns its rows: not at all; neighbours, or channels of the two halves,
+// in whole threads (the pairs a multiple of 4, of 8); any other number of pairs.  A
+// kernel each: one for all of them, whose registers the rarest width decides, took 140
+// us for 138 below, in fp16 160 for 140, into 4 bits 203 for 194 (fp16 226 for 203).
+enum Width { kStill, kNext, kHalves, kAnyWidth };
+
 // How a thread's eight channels are turned: by the same angles for all heads of
 // a token, so they are kept.  sn has its sign: channel e becomes
 // x[e] cs[e] + partner sn[e].
@@ -77,13 +83,14 @@ struct Turn {
   bool any, all;
 };
 
+template <Width WIDTH>
 __device__ __forceinline__ void load_turn(const RopeView& rope, uint32_t pos, uint32_t c, Turn& o) {
   const uint32_t F = rope.n_freq, d0 = 8 * c;
   const float* row = rope.table + (uint64_t)pos * 2 * F;
   o.any = d0 < 2 * F;
-  o.all = rope.interleaved ? F % 4 == 0 : F % 8 == 0;
+  o.all = F % 4 == 0;  // 2 F is a multiple of 8
   if (!o.any) return;
-  if (rope.interleaved && F % 4 == 0) {  // 2 F is a multiple of 8: all eight are turned
+  if (WIDTH == kNext || (WIDTH == kAnyWidth && rope.interleaved && F % 4 == 0)) {
     const float4 x = __ldg(reinterpret_cast<const float4*>(row + 4 * c)), y = __ldg(reinterpret_cast<const float4*>(row + F + 4 * c));
     const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -91,12 +98,12 @@ __device__ __forceinline__ void load_turn(const RopeView& rope, uint32_t pos, ui
       o.cs[k] = make_float2(xs[k], xs[k]);
       o.sn[k] = make_float2(-ys[k], ys[k]);
     }
-  } else if (!rope.interleaved && F % 8 == 0) {
-    const uint32_t i = d0 < F ? d0 : d0 - F;
-    const float sign = d0 < F ? -1.f : 1.f;
+  } else if (WIDTH == kHalves || F % 4 == 0) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float4 x = __ldg(reinterpret_cast<const float4*>(row + i) + k), y = __ldg(reinterpret_cast<const float4*>(row + F + i) + k);
+    for (uint32_t k = 0; k < 2; ++k) {
+      const uint32_t d = d0 + 4 * k, i = d < F ? d : d - F;
+      const float sign = d < F ? -1.f : 1.f;
+      const float4 x = __ldg(reinterpret_cast<const float4*>(row + i)), y = __ldg(reinterpret_cast<const float4*>(row + F + i));
       o.cs[2 * k] = make_float2(x.x, x.y);
       o.cs[2 * k + 1] = make_float2(x.z, x.w);
       o.sn[2 * k] = make_float2(sign * y.x, sign * y.y);
@@ -124,35 +131,52 @@ __device__ __forceinline__ void load_turn(const RopeView& rope, uint32_t pos, ui
   }
 }
 
+// The partners of channels d0 on, one by one; those of channels that are not turned
+// are themselves.
+__device__ __forceinline__ uint4 partners_apart(const char* row, uint32_t d0, uint32_t F, uint4 x) {
+  uint32_t p[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t d = d0 + e;
+    if (d < 2 * F) {
+      const uint32_t y = *reinterpret_cast<const uint16_t*>(row + 2 * (d < F ? d + F : d - F));
+      p[e / 2] = e & 1 ? (p[e / 2] & 0xFFFFu) | y << 16 : (p[e / 2] & 0xFFFF0000u) | y;
+    }
+  }
+  return make_uint4(p[0], p[1], p[2], p[3]);
+}
+
 // A row's channels turned; x: the thread's eight, row: all of them in global
 // memory.  By all lanes of the row (c: the lane's place among them).
-template <typename T, int LANES>
+template <typename T, int LANES, Width WIDTH>
 __device__ __forceinline__ uint4 turn_row(const RopeView& rope, const Turn& t, const uint4& x, const char* row, uint32_t c,
                                           bool live) {
   const uint32_t F = rope.n_freq;
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t p[4] = {x.x, x.y, x.z, x.w};
-  if (rope.interleaved) {
+  if (WIDTH == kNext || (WIDTH == kAnyWidth && rope.interleaved)) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) p[k] = __byte_perm(w[k], w[k], 0x1032);
-  } else if (F % 8 == 0) {
+  } else if (WIDTH == kHalves || F % 8 == 0) {
     const uint32_t f = F / 8, other = c < f ? c + f : c < 2 * f ? c - f : c;
 #pragma unroll
     for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(kFull, w[k], other, LANES);
-  } else if (live && t.any) {
+  } else if (F % 4 == 0) {  // half a thread's channels on: its lower four have another's upper ones for partners
+    auto other = [&](uint32_t d) { return (d < F ? d + F : d < 2 * F ? d - F : d) / 8; };
+    const uint32_t l0 = other(8 * c), l1 = other(8 * c + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t d = 8 * c + e;
-      if (d < 2 * F) {
-        const uint32_t y = *reinterpret_cast<const uint16_t*>(row + 2 * (d < F ? d + F : d - F));
-        p[e / 2] = e & 1 ? (p[e / 2] & 0xFFFFu) | y << 16 : (p[e / 2] & 0xFFFF0000u) | y;
-      }
-    }
+    for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(kFull, w[k ^ 2], k < 2 ? l0 : l1, LANES);
+  } else if (live && t.any) {
+    const uint4 y = partners_apart(row, 8 * c, F, x);
+    p[0] = y.x;
+    p[1] = y.y;
+    p[2] = y.z;
+    p[3] = y.w;
   }
   if (!t.any) return x;
   uint32_t o[4] = {w[0], w[1], w[2], w[3]};
   turn8<T>(o, p, t.cs, t.sn);
-  if (!t.all) {
+  if (WIDTH == kAnyWidth && !t.all) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) o[k] = (o[k] & t.mask[k]) | (w[k] & ~t.mask[k]);
   }
@@ -260,13 +284,13 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // A group of LANES threads stays with its token and takes `slice` of its rows, so that
 // the token's place and angles are found once for them; queries, keys and values in a
 // loop each, with what it needs in registers and no more (a loop over rows of all
-// kinds: 152 and 223 us, in fp16 169 and 253).  Each row is read and written once,
-// 0.86 GB for 34,692 tokens of 32 query and 8 key heads of 128: 140 us, 6.1 TB/s (fp16
-// 160 us); into pages of 4 bits 176 us (200 us), bound by its instructions, 187 for two
-// rows on average, at 73% of the issue slots.  (Several batches of tokens a CTA, to
-// wait for places less often: 157 and 216 us for 140 and 203.)  64 tokens 4.3 us, a
-// launch and four dependent reads.
-template <typename T, int LANES, bool FOUR>
+// kinds: 152 us for 140, into 4 bits 223 for 203).  Each row is read and written once,
+// 0.86 GB for 34,692 tokens of 32 query and 8 key heads of 128: 138 us, 6.2 TB/s; into
+// pages of 4 bits 158 us, bound by its instructions.  (Several batches of tokens a CTA,
+// to wait for places less often, were slower by 6%.)  Widths that are no multiple of 8
+// pairs 150 us, those of no multiple of 4 200 us.  64 tokens 4.3 us, a launch and four
+// dependent reads.
+template <typename T, int LANES, bool FOUR, Width WIDTH>
 __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
   constexpr uint32_t kTok = kWrThreads / LANES;
@@ -277,10 +301,10 @@ __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constan
   const int64_t t = (int64_t)t0 + threadIdx.x / LANES;
   const uint32_t c = threadIdx.x % LANES, D = a.kv.D, Hq = a.n_q_heads, H = a.kv.H;
   const bool live = at.k >= 0, real = 8 * c < D;
-  const bool turned = a.rope.table != nullptr;
+  constexpr bool turned = WIDTH != kStill;
   Turn angles;
   angles.any = false;
-  if (turned && live && real) load_turn(a.rope, at.pos, c, angles);
+  if (turned && live && real) load_turn<WIDTH>(a.rope, at.pos, c, angles);
   const uint32_t first = blockIdx.y * a.slice, end = first + a.slice < a.rows ? first + a.slice : a.rows;
   // n rows, a stride apart where they come from and where they go to; ROWS of them are
   // worked on while as many are loaded.
@@ -305,7 +329,7 @@ __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constan
       for (uint32_t u = 0; u < ROWS; ++u) {
         if (r0 + u >= n) break;  // the whole CTA
         uint4 y = x[u];
-        if (turn) y = turn_row<T, LANES>(a.rope, angles, x[u], from, c, live);
+        if (turn) y = turn_row<T, LANES, WIDTH>(a.rope, angles, x[u], from, c, live);
         __syncwarp();  // a row is written after all of it was read
         if (!QUANT) {
           if (live && real) *reinterpret_cast<uint4*>(to + 16 * c) = y;
@@ -340,8 +364,8 @@ __global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constan
     take(Now{}, std::integral_constant<bool, FOUR>{}, turned, a.kn + 2 * (t * a.kn_tok + r * a.kn_head), 2 * a.kn_head,
          a.kv.k + kUnit * (at.k + r * a.kv.ks_head), kUnit * a.kv.ks_head, n);
   if ((n = part(Hq + H, H, r)) > 0)
-    take(std::integral_constant<uint32_t, FOUR ? 1 : 4>{}, std::integral_constant<bool, FOUR>{}, false, a.vn + 2 * (t * a.vn_tok + r * a.vn_head), 2 * a.vn_head,
-         a.kv.v + kUnit * (at.v + r * a.kv.vs_head), kUnit * a.kv.vs_head, n);
+    take(std::integral_constant<uint32_t, FOUR ? 2 : 4>{}, std::integral_constant<bool, FOUR>{}, false,
+         a.vn + 2 * (t * a.vn_tok + r * a.vn_head), 2 * a.vn_head, a.kv.v + kUnit * (at.v + r * a.kv.vs_head), kUnit * a.kv.vs_head, n);
 }
 
 // Tokens back out of their pages: 0.46 GB in 73 us, 6.3 TB/s, at HBM's rate.
@@ -381,7 +405,8 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
 }
 
 // Rows of a CTA: as few as leave four CTAs for every SM, so that a call of few
-// tokens is spread, and at most kWrSlice (12; 16; 24; 32; 48 for 48 rows: 153, 146, 145, 140, 140 us).
+// tokens is spread, and at most kWrSlice (24; 32; 48 for 48 rows: 142, 138, 138 us,
+// into 4 bits and back 191, 191, 185).
 dim3 write_grid(WriteArgs& a, uint32_t tok) {
   const uint64_t blocks = (a.n_tok + tok - 1) / tok;
   uint64_t slice = blocks * a.rows / (4 * (uint64_t)num_sms());
@@ -390,11 +415,19 @@ dim3 write_grid(WriteArgs& a, uint32_t tok) {
   return dim3((uint32_t)blocks, (a.rows + a.slice - 1) / a.slice);
 }
 
+template <typename T, bool FOUR, Width WIDTH>
+void launch_width(WriteArgs& a, cudaStream_t s) {
+  const char* name = FOUR ? "k_kv4_append" : "k_kv_append_rope";
+  if (a.kv.D <= 64) PTC_KERNEL(name, s, (k_kv_write<T, 8, FOUR, WIDTH>), write_grid(a, kWrThreads / 8), kWrThreads, 0, a);
+  else PTC_KERNEL(name, s, (k_kv_write<T, 16, FOUR, WIDTH>), write_grid(a, kWrThreads / 16), kWrThreads, 0, a);
+}
 template <typename T, bool FOUR>
 void launch_write(WriteArgs& a, cudaStream_t s) {
-  const char* name = FOUR ? "k_kv4_append" : "k_kv_append_rope";
-  if (a.kv.D <= 64) PTC_KERNEL(name, s, (k_kv_write<T, 8, FOUR>), write_grid(a, kWrThreads / 8), kWrThreads, 0, a);
-  else PTC_KERNEL(name, s, (k_kv_write<T, 16, FOUR>), write_grid(a, kWrThreads / 16), kWrThreads, 0, a);
+  const uint32_t F = a.rope.n_freq;
+  if (FOUR && !a.rope.table) launch_width<T, FOUR, FOUR ? kStill : kAnyWidth>(a, s);
+  else if (a.rope.interleaved && F % 4 == 0) launch_width<T, FOUR, kNext>(a, s);
+  else if (!a.rope.interleaved && F % 8 == 0) launch_width<T, FOUR, kHalves>(a, s);
+  else launch_width<T, FOUR, kAnyWidth>(a, s);
 }
 template <typename T>
 void launch_read(WriteArgs& a, cudaStream_t s) {
