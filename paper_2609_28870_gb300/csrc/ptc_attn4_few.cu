@@ -280,9 +280,13 @@ struct Feed {
     vb = a.kv.v + w.h * a.kv.vs_head;
   }
 
-  // The chunk at hand's pages, of both blocks of 16 or of the lane's key.
+  // The chunk at hand's first key, or the lane's.
+  __device__ __forceinline__ uint32_t key() const {
+    return w.kv0 * kUnit + chunk * kChunk + (BLOCKS ? 0 : threadIdx.x & 31);
+  }
+  // Its pages, of both blocks of 16 or of the lane's key.
   __device__ __forceinline__ void ask(const Few4Args& a) {
-    const uint32_t lane = threadIdx.x & 31, key = w.kv0 * kUnit + chunk * kChunk + (BLOCKS ? 0 : lane);
+    const uint32_t key = this->key();
     const uint32_t at = a.kv.B == 1 ? key : __umulhi(key, a.div_mul) >> a.div_shift;
     const uint32_t* ids = a.kv.page_ids + w.page0;
     slot[0] = key - at * a.kv.B;
@@ -315,13 +319,14 @@ struct Feed {
   __device__ __forceinline__ void issue(const Few4Args& a, const Shared& sh, uint32_t ring) {
     if (more) {
       const uint32_t lane = threadIdx.x & 31, dst = ring + issued % S::kRing * S::kStage + 16 * lane;
+      const uint32_t key = this->key();
       ++issued;
       bool on[2];
       const char *k[2], *v[2];
 #pragma unroll
       for (int x = 0; x < (BLOCKS ? 2 : 1); ++x) {
         on[x] = id[x] < a.kv.n_pages;
-        if (!on[x] && id[x] != kNone) report(a.status, PTC_ERR_INVALID_ARG);
+        if (!on[x] && key + 16 * x < w.n) report(a.status, PTC_ERR_INVALID_ARG);  // (any id: a list may hold kNone)
         if (!on[x]) id[x] = slot[x] = 0;
         if (BLOCKS) {
           const uint32_t in = slot[x] * (S::kRow / 16);

@@ -1064,8 +1064,9 @@ __device__ __forceinline__ bool quant_role(const AttnArgs& a, TileShared& sh, ui
     if (lane == 0) rest = w;
     __syncwarp();
   };
+  auto key_of = [&] { return j * kKeys + row0 + lane; };
   auto ask = [&] {
-    const uint32_t key = j * kKeys + row0 + lane, at = a.kv.B == 1 ? key : __umulhi(key, a.div_mul) >> a.div_shift;
+    const uint32_t key = key_of(), at = a.kv.B == 1 ? key : __umulhi(key, a.div_mul) >> a.div_shift;
     slot = key - at * a.kv.B;
     id = key < n ? __ldg(ids + at) : kNone;
   };
@@ -1080,7 +1081,7 @@ __device__ __forceinline__ bool quant_role(const AttnArgs& a, TileShared& sh, ui
   auto issue = [&] {
     if (!values && more) {
       const bool on = id < a.kv.n_pages;
-      if (!on && id != kNone) report(a.status, PTC_ERR_INVALID_ARG);
+      if (!on && key_of() < n) report(a.status, PTC_ERR_INVALID_ARG);  // (any id: a list may hold kNone)
       rows = __ballot_sync(kFull, on);
       const uint32_t page = on ? id : 0, s = on ? slot : 0;
       k = kb + page * a.kv.ks_page + s * a.kv.ks_slot;
