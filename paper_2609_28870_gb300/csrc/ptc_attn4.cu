@@ -94,7 +94,7 @@ size_t copy_bytes(uint32_t n_req, uint32_t G, uint32_t n_kv_heads, uint32_t head
   if (!n_req || !n_page_ids || block_size % 8) return 0;
   if ((uint64_t)max_q_len * G < kCopyRows || n_tok * G < kCopyMean * n_req) return 0;
   const uint64_t page = 2ull * block_size * n_kv_heads * head_dim;
-  if (n_page_ids > kCopyBytes / 2 / page) return 0;
+  if (!page || n_page_ids > kCopyBytes / 2 / page) return 0;  // (sizes are asked for before the cache is checked)
   return (page * n_page_ids + 255) / 256 * 256;
 }
 
