@@ -47,13 +47,15 @@ constexpr int kCopyThreads = 256;
 
 struct CopyArgs {
   KvView kv;
+  const uint64_t* tok_off;
   uint32_t* ids;
   char* k;
   char* v;
 };
 
-// A CTA has an entry of the page lists.  One that a request needs becomes page i of
-// the copy (a page that the cache does not have: none); the others stay as they are.
+// A CTA has an entry of the page lists.  One that a request with new tokens needs
+// becomes page i of the copy (a page that the cache does not have: none); the others'
+// pages stay as they are, and nothing reads them.
 template <typename T, int LANES>
 __global__ void __launch_bounds__(kCopyThreads) k_kv4_copy(const __grid_constant__ CopyArgs a) {
   grid_dep_sync();
@@ -63,7 +65,8 @@ __global__ void __launch_bounds__(kCopyThreads) k_kv4_copy(const __grid_constant
   if (threadIdx.x == 0) {
     const uint32_t r = req_search(a.kv.page_off, 0, a.kv.n_req - 1, i);
     const uint64_t first = a.kv.page_off[r];
-    const bool needed = i >= first && i < a.kv.page_off[r + 1] && (i - first) * B < a.kv.kv_len[r];
+    const bool needed = i >= first && i < a.kv.page_off[r + 1] && (i - first) * B < a.kv.kv_len[r] &&
+                        a.tok_off[r] < a.tok_off[r + 1];
     const uint32_t id = needed ? a.kv.page_ids[i] : kNone;
     s_id = id < a.kv.n_pages ? id : kNone;
     a.ids[i] = id < a.kv.n_pages ? (uint32_t)i : kNone;
@@ -100,7 +103,7 @@ size_t copy_bytes(uint32_t n_req, uint32_t G, uint32_t n_kv_heads, uint32_t head
 
 template <typename T>
 ptc_status launch_copied(AttnArgs& a, char* ws, size_t bytes, cudaStream_t s) {
-  CopyArgs c{a.kv, reinterpret_cast<uint32_t*>(ws)};
+  CopyArgs c{a.kv, a.tok_off, reinterpret_cast<uint32_t*>(ws)};
   c.k = ws + (4 * a.kv.n_page_ids + 255) / 256 * 256;
   c.v = c.k + bytes;
   const uint32_t ctas = (uint32_t)a.kv.n_page_ids;

@@ -1,5 +1,6 @@
 """Attention over pages of 4 bits: ids of pages that the cache does not have are
-refused wherever a token needs them, the one with all bits set among them."""
+refused wherever a token needs them, the one with all bits set among them; pages
+that nothing needs are not worked on."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +55,30 @@ def test_pages_that_the_cache_does_not_have(name, D, dtype):
     for r, n in enumerate(c.total):
         c.page_ids[off[r] + -(-n // B):off[r + 1]] = -1
     check_attention4(c)
+
+
+@pytest.mark.parametrize("D", [128, 64])
+def test_a_chunk_beside_requests_without_new_tokens(D):
+    """The copy in 16 bits at the workspace's end (keys, then values, a page an entry of
+    the lists) has the pages of requests with new tokens, and those alone; what the
+    others' lists hold does not matter."""
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    from tests.kv4_util import Cache4, check_attention4
+    c = Cache4([(0, 400), (600, 700), (0, 90), (1, 50), (0, 0), (0, 33)], Hq=8, Hkv=2, D=D)
+    n, page, off = c.page_ids.shape[0], 2 * c.B * 2 * D, c.page_off.tolist()
+    size = lambda B: ptc.lib().ptc_kv4_attention_workspace_bytes(6, 8, 2, D, 600, 601, n, B)
+    need, copy = size(16), -(-n * page // 256) * 256
+    assert need == size(12) + -(-4 * n // 256) * 256 + 2 * copy  # (there is no copy of pages of 12)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    check_attention4(c, ws=ws)
+    made = [(x[:n * page].view(n, page) != 255).any(1).cpu() for x in (ws[need - 2 * copy:need - copy], ws[need - copy:])]
+    want = torch.zeros(n, dtype=torch.bool)
+    for r, (m, total) in enumerate(c.lens):
+        if m:
+            want[off[r]:off[r] + -(-total // c.B)] = True
+    assert all(torch.equal(x, want) for x in made)
+    for r, (m, _) in enumerate(c.lens):
+        if not m:
+            c.page_ids[off[r]:off[r + 1]] = -1
+    check_attention4(c, ws=ws)
