@@ -82,3 +82,16 @@ def test_a_chunk_beside_requests_without_new_tokens(D):
         if not m:
             c.page_ids[off[r]:off[r + 1]] = -1
     check_attention4(c, ws=ws)
+
+
+def test_a_cache_without_slots_is_refused():
+    import torch
+    import paper_2609_28870_gb300 as ptc
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    i64 = lambda x: torch.tensor(x, dtype=torch.int64, device="cuda")
+    k, v = (torch.zeros(3, 2, 0, 80, dtype=torch.uint8, device="cuda") for _ in range(2))
+    for T in (1, 4096):
+        q = torch.zeros(T, 8, 128, dtype=torch.bfloat16, device="cuda")
+        with pytest.raises(ptc.PtcError) as e:
+            ptc.ptc_kv4_attention(q, k, v, i32([0, 1]), i64([0, 2]), i64([0, T]), i32([T]), T)
+        assert e.value.name == "PTC_ERR_INVALID_ARG"
