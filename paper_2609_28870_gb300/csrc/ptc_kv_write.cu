@@ -69,10 +69,20 @@ __device__ __forceinline__ void find_places(const WriteArgs& a, uint64_t t0, Pla
 }
 
 // How a call turns its rows: not at all; neighbours, or channels of the two halves,
-// in whole threads (the pairs a multiple of 4, of 8); any other number of pairs.  A
+// in whole threads (the pairs a multiple of 4, of 8); any other number of pairs
+// (neighbours whose pairs are no multiple of 4, halves whose pairs are none of 8).  A
 // kernel each: one for all of them, whose registers the rarest width decides, took 140
 // us for 138 below, in fp16 160 for 140, into 4 bits 203 for 194 (fp16 226 for 203).
 enum Width { kStill, kNext, kHalves, kAnyWidth };
+
+// CTAs of an SM.  With four a thread has 64 registers, which do not hold all it needs: up
+// to 44 bytes of it are stored and loaded again, of kAnyWidth up to 68, in fp16 164.
+// There three are faster (50 pairs in halves 226 -> 214 us, in neighbours 173 -> 164, 36 in
+// halves 175 -> 165; in bf16 197 -> 201, 147 -> 156, 149 -> 158).
+template <typename T>
+constexpr int write_ctas(Width width) {
+  return width == kAnyWidth && !Half16<T>::kBf16 ? 3 : 4;
+}
 
 // How a thread's eight channels are turned: by the same angles for all heads of
 // a token, so they are kept.  sn has its sign: channel e becomes
@@ -90,7 +100,7 @@ __device__ __forceinline__ void load_turn(const RopeView& rope, uint32_t pos, ui
   o.any = d0 < 2 * F;
   o.all = F % 4 == 0;  // 2 F is a multiple of 8
   if (!o.any) return;
-  if (WIDTH == kNext || (WIDTH == kAnyWidth && rope.interleaved && F % 4 == 0)) {
+  if (WIDTH == kNext) {
     const float4 x = __ldg(reinterpret_cast<const float4*>(row + 4 * c)), y = __ldg(reinterpret_cast<const float4*>(row + F + 4 * c));
     const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -157,7 +167,7 @@ __device__ __forceinline__ uint4 turn_row(const RopeView& rope, const Turn& t, c
   if (WIDTH == kNext || (WIDTH == kAnyWidth && rope.interleaved)) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) p[k] = __byte_perm(w[k], w[k], 0x1032);
-  } else if (WIDTH == kHalves || F % 8 == 0) {
+  } else if (WIDTH == kHalves) {
     const uint32_t f = F / 8, other = c < f ? c + f : c < 2 * f ? c - f : c;
 #pragma unroll
     for (int k = 0; k < 4; ++k) p[k] = __shfl_sync(kFull, w[k], other, LANES);
@@ -287,11 +297,11 @@ __device__ __forceinline__ uint32_t quantise(const uint4& x, bool real, uint32_t
 // kinds: 152 us for 140, into 4 bits 223 for 203).  Each row is read and written once,
 // 0.86 GB for 34,692 tokens of 32 query and 8 key heads of 128: 138 us, 6.2 TB/s; into
 // pages of 4 bits 158 us, bound by its instructions.  (Several batches of tokens a CTA,
-// to wait for places less often, were slower by 6%.)  Widths that are no multiple of 8
-// pairs 150 us, those of no multiple of 4 200 us.  64 tokens 4.3 us, a launch and four
+// to wait for places less often, were slower by 6%.)  Halves of no multiple of 8
+// pairs 148 us, of no multiple of 4 197 us.  64 tokens 4.3 us, a launch and four
 // dependent reads.
 template <typename T, int LANES, bool FOUR, Width WIDTH>
-__global__ void __launch_bounds__(kWrThreads, 4) k_kv_write(const __grid_constant__ WriteArgs a) {
+__global__ void __launch_bounds__(kWrThreads, write_ctas<T>(WIDTH)) k_kv_write(const __grid_constant__ WriteArgs a) {
   grid_dep_sync();
   constexpr uint32_t kTok = kWrThreads / LANES;
   __shared__ Place s_at[kTok];
