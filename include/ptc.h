@@ -818,7 +818,7 @@ ptc_status ptc_kv4_read(const ptc_paged_kv* kv, const uint64_t* tok_off, uint64_
 /*
  * ptc_kv4_attention — ptc_paged_attention, without accumulated weights, over pages
  * of 4 bits: the same arguments, masks, roundings and refusals, and no request of
- * 2^31 - 256 tokens or more.  A tensor of queries and its outputs have the cache's
+ * more than 2^31 - 256 tokens.  A tensor of queries and its outputs have the cache's
  * dtype.  Where requests have thousands of query rows a key head the workspace has
  * room for the listed pages in 16 bits, up to 1 GB.
  */

@@ -9,6 +9,8 @@
 //   scores   S^T = K Q^T       16 keys x 8 query rows, mma.sync m16n8k16
 //   softmax  running maximum and sum of a query row in 32 bits
 //   values   O^T += V^T P^T    16 channels x 8 query rows, 16 keys at a time
+// The weights are rounded to the cache's 16 bits, as the instructions want both operands
+// alike (their sum is not rounded): at most 2^-8, in fp16 2^-11, of each.
 // A word of codes is eight neighbouring channels of a key, even ones in its low
 // half, so a shifted and masked word is two channels as K's operand wants them;
 // the low (high) halves of two keys' words together are one channel of both, as

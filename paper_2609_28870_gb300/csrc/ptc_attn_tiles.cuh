@@ -1047,7 +1047,7 @@ __device__ __forceinline__ bool quant_role(const AttnArgs& a, TileShared& sh, ui
   const uint32_t lane = threadIdx.x & 31, row0 = 32 * (threadIdx.x / 32 - 12);
   const uint32_t mine = tiles4 + row0 / 32 * Sh::kRing4 * kMine;
   // copies: every lane finds a row; item 2 j + 1, a tile's values, follows item 2 j, its keys.
-  // The walk waits in shared memory from one part to the next: 56 registers are few.
+  // The walk waits in shared memory from one part to the next: 72 registers are few.
   Walk& rest = reinterpret_cast<Walk*>(&sh + 1)[row0 / 32];
   bool more, values = false;
   uint32_t j = 0, end = 0, n = 0, id = kNone, slot = 0, rows = 0, issued = 0;

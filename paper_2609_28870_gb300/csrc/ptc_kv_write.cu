@@ -415,8 +415,12 @@ __global__ void __launch_bounds__(kWrThreads) k_kv4_read(const __grid_constant__
 }
 
 // Rows of a CTA: as few as leave four CTAs for every SM, so that a call of few
-// tokens is spread, and at most kWrSlice (24; 32; 48 for 48 rows: 142, 138, 138 us,
-// into 4 bits and back 191, 191, 185).
+// tokens is spread, and at most kWrSlice.  34,692 tokens, turned, and into 4 bits and
+// back, us:
+//   rows of a CTA, at most           3        6       12       24       48
+//   48 rows a token            205 287  163 225  146 199  142 191  138 185
+//   12                          57  82   47  66   42  60   42  60   42  60
+//   3                           19  31   19  31   19  31   19  31   19  31  (1: 28 45)
 dim3 write_grid(WriteArgs& a, uint32_t tok) {
   const uint64_t blocks = (a.n_tok + tok - 1) / tok;
   uint64_t slice = blocks * a.rows / (4 * (uint64_t)num_sms());

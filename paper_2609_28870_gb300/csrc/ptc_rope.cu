@@ -7,9 +7,9 @@ namespace ptc {
 namespace {
 
 // Angles are kept as fractions of a turn in 64-bit integers: a frequency f is
-// round(f / 2 pi * 2^64) of them a position (its error, 2^-53 of it, grows with
-// the position to 2^-32 of a turn at most), a position's angle the product modulo
-// 2^64, exact.  The two upper bits after rounding to the nearest quarter are the
+// floor(f / 2 pi * 2^64) of them a position (its error, 2^-52 of it and 2^-64 of a
+// turn, grows with the position: at angles of 2^24 it is below 2^-30 of a turn), a
+// position's angle the product modulo 2^64, exact.  The two upper bits after rounding to the nearest quarter are the
 // quarter; the rest, within an eighth of a turn, becomes 32-bit radians with a
 // relative error of 2^-23, and the Taylor series about 0 give both functions (next
 // terms: 1.7e-9 and 2.4e-9).  A thread has a frequency and goes down the positions, a

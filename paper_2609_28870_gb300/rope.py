@@ -52,8 +52,11 @@ def rope_frequencies(rot_dim: int, base: float = 10_000.0, scaling: str = "none"
     * "base": the base times factor ** (rot_dim / (rot_dim - 2)), which divides the
       slowest frequency by factor and leaves the fastest;
     * "parts": pairs of at most ``slow`` turns over the original positions divided
-      by factor, those of at least ``fast`` left, those between mixed in proportion;
-      cosines and sines are multiplied by 0.1 ln(factor) + 1."""
+      by factor, those of at least ``fast`` left, those between mixed in proportion
+      to their turns; cosines and sines are multiplied by 0.1 ln(factor) + 1.
+
+    (Models whose frequencies were mixed in another way, such as in proportion to
+    the pair's index between the two bounds, want others: ptc_rope_table takes any.)"""
     if rot_dim < 2 or rot_dim % 2 or not base > 0 or not factor >= 1:
         raise ValueError("rope_frequencies: expected an even rot_dim, a positive base and a factor of at least 1")
     i = torch.arange(0, rot_dim, 2, dtype=torch.float64)
